@@ -1,0 +1,375 @@
+"""Performance cases of the output head's operators: sampling an action or token
+from rows of logits, and distilling a student's rows from a teacher's top logits.
+
+A case is a dict of plain values:
+  kind      "sample" or "distill"
+  rows, V   rows of logits, entries (actions, tokens) of a row
+  dtype     of the logits: "f32", "bf16" or "f16"
+ sample, each of them one value for the call, or "rows" for one value per row:
+  T         temperature
+  top_k     entries kept (0 = all)
+  top_p     probability kept (1 = all)
+  min_p     smallest kept share of the largest probability (0 = all)
+ distill:
+  k         top logits the teacher gives for a row
+  tau       temperature
+  rest      the teacher also gives the log-sum of the entries it does not list
+  grad      the gradient is wanted beside the losses
+
+Sampling works on whole numbers, so that no order of summation changes a draw.
+With m the row's largest logit (a NaN counts as -inf) and c = log2(e) / T,
+z_i = (l_i - m) c in fp32 (0 where l_i = m); entry i weighs w_i = 2^40 2^z_i,
+as the whole number (P << 16) >> -n with n = rint(z), f = z - n and P the fp32
+value of EXP2 at f, truncated, in Horner form with one rounding per operation;
+entries with z < -41 weigh nothing.  Entries are ranked by logit, equal ones by
+index.  top_k keeps the first k; top_p keeps, of those, each whose predecessors
+weigh less than floor(p 2^24) / 2^24 of their sum W (and the first in any case); min_p
+drops what weighs less than floor(m 2^40).  The draw is the lowest index whose
+running sum of kept weights passes floor(u 2^24) / 2^24 of their sum.  Beside it
+comes its log-probability among the kept entries.
+
+Distilling: p is the softmax of the teacher's values over tau (the rest entry is
+one more value), q the student's softmax over tau, and a row's loss is
+tau^2 KL(p || q), all entries that the teacher does not list taken as one.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEVICE = "cuda"
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZES = {"f32": 4, "bf16": 2, "f16": 2}
+
+# 2^f on [-1/2, 1/2] times 2^24, lowest power first (relative error 1.9e-7 in fp32)
+EXP2 = tuple(c * 2.0 ** 24 for c in (1.0, float.fromhex("0x1.62e42ap-1"), float.fromhex("0x1.ebf9bcp-3"),
+                                     float.fromhex("0x1.c6b754p-5"), float.fromhex("0x1.3cea84p-7"),
+                                     float.fromhex("0x1.5bb994p-10")))
+LOG2E = float(np.float32(1.4426950408889634))
+LAST_Z = -41.0
+
+
+def _sample(name, rows, V, dtype, T=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    return dict(name=name, kind="sample", rows=rows, V=V, dtype=dtype, T=T, top_k=top_k, top_p=top_p, min_p=min_p)
+
+
+def _distill(name, rows, V, dtype, k, tau=1.0, rest=False, grad=True):
+    return dict(name=name, kind="distill", rows=rows, V=V, dtype=dtype, k=k, tau=tau, rest=rest, grad=grad)
+
+
+def listed():
+    return [
+        # the two actions of the cart-pole for a million environments: one step
+        # of a collection loop whose policy runs outside the simulator
+        _sample("act-2x1M", 1 << 20, 2, "f32"),
+        # a discretised control policy, a thousand bins, a mid-size batch
+        _sample("act-1000x4096", 4096, 1000, "f16", T=0.7),
+        # one request of a token server, the usual filters: latency
+        _sample("decode-1", 1, 131072, "bf16", T=0.8, top_k=50, top_p=0.95),
+        # a batch of requests, each with settings of its own, odd vocabulary
+        _sample("decode-64-mixed", 64, 50001, "bf16", T="rows", top_k="rows", top_p="rows", min_p="rows"),
+        # min-p alone on fp32 logits
+        _sample("decode-256-minp", 256, 32000, "f32", T=1.2, min_p=0.05),
+        # rollouts for on-policy learning: plain sampling, a large vocabulary
+        _sample("rollout-512-plain", 512, 151001, "bf16"),
+        # the largest: nucleus sampling for a thousand rollouts at a time
+        _sample("rollout-1024-topp", 1024, 131072, "bf16", top_p=0.9),
+        # the cart-pole policy taught from recorded p0: two actions, a million rows
+        _distill("teach-2x1M", 1 << 20, 2, "f32", k=2),
+        # a short prompt's rows on a large fp32 vocabulary: few rows, long ones
+        _distill("teach-8x262144", 8, 262144, "f32", k=64, tau=2.0, rest=True),
+        # validation: the losses alone, odd vocabulary
+        _distill("teach-eval-1024", 1024, 50001, "f16", k=20, grad=False),
+        # ragged rows of a mid-size vocabulary, fp32
+        _distill("teach-4097x5003", 4097, 5003, "f32", k=33, tau=1.5, rest=True),
+        # the largest: a training step's tokens on a large vocabulary
+        _distill("teach-2048x131072", 2048, 131072, "bf16", k=128, tau=2.0, rest=True),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    """Log-uniform over [lo, hi]; about one value in four a power of two."""
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    v = 2.0 ** round(math.log2(v)) if rng.random() < 0.25 else v
+    return max(lo, min(hi, int(round(v))))
+
+
+def draw(rng):
+    V = _log_int(rng, 2, 262144)
+    dtype = rng.choice(("f32", "bf16", "f16"))
+    if rng.random() < 0.5:
+        rows = _log_int(rng, 1, min(1 << 20, (1 << 27) // V // (SIZES[dtype] // 2)))
+        how = rng.choice(("plain", "top_k", "top_p", "min_p", "all", "rows"))
+        if how == "rows":
+            return _sample("", rows, V, dtype, T="rows", top_k="rows", top_p="rows", min_p="rows")
+        one = dict(T=rng.choice((1.0, round(rng.uniform(0.3, 1.5), 2))))
+        if how in ("top_k", "all"):
+            one["top_k"] = _log_int(rng, 1, 1000)
+        if how in ("top_p", "all"):
+            one["top_p"] = round(rng.uniform(0.5, 0.99), 2)
+        if how in ("min_p", "all"):
+            one["min_p"] = round(rng.uniform(0.01, 0.2), 2)
+        return _sample("", rows, V, dtype, **one)
+    rows = _log_int(rng, 1, min(1 << 20, (1 << 28) // V // (SIZES[dtype] // 2)))
+    k = _log_int(rng, 1, min(V, 256))
+    return _distill("", rows, V, dtype, k=k, tau=rng.choice((1.0, round(rng.uniform(0.5, 4.0), 2))),
+                    rest=k < V and rng.random() < 0.5, grad=rng.random() < 0.75)
+
+
+def _logits(rows, V, gen, sharpness):
+    """Rows as a trained head gives them: a bulk of unlikely entries, a few far
+    above it, and rows of very different sharpness."""
+    x = torch.randn((rows, V), generator=gen, device=DEVICE)
+    top = (x - 1.0).clamp_(min=0.0)
+    x.mul_(2.2).add_(top.square_(), alpha=1.2)
+    return x.mul_(sharpness)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEVICE)
+    gen.manual_seed(seed)
+    rows, V, dtype = case["rows"], case["V"], DTYPES[case["dtype"]]
+
+    def uniform(lo, hi):
+        return torch.rand((rows,), generator=gen, device=DEVICE) * (hi - lo) + lo
+
+    state = dict(case=case)
+    s = _logits(rows, V, gen, uniform(0.4, 1.2)[:, None])
+    if case["kind"] == "sample":
+        if V % 64 == 0:
+            s[:, V - V // 1024:] = -math.inf          # entries that only pad the row
+        state["logits"] = s.to(dtype)
+        state["u"] = torch.rand((rows,), generator=gen, device=DEVICE)
+        per_row = dict(
+            T=lambda: torch.where(uniform(0, 1) < 0.1, 0.0, uniform(0.3, 1.5)),         # one row in ten is greedy
+            top_k=lambda: torch.where(uniform(0, 1) < 0.5, 0.0, torch.exp(uniform(0, math.log(1000.0)))).int(),
+            top_p=lambda: torch.where(uniform(0, 1) < 0.4, 1.0, uniform(0.5, 0.99)),
+            min_p=lambda: torch.where(uniform(0, 1) < 0.6, 0.0, uniform(0.01, 0.2)))
+        for key, make in per_row.items():
+            state[key] = make() if case[key] == "rows" else case[key]
+    else:
+        tau, k = case["tau"], case["k"]
+        t = s + 0.7 * torch.randn((rows, V), generator=gen, device=DEVICE)
+        state["logits"] = s.to(dtype)
+        values, index = torch.topk(t, k, dim=1)
+        state["teacher"] = values.to(dtype)
+        state["index"] = index.to(torch.int32)
+        if case["rest"]:
+            t.scatter_(1, index, -math.inf)
+            state["rest"] = torch.logsumexp(t.div_(tau), dim=1)
+        else:
+            state["rest"] = None
+        state["weight"] = uniform(0.5, 1.5) if case["grad"] else None
+    if own:
+        import paper_2207_07736_amd as rl
+        state["head"] = rl.Head(rows, V)
+    return state
+
+
+def _column(value, like):
+    if torch.is_tensor(value):
+        return value[:, None]
+    return torch.full((like.shape[0], 1), value, device=like.device, dtype=torch.float32)
+
+
+def _plain_sample(state):
+    case = state["case"]
+    l = state["logits"].float()
+    rows, V = l.shape
+    l = torch.where(torch.isnan(l), -math.inf, l)
+    m = l.max(dim=1, keepdim=True).values
+    T = _column(state["T"], l)
+    greedy = ~(T > 0)
+    z = (l - m) * (LOG2E / torch.where(greedy, 1.0, T))
+    z = torch.where(l == m, 0.0, z)
+    live = (z >= LAST_Z) & (l > -math.inf)
+    z = torch.where(live, z, 0.0)
+    n = torch.round(z)
+    f = z - n
+    P = f * EXP2[5] + EXP2[4]
+    for power in (3, 2, 1, 0):
+        P = P * f + EXP2[power]
+    w = torch.bitwise_right_shift(P.to(torch.int64) * 65536, (-n).to(torch.int64))
+    w = torch.where(live, w, 0)
+    del z, n, f, P
+    kept = w
+    if case["top_k"] or case["top_p"] != 1.0:
+        order = torch.sort(l, dim=1, descending=True, stable=True).indices
+        ranked = torch.gather(w, 1, order)
+        k = _column(state["top_k"], l)
+        k = torch.where(k > 0, k, V)
+        ranked = torch.where(torch.arange(V, device=l.device) < k, ranked, 0)
+        total = ranked.sum(dim=1, keepdim=True)
+        p = _column(state["top_p"], l)
+        share = (p.clamp(0.0, 1.0) * 2.0 ** 24).to(torch.int64)
+        target = (total >> 24) * share + (((total & 0xFFFFFF) * share) >> 24)
+        before = ranked.cumsum(dim=1) - ranked
+        first = torch.arange(V, device=l.device) == 0
+        ranked = torch.where((before < target) | (p >= 1.0) | first, ranked, 0)
+        kept = torch.zeros_like(w).scatter_(1, order, ranked)
+        del order, before
+    if case["min_p"]:
+        least = (_column(state["min_p"], l).clamp(0.0, 1.0) * 2.0 ** 40).to(torch.int64)
+        kept = torch.where(w >= least, kept, 0)
+    running = kept.cumsum(dim=1)
+    total = running[:, -1:]
+    u = (state["u"][:, None].clamp(0.0, 1.0 - 2.0 ** -24) * 2.0 ** 24).to(torch.int64)
+    target = (total >> 24) * u + (((total & 0xFFFFFF) * u) >> 24)
+    token = (running <= target).sum(dim=1, keepdim=True)
+    token = torch.where(greedy, (l == m).to(torch.int8).argmax(dim=1, keepdim=True), token)
+    empty = m == -math.inf
+    chosen = torch.gather(l, 1, token.clamp(max=V - 1))
+    above = torch.where(chosen == m, 0.0, (chosen - m) / T)
+    logp = torch.where(greedy | empty, 0.0, above - torch.log(total.float() * 2.0 ** -40))
+    return torch.where(empty, -1, token)[:, 0].int(), logp[:, 0]
+
+
+def _plain_distill(state):
+    case = state["case"]
+    tau = case["tau"]
+    s = state["logits"].float() / tau
+    t = state["teacher"].float() / tau
+    index = state["index"].long()
+    if case["rest"]:
+        t = torch.cat((t, state["rest"][:, None]), dim=1)
+    t = t - t.max(dim=1, keepdim=True).values
+    log_p = t - torch.log(torch.exp(t).sum(dim=1, keepdim=True))
+    p = torch.exp(log_p)
+    s = s - s.max(dim=1, keepdim=True).values
+    e = torch.exp(s)
+    total = e.sum(dim=1, keepdim=True)
+    log_q = torch.gather(s, 1, index) - torch.log(total)
+    if case["rest"]:
+        unlisted = e.scatter(1, index, 0.0).sum(dim=1, keepdim=True)
+        log_q = torch.cat((log_q, torch.log(unlisted / total)), dim=1)
+    loss = tau * tau * (p * (log_p - log_q)).sum(dim=1)
+    if not case["grad"]:
+        return loss
+    g = e / total
+    listed_g = torch.gather(g, 1, index) - p[:, :index.shape[1]]
+    if case["rest"]:
+        g = g * (1.0 - p[:, -1:] / (unlisted / total))
+    g = g.scatter_(1, index, listed_g) * (tau * state["weight"][:, None])
+    return loss, g.to(state["logits"].dtype)
+
+
+def run(state):
+    case = state["case"]
+    if not own:
+        return _plain_sample(state) if case["kind"] == "sample" else _plain_distill(state)
+    head = state["head"]
+    if case["kind"] == "sample":
+        return head.sample(state["logits"], state["u"], temperature=state["T"], top_k=state["top_k"],
+                           top_p=state["top_p"], min_p=state["min_p"], logp=True)
+    if not case["grad"]:
+        return head.distill(state["logits"], state["teacher"], state["index"], temperature=case["tau"],
+                            rest=state["rest"], grad=False)
+    return head.distill(state["logits"], state["teacher"], state["index"], temperature=case["tau"], rest=state["rest"],
+                        weight=state["weight"])
+
+
+def work(case):
+    rows, V, e = case["rows"], case["V"], SIZES[case["dtype"]]
+    if case["kind"] == "sample":
+        per_row = sum(4 for key in ("T", "top_k", "top_p", "min_p") if case[key] == "rows")
+        # the logits, u and a row's settings in; token and log-probability out;
+        # difference, scale, exponential and sum for each entry
+        return dict(bytes=rows * (V * e + 4 + per_row + 8), flops=rows * V * 4)
+    # the logits, the teacher's values, indices, rest and the row's weight in; the
+    # loss and the gradient out; an exponential and a sum, then a product and a
+    # difference for each entry
+    row = V * e + case["k"] * (e + 4) + 4 + (4 if case["rest"] else 0)
+    row += V * e + 4 if case["grad"] else 0
+    return dict(bytes=rows * row, flops=rows * V * (6 if case["grad"] else 4))
+
+
+def _exact_sample_rows(l, u, T, k, p, least):
+    """Draws and log-probabilities of some rows, whole-number weights (numpy)."""
+    rows, V = l.shape
+    l = np.where(np.isnan(l), np.float32(-np.inf), l)
+    m = l.max(axis=1, keepdims=True)
+    greedy = ~(T > 0)
+    scale = (np.float32(LOG2E) / np.where(greedy, np.float32(1), T)).astype(np.float32)
+    with np.errstate(invalid="ignore"):
+        z = np.where(l == m, np.float32(0), (l - m) * scale)
+        live = (z >= np.float32(LAST_Z)) & (l > -np.inf)
+    z = np.where(live, z, np.float32(0))
+    n = np.rint(z)
+    f = z - n
+    P = np.full_like(f, np.float32(EXP2[5]))
+    for power in (4, 3, 2, 1, 0):
+        P = P * f + np.float32(EXP2[power])
+    w = np.where(live, (P.astype(np.int64) << 16) >> (-n).astype(np.int64), 0)
+    keep = np.ones((rows, V), dtype=bool)
+    if (k > 0).any() or (p < 1).any():
+        order = torch.sort(torch.from_numpy(l), dim=1, descending=True, stable=True).indices.numpy()
+        ranked = np.take_along_axis(w, order, axis=1)
+        place = np.arange(V)[None, :]
+        ok = place < np.where(k > 0, k, V)
+        ranked[~ok] = 0
+        total = ranked.sum(axis=1)
+        target = np.array([(int(t) * int(np.float32(min(max(q, 0), 1)) * 2 ** 24)) >> 24 for t, q in zip(total, p[:, 0])],
+                          dtype=np.int64)[:, None]
+        before = np.cumsum(ranked, axis=1) - ranked
+        ok &= (before < target) | (p >= 1) | (place == 0)
+        np.put_along_axis(keep, order, ok, axis=1)
+    keep &= w >= (np.clip(least, 0, 1).astype(np.float32) * np.float32(2.0 ** 40)).astype(np.int64)
+    keep &= w > 0
+    kept = np.where(keep, w, 0)
+    running = np.cumsum(kept, axis=1)
+    target = np.array([(int(t) * min(max(int(v * 2 ** 24), 0), 2 ** 24 - 1)) >> 24
+                       for t, v in zip(running[:, -1], u.tolist())], dtype=np.int64)
+    token = (running <= target[:, None]).sum(axis=1)
+    token = np.where(greedy[:, 0], np.argmax(l == m, axis=1), token)
+    empty = m[:, 0] == -np.inf
+    T64, l64, m64 = T.astype(np.float64), l.astype(np.float64), m.astype(np.float64)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        x = np.where(l == m, 0.0, (l64 - m64) / T64)
+        chosen = np.take_along_axis(x, np.minimum(token, V - 1)[:, None], axis=1)[:, 0]
+        logp = chosen - np.log(np.where(keep, np.exp(x), 0.0).sum(axis=1))
+    logp = np.where(greedy[:, 0] | empty, 0.0, logp)
+    return np.where(empty, -1, token).astype(np.int32), logp
+
+
+def exact(case, seed):
+    state = prepare(case, seed)
+    rows, V = case["rows"], case["V"]
+    block = max(1, (1 << 22) // V)
+    logits = state["logits"].float().cpu()
+
+    def column(value, dtype):
+        value = value.cpu().numpy() if torch.is_tensor(value) else np.full((rows,), value)
+        return value.astype(dtype)[:, None]
+
+    if case["kind"] == "sample":
+        u = state["u"].cpu().numpy()
+        per_row = [column(state[key], np.int64 if key == "top_k" else np.float32)
+                   for key in ("T", "top_k", "top_p", "min_p")]
+        parts = [_exact_sample_rows(logits[r:r + block].numpy(), u[r:r + block], *(v[r:r + block] for v in per_row))
+                 for r in range(0, rows, block)]
+        return tuple(torch.from_numpy(np.concatenate(part)) for part in zip(*parts))
+    tau = float(case["tau"])
+    teacher, index = state["teacher"].double().cpu() / tau, state["index"].long().cpu()
+    losses, grads = [], []
+    for r in range(0, rows, block):
+        s, t, i = logits[r:r + block].double() / tau, teacher[r:r + block], index[r:r + block]
+        lq = torch.log_softmax(s, dim=1)
+        listed = torch.zeros(lq.shape, dtype=torch.bool).scatter_(1, i, True)
+        if case["rest"]:
+            t = torch.cat((t, state["rest"][r:r + block, None].double().cpu()), dim=1)
+        lp = torch.log_softmax(t, dim=1)
+        loss = (lp[:, :case["k"]].exp() * (lp[:, :case["k"]] - lq.gather(1, i))).sum(dim=1)
+        ratio = torch.ones((s.shape[0], 1), dtype=torch.float64)
+        if case["rest"]:
+            lr = torch.logsumexp(lq.masked_fill(listed, -math.inf), dim=1)
+            share = lp[:, -1]
+            loss = loss + torch.where(share > -math.inf, share.exp() * (share - lr), 0.0)
+            ratio = 1.0 - torch.exp(share - lr)[:, None]
+        losses.append(tau * tau * loss)
+        if case["grad"]:
+            q = lq.exp()
+            g = torch.where(listed, q, q * ratio).scatter_add_(1, i, -lp[:, :case["k"]].exp())
+            grads.append(g * (tau * state["weight"][r:r + block, None].double().cpu()))
+    return (torch.cat(losses), torch.cat(grads)) if case["grad"] else torch.cat(losses)
