@@ -182,7 +182,7 @@ def _plain_sample(state):
     m = l.max(dim=1, keepdim=True).values
     T = _column(state["T"], l)
     greedy = ~(T > 0)
-    z = (l - m) * (LOG2E / torch.where(greedy, 1.0, T))
+    z = (l - m) * (torch.full_like(T, LOG2E) / torch.where(greedy, 1.0, T))
     z = torch.where(l == m, 0.0, z)
     live = (z >= LAST_Z) & (l > -math.inf)
     z = torch.where(live, z, 0.0)
