@@ -43,7 +43,7 @@ typedef enum {
     RLSIM_EUNSUPPORTED = -5  /* valid request this build does not implement */
 } rlsim_status;
 
-enum { RLSIM_F32 = 0, RLSIM_BF16 = 1 };       /* rlsim_policy.dtype */
+enum { RLSIM_F32 = 0, RLSIM_BF16 = 1, RLSIM_F16 = 2 };   /* rlsim_policy.dtype (not RLSIM_F16), logits */
 enum { RLSIM_F_NO_TERMINATION = 1u };         /* rlsim_cfg.flags: thresholds never fire */
 enum { RLSIM_MODEL_CARTPOLE = 0u, RLSIM_MODEL_CHAIN = 1u };   /* rlsim_cfg.model */
 
@@ -212,6 +212,112 @@ int rlsim_destroy(rlsim_t* h);
  * last rlsim_create failure.  The string stays valid until the next call on h
  * (or the thread's next create). */
 const char* rlsim_last_error(const rlsim_t* h);
+
+/* ------------------------------------------------------------------------
+ * The output head: operators on rows of logits, for policies other than the one
+ * built into rlsim_step_fused (the inference half of the data-collection loop,
+ * Background, "RL Training") and for what a learner does with the rows.
+ *
+ * A row is `vocab` consecutive logits (actions, or tokens) of RLSIM_F32,
+ * RLSIM_BF16 or RLSIM_F16, aligned to the element; rows start row_stride elements
+ * apart.  A handle serves calls of up to max_rows rows of up to max_vocab
+ * logits on its stream; every buffer is a DEVICE pointer that the caller owns.
+ * Calls allocate nothing and do not synchronise, so they can be captured. */
+typedef struct rlsim_head rlsim_head_t;       /* opaque handle */
+
+/* Errors: EINVAL (out NULL, max_rows not in [1, 2^30], max_vocab not in
+ * [1, 2^20]), ENOMEM, EDEVICE.  On error *out is NULL. */
+int rlsim_head_create(uint32_t max_rows, uint32_t max_vocab, void* stream, rlsim_head_t** out);
+
+/* Draw one entry of each row.  Each setting is one value for the call, or, where
+ * its pointer is not NULL, an array with a value for each row.
+ *
+ * m being the row's largest logit, entry i weighs 2^40 2^z_i, z_i =
+ * (l_i - m) log2(e) / temperature, as a whole number of 24 significant bits (0
+ * below z = -41): sums are exact, so the draw depends on the row, its settings and u
+ * alone, not on the batch or the machine's order of work.  Entries are ranked by
+ * logit, equal ones by index.  Filters, each on what the one before it left:
+ *   top_k        the first k entries (0, a negative row value or >= vocab: all)
+ *   top_p        entries whose predecessors weigh less than top_p of the sum, and
+ *                the first (>= 1 or NaN: all)
+ *   min_p        entries whose weight is at least min_p of the largest one's
+ *                (0, negative or NaN: all; counted as 1 above 1)
+ * token is the lowest index whose running sum of kept weights exceeds u times their
+ * sum; top_p and u count in units of 2^-24, rounded down, u within
+ * [0, 1 - 2^-24] (NaN: 0).  logp is the token's log-probability among the kept
+ * entries.  A temperature that is not > 0 takes the first of the largest logits
+ * (logp 0).  A NaN logit counts as -inf; +inf leaves only the entries that are
+ * +inf.  A row with no entry above -inf gives token -1, logp 0. */
+typedef struct {
+    int dtype;
+    const void* logits;
+    uint32_t rows, vocab;
+    uint64_t row_stride;                      /* elements, >= vocab */
+    const float* u;                           /* [rows] uniform numbers in [0, 1) */
+    float temperature;
+    uint32_t top_k;
+    float top_p;
+    float min_p;
+    const float* temperature_rows;            /* [rows] or NULL */
+    const int32_t* top_k_rows;                /* [rows] or NULL */
+    const float* top_p_rows;                  /* [rows] or NULL */
+    const float* min_p_rows;                  /* [rows] or NULL */
+    int32_t* token;                           /* [rows] out */
+    float* logp;                              /* [rows] out, or NULL */
+} rlsim_sample;
+
+/* Errors: EINVAL (NULL h, s, logits, u or token; an unknown dtype; rows, vocab or
+ * row_stride out of range; a misaligned pointer; a call-wide temperature that is
+ * negative or not finite, top_p or min_p negative or NaN); EDEVICE. */
+int rlsim_head_sample(rlsim_head_t* h, const rlsim_sample* s);
+
+/* Distil each row from a teacher's top logits: the teacher gives, for every row, k
+ * slots of (index, logit) and optionally `rest`, the log of the sum of
+ * exp(t / temperature) over the entries it does not list.  With p the softmax of the
+ * teacher's values over the temperature (rest is one more value), q the
+ * student's softmax over it, and the entries that are not listed taken as one,
+ *   loss = temperature^2 KL(p || q),   grad = weight * dloss / dlogits.
+ * Without rest p lives on the listed entries alone.
+ *
+ * A slot whose index is outside [0, vocab) (-1 by convention) is empty whatever
+ * its logit, and so is one whose index an earlier slot has.  A row without teacher
+ * mass (empty slots and logits of -inf, rest absent or -inf) has loss 0 and gradient 0
+ * whatever its student logits, and a row of weight 0 gradient 0.  A
+ * student logit of -inf has q = 0: loss +inf where p > 0.  A NaN in a row that
+ * counts gives NaN.  Teacher values are finite or -inf.
+ * Statistics are fp32; the gradient is rounded once to the logits' type. */
+typedef struct {
+    int dtype;                                /* of logits and grad */
+    const void* logits;
+    uint32_t rows, vocab;
+    uint64_t row_stride;                      /* elements, >= vocab */
+    int teacher_dtype;
+    const void* teacher;                      /* [rows][k] logits */
+    uint64_t teacher_stride;                  /* elements, >= k */
+    int index_bytes;                          /* 4: int32, 8: int64 */
+    const void* index;                        /* [rows][k] */
+    uint64_t index_stride;                    /* elements, >= k */
+    uint32_t k;                               /* slots, in [1, 1024] */
+    float temperature;                        /* in [2^-60, 2^60] */
+    const float* rest;                        /* [rows] or NULL */
+    const float* weight;                      /* [rows] or NULL (1): d total / d loss */
+    float* loss;                              /* [rows] out, or NULL */
+    void* grad;                               /* [rows][vocab] out, or NULL; may be logits itself
+                                                 with the same stride, must not overlap otherwise */
+    uint64_t grad_stride;                     /* elements, >= vocab */
+} rlsim_distill;
+
+/* Errors: EINVAL (NULL h, d, logits, teacher or index; loss and grad both NULL;
+ * unknown dtypes or index_bytes; sizes, strides or temperature out of range; a
+ * misaligned pointer; grad partly over logits); EDEVICE. */
+int rlsim_head_distill(rlsim_head_t* h, const rlsim_distill* d);
+
+/* Synchronise the stream and free the handle.  NULL is accepted (RLSIM_OK). */
+int rlsim_head_destroy(rlsim_head_t* h);
+
+/* Message of h's last failure ("" if none).  h == NULL: the calling thread's last
+ * failure without a handle.  Valid until the next call on h. */
+const char* rlsim_head_last_error(const rlsim_head_t* h);
 
 #ifdef __cplusplus
 }

@@ -15,6 +15,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "rlsim.hip")
+HEAD_SRC = os.path.join(HERE, "csrc", "head.hip")                 # the output head's operators
 LIB = os.path.join(HERE, "librlsim.so")
 PROBE_SRCS = [os.path.join(HERE, "csrc", "store_probe.hip")]      # includes math_probe.hip.h
 PROBE_LIB = os.path.join(HERE, "librlsim_probe.so")
@@ -44,9 +45,9 @@ def sources():
 
 
 def build(verbose: bool = False) -> str:
-    """Compile csrc/rlsim.hip into librlsim.so and the probe sources into
+    """Compile csrc/rlsim.hip and csrc/head.hip into librlsim.so and the probe sources into
     librlsim_probe.so next to this file (always).  Returns the main library."""
-    _compile([SRC], LIB, verbose)
+    _compile([SRC, HEAD_SRC], LIB, verbose)
     _compile(PROBE_SRCS, PROBE_LIB, verbose)
     return LIB
 

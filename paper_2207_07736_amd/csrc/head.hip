@@ -1,0 +1,311 @@
+// head.hip -- host runtime of the output head's operators (rlsim_head_* of
+// include/rlsim.h): argument checks, choice of the kernel's form, launch.
+#include "rlsim.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+#include <new>
+
+#include "head_dispatch.h"
+#include "k_distill.hip.h"
+#include "k_sample.hip.h"
+
+using namespace rlsim_dev;
+
+struct rlsim_head {
+    uint32_t max_rows = 0, max_vocab = 0;
+    int device = 0;
+    uint32_t cus = 1;
+    hipStream_t stream = nullptr;
+    char err[256] = "";
+};
+
+namespace {
+
+thread_local char g_head_err[256] = "";
+
+int head_fail(rlsim_head* h, int code, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    (void)vsnprintf(h ? h->err : g_head_err, sizeof h->err, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+// Makes the handle's device current for the scope, restoring the caller's.
+struct HeadDevice {
+    int prev = -1;
+    bool ok = true;
+    explicit HeadDevice(int dev)
+    {
+        if (hipGetDevice(&prev) != hipSuccess) { ok = false; return; }
+        if (prev != dev && hipSetDevice(dev) != hipSuccess) ok = false;
+    }
+    ~HeadDevice()
+    {
+        int cur = -1;
+        if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
+    }
+};
+
+bool known_dtype(int d) { return d == RLSIM_F32 || d == RLSIM_BF16 || d == RLSIM_F16; }
+uint32_t dtype_bytes(int d) { return d == RLSIM_F32 ? 4u : 2u; }
+bool aligned(const void* p, uint32_t bytes) { return (uintptr_t)p % bytes == 0u; }
+
+// The rows of logits of either operator; null if they are sound.
+const char* check_rows(const rlsim_head* h, int dtype, const void* logits, uint32_t rows, uint32_t vocab, uint64_t stride)
+{
+    if (!known_dtype(dtype)) return "unknown dtype";
+    if (!logits) return "logits is NULL";
+    if (rows == 0u || rows > h->max_rows) return "rows must be in [1, max_rows]";
+    if (vocab == 0u || vocab > h->max_vocab) return "vocab must be in [1, max_vocab]";
+    if (stride < vocab || stride > 1ull << 40) return "the row stride must be in [vocab, 2^40]";
+    if (!aligned(logits, dtype_bytes(dtype))) return "logits must be aligned to its element size";
+    return nullptr;
+}
+
+// Workgroups of a kernel that goes through `items` rows (or groups of rows).
+uint32_t head_grid(const rlsim_head* h, uint32_t items, uint32_t threads)
+{
+    return std::min(items, h->cus * (threads >= 1024u ? 2u : 2048u / threads));
+}
+
+// One template argument list for each element type and form.
+#define HEAD_FORMS(KERNEL, D, form, grid, shared, stream, args)                                                              \
+    do {                                                                                                                     \
+        if (form.threads == 64u && form.strips == 2u)                                                                        \
+            hipLaunchKernelGGL((KERNEL<D, 64, 2>), dim3(grid), dim3(64), shared, stream, args);                              \
+        else if (form.threads == 64u)                                                                                        \
+            hipLaunchKernelGGL((KERNEL<D, 64, 4>), dim3(grid), dim3(64), shared, stream, args);                              \
+        else if (form.threads == 256u && form.strips == 4u)                                                                  \
+            hipLaunchKernelGGL((KERNEL<D, 256, 4>), dim3(grid), dim3(256), shared, stream, args);                            \
+        else if (form.threads == 256u)                                                                                       \
+            hipLaunchKernelGGL((KERNEL<D, 256, 8>), dim3(grid), dim3(256), shared, stream, args);                            \
+        else if (form.strips == 4u)                                                                                          \
+            hipLaunchKernelGGL((KERNEL<D, 1024, 4>), dim3(grid), dim3(1024), shared, stream, args);                          \
+        else if (form.strips == 8u)                                                                                          \
+            hipLaunchKernelGGL((KERNEL<D, 1024, 8>), dim3(grid), dim3(1024), shared, stream, args);                          \
+        else if (form.strips == 16u)                                                                                         \
+            hipLaunchKernelGGL((KERNEL<D, 1024, 16>), dim3(grid), dim3(1024), shared, stream, args);                         \
+        else                                                                                                                 \
+            hipLaunchKernelGGL((KERNEL<D, 1024, 0>), dim3(grid), dim3(1024), shared, stream, args);                          \
+    } while (0)
+
+#define HEAD_TINY(KERNEL, D, vocab, grid, stream, args)                                                                      \
+    do {                                                                                                                     \
+        if (vocab <= 2u) hipLaunchKernelGGL((KERNEL<D, 2>), dim3(grid), dim3(256), 0, stream, args);                         \
+        else if (vocab <= 4u) hipLaunchKernelGGL((KERNEL<D, 4>), dim3(grid), dim3(256), 0, stream, args);                    \
+        else if (vocab <= 8u) hipLaunchKernelGGL((KERNEL<D, 8>), dim3(grid), dim3(256), 0, stream, args);                    \
+        else if (vocab <= 16u) hipLaunchKernelGGL((KERNEL<D, 16>), dim3(grid), dim3(256), 0, stream, args);                  \
+        else if (vocab <= 32u) hipLaunchKernelGGL((KERNEL<D, 32>), dim3(grid), dim3(256), 0, stream, args);                  \
+        else hipLaunchKernelGGL((KERNEL<D, 64>), dim3(grid), dim3(256), 0, stream, args);                                    \
+    } while (0)
+
+uint32_t tiny_grid(const rlsim_head* h, uint32_t rows, uint32_t vocab)
+{
+    uint32_t lanes = 2u;
+    while (lanes < vocab) lanes *= 2u;
+    const uint32_t per_group = 256u / lanes;
+    return head_grid(h, (rows + per_group - 1u) / per_group, 256u);
+}
+
+template <int D>
+void launch_sample(const rlsim_head* h, const SampleArgs& a)
+{
+    if (a.V <= kHeadTinyVocab) {
+        const uint32_t grid = tiny_grid(h, a.rows, a.V);
+        HEAD_TINY(k_sample_tiny, D, a.V, grid, h->stream, a);
+        return;
+    }
+    const HeadForm form = head_form(a.V, Elem<D>::kBytes);
+    const uint32_t grid = head_grid(h, a.rows, form.threads);
+    HEAD_FORMS(k_sample, D, form, grid, 0, h->stream, a);
+}
+
+template <int D>
+void launch_distill(const rlsim_head* h, const DistillArgs& a)
+{
+    if (a.V <= kHeadTinyVocab) {
+        const uint32_t grid = tiny_grid(h, a.rows, a.V);
+        HEAD_TINY(k_distill_tiny, D, a.V, grid, h->stream, a);
+        return;
+    }
+    const HeadForm form = head_form(a.V, Elem<D>::kBytes);
+    const uint32_t grid = head_grid(h, a.rows, form.threads);
+    const uint32_t shared = distill_shared_bytes(a.k, a.V, a.rest != nullptr);
+    HEAD_FORMS(k_distill, D, form, grid, shared, h->stream, a);
+}
+
+// A kernel may use more than 64 KB of dynamic shared memory only once it is told so.
+template <int D>
+hipError_t allow_shared()
+{
+    const int bytes = (int)distill_shared_bytes(kHeadMaxTeacher, kHeadMaxVocab, true);
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(k_distill<D, 1024, 0>),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+// The bytes that `rows` rows of `row` bytes take, `stride` bytes apart.
+struct Span { uintptr_t first, last; };
+Span span(const void* p, uint32_t rows, uint64_t stride, uint64_t row)
+{
+    return {(uintptr_t)p, (uintptr_t)p + (uint64_t)(rows - 1u) * stride + row};
+}
+bool overlap(Span a, Span b) { return a.first < b.last && b.first < a.last; }
+
+}  // namespace
+
+extern "C" {
+
+int rlsim_head_create(uint32_t max_rows, uint32_t max_vocab, void* stream, rlsim_head_t** out)
+{
+    if (!out) return head_fail(nullptr, RLSIM_EINVAL, "rlsim_head_create: out is NULL");
+    *out = nullptr;
+    if (max_rows == 0u || max_rows > 1u << 30)
+        return head_fail(nullptr, RLSIM_EINVAL, "rlsim_head_create: max_rows must be in [1, 2^30]");
+    if (max_vocab == 0u || max_vocab > kHeadMaxVocab)
+        return head_fail(nullptr, RLSIM_EINVAL, "rlsim_head_create: max_vocab must be in [1, 2^20]");
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    int cus = 0;
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device);
+    if (e == hipSuccess) e = allow_shared<kHeadF32>();
+    if (e == hipSuccess) e = allow_shared<kHeadBF16>();
+    if (e == hipSuccess) e = allow_shared<kHeadF16>();
+    if (e != hipSuccess) return head_fail(nullptr, RLSIM_EDEVICE, "rlsim_head_create: %s", hipGetErrorString(e));
+    rlsim_head* h = new (std::nothrow) rlsim_head;
+    if (!h) return head_fail(nullptr, RLSIM_ENOMEM, "rlsim_head_create: host allocation failed");
+    h->max_rows = max_rows;
+    h->max_vocab = max_vocab;
+    h->device = device;
+    h->cus = (uint32_t)std::max(cus, 1);
+    h->stream = static_cast<hipStream_t>(stream);
+    *out = h;
+    return RLSIM_OK;
+}
+
+int rlsim_head_sample(rlsim_head_t* h, const rlsim_sample* s)
+{
+    if (!h) return head_fail(nullptr, RLSIM_EINVAL, "rlsim_head_sample: handle is NULL");
+    if (!s) return head_fail(h, RLSIM_EINVAL, "rlsim_head_sample: arguments are NULL");
+    if (const char* what = check_rows(h, s->dtype, s->logits, s->rows, s->vocab, s->row_stride))
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_sample: %s", what);
+    if (!s->u || !s->token) return head_fail(h, RLSIM_EINVAL, "rlsim_head_sample: u or token is NULL");
+    const void* words[] = {s->u, s->token, s->logp, s->temperature_rows, s->top_k_rows, s->top_p_rows, s->min_p_rows};
+    for (const void* p : words)
+        if (!aligned(p, 4u)) return head_fail(h, RLSIM_EINVAL, "rlsim_head_sample: a 32-bit array is not 4-byte aligned");
+    if (!s->temperature_rows && !(std::isfinite(s->temperature) && s->temperature >= 0.0f))
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_sample: temperature must be finite and >= 0");
+    if (!s->top_p_rows && !(s->top_p >= 0.0f)) return head_fail(h, RLSIM_EINVAL, "rlsim_head_sample: top_p must be >= 0");
+    if (!s->min_p_rows && !(s->min_p >= 0.0f)) return head_fail(h, RLSIM_EINVAL, "rlsim_head_sample: min_p must be >= 0");
+    HeadDevice g(h->device);
+    if (!g.ok) return head_fail(h, RLSIM_EDEVICE, "rlsim_head_sample: cannot select the handle's device");
+    SampleArgs a{};
+    a.logits = s->logits;
+    a.stride = s->row_stride;
+    a.rows = s->rows;
+    a.V = s->vocab;
+    a.T = s->temperature;
+    a.top_p = s->top_p;
+    a.min_p = s->min_p;
+    a.top_k = s->top_k;
+    a.T_rows = s->temperature_rows;
+    a.top_k_rows = s->top_k_rows;
+    a.top_p_rows = s->top_p_rows;
+    a.min_p_rows = s->min_p_rows;
+    a.u = s->u;
+    a.token = s->token;
+    a.logp = s->logp;
+    if (s->dtype == RLSIM_F32) launch_sample<kHeadF32>(h, a);
+    else if (s->dtype == RLSIM_BF16) launch_sample<kHeadBF16>(h, a);
+    else launch_sample<kHeadF16>(h, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return head_fail(h, RLSIM_EDEVICE, "rlsim_head_sample: launch: %s", hipGetErrorString(e));
+    return RLSIM_OK;
+}
+
+int rlsim_head_distill(rlsim_head_t* h, const rlsim_distill* d)
+{
+    if (!h) return head_fail(nullptr, RLSIM_EINVAL, "rlsim_head_distill: handle is NULL");
+    if (!d) return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: arguments are NULL");
+    if (const char* what = check_rows(h, d->dtype, d->logits, d->rows, d->vocab, d->row_stride))
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: %s", what);
+    if (d->k == 0u || d->k > kHeadMaxTeacher)
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: k must be in [1, %u]", kHeadMaxTeacher);
+    if (!known_dtype(d->teacher_dtype)) return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: unknown teacher_dtype");
+    if (d->index_bytes != 4 && d->index_bytes != 8)
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: index_bytes must be 4 or 8");
+    if (!d->teacher || !d->index) return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: teacher or index is NULL");
+    if (!aligned(d->teacher, dtype_bytes(d->teacher_dtype)) || !aligned(d->index, (uint32_t)d->index_bytes))
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: teacher or index is not aligned to its element size");
+    if (d->teacher_stride < d->k || d->index_stride < d->k || d->teacher_stride > 1ull << 40 || d->index_stride > 1ull << 40)
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: teacher and index strides must be in [k, 2^40]");
+    // 1 / temperature and its product with log2(e) have to be finite and not 0
+    if (!(d->temperature >= 0x1.0p-60f && d->temperature <= 0x1.0p60f))
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: temperature must be in [2^-60, 2^60]");
+    const void* words[] = {d->rest, d->weight, d->loss};
+    for (const void* p : words)
+        if (!aligned(p, 4u)) return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: a float array is not 4-byte aligned");
+    if (!d->loss && !d->grad) return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: neither loss nor grad is wanted");
+    if (d->grad) {
+        const uint32_t bytes = dtype_bytes(d->dtype);
+        if (!aligned(d->grad, bytes)) return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: grad is not aligned to its element size");
+        if (d->grad_stride < d->vocab || d->grad_stride > 1ull << 40)
+            return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: grad_stride must be in [vocab, 2^40]");
+        const bool in_place = d->grad == d->logits && d->grad_stride == d->row_stride;
+        const Span g = span(d->grad, d->rows, d->grad_stride * bytes, (uint64_t)d->vocab * bytes);
+        const Span l = span(d->logits, d->rows, d->row_stride * bytes, (uint64_t)d->vocab * bytes);
+        if (!in_place && overlap(g, l))
+            return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: grad overlaps logits without being the same rows");
+    }
+    HeadDevice g(h->device);
+    if (!g.ok) return head_fail(h, RLSIM_EDEVICE, "rlsim_head_distill: cannot select the handle's device");
+    DistillArgs a{};
+    a.logits = d->logits;
+    a.stride = d->row_stride;
+    a.rows = d->rows;
+    a.V = d->vocab;
+    a.teacher = d->teacher;
+    a.teacher_stride = d->teacher_stride;
+    a.teacher_dtype = d->teacher_dtype;
+    a.index = d->index;
+    a.index_stride = d->index_stride;
+    a.index64 = d->index_bytes == 8 ? 1u : 0u;
+    a.k = d->k;
+    a.tau = d->temperature;
+    a.inv_tau = 1.0 / (double)d->temperature;
+    a.scale = (float)(1.4426950408889634 / (double)d->temperature);
+    a.rest = d->rest;
+    a.weight = d->weight;
+    a.loss = d->loss;
+    a.grad = d->grad;
+    a.grad_stride = d->grad_stride;
+    if (d->dtype == RLSIM_F32) launch_distill<kHeadF32>(h, a);
+    else if (d->dtype == RLSIM_BF16) launch_distill<kHeadBF16>(h, a);
+    else launch_distill<kHeadF16>(h, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return head_fail(h, RLSIM_EDEVICE, "rlsim_head_distill: launch: %s", hipGetErrorString(e));
+    return RLSIM_OK;
+}
+
+int rlsim_head_destroy(rlsim_head_t* h)
+{
+    if (!h) return RLSIM_OK;
+    int rc = RLSIM_OK;
+    {
+        HeadDevice g(h->device);
+        if (hipStreamSynchronize(h->stream) != hipSuccess) rc = RLSIM_EDEVICE;
+    }
+    delete h;
+    return rc;
+}
+
+const char* rlsim_head_last_error(const rlsim_head_t* h) { return h ? h->err : g_head_err; }
+
+}  // extern "C"

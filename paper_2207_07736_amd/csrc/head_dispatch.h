@@ -1,0 +1,28 @@
+// head_dispatch.h -- which form of an output-head kernel a call runs, as functions
+// of its sizes alone (plain C++).  All forms give the same draws.
+#pragma once
+
+#include <stdint.h>
+
+namespace rlsim_dev {
+
+// Rows of up to 64 entries: a power of two of lanes to a row, one entry a lane.
+constexpr uint32_t kHeadTinyVocab = 64u;
+
+// Threads to a row and strips of 64 16-byte vectors a wave of them holds in
+// registers (0: the row is read again in each pass), for rows of more entries.
+struct HeadForm { uint32_t threads, strips; };
+inline HeadForm head_form(uint32_t vocab, uint32_t elem_bytes)
+{
+    const uint32_t vectors = vocab / (16u / elem_bytes);
+    if (vectors <= 64u * 2u) return {64u, 2u};
+    if (vectors <= 64u * 4u) return {64u, 4u};
+    if (vectors <= 256u * 4u) return {256u, 4u};
+    if (vectors <= 256u * 8u) return {256u, 8u};
+    if (vectors <= 1024u * 4u) return {1024u, 4u};
+    if (vectors <= 1024u * 8u) return {1024u, 8u};
+    if (vectors <= 1024u * 16u) return {1024u, 16u};
+    return {1024u, 0u};
+}
+
+}  // namespace rlsim_dev

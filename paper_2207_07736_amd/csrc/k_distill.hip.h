@@ -1,0 +1,390 @@
+// k_distill.hip.h -- distillation of a student's rows of logits from the top
+// logits of a teacher: the loss of each row and its gradient.
+//
+// The teacher gives k slots of (entry, logit) and, optionally, r, the log of the sum
+// of exp(t / tau) over the entries it does not list.  p is the softmax of t / tau (and
+// r), q the student's softmax of s / tau, and
+//   loss      = tau^2 [ sum_j p_j (ln p_j - ln q_j) + p_r (ln p_r - ln q_r) ]
+//   dloss/ds  = tau (q - p) at a listed entry, tau q (1 - p_r / q_r) elsewhere,
+// q_r being the unlisted entries' part of q.  q_r is summed over these entries alone, against
+// the largest of them (a bit for each entry of the row says which are listed): as
+// 1 - sum q_j it would vanish in rounding where the teacher lists nearly all of the mass.
+// Statistics are fp32; a gradient is rounded once, to the logits' type.
+//
+// A slot is left out if its entry lies outside the row (-1 marks an empty one) or
+// stands in an earlier slot.  A row without any teacher mass has loss 0 and gradient 0
+// whatever its logits; so has the gradient of a row of weight 0.
+//
+// k_distill_tiny: rows of up to 64 entries, a power of two of lanes to a row.
+// k_distill: longer rows, one workgroup to a row, held in registers where it fits
+// (Row), so that loss and gradient cost one read and one write of it.  The gradient
+// may overwrite the logits: a thread writes only what it has read, and the listed
+// entries' exponentials are taken before the first write.
+#pragma once
+
+#include "head_common.hip.h"
+
+namespace rlsim_dev {
+
+struct DistillArgs {
+    const void* logits;
+    uint64_t stride;              // elements from row to row
+    uint32_t rows, V;
+    const void* teacher;          // [rows][k] logits
+    uint64_t teacher_stride;
+    int teacher_dtype;
+    const void* index;            // [rows][k] entries, int32 or int64
+    uint64_t index_stride;
+    uint32_t index64, k;
+    float tau, scale;             // scale: log2(e) / tau
+    double inv_tau;
+    const float* rest;            // [rows] or null
+    const float* weight;          // [rows] or null (1)
+    float* loss;                  // [rows] or null
+    void* grad;                   // or null
+    uint64_t grad_stride;
+};
+
+constexpr uint32_t kNoEntry = 0xFFFFFFFFu;
+
+// A teacher slot: its entry (kNoEntry: left out) and its logit.
+struct Slot { uint32_t entry; float t; };
+__device__ __forceinline__ Slot load_slot(const DistillArgs& a, uint64_t row, uint32_t j)
+{
+    Slot s{kNoEntry, -__builtin_inff()};
+    const uint64_t at = row * a.index_stride + j;
+    const int64_t i = a.index64 ? static_cast<const int64_t*>(a.index)[at] : (int64_t)static_cast<const int32_t*>(a.index)[at];
+    if (i >= 0 && i < (int64_t)a.V) {
+        s.entry = (uint32_t)i;
+        const float t = load_any(a.teacher, row * a.teacher_stride + j, a.teacher_dtype);
+        s.t = t == t ? t : __builtin_inff();      // a NaN must not look like an empty row
+    }
+    return s;
+}
+__device__ __forceinline__ float rest_value(const DistillArgs& a, uint64_t row)
+{
+    const float r = a.rest[row];
+    return r == r ? r : __builtin_inff();
+}
+
+// e^((s - m) / tau) on the exp2 unit, for the row's entries
+__device__ __forceinline__ float exp_entry(const DistillArgs& a, float s, float m)
+{
+    return __builtin_amdgcn_exp2f((s - m) * a.scale);
+}
+// e^x for the few values whose error would show in the loss: the exponent's whole part
+// apart, the rest of it within [-1/2, 1/2] on the unit
+__device__ __forceinline__ float exp_slot(double x)
+{
+    const double z = x * 1.4426950408889634;
+    const double n = __builtin_rint(__builtin_fmax(z, -1000.0));
+    return __builtin_ldexpf(__builtin_amdgcn_exp2f((float)(z - n)), (int)n);
+}
+
+struct Log32 {
+    __device__ double operator()(double x) const { return (double)__builtin_logf((float)x); }
+};
+struct Log64 {
+    __device__ double operator()(double x) const { return ::log(x); }
+};
+
+// The loss is ln(sum of student exponentials / sum of teacher ones) plus the mean over p of
+// (t - mt) / tau - (s - m) / tau, the logits against their largest.  It is small where
+// the student follows its teacher, so what is left of it after the cancellation needs
+// more than fp32: differences, and in longer rows sums and logarithms, are in 64
+// bits, which for a few values a row costs nothing beside the row.
+// e (x - y) with 0 for e = 0
+__device__ __forceinline__ double excess(float e, double x, double y)
+{
+    return e == 0.0f ? 0.0 : (double)e * (x - y);
+}
+
+// A student's row: the largest logit m, and mu and sum, the largest of the pass's entries
+// (the unlisted ones where there is a rest, else all) and the sum of their exponentials
+// against it, which so cannot vanish beside the listed ones'.  listed: the others' sum
+// against m.  0 stands for a largest logit of -inf.
+struct Student {
+    float m, mu;
+    double sum, whole;
+    float share;                                  // e^((mu - m) / tau)
+};
+// ln of an entry's part of `whole`, and (log_rest) of the unlisted entries'
+__device__ __forceinline__ double log_part(const DistillArgs& a, float logit, float m)
+{
+    return ((double)logit - (double)m) * a.inv_tau;
+}
+__device__ __forceinline__ Student student_row(const DistillArgs& a, float m, float mu, double sum, double listed)
+{
+    Student s{m, mu, sum, 0.0, 0.0f};
+    s.share = sum == 0.0 ? 0.0f : exp_slot(log_part(a, mu, m));
+    s.whole = listed + sum * s.share;
+    return s;
+}
+template <class Log>
+__device__ __forceinline__ double log_rest(const DistillArgs& a, const Student& s, Log log)
+{
+    return s.sum == 0.0 ? -__builtin_inf() : log_part(a, s.mu, s.m) + log(s.sum);
+}
+// `excesses`: their sum over the teacher's values, whose exponentials sum to sum_t
+template <class Log>
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const Student& s, double excesses, double sum_t, Log log)
+{
+    const double mean = excesses / sum_t;         // +inf where q = 0 < p
+    return a.tau * a.tau * (float)(s.whole == 0.0 ? mean : mean + log(s.whole / sum_t));
+}
+
+// What a row's gradient is made of: listed entries e^((s - m) / tau) listed - p weighted,
+// others e^((s - mu) / tau) other.
+struct GradScale { float weighted, listed, other; };
+__device__ __forceinline__ GradScale grad_scale(const DistillArgs& a, const Student& s, float weight, float p_rest)
+{
+    GradScale g;
+    g.weighted = a.tau * weight;
+    const float inv = s.whole == 0.0 ? 0.0f : 1.0f / (float)s.whole;     // a row of -inf: q = 0
+    g.listed = g.weighted * inv;
+    g.other = g.weighted * (s.share * inv - (p_rest == 0.0f || s.sum == 0.0 ? 0.0f : p_rest / (float)s.sum));
+    return g;
+}
+
+// ---------------------------------------------------------------------------
+template <int D, int G>
+__global__ __launch_bounds__(256) void k_distill_tiny(DistillArgs a)
+{
+    using El = Elem<D>;
+    const uint32_t e = threadIdx.x % G;
+    const uint32_t per_group = 256u / G;
+    const float none = -__builtin_inff();
+    auto row_max = [](float x) {
+#pragma unroll
+        for (int off = G / 2; off >= 1; off /= 2) x = __builtin_fmaxf(x, __shfl_xor(x, off, G));
+        return x;
+    };
+    auto row_total = [](float x) {
+#pragma unroll
+        for (int off = G / 2; off >= 1; off /= 2) x += __shfl_xor(x, off, G);
+        return x;
+    };
+    for (uint32_t first = blockIdx.x * per_group; first < a.rows; first += gridDim.x * per_group) {
+        const uint32_t row = first + threadIdx.x / G;
+        const bool live_row = row < a.rows;
+        const uint32_t r = live_row ? row : a.rows - 1u;
+        const float s = e < a.V ? El::one(static_cast<const typename El::Word*>(a.logits)[(uint64_t)r * a.stride + e]) : none;
+        const float weight = a.weight ? a.weight[r] : 1.0f;
+        const float rest = a.rest ? rest_value(a, r) : none;
+        // this entry's slot: the first that names it
+        bool listed = false;
+        float t = none;
+        for (uint32_t j0 = 0; j0 < a.k; j0 += G) {
+            const Slot slot = j0 + e < a.k ? load_slot(a, r, j0 + e) : Slot{kNoEntry, none};
+            const uint32_t n = min((uint32_t)G, a.k - j0);
+            for (uint32_t j = 0; j < n; ++j) {
+                const uint32_t entry = (uint32_t)__shfl((int)slot.entry, (int)j, G);
+                const float tj = __shfl(slot.t, (int)j, G);
+                t = entry == e && !listed ? tj : t;
+                listed = listed || entry == e;
+            }
+        }
+        const double mt = __builtin_fmax((double)row_max(t) * a.inv_tau, (double)rest);
+        const bool apart = a.rest && listed;          // not among the entries of the rest
+        const float m0 = row_max(s), mu0 = row_max(apart ? none : s);
+        const float m = m0 == none ? 0.0f : m0, mu = mu0 == none ? 0.0f : mu0;
+        const bool empty = mt == -__builtin_inf();
+        const double x = (double)t * a.inv_tau - mt, x_rest = (double)rest - mt;
+        const float et = listed ? exp_slot(x) : 0.0f, e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
+        const float sum_t = row_total(et) + e_rest;
+        const float p = et / sum_t, p_rest = a.rest ? e_rest / sum_t : 0.0f;
+        const float es = e >= a.V ? 0.0f : apart ? exp_slot(log_part(a, s, m)) : exp_entry(a, s, mu);
+        const float sum = row_total(apart ? 0.0f : es);
+        const Student st = student_row(a, m, mu, sum, row_total(apart ? es : 0.0f));
+        double d = row_total(listed ? (float)excess(et, x, log_part(a, s, m)) : 0.0f);
+        if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log32()));
+        if (!live_row) continue;
+        if (a.loss && e == 0u) a.loss[row] = empty ? 0.0f : row_loss(a, st, d, sum_t, Log32());
+        if (a.grad && e < a.V) {
+            const GradScale g = grad_scale(a, st, weight, p_rest);
+            float ds = es * (apart ? g.listed : g.other) - (listed ? p * g.weighted : 0.0f);
+            if (empty || weight == 0.0f) ds = 0.0f;
+            static_cast<typename El::Word*>(a.grad)[(uint64_t)row * a.grad_stride + e] = El::word(ds);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Shared memory beside the floats of the reductions: k entries, k teacher values
+// (then probabilities), k student exponentials and, with a rest, a bit for each entry
+// of the row.
+inline __host__ __device__ uint32_t distill_shared_bytes(uint32_t k, uint32_t V, bool rest)
+{
+    return 12u * k + (rest ? (V + 31u) / 32u * 4u : 0u);
+}
+
+template <int D, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_distill(DistillArgs a)
+{
+    using R = Row<D, NT, NV>;
+    using El = Elem<D>;
+    constexpr uint32_t E = R::E;
+    constexpr int NW = NT / 64;
+    __shared__ float sh[3][NW];
+    __shared__ double sh64[4][NW];
+    extern __shared__ uint32_t slots[];
+    uint32_t* const entry = slots;
+    float* const prob = reinterpret_cast<float*>(slots + a.k);          // t, then p
+    float* const logit = reinterpret_cast<float*>(slots + 2u * a.k);    // the student's
+    uint32_t* const bits = slots + 3u * a.k;
+    const uint32_t tid = threadIdx.x;
+    const float none = -__builtin_inff();
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        R x;
+        x.open(a.logits, row, a.stride, a.V);
+        char* const grad = a.grad ? static_cast<char*>(a.grad) + row * a.grad_stride * El::kBytes : nullptr;
+        auto store = [&](uint32_t i, const Vec16& v) {
+            typename El::Run r;
+            for (uint32_t j = 0; j < 4u; ++j) r.w[j] = v.w[j];
+            if (i < x.vectors) reinterpret_cast<typename El::Run*>(grad)[i] = r;
+        };
+        auto store_one = [&](uint32_t i, float v) { reinterpret_cast<typename El::Word*>(grad)[i] = El::word(v); };
+        const float weight = a.weight ? a.weight[row] : 1.0f;
+        const float rest = a.rest ? rest_value(a, row) : none;
+        for (uint32_t j = tid; j < a.k; j += NT) {
+            const Slot s = load_slot(a, row, j);
+            entry[j] = s.entry;
+            prob[j] = s.t;
+        }
+        if (a.rest)
+            for (uint32_t j = tid; j < (a.V + 31u) / 32u; j += NT) bits[j] = 0u;
+        __syncthreads();
+        // leave out slots that repeat an earlier one's entry; the others' student logits
+        uint32_t repeats = 0u;            // a bit for each of this thread's slots
+        float top_t = none;
+        for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) {
+            const uint32_t mine = entry[j];
+            if (mine == kNoEntry) continue;
+            bool again = false;
+            for (uint32_t i = 0; i < j; ++i) again = again || entry[i] == mine;
+            if (again) {
+                repeats |= b;
+            } else {
+                top_t = __builtin_fmaxf(top_t, prob[j]);
+                logit[j] = x.entry(mine);
+                if (a.rest) atomicOr(&bits[mine / 32u], 1u << (mine % 32u));
+            }
+        }
+        const double mt = __builtin_fmax((double)group_max<NW>(top_t, sh[0]) * a.inv_tau, (double)rest);
+        __syncthreads();
+        const bool empty = mt == -__builtin_inf();
+        auto teacher = [&](uint32_t j) { return (double)prob[j] * a.inv_tau - mt; };
+        if (empty || (weight == 0.0f && !a.loss)) {
+            if (a.loss && tid == 0u) a.loss[row] = 0.0f;
+            if (grad) {
+                for (uint32_t v = 0; v < x.seg; ++v)
+                    if (x.any(v)) store(x.index(v), Vec16{{0u, 0u, 0u, 0u}});
+                if (tid < x.tail) store_one(x.vectors * E + tid, 0.0f);
+            }
+            __syncthreads();
+            continue;
+        }
+        double part = 0.0;
+        for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) {
+            if (repeats & b) entry[j] = kNoEntry;
+            if (entry[j] != kNoEntry) part += (double)exp_slot(teacher(j));
+        }
+        const double x_rest = (double)rest - mt;
+        const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
+        const double sum_t = group_total<NW>(part, sh64[0]) + (double)e_rest;
+        const float inv_t = 1.0f / (float)sum_t, p_rest = a.rest ? e_rest * inv_t : 0.0f;
+        // the student's row; with a rest, without the listed entries
+        auto unlisted = [&](const Vec16& y, uint32_t i) {
+            Vec16 v = y;
+            const uint32_t first = i * E;
+            const uint32_t b = a.rest && i < x.vectors ? bits[first / 32u] >> (first % 32u) & ((1u << E) - 1u) : 0u;
+            if (b) {
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) v = b >> e & 1u ? El::with_neg_inf(v, e) : v;
+            }
+            return v;
+        };
+        if (a.rest) {
+            if (NV) x.apply(unlisted);
+            const uint32_t i = x.vectors * E + x.lane;
+            if (x.lane < x.tail && (bits[i / 32u] >> (i % 32u) & 1u)) x.last = none;
+        }
+        auto each = [&](auto f) {
+            x.each_vector([&](const Vec16& y, uint32_t i) {
+                const Vec16 v = NV ? y : unlisted(y, i);
+                float s[E];
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) s[e] = El::get(v, e);
+                f(s);
+            });
+        };
+        float top = x.last;
+        each([&](const float (&s)[E]) {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) top = __builtin_fmaxf(top, s[e]);
+        });
+        const float mu0 = group_max<NW>(top, sh[1]);
+        const float mu = mu0 == none ? 0.0f : mu0;
+        // a vector's entries by pairs, then the vectors: short chains of roundings
+        float m = mu0, sum = x.wave == 0u ? exp_entry(a, x.last, mu) : 0.0f;
+        each([&](const float (&s)[E]) {
+            float v[E];
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) v[e] = exp_entry(a, s[e], mu);
+#pragma unroll
+            for (uint32_t n = E / 2u; n >= 1u; n /= 2u)
+#pragma unroll
+                for (uint32_t e = 0; e < n; ++e) v[e] += v[e + n];
+            sum += v[0];
+        });
+        const double all = group_total<NW>((double)sum, sh64[1]);
+        double listed = 0.0;
+        if (a.rest) {
+            top = none;
+            for (uint32_t j = tid; j < a.k; j += NT)
+                if (entry[j] != kNoEntry) top = __builtin_fmaxf(top, logit[j]);
+            m = __builtin_fmaxf(m, group_max<NW>(top, sh[2]));
+        }
+        m = m == none ? 0.0f : m;
+        if (a.rest) {
+            for (uint32_t j = tid; j < a.k; j += NT)
+                if (entry[j] != kNoEntry) listed += (double)exp_slot(log_part(a, logit[j], m));
+            listed = group_total<NW>(listed, sh64[2]);
+        }
+        const Student st = student_row(a, m, mu, all, listed);
+        double d = 0.0;
+        for (uint32_t j = tid; j < a.k; j += NT) {
+            if (entry[j] == kNoEntry) continue;
+            const double t = teacher(j);
+            const float e = exp_slot(t);
+            d += excess(e, t, log_part(a, logit[j], m));
+            prob[j] = e * inv_t;
+        }
+        if (a.loss) {
+            d = group_total<NW>(d, sh64[3]);
+            if (tid == 0u) {
+                if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log64()));
+                a.loss[row] = row_loss(a, st, d, sum_t, Log64());
+            }
+        }
+        if (grad) {
+            const GradScale g = grad_scale(a, st, weight, p_rest);
+            const bool zero = weight == 0.0f;
+            auto other = [&](float s) { return zero ? 0.0f : exp_entry(a, s, mu) * g.other; };
+            x.each_vector([&](const Vec16& y, uint32_t i) {
+                float f[E];
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) f[e] = other(El::get(y, e));
+                store(i, El::pack(f));
+            });
+            if (tid < x.tail) store_one(x.vectors * E + tid, other(x.last));
+            __syncthreads();              // the listed entries over what the row's pass wrote
+            for (uint32_t j = tid; j < a.k; j += NT)
+                if (entry[j] != kNoEntry)
+                    store_one(entry[j], zero ? 0.0f : exp_slot(log_part(a, logit[j], m)) * g.listed - prob[j] * g.weighted);
+        }
+        __syncthreads();                  // the row's shared memory is used again
+    }
+}
+
+}  // namespace rlsim_dev

@@ -1,0 +1,650 @@
+// k_sample.hip.h -- draw one entry of each row of logits from given uniform
+// numbers, after temperature, top-k, top-p and min-p.
+//
+// With m the row's largest logit (NaN counts as -inf), c = log2(e) / T and
+// z_i = (l_i - m) c, entry i weighs w_i = 2^40 2^z_i.  Weights are whole numbers
+// (entry_weight), so every sum is exact and no split of a row over lanes, waves or
+// strips changes a draw.  Entries are ranked by logit, equal ones by index; every
+// filter keeps a first part of that order:
+//   top-k   the first k entries
+//   top-p   of those, each whose predecessors weigh less than
+//           floor(p 2^24) W / 2^24 (rounded down), W their sum; and the first
+//   min-p   each that weighs at least floor(min_p 2^40)
+// The draw is the lowest index whose running sum of kept weights exceeds
+// floor(u 2^24) W' / 2^24 (rounded down), W' the kept sum.  The
+// log-probability is (l - m) / T - ln(W' / 2^40).
+//
+// k_sample_tiny: rows of up to 64 entries, a power of two of lanes to a row; ranks
+// by comparing every pair of a row's lanes.
+// k_sample: longer rows, one workgroup to a row, held in registers where it fits
+// (Row).  The end of the kept part is found without sorting: the entries' weights
+// and counts are binned by z in steps of 1/8, the bin in which the cut lies is
+// gathered, and an ever finer part of the rank's 64-bit code (logit, then index) is
+// binned until few enough entries are left to compare each with each.
+#pragma once
+
+#include "head_common.hip.h"
+
+namespace rlsim_dev {
+
+struct SampleArgs {
+    const void* logits;
+    uint64_t stride;              // elements from row to row
+    uint32_t rows, V;
+    float T, top_p, min_p;        // one value for the call ...
+    uint32_t top_k;               // (0: all)
+    const float* T_rows;          // ... or one for each row, where not null
+    const int32_t* top_k_rows;
+    const float* top_p_rows;
+    const float* min_p_rows;
+    const float* u;
+    int32_t* token;
+    float* logp;                  // or null
+};
+
+// A row's settings.  T <= 0 or NaN: the first of the largest entries.
+struct SampleRow {
+    float T, c;
+    uint32_t k;                   // V: all
+    uint32_t p24;                 // floor(p 2^24), 2^24: all
+    uint64_t least;               // smallest weight kept
+    uint32_t u24;
+    bool greedy;
+};
+
+constexpr uint32_t kAllP = 1u << 24;
+
+__device__ __forceinline__ SampleRow sample_row(const SampleArgs& a, uint32_t row)
+{
+    SampleRow s;
+    s.T = a.T_rows ? a.T_rows[row] : a.T;
+    const int32_t k = a.top_k_rows ? a.top_k_rows[row] : (int32_t)(a.top_k < a.V ? a.top_k : 0u);
+    const float p = a.top_p_rows ? a.top_p_rows[row] : a.top_p;
+    const float min_p = a.min_p_rows ? a.min_p_rows[row] : a.min_p;
+    s.k = k > 0 && (uint32_t)k < a.V ? (uint32_t)k : a.V;
+    s.p24 = p < 1.0f ? (uint32_t)(__builtin_fmaxf(p, 0.0f) * 0x1p24f) : kAllP;     // NaN: all
+    s.least = min_p > 0.0f ? (uint64_t)(__builtin_fminf(min_p, 1.0f) * 0x1p40f) : 0u;
+    s.u24 = (uint32_t)(__builtin_fminf(__builtin_fmaxf(a.u[row], 0.0f), 1.0f - 0x1p-24f) * 0x1p24f);
+    s.greedy = !(s.T > 0.0f) || s.k == 1u;
+    s.c = 0x1.715476p+0f / s.T;
+    return s;
+}
+
+// floor(whole share / 2^24) for share <= 2^24 and whole < 2^62
+__device__ __forceinline__ uint64_t share24(uint64_t whole, uint32_t share)
+{
+    return (whole >> 24) * share + (((whole & 0xFFFFFFu) * share) >> 24);
+}
+
+// z = (l - m) c, 0 for the largest entries (also where m or c is infinite); weights
+// are 0 where z < kLastZ or NaN.
+constexpr float kLastZ = -41.0f;
+__device__ __forceinline__ float entry_z(float l, float m, float c) { return l == m ? 0.0f : (l - m) * c; }
+
+// 2^40 2^z as a whole number: 2^f on [-1/2, 1/2] in fp32, Horner form with one
+// rounding per operation and coefficients scaled by 2^24 (relative error 1.9e-7),
+// truncated, then shifted by the whole part of z.
+__device__ __forceinline__ uint64_t entry_weight(float z)
+{
+    const float n = __builtin_rintf(z);
+    const float f = z - n;
+    float P = f * 0x1.5bb994p+14f + 0x1.3cea84p+17f;
+    P = P * f + 0x1.c6b754p+19f;
+    P = P * f + 0x1.ebf9bcp+21f;
+    P = P * f + 0x1.62e42ap+23f;
+    P = P * f + 0x1p24f;
+    const uint64_t w = ((uint64_t)(uint32_t)P << 16) >> ((uint32_t)-n & 63u);
+    return z >= kLastZ ? w : 0u;
+}
+
+// Ascending in rank: larger logits first, then lower indices.  -0 and +0 are equal.
+__device__ __forceinline__ uint64_t rank_code(float l, uint32_t i)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, l + 0.0f);
+    const uint32_t down = b >> 31 ? b : ~b & 0x7FFFFFFFu;
+    return (uint64_t)down << 32 | i;
+}
+
+__device__ __forceinline__ float sample_logp(float l, float m, float T, uint64_t whole)
+{
+    const float above = l == m ? 0.0f : (l - m) / T;
+    return above - __builtin_logf((float)whole * 0x1p-40f);
+}
+
+// ---------------------------------------------------------------------------
+template <int D, int G>
+__global__ __launch_bounds__(256) void k_sample_tiny(SampleArgs a)
+{
+    using El = Elem<D>;
+    const uint32_t e = threadIdx.x % G;
+    const uint32_t per_group = 256u / G;
+    // every lane of a wave runs the same number of rounds
+    for (uint32_t first = blockIdx.x * per_group; first < a.rows; first += gridDim.x * per_group) {
+        const uint32_t row = first + threadIdx.x / G;
+        const bool live_row = row < a.rows;
+        const uint32_t r = live_row ? row : a.rows - 1u;
+        const SampleRow s = sample_row(a, r);
+        float l = -__builtin_inff();
+        if (e < a.V) {
+            const float x = El::one(static_cast<const typename El::Word*>(a.logits)[(uint64_t)r * a.stride + e]);
+            l = x == x ? x : l;
+        }
+        float m = l;
+#pragma unroll
+        for (int off = G / 2; off >= 1; off /= 2) m = __builtin_fmaxf(m, __shfl_xor(m, off, G));
+        uint64_t w = l > -__builtin_inff() ? entry_weight(entry_z(l, m, s.c)) : 0u;
+        uint32_t rank = 0u;               // entries before this one, and what they weigh
+        uint64_t before = 0u;
+        if (s.k < a.V || s.p24 < kAllP || s.greedy) {
+            for (uint32_t j = 0; j < a.V; ++j) {
+                const float lj = __shfl(l, (int)j, G);
+                const uint64_t wj = __shfl(w, (int)j, G);
+                const bool ahead = lj > l || (lj == l && j < e);
+                rank += ahead ? 1u : 0u;
+                before += ahead ? wj : 0u;
+            }
+            uint64_t whole = rank < s.k ? w : 0u;
+#pragma unroll
+            for (int off = G / 2; off >= 1; off /= 2) whole += __shfl_xor(whole, off, G);
+            const bool keep = rank == 0u || (!s.greedy && rank < s.k && (s.p24 == kAllP || before < share24(whole, s.p24)));
+            w = keep ? w : 0u;
+        }
+        w = w >= s.least ? w : 0u;
+        uint64_t running = w;
+#pragma unroll
+        for (int off = 1; off < G; off *= 2) {
+            const uint64_t x = __shfl_up(running, (unsigned)off, G);
+            running += e >= (uint32_t)off ? x : 0u;
+        }
+        const uint64_t whole = __shfl(running, G - 1, G);
+        const uint64_t target = share24(whole, s.u24);
+        // one lane of a row holds the step in which the running sum passes the target
+        if (live_row && running > target && running - w <= target) {
+            a.token[row] = (int32_t)e;
+            if (a.logp) a.logp[row] = s.greedy ? 0.0f : sample_logp(l, m, s.T, whole);
+        }
+        if (live_row && e == 0u && m == -__builtin_inff()) {
+            a.token[row] = -1;
+            if (a.logp) a.logp[row] = 0.0f;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+constexpr uint32_t kBins = 384u;          // bins of z: -8 z, 0 .. 328
+constexpr uint32_t kSubBins = 256u;       // bins of eight bits of a code
+constexpr uint32_t kFew = 128u;           // entries compared each with each
+
+template <int NT>
+struct SampleShared {
+    static constexpr uint32_t NW = NT / 64;
+    static constexpr uint32_t kList = NT == 64 ? 256u : NT == 256 ? 1024u : 4096u;
+    float f[NW];
+    uint64_t sum[NW + 1], group[NW];
+    uint32_t n[kBins];
+    uint64_t w[kBins];
+    uint32_t sub_n[kSubBins];
+    uint64_t sub_w[kSubBins];
+    uint64_t list_code[kList], list_w[kList];
+    uint64_t few_code[kFew], few_w[kFew];
+    uint32_t found;                       // bin of the cut
+    uint64_t before_n, before_w;          // entries, and weight, of the bins before it
+    uint64_t cut, cut_w;                  // code of the entry looked for, weight up to it
+    uint32_t count, few, low, best;
+};
+
+// First bin at which the running sum of counts (by_weight: of weights) reaches
+// `target`; B bins, B / 64 to a lane.  Run by the first wave.
+template <uint32_t B, class Sh>
+__device__ __forceinline__ void find_bin(Sh& sh, const uint32_t* n, const uint64_t* w, bool by_weight, uint64_t target)
+{
+    constexpr uint32_t P = B / 64u;
+    const uint32_t lane = threadIdx.x;
+    uint64_t sn = 0u, sw = 0u;
+#pragma unroll
+    for (uint32_t j = 0; j < P; ++j) {
+        sn += n[lane * P + j];
+        sw += w[lane * P + j];
+    }
+    const uint64_t tn = wave_scan(sn), tw = wave_scan(sw);
+    uint64_t bn = tn - sn, bw = tw - sw;
+    const uint64_t before = by_weight ? bw : bn, upto = by_weight ? tw : tn;
+    if (before < target && target <= upto) {
+#pragma unroll
+        for (uint32_t j = 0; j < P; ++j) {
+            const uint64_t n_j = n[lane * P + j], w_j = w[lane * P + j];
+            const uint64_t b = by_weight ? bw : bn, m = by_weight ? w_j : n_j;
+            if (b < target && target <= b + m) {
+                sh.found = lane * P + j;
+                sh.before_n = bn;
+                sh.before_w = bw;
+            }
+            bn += n_j;
+            bw += w_j;
+        }
+    }
+}
+
+// Entries among which one is looked for: those whose code - first, shifted by
+// `shift`, is `prefix` (64: all); n of them, behind others of the given count and
+// weight.
+struct Among {
+    uint64_t first, prefix;
+    uint32_t shift, n;
+    uint64_t before_n, before_w;
+    __device__ __forceinline__ bool holds(uint64_t code) const { return shift == 64u || (code - first) >> shift == prefix; }
+};
+
+// Narrow `in` by eight bits of the codes: to the bin in which the running count
+// (by_weight: weight) in the codes' order reaches `target`.  visit(f) calls f(code,
+// weight) for this thread's entries.
+template <uint32_t NT, class Sh, class Visit>
+__device__ __forceinline__ void narrow(Sh& sh, Among& in, Visit visit, bool by_weight, uint64_t target)
+{
+    const uint32_t down = in.shift < 8u ? 0u : in.shift - 8u;
+    for (uint32_t j = threadIdx.x; j < kSubBins; j += NT) {
+        sh.sub_n[j] = 0u;
+        sh.sub_w[j] = 0u;
+    }
+    __syncthreads();
+    visit([&](uint64_t code, uint64_t w) {
+        if (in.holds(code)) {
+            const uint32_t b = (uint32_t)((code - in.first) >> down) & 255u;
+            atomicAdd(&sh.sub_n[b], 1u);
+            atomicAdd((unsigned long long*)&sh.sub_w[b], (unsigned long long)w);
+        }
+    });
+    __syncthreads();
+    if (threadIdx.x < 64u)
+        find_bin<kSubBins>(sh, sh.sub_n, sh.sub_w, by_weight, target - (by_weight ? in.before_w : in.before_n));
+    __syncthreads();
+    in.prefix = (in.shift == 64u ? 0u : in.prefix << (in.shift - down)) | sh.found;
+    in.shift = down;
+    in.n = sh.sub_n[sh.found];
+    in.before_n += sh.before_n;
+    in.before_w += sh.before_w;
+    __syncthreads();
+}
+
+// The listed entry at which the running count (by_weight: weight) in the order of the
+// codes reaches `target`: its code goes to sh.cut, the weight up to and with it to
+// sh.cut_w.  code_of and weight_of give a listed entry's.
+template <uint32_t NT, class Sh, class Code, class Weight>
+__device__ __forceinline__ void find_listed(Sh& sh, Among in, uint32_t listed, Code code_of, Weight weight_of, bool by_weight,
+                                            uint64_t target)
+{
+    auto visit = [&](auto f) {
+        for (uint32_t j = threadIdx.x; j < listed; j += NT) f(code_of(j), weight_of(j));
+    };
+    while (in.n > kFew) narrow<NT>(sh, in, visit, by_weight, target);
+    if (threadIdx.x == 0u) sh.few = 0u;
+    __syncthreads();
+    visit([&](uint64_t code, uint64_t w) {
+        if (in.holds(code)) {
+            const uint32_t at = atomicAdd(&sh.few, 1u);
+            sh.few_code[at] = code;
+            sh.few_w[at] = w;
+        }
+    });
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < in.n; i += NT) {
+        const uint64_t code = sh.few_code[i], own = sh.few_w[i];
+        uint64_t bn = in.before_n, bw = in.before_w;
+        for (uint32_t j = 0; j < in.n; ++j) {
+            const bool ahead = sh.few_code[j] < code;
+            bn += ahead ? 1u : 0u;
+            bw += ahead ? sh.few_w[j] : 0u;
+        }
+        const uint64_t b = by_weight ? bw : bn, mine = by_weight ? own : 1u;
+        if (b < target && target <= b + mine) {
+            sh.cut = code;
+            sh.cut_w = bw + own;
+        }
+    }
+    __syncthreads();
+}
+
+// The shift by which codes of `bits` bits show their first eight.
+__device__ __forceinline__ uint32_t first_shift(uint32_t bits) { return bits > 8u ? bits - 8u : 0u; }
+
+template <int D, int NT, int NV>
+struct SampleGroup {
+    using R = Row<D, NT, NV>;
+    using Sh = SampleShared<NT>;
+    using El = Elem<D>;
+    static constexpr uint32_t E = R::E, NW = R::NW;
+
+    const SampleArgs& a;
+    Sh& sh;
+    R& x;
+    const SampleRow& s;
+    const uint32_t row;
+    const float m;
+
+    __device__ __forceinline__ float z(float l) const { return entry_z(l, m, s.c); }
+    __device__ __forceinline__ void answer(uint32_t i, float logp) const
+    {
+        a.token[row] = (int32_t)i;
+        if (a.logp) a.logp[row] = logp;
+    }
+
+    // The draw from the whole row, with the weights weigh(entry, index): the wave's
+    // part, then the thread's, then the entry in which the running sum passes the
+    // target.  `mine` and `end` are this thread's sums over its vectors and its tail entry.
+    template <class F>
+    __device__ __forceinline__ void draw(uint64_t mine, uint64_t end, F weigh)
+    {
+        mine = wave_total(mine);
+        if (x.lane == 0u) sh.sum[x.wave] = mine;
+        if (x.wave == 0u) {
+            const uint64_t t = wave_total(end);
+            if (x.lane == 0u) sh.sum[NW] = t;
+        }
+        __syncthreads();
+        uint64_t whole = 0u;
+        for (uint32_t j = 0; j <= NW; ++j) whole += sh.sum[j];
+        const uint64_t target = share24(whole, s.u24);
+        uint64_t before = 0u;
+        uint32_t part = 0u;
+        while (part < NW && before + sh.sum[part] <= target) before += sh.sum[part++];
+        if (part == NW) {                 // the tail's lanes
+            if (x.wave == 0u) {
+                const uint64_t upto = before + wave_scan(end);
+                if (upto > target && upto - end <= target) answer(x.vectors * E + x.lane, sample_logp(x.last, m, s.T, whole));
+            }
+            return;
+        }
+        // the part's vectors, a run of consecutive ones to each thread
+        const uint32_t run = (x.seg * 64u + NT - 1u) / NT;
+        const uint32_t v0 = part * x.seg * 64u + threadIdx.x * run;
+        const uint32_t limit = min((part + 1u) * x.seg * 64u, x.vectors), v1 = min(v0 + run, limit);
+        uint64_t own = 0u;
+        for (uint32_t v = v0; v < v1; ++v) {
+            const Vec16 y = x.vector(v);
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) own += weigh(El::get(y, e), v * E + e);
+        }
+        uint64_t upto = wave_scan(own);
+        if (NW > 1u) {
+            if (x.lane == 63u) sh.group[x.wave] = upto;
+            __syncthreads();
+            for (uint32_t j = 0; j < x.wave; ++j) before += sh.group[j];
+        }
+        upto += before;
+        if (upto > target && upto - own <= target) {
+            uint64_t t = upto - own;
+            for (uint32_t i = v0 * E; i < v1 * E; ++i) {
+                const float l = x.entry(i);
+                t += weigh(l, i);
+                if (t > target) {
+                    answer(i, sample_logp(l, m, s.T, whole));
+                    break;
+                }
+            }
+        }
+    }
+
+    // List the entry if z >= from.  sh.count counts (only the first kList are listed),
+    // sh.low gets the logit part of the lowest rank.
+    __device__ __forceinline__ void list_one(float l, uint32_t i, float from)
+    {
+        const float zi = z(l);
+        if (zi >= from) {
+            const uint64_t code = rank_code(l, i);
+            const uint32_t at = atomicAdd(&sh.count, 1u);
+            if (at < Sh::kList) {
+                sh.list_code[at] = code;
+                sh.list_w[at] = entry_weight(zi);
+            }
+            atomicMax(&sh.low, (uint32_t)(code >> 32));
+        }
+    }
+    // The same for a vector's entries; also(z) sees each of them.  Few are listed: they
+    // are read again one by one, which keeps the code small.
+    template <class F>
+    __device__ __forceinline__ void list_vector(const Vec16& y, uint32_t v, float from, F also)
+    {
+        uint32_t near = 0u;
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e) {
+            const float zi = z(El::get(y, e));
+            also(zi);
+            near |= zi >= from ? 1u << e : 0u;
+        }
+        while (near) {
+            const uint32_t i = v * E + (uint32_t)__builtin_ctz(near);
+            list_one(x.entry(i), i, from);
+            near &= near - 1u;
+        }
+    }
+    __device__ __forceinline__ void clear_list()
+    {
+        __syncthreads();
+        if (threadIdx.x == 0u) {
+            sh.count = 0u;
+            sh.low = 0u;
+        }
+        __syncthreads();
+    }
+
+    // Cut and draw from the list.  `all`: no live entry is missing from it; whole: the
+    // row's weight where top-p is the first cut, else 0.  False: the list does not reach
+    // the cut.
+    __device__ __forceinline__ bool draw_listed(bool all, uint64_t whole)
+    {
+        const uint32_t listed = sh.count;
+        if (listed > Sh::kList) return false;
+        uint64_t weight = 0u;             // of the list
+        for (uint32_t j = threadIdx.x; j < listed; j += NT) weight += sh.list_w[j];
+        weight = wave_total(weight);
+        if (x.lane == 0u) sh.sum[x.wave] = weight;
+        __syncthreads();
+        weight = 0u;
+        for (uint32_t j = 0; j < NW; ++j) weight += sh.sum[j];
+        const uint64_t first = rank_code(m, 0u);
+        const uint32_t span = sh.low - (uint32_t)(first >> 32);
+        const uint32_t bits = span ? 64u - (uint32_t)__builtin_clz(span) : 32u - (uint32_t)__builtin_clz(a.V);
+        const Among rank{first, 0u, first_shift(bits) + 8u, listed, 0u, 0u};
+        auto code = [&](uint32_t j) { return sh.list_code[j]; };
+        auto plain = [&](uint32_t j) { return sh.list_w[j]; };
+        uint64_t cut = ~0ull;
+        // top-k, then top-p: one piece of code for both
+        for (uint32_t by_weight = 0u; by_weight < 2u; ++by_weight) {
+            uint64_t target = s.k;
+            if (by_weight == 0u) {
+                if (s.k == a.V) continue;
+                if (listed < s.k && !all) return false;
+                if (listed <= s.k) {
+                    whole = weight;
+                    continue;
+                }
+            } else {
+                if (s.p24 == kAllP) continue;
+                target = share24(whole, s.p24);
+                target = target ? target : 1u;
+                if (weight < target) return false;
+            }
+            find_listed<NT>(sh, rank, listed, code, plain, by_weight != 0u, target);
+            cut = sh.cut;
+            if (by_weight == 0u) whole = sh.cut_w;
+        }
+        // what is left, by index
+        auto index = [&](uint32_t j) { return sh.list_code[j] & 0xFFFFFFFFu; };
+        auto kept = [&](uint32_t j) {
+            const uint64_t w = sh.list_w[j];
+            return sh.list_code[j] <= cut && w >= s.least ? w : 0u;
+        };
+        weight = 0u;
+        for (uint32_t j = threadIdx.x; j < listed; j += NT) weight += kept(j);
+        weight = wave_total(weight);
+        __syncthreads();
+        if (x.lane == 0u) sh.sum[x.wave] = weight;
+        __syncthreads();
+        weight = 0u;
+        for (uint32_t j = 0; j < NW; ++j) weight += sh.sum[j];
+        const Among order{0u, 0u, first_shift(32u - (uint32_t)__builtin_clz(a.V)) + 8u, listed, 0u, 0u};
+        find_listed<NT>(sh, order, listed, index, kept, true, share24(weight, s.u24) + 1u);
+        if (threadIdx.x == 0u) {
+            const uint32_t i = (uint32_t)sh.cut;
+            answer(i, sample_logp(x.entry(i), m, s.T, weight));
+        }
+        return true;
+    }
+
+    // Cut and draw where too many entries are close to the largest: bins of z for the
+    // whole row, the cut's bin listed, then a pass over the row.
+    __device__ __forceinline__ void draw_dense()
+    {
+        auto each_live = [&](auto f) {
+            x.each_again([&](float l, uint32_t i) {
+                const float zi = z(l);
+                if (zi >= kLastZ) f(l, i, zi);
+            });
+        };
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < kBins; j += NT) {
+            sh.n[j] = 0u;
+            sh.w[j] = 0u;
+        }
+        __syncthreads();
+        each_live([&](float, uint32_t, float zi) {
+            const uint32_t b = (uint32_t)(zi * -8.0f);
+            atomicAdd(&sh.n[b], 1u);
+            atomicAdd((unsigned long long*)&sh.w[b], (unsigned long long)entry_weight(zi));
+        });
+        __syncthreads();
+        uint64_t n = 0u, whole = 0u;      // the row's, in every thread
+        for (uint32_t j = x.lane; j < kBins; j += 64u) {
+            n += sh.n[j];
+            whole += sh.w[j];
+        }
+        n = wave_total(n);
+        whole = wave_total(whole);
+        uint64_t cut = ~0ull;
+        for (uint32_t by_weight = 0u; by_weight < 2u; ++by_weight) {
+            uint64_t target = s.k;
+            if (by_weight == 0u) {
+                if (n <= s.k) continue;
+            } else {
+                if (s.p24 == kAllP) continue;
+                target = share24(whole, s.p24);
+                target = target ? target : 1u;
+            }
+            __syncthreads();
+            if (threadIdx.x < 64u) find_bin<kBins>(sh, sh.n, sh.w, by_weight != 0u, target);
+            __syncthreads();
+            const uint32_t bin = sh.found;
+            Among in{0u, 0u, 64u, sh.n[bin], sh.before_n, sh.before_w};
+            auto visit = [&](auto f) {
+                each_live([&](float l, uint32_t i, float zi) {
+                    if ((uint32_t)(zi * -8.0f) == bin) f(rank_code(l, i), entry_weight(zi));
+                });
+            };
+            __syncthreads();
+            while (in.n > Sh::kList) narrow<NT>(sh, in, visit, by_weight != 0u, target);
+            clear_list();
+            visit([&](uint64_t code, uint64_t w) {
+                if (in.holds(code)) {
+                    const uint32_t at = atomicAdd(&sh.count, 1u);
+                    sh.list_code[at] = code;
+                    sh.list_w[at] = w;
+                }
+            });
+            __syncthreads();
+            find_listed<NT>(sh, in, in.n, [&](uint32_t j) { return sh.list_code[j]; },
+                            [&](uint32_t j) { return sh.list_w[j]; }, by_weight != 0u, target);
+            cut = sh.cut;
+            if (by_weight == 0u) whole = sh.cut_w;
+        }
+        auto weigh = [&](float l, uint32_t i) {
+            const float zi = z(l);
+            const uint64_t w = zi >= kLastZ && rank_code(l, i) <= cut ? entry_weight(zi) : 0u;
+            return w >= s.least ? w : 0u;
+        };
+        uint64_t mine = 0u;
+        x.each_again_vectors([&](float l, uint32_t i) { mine += weigh(l, i); });
+        draw(mine, x.lane < x.tail ? weigh(x.last, x.vectors * E + x.lane) : 0u, weigh);
+    }
+};
+
+// z from which entries are listed at first: with a top-p or top-k cut, where the cut is
+// expected (a thousandth of the largest weight), then further down.
+constexpr float kNearZ = -10.0f, kFarZ = -24.0f;
+
+template <int D, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
+{
+    using R = Row<D, NT, NV>;
+    constexpr uint32_t E = R::E;
+    __shared__ SampleShared<NT> sh;
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        R x;
+        x.open(a.logits, row, a.stride, a.V);
+        const SampleRow s = sample_row(a, row);
+        if (threadIdx.x == 0u) {
+            sh.best = 0xFFFFFFFFu;
+            sh.count = 0u;
+            sh.low = 0u;
+        }
+        const float m = group_max<R::NW>(x.max(), sh.f);
+        if (R::NW == 1u) __syncthreads();
+        SampleGroup<D, NT, NV> g{a, sh, x, s, row, m};
+        const bool cut = s.k < a.V || s.p24 < kAllP;
+        if (m == -__builtin_inff()) {
+            if (threadIdx.x == 0u) {
+                a.token[row] = -1;
+                if (a.logp) a.logp[row] = 0.0f;
+            }
+        } else if (s.greedy) {
+            uint32_t at = 0xFFFFFFFFu;
+            x.each_and_tail([&](float l, uint32_t i) { at = l == m && i < at ? i : at; });
+            if (at != 0xFFFFFFFFu) atomicMin(&sh.best, at);
+            __syncthreads();
+            if (threadIdx.x == 0u) {
+                a.token[row] = (int32_t)sh.best;
+                if (a.logp) a.logp[row] = 0.0f;
+            }
+        } else if (!cut && s.least == 0u) {
+            uint64_t mine = 0u;
+            auto weigh = [&](float l, uint32_t) { return entry_weight(g.z(l)); };
+            x.each([&](float l, uint32_t i) { mine += weigh(l, i); });
+            g.draw(mine, x.lane < x.tail ? weigh(x.last, 0u) : 0u, weigh);
+        } else {
+            // the weight of the row is needed where top-p is the first cut
+            const bool weigh_all = s.k == a.V && s.p24 < kAllP;
+            // without a cut the list has to reach min-p's: a margin of 0.01 in z, far more
+            // than the weights' error
+            const float least_z = __builtin_log2f((float)s.least) - 40.01f;
+            const float from = cut ? kNearZ : __builtin_fmaxf(least_z, kLastZ);
+            uint64_t mine = 0u;
+            if (weigh_all) {
+                x.each_vector([&](const Vec16& y, uint32_t v) {
+                    g.list_vector(y, v, from, [&](float z) { mine += entry_weight(z); });
+                });
+                if (x.wave == 0u) mine += entry_weight(g.z(x.last));
+            } else {
+                x.each_vector([&](const Vec16& y, uint32_t v) { g.list_vector(y, v, from, [](float) {}); });
+            }
+            if (x.wave == 0u) g.list_one(x.last, x.vectors * E + x.lane, from);
+            uint64_t whole = 0u;
+            if (weigh_all) {
+                mine = wave_total(mine);
+                if (x.lane == 0u) sh.group[x.wave] = mine;
+            }
+            __syncthreads();
+            if (weigh_all)
+                for (uint32_t j = 0; j < R::NW; ++j) whole += sh.group[j];
+            bool done = g.draw_listed(false, whole);
+            if (!done && cut && sh.count <= SampleShared<NT>::kList) {
+                g.clear_list();
+                x.each_again([&](float l, uint32_t i) { g.list_one(l, i, kFarZ); });
+                __syncthreads();
+                done = g.draw_listed(false, whole);
+            }
+            if (!done) g.draw_dense();
+        }
+        __syncthreads();                  // the row's shared memory is used again
+    }
+}
+
+}  // namespace rlsim_dev

@@ -22,13 +22,15 @@ RLSIM_ESTATE = -4
 RLSIM_EUNSUPPORTED = -5
 RLSIM_F32 = 0
 RLSIM_BF16 = 1
+RLSIM_F16 = 2
 RLSIM_F_NO_TERMINATION = 1
 RLSIM_MODEL_CARTPOLE = 0
 RLSIM_MODEL_CHAIN = 1
 
 # every entry point include/rlsim.h declares
 EXPORTS = ("rlsim_cfg_default", "rlsim_create", "rlsim_reset", "rlsim_step_fused", "rlsim_get_state",
-           "rlsim_set_state", "rlsim_destroy", "rlsim_last_error")
+           "rlsim_set_state", "rlsim_destroy", "rlsim_last_error", "rlsim_head_create", "rlsim_head_sample",
+           "rlsim_head_distill", "rlsim_head_destroy", "rlsim_head_last_error")
 
 
 class RlsimError(RuntimeError):
