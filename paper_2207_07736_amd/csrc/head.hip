@@ -123,9 +123,11 @@ void launch_sample(const rlsim_head* h, const SampleArgs& a)
         HEAD_TINY(k_sample_tiny, D, a.V, grid, h->stream, a);
         return;
     }
-    const HeadForm form = head_form(a.V, Elem<D>::kBytes);
-    const uint32_t grid = head_grid(h, a.rows, form.threads);
-    HEAD_FORMS(k_sample, D, form, grid, 0, h->stream, a);
+    const uint32_t threads = head_threads(a.V, Elem<D>::kBytes);
+    const dim3 grid(head_grid(h, a.rows, threads)), block(threads);
+    if (threads == 64u) hipLaunchKernelGGL((k_sample<D, 64>), grid, block, 0, h->stream, a);
+    else if (threads == 256u) hipLaunchKernelGGL((k_sample<D, 256>), grid, block, 0, h->stream, a);
+    else hipLaunchKernelGGL((k_sample<D, 1024>), grid, block, 0, h->stream, a);
 }
 
 template <int D>

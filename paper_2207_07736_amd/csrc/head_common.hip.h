@@ -19,6 +19,7 @@ template <int D> struct Elem;
 template <> struct Elem<kHeadF32> {
     static constexpr uint32_t kBytes = 4u, kPerVec = 4u;
     static constexpr uint32_t kNegInf = 0xFF800000u;             // a word of -inf entries
+    static constexpr uint32_t kZeroBits = 0u;                    // of an entry as a float
     struct __attribute__((packed, aligned(4))) Run { uint32_t w[4]; };
     using Word = uint32_t;
     __device__ static float get(const Vec16& v, uint32_t e) { return __builtin_bit_cast(float, v.w[e]); }
@@ -33,6 +34,7 @@ template <> struct Elem<kHeadF32> {
 template <> struct Elem<kHeadBF16> {
     static constexpr uint32_t kBytes = 2u, kPerVec = 8u;
     static constexpr uint32_t kNegInf = 0xFF80FF80u;
+    static constexpr uint32_t kZeroBits = 16u;
     struct __attribute__((packed, aligned(2))) Run { uint32_t w[4]; };
     using Word = uint16_t;
     __device__ static float get(const Vec16& v, uint32_t e)
@@ -59,6 +61,7 @@ template <> struct Elem<kHeadBF16> {
 template <> struct Elem<kHeadF16> {
     static constexpr uint32_t kBytes = 2u, kPerVec = 8u;
     static constexpr uint32_t kNegInf = 0xFC00FC00u;
+    static constexpr uint32_t kZeroBits = 13u;
     struct __attribute__((packed, aligned(2))) Run { uint32_t w[4]; };
     using Word = uint16_t;
     __device__ static float get(const Vec16& v, uint32_t e)
@@ -165,8 +168,27 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x)
 }
 __device__ __forceinline__ uint64_t wave_total(uint64_t x) { return lane_u64(wave_scan(x), 63); }
 
+__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+    x = max(x, dpp_u32<0x111, 0xf>(0u, x));
+    x = max(x, dpp_u32<0x112, 0xf>(0u, x));
+    x = max(x, dpp_u32<0x114, 0xf>(0u, x));
+    x = max(x, dpp_u32<0x118, 0xf>(0u, x));
+    x = max(x, dpp_u32<0x142, 0xa>(0u, x));
+    x = max(x, dpp_u32<0x143, 0xc>(0u, x));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
 // A wave-uniform value in a scalar register.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ float uniform(float x)
+{
+    return __builtin_bit_cast(float, uniform(__builtin_bit_cast(uint32_t, x)));
+}
+__device__ __forceinline__ uint64_t uniform(uint64_t x)
+{
+    return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x);
+}
 
 // The largest value / the sum over a workgroup of NW waves, in every thread; `sh`
 // holds NW floats that no thread still reads from an earlier use.  Waves are added
@@ -249,7 +271,21 @@ struct Row {
         if (any(v) && index(v) < vectors) x = vector(index(v));
         return x;
     }
-    // f(vector, number of the vector) for each vector of this lane
+    // f(vector, number of the vector) for each vector of this lane; U strips are loaded
+    // before the first of them is used
+    template <int U, class F>
+    __device__ __forceinline__ void stream(F f) const
+    {
+#pragma unroll 1
+        for (uint32_t v = 0; v < seg && any(v); v += (uint32_t)U) {
+            Vec16 y[U];
+#pragma unroll
+            for (uint32_t j = 0; j < (uint32_t)U; ++j) y[j] = load(v + j);
+#pragma unroll
+            for (uint32_t j = 0; j < (uint32_t)U; ++j)
+                if (any(v + j)) f(y[j], index(v + j));
+        }
+    }
     template <class F>
     __device__ __forceinline__ void each_vector(F f) const
     {
@@ -258,8 +294,7 @@ struct Row {
             for (uint32_t v = 0; v < (uint32_t)NV; ++v)
                 if (any(v)) f(reg[v], index(v));
         } else {
-            for (uint32_t v = 0; v < seg; ++v)
-                if (any(v)) f(load(v), index(v));
+            stream<4>(f);
         }
     }
     // each vector replaced by f(vector, its number); registers only
@@ -290,13 +325,10 @@ struct Row {
     template <class F>
     __device__ __forceinline__ void each_again_vectors(F f) const
     {
-#pragma unroll 1
-        for (uint32_t v = 0; v < seg; ++v) {
-            if (!any(v)) break;
-            const Vec16 y = load(v);
+        stream<1>([&](const Vec16& y, uint32_t i) {
 #pragma unroll
-            for (uint32_t e = 0; e < E; ++e) f(El::get(y, e), index(v) * E + e);
-        }
+            for (uint32_t e = 0; e < E; ++e) f(El::get(y, e), i * E + e);
+        });
     }
     template <class F>
     __device__ __forceinline__ void each_again(F f) const

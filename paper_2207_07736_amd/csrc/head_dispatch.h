@@ -25,4 +25,11 @@ inline HeadForm head_form(uint32_t vocab, uint32_t elem_bytes)
     return {1024u, 0u};
 }
 
+// Threads to a row of the sampling kernel, for rows of more entries than the tiny form's.
+inline uint32_t head_threads(uint32_t vocab, uint32_t elem_bytes)
+{
+    const uint32_t vectors = vocab / (16u / elem_bytes);
+    return vectors <= 64u * 4u ? 64u : vectors <= 256u * 8u ? 256u : 1024u;
+}
+
 }  // namespace rlsim_dev

@@ -82,27 +82,47 @@ constexpr float kLastZ = -41.0f;
 __device__ __forceinline__ float entry_z(float l, float m, float c) { return l == m ? 0.0f : (l - m) * c; }
 
 // 2^40 2^z as a whole number: 2^f on [-1/2, 1/2] in fp32, Horner form with one
-// rounding per operation and coefficients scaled by 2^24 (relative error 1.9e-7),
-// truncated, then shifted by the whole part of z.
-__device__ __forceinline__ uint64_t entry_weight(float z)
+// rounding per operation (relative error 1.9e-7), truncated to 24 bits and shifted by the
+// whole part of z.  Coefficients scaled by 2^40, so that P 2^n is the weight before its
+// fraction is cut off; it needs at most 24 bits, so fp32 holds it too.
+// z + 1.5 2^23 rounds z to the whole number n that its low bits then show.  Below -41
+// (and for NaN, which the maximum turns into -63) P 2^n is less than 1.
+__device__ __forceinline__ float entry_weight32(float z)
 {
-    const float n = __builtin_rintf(z);
-    const float f = z - n;
-    float P = f * 0x1.5bb994p+14f + 0x1.3cea84p+17f;
-    P = P * f + 0x1.c6b754p+19f;
-    P = P * f + 0x1.ebf9bcp+21f;
-    P = P * f + 0x1.62e42ap+23f;
-    P = P * f + 0x1p24f;
-    const uint64_t w = ((uint64_t)(uint32_t)P << 16) >> ((uint32_t)-n & 63u);
-    return z >= kLastZ ? w : 0u;
+    z = __builtin_fmaxf(z, -63.0f);
+    const float y = z + 0x1.8p23f;
+    const float f = z - (y - 0x1.8p23f);
+    float P = f * 0x1.5bb994p+30f + 0x1.3cea84p+33f;
+    P = P * f + 0x1.c6b754p+35f;
+    P = P * f + 0x1.ebf9bcp+37f;
+    P = P * f + 0x1.62e42ap+39f;
+    P = P * f + 0x1p40f;
+    return __builtin_truncf(__builtin_bit_cast(float, __builtin_bit_cast(uint32_t, P)
+                                                          + (__builtin_bit_cast(uint32_t, y) << 23)));
 }
+__device__ __forceinline__ uint64_t whole_weight(float w)        // w < 2^41, a whole number
+{
+    const float high = __builtin_truncf(w * 0x1p-32f);
+    return (uint64_t)(uint32_t)high << 32 | (uint32_t)__builtin_fmaf(high, -0x1p32f, w);
+}
+__device__ __forceinline__ uint64_t entry_weight(float z) { return whole_weight(entry_weight32(z)); }
 
-// Ascending in rank: larger logits first, then lower indices.  -0 and +0 are equal.
-__device__ __forceinline__ uint64_t rank_code(float l, uint32_t i)
+// A whole number ascending in rank: larger logits first, then lower indices, -0 and +0
+// equal.  `ibits` bits hold an index; above them stand the logit's bits, without those
+// that are 0 in the row's type.
+template <int D>
+__device__ __forceinline__ uint64_t rank_code(float l, uint32_t i, uint32_t ibits)
 {
     const uint32_t b = __builtin_bit_cast(uint32_t, l + 0.0f);
-    const uint32_t down = b >> 31 ? b : ~b & 0x7FFFFFFFu;
-    return (uint64_t)down << 32 | i;
+    const uint32_t down = b >> 31 ? b : 0x7FFFFFFFu - b;
+    return (uint64_t)(down >> Elem<D>::kZeroBits) << ibits | i;
+}
+template <int D>
+__device__ __forceinline__ float rank_logit(uint64_t code, uint32_t ibits)
+{
+    constexpr uint32_t Z = Elem<D>::kZeroBits;
+    const uint32_t down = (uint32_t)(code >> ibits) << Z;
+    return __builtin_bit_cast(float, down >> 31 ? down : 0x7FFFFFFFu - (down | ((1u << Z) - 1u)));
 }
 
 __device__ __forceinline__ float sample_logp(float l, float m, float T, uint64_t whole)
@@ -171,26 +191,35 @@ __global__ __launch_bounds__(256) void k_sample_tiny(SampleArgs a)
 }
 
 // ---------------------------------------------------------------------------
-constexpr uint32_t kBins = 384u;          // bins of z: -8 z, 0 .. 328
 constexpr uint32_t kSubBins = 256u;       // bins of eight bits of a code
 constexpr uint32_t kFew = 128u;           // entries compared each with each
 
 template <int NT>
 struct SampleShared {
     static constexpr uint32_t NW = NT / 64;
-    static constexpr uint32_t kList = NT == 64 ? 256u : NT == 256 ? 1024u : 4096u;
+    static constexpr uint32_t kList = NT == 64 ? 256u : NT == 256 ? 1024u : 3072u;
+    // bins of z: -kPerZ z, 0 .. 41 kPerZ, padded to a multiple of 64; in longer rows finer
+    // ones, so that the bin of a cut fits the list
+    static constexpr uint32_t kPerZ = NT == 1024 ? 16u : 8u;
+    static constexpr uint32_t kUsedBins = 41u * kPerZ + 1u, kBins = (kUsedBins + 63u) / 64u * 64u;
+    static constexpr uint32_t kParts = NT == 1024 ? 8u : NW;      // of a row, with bins of their own
     float f[NW];
     uint64_t sum[NW + 1], group[NW];
-    uint32_t n[kBins];
+    uint64_t part_w[kParts][kUsedBins];
     uint64_t w[kBins];
-    uint32_t sub_n[kSubBins];
-    uint64_t sub_w[kSubBins];
-    uint64_t list_code[kList], list_w[kList];
-    uint64_t few_code[kFew], few_w[kFew];
+    uint32_t n[kBins];
+    union {
+        struct {
+            uint64_t sub_w[kSubBins];
+            uint32_t sub_n[kSubBins];
+        };
+        struct { uint64_t few_code[kFew], few_w[kFew]; };
+    };
+    uint64_t list_code[kList];
     uint32_t found;                       // bin of the cut
     uint64_t before_n, before_w;          // entries, and weight, of the bins before it
     uint64_t cut, cut_w;                  // code of the entry looked for, weight up to it
-    uint32_t count, few, low, best;
+    uint32_t count, few, near, far, best;  // near, far: the list's logit parts' range (near: inverted)
 };
 
 // First bin at which the running sum of counts (by_weight: of weights) reaches
@@ -304,12 +333,9 @@ __device__ __forceinline__ void find_listed(Sh& sh, Among in, uint32_t listed, C
     __syncthreads();
 }
 
-// The shift by which codes of `bits` bits show their first eight.
-__device__ __forceinline__ uint32_t first_shift(uint32_t bits) { return bits > 8u ? bits - 8u : 0u; }
-
-template <int D, int NT, int NV>
+template <int D, int NT>
 struct SampleGroup {
-    using R = Row<D, NT, NV>;
+    using R = Row<D, NT, 0>;
     using Sh = SampleShared<NT>;
     using El = Elem<D>;
     static constexpr uint32_t E = R::E, NW = R::NW;
@@ -320,8 +346,10 @@ struct SampleGroup {
     const SampleRow& s;
     const uint32_t row;
     const float m;
+    const uint32_t ibits;         // of an index
 
     __device__ __forceinline__ float z(float l) const { return entry_z(l, m, s.c); }
+    static __device__ __forceinline__ uint32_t bin_of(float z) { return (uint32_t)(z * -(float)Sh::kPerZ); }
     __device__ __forceinline__ void answer(uint32_t i, float logp) const
     {
         a.token[row] = (int32_t)i;
@@ -330,10 +358,11 @@ struct SampleGroup {
 
     // The draw from the whole row, with the weights weigh(entry, index): the wave's
     // part, then the thread's, then the entry in which the running sum passes the
-    // target.  `mine` and `end` are this thread's sums over its vectors and its tail entry.
+    // target.  `mine` is this thread's sum over its vectors.
     template <class F>
-    __device__ __forceinline__ void draw(uint64_t mine, uint64_t end, F weigh)
+    __device__ __forceinline__ void draw(uint64_t mine, F weigh)
     {
+        const uint64_t end = x.lane < x.tail ? weigh(x.last, x.vectors * E + x.lane) : 0u;
         mine = wave_total(mine);
         if (x.lane == 0u) sh.sum[x.wave] = mine;
         if (x.wave == 0u) {
@@ -341,13 +370,22 @@ struct SampleGroup {
             if (x.lane == 0u) sh.sum[NW] = t;
         }
         __syncthreads();
+        pick(NW, x.seg * 64u, weigh);
+    }
+    // The same from the sums in sh.sum: of `parts` parts, `vectors` vectors each, and the tail.
+    template <class F>
+    __device__ __forceinline__ void pick(uint32_t parts, uint32_t vectors, F weigh)
+    {
+        const uint64_t end = x.lane < x.tail ? weigh(x.last, x.vectors * E + x.lane) : 0u;
         uint64_t whole = 0u;
-        for (uint32_t j = 0; j <= NW; ++j) whole += sh.sum[j];
+        for (uint32_t j = 0; j <= parts; ++j) whole += sh.sum[j];
+        whole = uniform(whole);
         const uint64_t target = share24(whole, s.u24);
         uint64_t before = 0u;
         uint32_t part = 0u;
-        while (part < NW && before + sh.sum[part] <= target) before += sh.sum[part++];
-        if (part == NW) {                 // the tail's lanes
+        while (part < parts && before + sh.sum[part] <= target) before += sh.sum[part++];
+        part = uniform(part);
+        if (part == parts) {              // the tail's lanes
             if (x.wave == 0u) {
                 const uint64_t upto = before + wave_scan(end);
                 if (upto > target && upto - end <= target) answer(x.vectors * E + x.lane, sample_logp(x.last, m, s.T, whole));
@@ -355,9 +393,9 @@ struct SampleGroup {
             return;
         }
         // the part's vectors, a run of consecutive ones to each thread
-        const uint32_t run = (x.seg * 64u + NT - 1u) / NT;
-        const uint32_t v0 = part * x.seg * 64u + threadIdx.x * run;
-        const uint32_t limit = min((part + 1u) * x.seg * 64u, x.vectors), v1 = min(v0 + run, limit);
+        const uint32_t run = (vectors + NT - 1u) / NT;
+        const uint32_t v0 = part * vectors + threadIdx.x * run;
+        const uint32_t limit = min((part + 1u) * vectors, x.vectors), v1 = min(v0 + run, limit);
         uint64_t own = 0u;
         for (uint32_t v = v0; v < v1; ++v) {
             const Vec16 y = x.vector(v);
@@ -384,94 +422,106 @@ struct SampleGroup {
         }
     }
 
-    // List the entry if z >= from.  sh.count counts (only the first kList are listed),
-    // sh.low gets the logit part of the lowest rank.
-    __device__ __forceinline__ void list_one(float l, uint32_t i, float from)
+    // Append to the list, for the whole wave: the entries e whose bit is set in `hits`, with
+    // the codes code_of(e).  sh.count counts; only the first kList are listed.
+    template <uint32_t N, class F>
+    __device__ __forceinline__ void append(uint32_t hits, F code_of)
     {
-        const float zi = z(l);
-        if (zi >= from) {
-            const uint64_t code = rank_code(l, i);
-            const uint32_t at = atomicAdd(&sh.count, 1u);
-            if (at < Sh::kList) {
-                sh.list_code[at] = code;
-                sh.list_w[at] = entry_weight(zi);
+        if (__ballot(hits != 0u) == 0u) return;
+        const uint32_t n = (uint32_t)__builtin_popcount(hits), upto = wave_scan(n);
+        uint32_t at = 0u;
+        if (x.lane == 63u) at = atomicAdd(&sh.count, upto);
+        at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + upto - n;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+            if (hits >> e & 1u) {
+                if (at < Sh::kList) sh.list_code[at] = code_of(e);
+                ++at;
             }
-            atomicMax(&sh.low, (uint32_t)(code >> 32));
         }
     }
-    // The same for a vector's entries; also(z) sees each of them.  Few are listed: they
-    // are read again one by one, which keeps the code small.
+    __device__ __forceinline__ uint64_t listed_weight(uint32_t j) const { return entry_weight(z(rank_logit<D>(sh.list_code[j], ibits))); }
+    __device__ __forceinline__ uint64_t code(float l, uint32_t i) const { return rank_code<D>(l, i, ibits); }
+    // Append the row's entries for which want(entry) holds.
     template <class F>
-    __device__ __forceinline__ void list_vector(const Vec16& y, uint32_t v, float from, F also)
+    __device__ __forceinline__ void append_vector(const Vec16& y, uint32_t v, F want)
     {
-        uint32_t near = 0u;
+        uint32_t hits = 0u;
 #pragma unroll
-        for (uint32_t e = 0; e < E; ++e) {
-            const float zi = z(El::get(y, e));
-            also(zi);
-            near |= zi >= from ? 1u << e : 0u;
-        }
-        while (near) {
-            const uint32_t i = v * E + (uint32_t)__builtin_ctz(near);
-            list_one(x.entry(i), i, from);
-            near &= near - 1u;
-        }
+        for (uint32_t e = 0; e < E; ++e) hits |= want(El::get(y, e)) ? 1u << e : 0u;
+        append<E>(hits, [&](uint32_t e) { return code(El::get(y, e), v * E + e); });
+    }
+    template <class F>
+    __device__ __forceinline__ void append_tail(F want)
+    {
+        if (x.wave == 0u)
+            append<1>(want(x.last) ? 1u : 0u, [&](uint32_t) { return code(x.last, x.vectors * E + x.lane); });
     }
     __device__ __forceinline__ void clear_list()
     {
         __syncthreads();
         if (threadIdx.x == 0u) {
             sh.count = 0u;
-            sh.low = 0u;
+            sh.near = 0u;
+            sh.far = 0u;
         }
         __syncthreads();
     }
+    // The range of the `n` listed codes; returns them as the entries among which to look,
+    // behind others of the given count and weight.
+    __device__ __forceinline__ Among close_list(uint32_t n, uint64_t before_n, uint64_t before_w)
+    {
+        uint32_t far = 0u, near = 0u;
+        for (uint32_t j = threadIdx.x; j < n; j += NT) {
+            const uint64_t c = sh.list_code[j];
+            far = max(far, (uint32_t)(c >> ibits));
+            near = max(near, ~(uint32_t)(c >> ibits));
+        }
+        return range(far, near, n, before_n, before_w);
+    }
+    __device__ __forceinline__ Among range(uint32_t far, uint32_t near, uint32_t n, uint64_t before_n, uint64_t before_w)
+    {
+        far = wave_max(far);
+        near = wave_max(near);
+        if (x.lane == 0u && far) {
+            atomicMax(&sh.far, far);
+            atomicMax(&sh.near, near);
+        }
+        __syncthreads();
+        const uint32_t first = ~sh.near, span = sh.far - first;
+        const uint32_t bits = span ? ibits + 32u - (uint32_t)__builtin_clz(span) : ibits;
+        return Among{(uint64_t)first << ibits, 0u, max(bits, 8u), n, before_n, before_w};
+    }
 
-    // Cut and draw from the list.  `all`: no live entry is missing from it; whole: the
-    // row's weight where top-p is the first cut, else 0.  False: the list does not reach
-    // the cut.
-    __device__ __forceinline__ bool draw_listed(bool all, uint64_t whole)
+    // Cut and draw from the list; top-p is not the first cut.  False: the list does not
+    // reach the cut.
+    __device__ __forceinline__ bool draw_listed()
     {
         const uint32_t listed = sh.count;
-        if (listed > Sh::kList) return false;
-        uint64_t weight = 0u;             // of the list
-        for (uint32_t j = threadIdx.x; j < listed; j += NT) weight += sh.list_w[j];
-        weight = wave_total(weight);
-        if (x.lane == 0u) sh.sum[x.wave] = weight;
-        __syncthreads();
-        weight = 0u;
-        for (uint32_t j = 0; j < NW; ++j) weight += sh.sum[j];
-        const uint64_t first = rank_code(m, 0u);
-        const uint32_t span = sh.low - (uint32_t)(first >> 32);
-        const uint32_t bits = span ? 64u - (uint32_t)__builtin_clz(span) : 32u - (uint32_t)__builtin_clz(a.V);
-        const Among rank{first, 0u, first_shift(bits) + 8u, listed, 0u, 0u};
+        if (listed > Sh::kList || listed == 0u || (s.k < a.V && listed < s.k)) return false;
+        const Among rank = close_list(listed, 0u, 0u);
+        uint64_t whole = 0u, weight = 0u;
         auto code = [&](uint32_t j) { return sh.list_code[j]; };
-        auto plain = [&](uint32_t j) { return sh.list_w[j]; };
+        auto plain = [&](uint32_t j) { return listed_weight(j); };
         uint64_t cut = ~0ull;
         // top-k, then top-p: one piece of code for both
         for (uint32_t by_weight = 0u; by_weight < 2u; ++by_weight) {
             uint64_t target = s.k;
             if (by_weight == 0u) {
                 if (s.k == a.V) continue;
-                if (listed < s.k && !all) return false;
-                if (listed <= s.k) {
-                    whole = weight;
-                    continue;
-                }
             } else {
                 if (s.p24 == kAllP) continue;
                 target = share24(whole, s.p24);
                 target = target ? target : 1u;
-                if (weight < target) return false;
             }
             find_listed<NT>(sh, rank, listed, code, plain, by_weight != 0u, target);
             cut = sh.cut;
             if (by_weight == 0u) whole = sh.cut_w;
         }
         // what is left, by index
-        auto index = [&](uint32_t j) { return sh.list_code[j] & 0xFFFFFFFFu; };
+        auto index = [&](uint32_t j) { return sh.list_code[j] & ((1ull << ibits) - 1u); };
         auto kept = [&](uint32_t j) {
-            const uint64_t w = sh.list_w[j];
+            const uint64_t w = listed_weight(j);
             return sh.list_code[j] <= cut && w >= s.least ? w : 0u;
         };
         weight = 0u;
@@ -482,7 +532,7 @@ struct SampleGroup {
         __syncthreads();
         weight = 0u;
         for (uint32_t j = 0; j < NW; ++j) weight += sh.sum[j];
-        const Among order{0u, 0u, first_shift(32u - (uint32_t)__builtin_clz(a.V)) + 8u, listed, 0u, 0u};
+        const Among order{0u, 0u, max(ibits, 8u), listed, 0u, 0u};
         find_listed<NT>(sh, order, listed, index, kept, true, share24(weight, s.u24) + 1u);
         if (threadIdx.x == 0u) {
             const uint32_t i = (uint32_t)sh.cut;
@@ -491,30 +541,148 @@ struct SampleGroup {
         return true;
     }
 
+    // Draw where top-p is the first cut.  One pass bins the weights by z, each wave's part
+    // of the row in bins of its own: they give the row's weight and the bin in which the
+    // cut lies, and later the parts' kept weights without another pass.  The entries of
+    // that bin are listed and the cut found among them.
+    __device__ __forceinline__ void draw_top_p()
+    {
+        for (uint32_t j = threadIdx.x; j < Sh::kParts * Sh::kUsedBins; j += NT) (&sh.part_w[0][0])[j] = 0u;
+        __syncthreads();
+        const uint32_t waves = NW / Sh::kParts;       // to a part
+        uint64_t* const mine = sh.part_w[x.wave / waves];
+        auto bin = [&](float l) {
+            const float zi = (l - m) * s.c;
+            const float w = entry_weight32(zi);
+            if (w > 0.0f) atomicAdd((unsigned long long*)&mine[bin_of(zi)], (unsigned long long)whole_weight(w));
+        };
+        x.each([&](float l, uint32_t) { bin(l); });
+        if (x.wave == 0u) bin(x.last);                // the tail counts to the first part here
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < Sh::kBins; j += NT) {
+            uint64_t w = 0u;
+            if (j < Sh::kUsedBins)
+                for (uint32_t q = 0; q < Sh::kParts; ++q) w += sh.part_w[q][j];
+            sh.w[j] = w;
+        }
+        __syncthreads();
+        uint64_t whole = 0u;
+        for (uint32_t j = x.lane; j < Sh::kBins; j += 64u) whole += sh.w[j];
+        whole = wave_total(whole);
+        uint64_t target = share24(whole, s.p24);
+        target = target ? target : 1u;
+        if (threadIdx.x < 64u) find_bin<Sh::kBins>(sh, sh.n, sh.w, true, target);     // (counts are not looked at)
+        __syncthreads();
+        const uint32_t b = sh.found;
+        const uint64_t before_w = sh.before_w;
+        auto in_bin = [&](float l) {
+            const float zi = (l - m) * s.c;
+            return zi >= kLastZ && bin_of(zi) == b;
+        };
+        x.each_vector([&](const Vec16& y, uint32_t v) { append_vector(y, v, in_bin); });
+        append_tail(in_bin);
+        __syncthreads();
+        const uint32_t n = sh.count;
+        const bool listed = n <= Sh::kList;
+        const Among in = listed ? close_list(n, 0u, before_w) : narrow_to_list(b, n, 0u, before_w, true, target);
+        find_listed<NT>(sh, in, in.n, [&](uint32_t j) { return sh.list_code[j]; }, [&](uint32_t j) { return listed_weight(j); },
+                        true, target);
+        const uint64_t cut = sh.cut;
+        auto weigh = [&](float l, uint32_t i) { return weigh_kept(l, i, cut); };
+        if (!listed || s.least) {
+            uint64_t mine = 0u;
+            x.each_again_vectors([&](float l, uint32_t i) { mine += weigh(l, i); });
+            draw(mine, weigh);
+            return;
+        }
+        // a part's kept weight: the bins before the cut's, and what of that one is kept
+        for (uint32_t q = x.wave; q < Sh::kParts; q += NW) {
+            uint64_t w = 0u;
+            for (uint32_t j = x.lane; j < b; j += 64u) w += sh.part_w[q][j];
+            w = wave_total(w);
+            if (x.lane == 0u) sh.sum[q] = w;
+        }
+        __syncthreads();
+        const uint32_t part_vectors = x.seg * 64u * waves;
+        for (uint32_t j = threadIdx.x; j < in.n; j += NT)
+            if (sh.list_code[j] <= cut) {
+                const uint32_t v = (uint32_t)(sh.list_code[j] & ((1ull << ibits) - 1u)) / E;
+                atomicAdd((unsigned long long*)&sh.sum[v < x.vectors ? v / part_vectors : 0u], (unsigned long long)listed_weight(j));
+            }
+        __syncthreads();
+        if (x.wave == 0u) {
+            const uint64_t end = wave_total(x.lane < x.tail ? weigh(x.last, x.vectors * E + x.lane) : 0u);
+            if (x.lane == 0u) {
+                sh.sum[0] -= end;
+                sh.sum[Sh::kParts] = end;
+            }
+        }
+        __syncthreads();
+        pick(Sh::kParts, part_vectors, weigh);
+    }
+    __device__ __forceinline__ uint64_t weigh_kept(float l, uint32_t i, uint64_t cut) const
+    {
+        const float zi = z(l);
+        const uint64_t w = zi >= kLastZ && code(l, i) <= cut ? entry_weight(zi) : 0u;
+        return w >= s.least ? w : 0u;
+    }
+
+    // f(entry, index, z) for the row's live entries, from another read
+    template <class F>
+    __device__ __forceinline__ void each_live(F f)
+    {
+        x.each_again([&](float l, uint32_t i) {
+            const float zi = z(l);
+            if (zi >= kLastZ) f(l, i, zi);
+        });
+    }
+    // Where a bin of z holds more entries than the list: narrow them by their codes until
+    // the list takes what is left, and list it.
+    __device__ __forceinline__ Among narrow_to_list(uint32_t bin, uint32_t n, uint64_t before_n, uint64_t before_w, bool by_weight,
+                                                    uint64_t target)
+    {
+        Among in{0u, 0u, 64u, n, before_n, before_w};
+        auto visit = [&](auto f) {
+            each_live([&](float l, uint32_t i, float zi) {
+                if (bin_of(zi) == bin) f(code(l, i), entry_weight(zi));
+            });
+        };
+        if (n > Sh::kList) {              // the range of the bin's codes
+            clear_list();
+            uint32_t far = 0u, near = 0u;
+            visit([&](uint64_t c, uint64_t) {
+                far = max(far, (uint32_t)(c >> ibits));
+                near = max(near, ~(uint32_t)(c >> ibits));
+            });
+            in = range(far, near, n, before_n, before_w);
+        }
+        while (in.n > Sh::kList) narrow<NT>(sh, in, visit, by_weight, target);
+        clear_list();
+        visit([&](uint64_t c, uint64_t) {
+            if (in.holds(c)) sh.list_code[atomicAdd(&sh.count, 1u)] = c;
+        });
+        __syncthreads();
+        return close_list(in.n, in.before_n, in.before_w);
+    }
+
     // Cut and draw where too many entries are close to the largest: bins of z for the
     // whole row, the cut's bin listed, then a pass over the row.
     __device__ __forceinline__ void draw_dense()
     {
-        auto each_live = [&](auto f) {
-            x.each_again([&](float l, uint32_t i) {
-                const float zi = z(l);
-                if (zi >= kLastZ) f(l, i, zi);
-            });
-        };
         __syncthreads();
-        for (uint32_t j = threadIdx.x; j < kBins; j += NT) {
+        for (uint32_t j = threadIdx.x; j < Sh::kBins; j += NT) {
             sh.n[j] = 0u;
             sh.w[j] = 0u;
         }
         __syncthreads();
         each_live([&](float, uint32_t, float zi) {
-            const uint32_t b = (uint32_t)(zi * -8.0f);
+            const uint32_t b = bin_of(zi);
             atomicAdd(&sh.n[b], 1u);
             atomicAdd((unsigned long long*)&sh.w[b], (unsigned long long)entry_weight(zi));
         });
         __syncthreads();
         uint64_t n = 0u, whole = 0u;      // the row's, in every thread
-        for (uint32_t j = x.lane; j < kBins; j += 64u) {
+        for (uint32_t j = x.lane; j < Sh::kBins; j += 64u) {
             n += sh.n[j];
             whole += sh.w[j];
         }
@@ -531,51 +699,30 @@ struct SampleGroup {
                 target = target ? target : 1u;
             }
             __syncthreads();
-            if (threadIdx.x < 64u) find_bin<kBins>(sh, sh.n, sh.w, by_weight != 0u, target);
+            if (threadIdx.x < 64u) find_bin<Sh::kBins>(sh, sh.n, sh.w, by_weight != 0u, target);
             __syncthreads();
             const uint32_t bin = sh.found;
-            Among in{0u, 0u, 64u, sh.n[bin], sh.before_n, sh.before_w};
-            auto visit = [&](auto f) {
-                each_live([&](float l, uint32_t i, float zi) {
-                    if ((uint32_t)(zi * -8.0f) == bin) f(rank_code(l, i), entry_weight(zi));
-                });
-            };
-            __syncthreads();
-            while (in.n > Sh::kList) narrow<NT>(sh, in, visit, by_weight != 0u, target);
-            clear_list();
-            visit([&](uint64_t code, uint64_t w) {
-                if (in.holds(code)) {
-                    const uint32_t at = atomicAdd(&sh.count, 1u);
-                    sh.list_code[at] = code;
-                    sh.list_w[at] = w;
-                }
-            });
-            __syncthreads();
+            const Among in = narrow_to_list(bin, sh.n[bin], sh.before_n, sh.before_w, by_weight != 0u, target);
             find_listed<NT>(sh, in, in.n, [&](uint32_t j) { return sh.list_code[j]; },
-                            [&](uint32_t j) { return sh.list_w[j]; }, by_weight != 0u, target);
+                            [&](uint32_t j) { return listed_weight(j); }, by_weight != 0u, target);
             cut = sh.cut;
             if (by_weight == 0u) whole = sh.cut_w;
         }
-        auto weigh = [&](float l, uint32_t i) {
-            const float zi = z(l);
-            const uint64_t w = zi >= kLastZ && rank_code(l, i) <= cut ? entry_weight(zi) : 0u;
-            return w >= s.least ? w : 0u;
-        };
+        auto weigh = [&](float l, uint32_t i) { return weigh_kept(l, i, cut); };
         uint64_t mine = 0u;
         x.each_again_vectors([&](float l, uint32_t i) { mine += weigh(l, i); });
-        draw(mine, x.lane < x.tail ? weigh(x.last, x.vectors * E + x.lane) : 0u, weigh);
+        draw(mine, weigh);
     }
 };
 
-// z from which entries are listed at first: with a top-p or top-k cut, where the cut is
-// expected (a thousandth of the largest weight), then further down.
+// z from which entries are listed at first: with a top-k cut, where it is expected (a
+// thousandth of the largest weight), then further down.
 constexpr float kNearZ = -10.0f, kFarZ = -24.0f;
 
-template <int D, int NT, int NV>
-__global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
+template <int D, int NT>
+__global__ __launch_bounds__(NT, 8) void k_sample(SampleArgs a)
 {
-    using R = Row<D, NT, NV>;
-    constexpr uint32_t E = R::E;
+    using R = Row<D, NT, 0>;
     __shared__ SampleShared<NT> sh;
     for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         R x;
@@ -584,11 +731,12 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
         if (threadIdx.x == 0u) {
             sh.best = 0xFFFFFFFFu;
             sh.count = 0u;
-            sh.low = 0u;
+            sh.near = 0u;
+            sh.far = 0u;
         }
-        const float m = group_max<R::NW>(x.max(), sh.f);
+        const float m = uniform(group_max<R::NW>(x.max(), sh.f));
         if (R::NW == 1u) __syncthreads();
-        SampleGroup<D, NT, NV> g{a, sh, x, s, row, m};
+        SampleGroup<D, NT> g{a, sh, x, s, row, m, 32u - (uint32_t)__builtin_clz(a.V)};
         const bool cut = s.k < a.V || s.p24 < kAllP;
         if (m == -__builtin_inff()) {
             if (threadIdx.x == 0u) {
@@ -604,42 +752,31 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
                 a.token[row] = (int32_t)sh.best;
                 if (a.logp) a.logp[row] = 0.0f;
             }
+        } else if (!(m < __builtin_inff() && s.c < __builtin_inff())) {
+            g.draw_dense();
         } else if (!cut && s.least == 0u) {
-            uint64_t mine = 0u;
-            auto weigh = [&](float l, uint32_t) { return entry_weight(g.z(l)); };
-            x.each([&](float l, uint32_t i) { mine += weigh(l, i); });
-            g.draw(mine, x.lane < x.tail ? weigh(x.last, 0u) : 0u, weigh);
+            double mine = 0.0;            // whole numbers, less than 2^53
+            x.each([&](float l, uint32_t) { mine += (double)entry_weight32((l - m) * s.c); });
+            g.draw((uint64_t)mine, [&](float l, uint32_t) { return entry_weight((l - m) * s.c); });
+        } else if (s.k == a.V && s.p24 < kAllP) {
+            g.draw_top_p();
         } else {
-            // the weight of the row is needed where top-p is the first cut
-            const bool weigh_all = s.k == a.V && s.p24 < kAllP;
             // without a cut the list has to reach min-p's: a margin of 0.01 in z, far more
             // than the weights' error
             const float least_z = __builtin_log2f((float)s.least) - 40.01f;
-            const float from = cut ? kNearZ : __builtin_fmaxf(least_z, kLastZ);
-            uint64_t mine = 0u;
-            if (weigh_all) {
-                x.each_vector([&](const Vec16& y, uint32_t v) {
-                    g.list_vector(y, v, from, [&](float z) { mine += entry_weight(z); });
-                });
-                if (x.wave == 0u) mine += entry_weight(g.z(x.last));
-            } else {
-                x.each_vector([&](const Vec16& y, uint32_t v) { g.list_vector(y, v, from, [](float) {}); });
-            }
-            if (x.wave == 0u) g.list_one(x.last, x.vectors * E + x.lane, from);
-            uint64_t whole = 0u;
-            if (weigh_all) {
-                mine = wave_total(mine);
-                if (x.lane == 0u) sh.group[x.wave] = mine;
-            }
-            __syncthreads();
-            if (weigh_all)
-                for (uint32_t j = 0; j < R::NW; ++j) whole += sh.group[j];
-            bool done = g.draw_listed(false, whole);
-            if (!done && cut && sh.count <= SampleShared<NT>::kList) {
-                g.clear_list();
-                x.each_again([&](float l, uint32_t i) { g.list_one(l, i, kFarZ); });
+            auto list = [&](float from) {
+                auto want = [&](float l) { return (l - m) * s.c >= from; };
+                x.each_vector([&](const Vec16& y, uint32_t v) { g.append_vector(y, v, want); });
+                g.append_tail(want);
                 __syncthreads();
-                done = g.draw_listed(false, whole);
+            };
+            bool done = false;
+#pragma unroll 1
+            for (uint32_t far = 0u; far < 2u && !done; ++far) {
+                if (far) g.clear_list();
+                list(!cut ? __builtin_fmaxf(least_z, kLastZ) : far ? kFarZ : kNearZ);
+                done = g.draw_listed();
+                if (!cut || sh.count > SampleShared<NT>::kList) break;
             }
             if (!done) g.draw_dense();
         }
