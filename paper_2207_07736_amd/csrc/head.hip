@@ -87,12 +87,6 @@ uint32_t head_grid(const rlsim_head* h, uint32_t items, uint32_t threads)
             hipLaunchKernelGGL((KERNEL<D, 256, 4>), dim3(grid), dim3(256), shared, stream, args);                            \
         else if (form.threads == 256u)                                                                                       \
             hipLaunchKernelGGL((KERNEL<D, 256, 8>), dim3(grid), dim3(256), shared, stream, args);                            \
-        else if (form.strips == 4u)                                                                                          \
-            hipLaunchKernelGGL((KERNEL<D, 1024, 4>), dim3(grid), dim3(1024), shared, stream, args);                          \
-        else if (form.strips == 8u)                                                                                          \
-            hipLaunchKernelGGL((KERNEL<D, 1024, 8>), dim3(grid), dim3(1024), shared, stream, args);                          \
-        else if (form.strips == 16u)                                                                                         \
-            hipLaunchKernelGGL((KERNEL<D, 1024, 16>), dim3(grid), dim3(1024), shared, stream, args);                         \
         else                                                                                                                 \
             hipLaunchKernelGGL((KERNEL<D, 1024, 0>), dim3(grid), dim3(1024), shared, stream, args);                          \
     } while (0)
@@ -140,7 +134,7 @@ void launch_distill(const rlsim_head* h, const DistillArgs& a)
     }
     const HeadForm form = head_form(a.V, Elem<D>::kBytes);
     const uint32_t grid = head_grid(h, a.rows, form.threads);
-    const uint32_t shared = distill_shared_bytes(a.k, a.V, a.rest != nullptr);
+    const uint32_t shared = distill_shared_bytes(a.k, a.V);
     HEAD_FORMS(k_distill, D, form, grid, shared, h->stream, a);
 }
 
@@ -148,7 +142,7 @@ void launch_distill(const rlsim_head* h, const DistillArgs& a)
 template <int D>
 hipError_t allow_shared()
 {
-    const int bytes = (int)distill_shared_bytes(kHeadMaxTeacher, kHeadMaxVocab, true);
+    const int bytes = (int)distill_shared_bytes(kHeadMaxTeacher, kHeadMaxVocab);
     return hipFuncSetAttribute(reinterpret_cast<const void*>(k_distill<D, 1024, 0>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }

@@ -185,39 +185,28 @@ __device__ __forceinline__ float uniform(float x)
 {
     return __builtin_bit_cast(float, uniform(__builtin_bit_cast(uint32_t, x)));
 }
+__device__ __forceinline__ uint64_t uniform(uint64_t x);
+__device__ __forceinline__ double uniform(double x)
+{
+    return __builtin_bit_cast(double, uniform(__builtin_bit_cast(uint64_t, x)));
+}
 __device__ __forceinline__ uint64_t uniform(uint64_t x)
 {
     return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x);
 }
 
-// The largest value / the sum over a workgroup of NW waves, in every thread; `sh`
-// holds NW floats that no thread still reads from an earlier use.  Waves are added
-// in their order.
+// The largest value over a workgroup of NW waves, in every thread and wave-uniform; `sh`
+// holds NW values that no thread still reads from an earlier use.
 template <int NW>
 __device__ __forceinline__ float group_max(float x, float* sh)
 {
     x = wave_max(x);
     if (NW == 1) return x;
-    if (threadIdx.x % 64u == 0u) sh[threadIdx.x / 64u] = x;
+    const uint32_t lane = threadIdx.x % 64u;
+    if (lane == 0u) sh[threadIdx.x / 64u] = x;
     __syncthreads();
-    x = sh[0];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) x = __builtin_fmaxf(x, sh[w]);
-    return x;
+    return wave_max(lane < (uint32_t)NW ? sh[lane] : -__builtin_inff());
 }
-template <int NW, class T>
-__device__ __forceinline__ T group_total(T x, T* sh)
-{
-    x = wave_total(x);
-    if (NW == 1) return x;
-    if (threadIdx.x % 64u == 0u) sh[threadIdx.x / 64u] = x;
-    __syncthreads();
-    x = sh[0];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) x += sh[w];
-    return x;
-}
-
 // ---------------------------------------------------------------------------
 // A row as a workgroup of NT threads sees it: whole 16-byte vectors, then up to
 // kPerVec - 1 entries of tail, one to a lane of the first wave.  A wave owns `seg`
@@ -296,14 +285,6 @@ struct Row {
         } else {
             stream<4>(f);
         }
-    }
-    // each vector replaced by f(vector, its number); registers only
-    template <class F>
-    __device__ __forceinline__ void apply(F f)
-    {
-#pragma unroll
-        for (uint32_t v = 0; v < (uint32_t)NV; ++v)
-            if (any(v)) reg[v] = f(reg[v], index(v));
     }
     // f(entry, its index) for each entry of this lane's vectors
     template <class F>

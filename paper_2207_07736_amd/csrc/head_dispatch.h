@@ -19,9 +19,6 @@ inline HeadForm head_form(uint32_t vocab, uint32_t elem_bytes)
     if (vectors <= 64u * 4u) return {64u, 4u};
     if (vectors <= 256u * 4u) return {256u, 4u};
     if (vectors <= 256u * 8u) return {256u, 8u};
-    if (vectors <= 1024u * 4u) return {1024u, 4u};
-    if (vectors <= 1024u * 8u) return {1024u, 8u};
-    if (vectors <= 1024u * 16u) return {1024u, 16u};
     return {1024u, 0u};
 }
 

@@ -210,28 +210,25 @@ __global__ __launch_bounds__(256) void k_distill_tiny(DistillArgs a)
 }
 
 // ---------------------------------------------------------------------------
-// Shared memory beside the floats of the reductions: k entries, k teacher values
-// (then probabilities), k student exponentials and, with a rest, a bit for each entry
-// of the row.
-inline __host__ __device__ uint32_t distill_shared_bytes(uint32_t k, uint32_t V, bool rest)
-{
-    return 12u * k + (rest ? (V + 31u) / 32u * 4u : 0u);
-}
+// Shared memory beside the reductions': a bit for each entry of the row that is listed,
+// then k entries, k teacher logits (then probabilities) and k student logits.
+inline __host__ __device__ uint32_t distill_shared_bytes(uint32_t k, uint32_t V) { return (V + 31u) / 32u * 4u + 12u * k; }
 
 template <int D, int NT, int NV>
-__global__ __launch_bounds__(NT) void k_distill(DistillArgs a)
+__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs a)
 {
     using R = Row<D, NT, NV>;
     using El = Elem<D>;
     constexpr uint32_t E = R::E;
     constexpr int NW = NT / 64;
-    __shared__ float sh[3][NW];
-    __shared__ double sh64[4][NW];
-    extern __shared__ uint32_t slots[];
-    uint32_t* const entry = slots;
-    float* const prob = reinterpret_cast<float*>(slots + a.k);          // t, then p
-    float* const logit = reinterpret_cast<float*>(slots + 2u * a.k);    // the student's
-    uint32_t* const bits = slots + 3u * a.k;
+    __shared__ float sh_max[3][NW];
+    __shared__ double sh_sum[4][NW];
+    __shared__ uint32_t again, mass;      // whether a slot repeats an earlier one's entry; any has mass
+    extern __shared__ uint32_t bits[];
+    const uint32_t words = (a.V + 31u) / 32u;
+    uint32_t* const entry = bits + words;
+    float* const prob = reinterpret_cast<float*>(entry + a.k);          // t, then p
+    float* const logit = prob + a.k;                                    // the student's
     const uint32_t tid = threadIdx.x;
     const float none = -__builtin_inff();
     for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -244,36 +241,41 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs a)
             if (i < x.vectors) reinterpret_cast<typename El::Run*>(grad)[i] = r;
         };
         auto store_one = [&](uint32_t i, float v) { reinterpret_cast<typename El::Word*>(grad)[i] = El::word(v); };
-        const float weight = a.weight ? a.weight[row] : 1.0f;
-        const float rest = a.rest ? rest_value(a, row) : none;
+        const float weight = uniform(a.weight ? a.weight[row] : 1.0f);
+        const float rest = uniform(a.rest ? rest_value(a, row) : none);
         for (uint32_t j = tid; j < a.k; j += NT) {
             const Slot s = load_slot(a, row, j);
             entry[j] = s.entry;
             prob[j] = s.t;
+            if (s.entry != kNoEntry) logit[j] = x.entry(s.entry);
         }
-        if (a.rest)
-            for (uint32_t j = tid; j < (a.V + 31u) / 32u; j += NT) bits[j] = 0u;
+        for (uint32_t j = tid; j < words; j += NT) bits[j] = 0u;
+        if (tid == 0u) {
+            again = 0u;
+            mass = 0u;
+        }
         __syncthreads();
-        // leave out slots that repeat an earlier one's entry; the others' student logits
-        uint32_t repeats = 0u;            // a bit for each of this thread's slots
-        float top_t = none;
-        for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) {
-            const uint32_t mine = entry[j];
-            if (mine == kNoEntry) continue;
-            bool again = false;
-            for (uint32_t i = 0; i < j; ++i) again = again || entry[i] == mine;
-            if (again) {
-                repeats |= b;
-            } else {
-                top_t = __builtin_fmaxf(top_t, prob[j]);
-                logit[j] = x.entry(mine);
-                if (a.rest) atomicOr(&bits[mine / 32u], 1u << (mine % 32u));
+        for (uint32_t j = tid; j < a.k; j += NT) {
+            const uint32_t i = entry[j];
+            if (i == kNoEntry) continue;
+            if (atomicOr(&bits[i / 32u], 1u << (i % 32u)) >> (i % 32u) & 1u) again = 1u;
+            if (prob[j] != none) mass = 1u;
+        }
+        __syncthreads();
+        bool empty = mass == 0u && rest == none;
+        if (again) {                      // leave out the slots that repeat an earlier one's entry
+            uint32_t gone = 0u, left = 0u;            // a bit for each of this thread's slots
+            for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) {
+                bool repeats = false;
+                for (uint32_t i = 0; i < j; ++i) repeats = repeats || entry[i] == entry[j];
+                gone |= repeats ? b : 0u;
+                left |= !repeats && entry[j] != kNoEntry && prob[j] != none ? 1u : 0u;
             }
+            __syncthreads();
+            for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1)
+                if (gone & b) entry[j] = kNoEntry;
+            empty = __syncthreads_or((int)left) == 0 && rest == none;
         }
-        const double mt = __builtin_fmax((double)group_max<NW>(top_t, sh[0]) * a.inv_tau, (double)rest);
-        __syncthreads();
-        const bool empty = mt == -__builtin_inf();
-        auto teacher = [&](uint32_t j) { return (double)prob[j] * a.inv_tau - mt; };
         if (empty || (weight == 0.0f && !a.loss)) {
             if (a.loss && tid == 0u) a.loss[row] = 0.0f;
             if (grad) {
@@ -284,15 +286,6 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs a)
             __syncthreads();
             continue;
         }
-        double part = 0.0;
-        for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) {
-            if (repeats & b) entry[j] = kNoEntry;
-            if (entry[j] != kNoEntry) part += (double)exp_slot(teacher(j));
-        }
-        const double x_rest = (double)rest - mt;
-        const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
-        const double sum_t = group_total<NW>(part, sh64[0]) + (double)e_rest;
-        const float inv_t = 1.0f / (float)sum_t, p_rest = a.rest ? e_rest * inv_t : 0.0f;
         // the student's row; with a rest, without the listed entries
         auto unlisted = [&](const Vec16& y, uint32_t i) {
             Vec16 v = y;
@@ -304,73 +297,100 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs a)
             }
             return v;
         };
-        if (a.rest) {
-            if (NV) x.apply(unlisted);
-            const uint32_t i = x.vectors * E + x.lane;
-            if (x.lane < x.tail && (bits[i / 32u] >> (i % 32u) & 1u)) x.last = none;
-        }
-        auto each = [&](auto f) {
-            x.each_vector([&](const Vec16& y, uint32_t i) {
-                const Vec16 v = NV ? y : unlisted(y, i);
-                float s[E];
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e) s[e] = El::get(v, e);
-                f(s);
-            });
+        const uint32_t at = x.vectors * E + x.lane;
+        if (a.rest && x.lane < x.tail && (bits[at / 32u] >> (at % 32u) & 1u)) x.last = none;
+        // One pass: each thread's largest entry and the exponentials' sum against it, which
+        // shrinks as a larger one comes.  It starts from the type's lowest value, so that a
+        // row of -inf has a sum of 0.  A vector is added by pairs: short chains of roundings.
+        const float lowest = -3.40282347e38f;
+        float mine = lowest, sum = 0.0f;
+        auto add = [&](float top, float shrink, float terms) {
+            mine = top;
+            sum = __builtin_fmaf(sum, shrink, terms);
         };
-        float top = x.last;
-        each([&](const float (&s)[E]) {
+        x.each_vector([&](const Vec16& y, uint32_t i) {
+            const Vec16 v = unlisted(y, i);
+            float s[E], top = mine;
 #pragma unroll
-            for (uint32_t e = 0; e < E; ++e) top = __builtin_fmaxf(top, s[e]);
-        });
-        const float mu0 = group_max<NW>(top, sh[1]);
-        const float mu = mu0 == none ? 0.0f : mu0;
-        // a vector's entries by pairs, then the vectors: short chains of roundings
-        float m = mu0, sum = x.wave == 0u ? exp_entry(a, x.last, mu) : 0.0f;
-        each([&](const float (&s)[E]) {
-            float v[E];
+            for (uint32_t e = 0; e < E; ++e) {
+                s[e] = El::get(v, e);
+                top = __builtin_fmaxf(top, s[e]);
+            }
 #pragma unroll
-            for (uint32_t e = 0; e < E; ++e) v[e] = exp_entry(a, s[e], mu);
+            for (uint32_t e = 0; e < E; ++e) s[e] = exp_entry(a, s[e], top);
 #pragma unroll
             for (uint32_t n = E / 2u; n >= 1u; n /= 2u)
 #pragma unroll
-                for (uint32_t e = 0; e < n; ++e) v[e] += v[e + n];
-            sum += v[0];
+                for (uint32_t e = 0; e < n; ++e) s[e] += s[e + n];
+            add(top, exp_entry(a, mine, top), s[0]);
         });
-        const double all = group_total<NW>((double)sum, sh64[1]);
-        double listed = 0.0;
-        if (a.rest) {
-            top = none;
-            for (uint32_t j = tid; j < a.k; j += NT)
-                if (entry[j] != kNoEntry) top = __builtin_fmaxf(top, logit[j]);
-            m = __builtin_fmaxf(m, group_max<NW>(top, sh[2]));
+        if (x.wave == 0u) {
+            const float top = __builtin_fmaxf(mine, x.last);
+            add(top, exp_entry(a, mine, top), exp_entry(a, x.last, top));
         }
-        m = m == none ? 0.0f : m;
-        if (a.rest) {
-            for (uint32_t j = tid; j < a.k; j += NT)
-                if (entry[j] != kNoEntry) listed += (double)exp_slot(log_part(a, logit[j], m));
-            listed = group_total<NW>(listed, sh64[2]);
-        }
-        const Student st = student_row(a, m, mu, all, listed);
-        double d = 0.0;
+        // the largest values of the row, the listed entries and the teacher's
+        float top_l = lowest, top_t = none;
         for (uint32_t j = tid; j < a.k; j += NT) {
             if (entry[j] == kNoEntry) continue;
-            const double t = teacher(j);
-            const float e = exp_slot(t);
-            d += excess(e, t, log_part(a, logit[j], m));
-            prob[j] = e * inv_t;
+            top_l = __builtin_fmaxf(top_l, logit[j]);
+            top_t = __builtin_fmaxf(top_t, prob[j]);
         }
-        if (a.loss) {
-            d = group_total<NW>(d, sh64[3]);
-            if (tid == 0u) {
-                if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log64()));
-                a.loss[row] = row_loss(a, st, d, sum_t, Log64());
+        float mu = wave_max(mine);
+        top_l = wave_max(top_l);
+        top_t = wave_max(top_t);
+        if (NW > 1) {
+            if (x.lane == 0u) {
+                sh_max[0][x.wave] = mu;
+                sh_max[1][x.wave] = top_l;
+                sh_max[2][x.wave] = top_t;
             }
+            __syncthreads();
+            const uint32_t q = min(x.lane, (uint32_t)NW - 1u);
+            mu = wave_max(sh_max[0][q]);
+            top_l = wave_max(sh_max[1][q]);
+            top_t = wave_max(sh_max[2][q]);
         }
+        const float m = a.rest ? __builtin_fmaxf(mu, top_l) : mu;
+        const double mt = uniform(__builtin_fmax((double)top_t * a.inv_tau, (double)rest));
+        // the sums, and the excesses of the loss
+        double part = (double)(sum * exp_entry(a, mine, mu)), listed = 0.0, sum_t = 0.0, d = 0.0;
+        for (uint32_t j = tid; j < a.k; j += NT) {
+            if (entry[j] == kNoEntry) continue;
+            const double t = (double)prob[j] * a.inv_tau - mt, y = log_part(a, logit[j], m);
+            const float e = exp_slot(t);
+            prob[j] = e;
+            sum_t += (double)e;
+            d += excess(e, t, y);
+            if (a.rest) listed += (double)exp_slot(y);
+        }
+        part = wave_total(part);
+        listed = wave_total(listed);
+        sum_t = wave_total(sum_t);
+        d = wave_total(d);
+        if (NW > 1) {
+            if (x.lane == 0u) {
+                sh_sum[0][x.wave] = part;
+                sh_sum[1][x.wave] = listed;
+                sh_sum[2][x.wave] = sum_t;
+                sh_sum[3][x.wave] = d;
+            }
+            __syncthreads();
+            const bool in = x.lane < (uint32_t)NW;
+            part = wave_total(in ? sh_sum[0][x.lane] : 0.0);
+            listed = wave_total(in ? sh_sum[1][x.lane] : 0.0);
+            sum_t = wave_total(in ? sh_sum[2][x.lane] : 0.0);
+            d = wave_total(in ? sh_sum[3][x.lane] : 0.0);
+        }
+        const double x_rest = (double)rest - mt;
+        const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
+        sum_t += (double)e_rest;
+        const float inv_t = uniform(1.0f / (float)sum_t), p_rest = a.rest ? e_rest * inv_t : 0.0f;
+        const Student st = student_row(a, m, mu, part, listed);
         if (grad) {
             const GradScale g = grad_scale(a, st, weight, p_rest);
             const bool zero = weight == 0.0f;
-            auto other = [&](float s) { return zero ? 0.0f : exp_entry(a, s, mu) * g.other; };
+            const float scale = uniform(g.other);
+            auto other = [&](float s) { return zero ? 0.0f : exp_entry(a, s, mu) * scale; };
             x.each_vector([&](const Vec16& y, uint32_t i) {
                 float f[E];
 #pragma unroll
@@ -381,7 +401,11 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs a)
             __syncthreads();              // the listed entries over what the row's pass wrote
             for (uint32_t j = tid; j < a.k; j += NT)
                 if (entry[j] != kNoEntry)
-                    store_one(entry[j], zero ? 0.0f : exp_slot(log_part(a, logit[j], m)) * g.listed - prob[j] * g.weighted);
+                    store_one(entry[j], zero ? 0.0f : exp_slot(log_part(a, logit[j], m)) * g.listed - prob[j] * inv_t * g.weighted);
+        }
+        if (a.loss && tid == 0u) {
+            if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log64()));
+            a.loss[row] = row_loss(a, st, d, sum_t, Log64());
         }
         __syncthreads();                  // the row's shared memory is used again
     }

@@ -85,11 +85,11 @@ __device__ __forceinline__ float entry_z(float l, float m, float c) { return l =
 // rounding per operation (relative error 1.9e-7), truncated to 24 bits and shifted by the
 // whole part of z.  Coefficients scaled by 2^40, so that P 2^n is the weight before its
 // fraction is cut off; it needs at most 24 bits, so fp32 holds it too.
-// z + 1.5 2^23 rounds z to the whole number n that its low bits then show.  Below -41
-// (and for NaN, which the maximum turns into -63) P 2^n is less than 1.
+// z + 1.5 2^23 rounds z to the whole number n that its low bits then show.  At -41, to
+// which the maximum raises all below it and NaN, P 2^n is less than 1.
 __device__ __forceinline__ float entry_weight32(float z)
 {
-    z = __builtin_fmaxf(z, -63.0f);
+    z = __builtin_fmaxf(z, kLastZ);
     const float y = z + 0x1.8p23f;
     const float f = z - (y - 0x1.8p23f);
     float P = f * 0x1.5bb994p+30f + 0x1.3cea84p+33f;
@@ -446,6 +446,10 @@ struct SampleGroup {
     template <class F>
     __device__ __forceinline__ void append_vector(const Vec16& y, uint32_t v, F want)
     {
+        bool any = false;
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e) any = any | want(El::get(y, e));
+        if (__ballot(any) == 0u) return;
         uint32_t hits = 0u;
 #pragma unroll
         for (uint32_t e = 0; e < E; ++e) hits |= want(El::get(y, e)) ? 1u << e : 0u;
@@ -553,8 +557,7 @@ struct SampleGroup {
         uint64_t* const mine = sh.part_w[x.wave / waves];
         auto bin = [&](float l) {
             const float zi = (l - m) * s.c;
-            const float w = entry_weight32(zi);
-            if (w > 0.0f) atomicAdd((unsigned long long*)&mine[bin_of(zi)], (unsigned long long)whole_weight(w));
+            if (zi > kLastZ) atomicAdd((unsigned long long*)&mine[bin_of(zi)], (unsigned long long)entry_weight(zi));
         };
         x.each([&](float l, uint32_t) { bin(l); });
         if (x.wave == 0u) bin(x.last);                // the tail counts to the first part here
@@ -575,9 +578,11 @@ struct SampleGroup {
         __syncthreads();
         const uint32_t b = sh.found;
         const uint64_t before_w = sh.before_w;
+        // bin_of(z) == b: the bins' ends are exact in fp32
+        const float upper = -(float)b / (float)Sh::kPerZ, lower = -(float)(b + 1u) / (float)Sh::kPerZ;
         auto in_bin = [&](float l) {
             const float zi = (l - m) * s.c;
-            return zi >= kLastZ && bin_of(zi) == b;
+            return zi <= upper && zi > lower;
         };
         x.each_vector([&](const Vec16& y, uint32_t v) { append_vector(y, v, in_bin); });
         append_tail(in_bin);
@@ -720,7 +725,7 @@ struct SampleGroup {
 constexpr float kNearZ = -10.0f, kFarZ = -24.0f;
 
 template <int D, int NT>
-__global__ __launch_bounds__(NT, 8) void k_sample(SampleArgs a)
+__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_sample(SampleArgs a)
 {
     using R = Row<D, NT, 0>;
     __shared__ SampleShared<NT> sh;
