@@ -22,6 +22,8 @@ struct rlsim_head {
     int device = 0;
     uint32_t cus = 1;
     hipStream_t stream = nullptr;
+    char* work = nullptr;       // what the workgroups that share a row hand on (SampleSplit)
+    uint32_t split_rows = 0;    // most rows of such a call
     char err[256] = "";
 };
 
@@ -109,12 +111,45 @@ uint32_t tiny_grid(const rlsim_head* h, uint32_t rows, uint32_t vocab)
     return head_grid(h, (rows + per_group - 1u) / per_group, 256u);
 }
 
+// The workspace of the calls that share rows, and its parts.
+constexpr uint64_t kSplitGroupBytes = 4u + 4u + 8u + 8u * kSplitBins, kSplitRowBytes = 8u * kSplitList + 4u;
+uint64_t split_bytes(uint32_t rows) { return kSplitGroups * kSplitGroupBytes + rows * kSplitRowBytes; }
+SampleSplit sample_split(const rlsim_head* h)
+{
+    SampleSplit p{};
+    char* at = h->work;
+    p.sum = reinterpret_cast<uint64_t*>(at);
+    at += 8u * kSplitGroups;
+    p.part_w = reinterpret_cast<uint64_t*>(at);
+    at += 8ull * kSplitGroups * kSplitBins;
+    p.list = reinterpret_cast<uint64_t*>(at);
+    at += 8ull * kSplitList * h->split_rows;
+    p.top = reinterpret_cast<float*>(at);
+    at += 4u * kSplitGroups;
+    p.top_at = reinterpret_cast<uint32_t*>(at);
+    at += 4u * kSplitGroups;
+    p.count = reinterpret_cast<uint32_t*>(at);
+    return p;
+}
+
 template <int D>
 void launch_sample(const rlsim_head* h, const SampleArgs& a)
 {
     if (a.V <= kHeadTinyVocab) {
         const uint32_t grid = tiny_grid(h, a.rows, a.V);
         HEAD_TINY(k_sample_tiny, D, a.V, grid, h->stream, a);
+        return;
+    }
+    const uint32_t shared_by = a.rows <= h->split_rows ? sample_chunks(a.rows, a.V, Elem<D>::kBytes, h->cus) : 1u;
+    if (shared_by > 1u && a.rows * shared_by <= kSplitGroups) {
+        SampleSplit p = sample_split(h);
+        const uint32_t strip = 64u * Elem<D>::kPerVec, strips = (a.V + strip - 1u) / strip;
+        p.chunk = (strips + shared_by - 1u) / shared_by * strip;
+        p.chunks = (a.V + p.chunk - 1u) / p.chunk;
+        const dim3 grid(p.chunks, a.rows), block(kSplitThreads);
+        hipLaunchKernelGGL(k_sample_top<D>, grid, block, 0, h->stream, a, p);
+        hipLaunchKernelGGL(k_sample_chunk<D>, grid, block, 0, h->stream, a, p);
+        hipLaunchKernelGGL(k_sample_draw<D>, dim3(a.rows), block, 0, h->stream, a, p);
         return;
     }
     const uint32_t threads = head_threads(a.V, Elem<D>::kBytes);
@@ -177,6 +212,20 @@ int rlsim_head_create(uint32_t max_rows, uint32_t max_vocab, void* stream, rlsim
     if (e != hipSuccess) return head_fail(nullptr, RLSIM_EDEVICE, "rlsim_head_create: %s", hipGetErrorString(e));
     rlsim_head* h = new (std::nothrow) rlsim_head;
     if (!h) return head_fail(nullptr, RLSIM_ENOMEM, "rlsim_head_create: host allocation failed");
+    h->split_rows = std::min(max_rows, kSplitGroups / 2u);
+    const size_t bytes = split_bytes(h->split_rows);
+    e = hipMalloc(reinterpret_cast<void**>(&h->work), bytes);
+    if (e == hipSuccess) {
+        e = hipMemsetAsync(h->work, 0, bytes, static_cast<hipStream_t>(stream));   // a call finds its counters at 0
+        if (e == hipSuccess) e = hipStreamSynchronize(static_cast<hipStream_t>(stream));
+    }
+    if (e != hipSuccess) {
+        const int code = e == hipErrorOutOfMemory ? RLSIM_ENOMEM : RLSIM_EDEVICE;
+        if (h->work) (void)hipFree(h->work);
+        delete h;
+        (void)hipGetLastError();
+        return head_fail(nullptr, code, "rlsim_head_create: %s", hipGetErrorString(e));
+    }
     h->max_rows = max_rows;
     h->max_vocab = max_vocab;
     h->device = device;
@@ -297,6 +346,7 @@ int rlsim_head_destroy(rlsim_head_t* h)
     {
         HeadDevice g(h->device);
         if (hipStreamSynchronize(h->stream) != hipSuccess) rc = RLSIM_EDEVICE;
+        if (h->work) (void)hipFree(h->work);
     }
     delete h;
     return rc;

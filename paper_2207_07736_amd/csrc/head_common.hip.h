@@ -208,7 +208,7 @@ __device__ __forceinline__ float group_max(float x, float* sh)
     return wave_max(lane < (uint32_t)NW ? sh[lane] : -__builtin_inff());
 }
 // ---------------------------------------------------------------------------
-// A row as a workgroup of NT threads sees it: whole 16-byte vectors, then up to
+// A row (V entries of it, `from` entries behind its start) as a workgroup of NT threads sees it: whole 16-byte vectors, then up to
 // kPerVec - 1 entries of tail, one to a lane of the first wave.  A wave owns `seg`
 // consecutive strips of 64 vectors, so that index order is (wave, strip, lane,
 // entry).  NV > 0: up to NV strips a wave, held in registers from one read of the
@@ -226,9 +226,9 @@ struct Row {
     Vec16 reg[NV ? NV : 1];
     float last;                                   // this lane's entry of the tail (first wave)
 
-    __device__ __forceinline__ void open(const void* logits, uint64_t row, uint64_t stride, uint32_t V)
+    __device__ __forceinline__ void open(const void* logits, uint64_t row, uint64_t stride, uint32_t V, uint32_t from = 0u)
     {
-        p = static_cast<const char*>(logits) + row * stride * El::kBytes;
+        p = static_cast<const char*>(logits) + (row * stride + from) * El::kBytes;
         vectors = V / E;
         tail = V % E;
         seg = (vectors + 64u * NW - 1u) / (64u * NW);

@@ -29,4 +29,14 @@ inline uint32_t head_threads(uint32_t vocab, uint32_t elem_bytes)
     return vectors <= 64u * 4u ? 64u : vectors <= 256u * 8u ? 256u : 1024u;
 }
 
+// Workgroups that share a row of the sampling kernel (1: it has one of its own), for rows
+// longer than the tiny form's.
+inline uint32_t sample_chunks(uint32_t rows, uint32_t vocab, uint32_t elem_bytes, uint32_t cus)
+{
+    const uint32_t vectors = vocab / (16u / elem_bytes);
+    const uint32_t by_rows = 2u * cus / rows, by_size = vectors / 1024u;
+    const uint32_t chunks = by_rows < by_size ? by_rows : by_size;
+    return chunks < 2u ? 1u : chunks < 32u ? chunks : 32u;
+}
+
 }  // namespace rlsim_dev

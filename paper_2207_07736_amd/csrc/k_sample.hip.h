@@ -42,6 +42,22 @@ struct SampleArgs {
     float* logp;                  // or null
 };
 
+// A call of few rows shares each among several workgroups, a chunk of `chunk` entries (a
+// multiple of 64 vectors) to each; what they hand on, by workgroup (row * chunks + chunk) or row.
+constexpr uint32_t kSplitGroups = 1024u;  // most workgroups of such a call
+constexpr uint32_t kSplitChunks = 32u;    // most chunks of a row
+constexpr uint32_t kSplitList = 3072u;    // entries listed for a row
+constexpr uint32_t kSplitBins = 657u;
+struct SampleSplit {
+    uint32_t chunk, chunks;
+    float* top;                   // [groups] largest entry of the chunk
+    uint32_t* top_at;             // [groups] the first one's index
+    uint64_t* sum;                // [groups] weight
+    uint64_t* part_w;             // [groups][kSplitBins] weights by bins of z
+    uint64_t* list;               // [rows][kSplitList] codes
+    uint32_t* count;              // [rows] entries listed, 0 between calls
+};
+
 // A row's settings.  T <= 0 or NaN: the first of the largest entries.
 struct SampleRow {
     float T, c;
@@ -204,7 +220,7 @@ struct SampleShared {
     static constexpr uint32_t kUsedBins = 41u * kPerZ + 1u, kBins = (kUsedBins + 63u) / 64u * 64u;
     static constexpr uint32_t kParts = NT == 1024 ? 8u : NW;      // of a row, with bins of their own
     float f[NW];
-    uint64_t sum[NW + 1], group[NW];
+    uint64_t sum[kSplitChunks + 1u], group[NW];
     uint64_t part_w[kParts][kUsedBins];
     uint64_t w[kBins];
     uint32_t n[kBins];
@@ -316,22 +332,35 @@ __device__ __forceinline__ void find_listed(Sh& sh, Among in, uint32_t listed, C
         }
     });
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < in.n; i += NT) {
-        const uint64_t code = sh.few_code[i], own = sh.few_w[i];
-        uint64_t bn = in.before_n, bw = in.before_w;
-        for (uint32_t j = 0; j < in.n; ++j) {
+    // L lanes to an entry share the comparisons
+    constexpr uint32_t L = NT > kFew ? NT / kFew : 1u;
+    for (uint32_t i = threadIdx.x / L; i < kFew; i += NT / L) {
+        const bool real = i < in.n;
+        const uint64_t code = real ? sh.few_code[i] : 0u, own = real ? sh.few_w[i] : 0u;
+        uint32_t ahead_n = 0u;
+        uint64_t ahead_w = 0u;
+        for (uint32_t j = threadIdx.x % L; j < in.n; j += L) {
             const bool ahead = sh.few_code[j] < code;
-            bn += ahead ? 1u : 0u;
-            bw += ahead ? sh.few_w[j] : 0u;
+            ahead_n += ahead ? 1u : 0u;
+            ahead_w += ahead ? sh.few_w[j] : 0u;
         }
-        const uint64_t b = by_weight ? bw : bn, mine = by_weight ? own : 1u;
-        if (b < target && target <= b + mine) {
+#pragma unroll
+        for (int off = (int)L / 2; off >= 1; off /= 2) {
+            ahead_n += (uint32_t)__shfl_xor((int)ahead_n, off, 64);
+            ahead_w += __shfl_xor(ahead_w, off, 64);
+        }
+        const uint64_t bw = in.before_w + ahead_w, b = by_weight ? bw : in.before_n + ahead_n, mine = by_weight ? own : 1u;
+        if (real && b < target && target <= b + mine) {
             sh.cut = code;
             sh.cut_w = bw + own;
         }
     }
     __syncthreads();
 }
+
+// z from which entries are listed at first: with a top-k cut, where it is expected (a
+// thousandth of the largest weight), then further down.
+constexpr float kNearZ = -10.0f, kFarZ = -24.0f;
 
 template <int D, int NT>
 struct SampleGroup {
@@ -347,6 +376,7 @@ struct SampleGroup {
     const uint32_t row;
     const float m;
     const uint32_t ibits;         // of an index
+    const uint32_t from;          // index of x's first entry
 
     __device__ __forceinline__ float z(float l) const { return entry_z(l, m, s.c); }
     static __device__ __forceinline__ uint32_t bin_of(float z) { return (uint32_t)(z * -(float)Sh::kPerZ); }
@@ -453,13 +483,13 @@ struct SampleGroup {
         uint32_t hits = 0u;
 #pragma unroll
         for (uint32_t e = 0; e < E; ++e) hits |= want(El::get(y, e)) ? 1u << e : 0u;
-        append<E>(hits, [&](uint32_t e) { return code(El::get(y, e), v * E + e); });
+        append<E>(hits, [&](uint32_t e) { return code(El::get(y, e), from + v * E + e); });
     }
     template <class F>
     __device__ __forceinline__ void append_tail(F want)
     {
         if (x.wave == 0u)
-            append<1>(want(x.last) ? 1u : 0u, [&](uint32_t) { return code(x.last, x.vectors * E + x.lane); });
+            append<1>(want(x.last) ? 1u : 0u, [&](uint32_t) { return code(x.last, from + x.vectors * E + x.lane); });
     }
     __device__ __forceinline__ void clear_list()
     {
@@ -545,27 +575,31 @@ struct SampleGroup {
         return true;
     }
 
-    // Draw where top-p is the first cut.  One pass bins the weights by z, each wave's part
-    // of the row in bins of its own: they give the row's weight and the bin in which the
-    // cut lies, and later the parts' kept weights without another pass.  The entries of
-    // that bin are listed and the cut found among them.
-    __device__ __forceinline__ void draw_top_p()
+    // Draw where top-p is the first cut.  One pass bins the weights by z, each part of the
+    // row in bins of its own: they give the row's weight and the bin in which the cut lies,
+    // and later the parts' kept weights without another pass.  The entries of that bin are
+    // listed and the cut found among them.
+    __device__ __forceinline__ void bin_weights()
     {
         for (uint32_t j = threadIdx.x; j < Sh::kParts * Sh::kUsedBins; j += NT) (&sh.part_w[0][0])[j] = 0u;
         __syncthreads();
-        const uint32_t waves = NW / Sh::kParts;       // to a part
-        uint64_t* const mine = sh.part_w[x.wave / waves];
+        uint64_t* const mine = sh.part_w[x.wave / (NW / Sh::kParts)];
         auto bin = [&](float l) {
             const float zi = (l - m) * s.c;
             if (zi > kLastZ) atomicAdd((unsigned long long*)&mine[bin_of(zi)], (unsigned long long)entry_weight(zi));
         };
         x.each([&](float l, uint32_t) { bin(l); });
-        if (x.wave == 0u) bin(x.last);                // the tail counts to the first part here
+        if (x.wave == 0u) bin(x.last);
         __syncthreads();
+    }
+    // part_w: [parts][kUsedBins], parts of part_vectors vectors; the row's tail counts to
+    // part `tail_part`.
+    __device__ __forceinline__ void draw_top_p(const uint64_t* part_w, uint32_t parts, uint32_t part_vectors, uint32_t tail_part)
+    {
         for (uint32_t j = threadIdx.x; j < Sh::kBins; j += NT) {
             uint64_t w = 0u;
             if (j < Sh::kUsedBins)
-                for (uint32_t q = 0; q < Sh::kParts; ++q) w += sh.part_w[q][j];
+                for (uint32_t q = 0; q < parts; ++q) w += part_w[q * Sh::kUsedBins + j];
             sh.w[j] = w;
         }
         __syncthreads();
@@ -601,29 +635,35 @@ struct SampleGroup {
             return;
         }
         // a part's kept weight: the bins before the cut's, and what of that one is kept
-        for (uint32_t q = x.wave; q < Sh::kParts; q += NW) {
+        for (uint32_t q = x.wave; q < parts; q += NW) {
             uint64_t w = 0u;
-            for (uint32_t j = x.lane; j < b; j += 64u) w += sh.part_w[q][j];
+            for (uint32_t j = x.lane; j < b; j += 64u) w += part_w[q * Sh::kUsedBins + j];
             w = wave_total(w);
             if (x.lane == 0u) sh.sum[q] = w;
         }
         __syncthreads();
-        const uint32_t part_vectors = x.seg * 64u * waves;
         for (uint32_t j = threadIdx.x; j < in.n; j += NT)
             if (sh.list_code[j] <= cut) {
                 const uint32_t v = (uint32_t)(sh.list_code[j] & ((1ull << ibits) - 1u)) / E;
-                atomicAdd((unsigned long long*)&sh.sum[v < x.vectors ? v / part_vectors : 0u], (unsigned long long)listed_weight(j));
+                atomicAdd((unsigned long long*)&sh.sum[v < x.vectors ? v / part_vectors : tail_part],
+                          (unsigned long long)listed_weight(j));
             }
         __syncthreads();
+        pick_parts(parts, part_vectors, tail_part, weigh);
+    }
+    // pick() where sh.sum counts the tail to part tail_part
+    template <class F>
+    __device__ __forceinline__ void pick_parts(uint32_t parts, uint32_t part_vectors, uint32_t tail_part, F weigh)
+    {
         if (x.wave == 0u) {
             const uint64_t end = wave_total(x.lane < x.tail ? weigh(x.last, x.vectors * E + x.lane) : 0u);
             if (x.lane == 0u) {
-                sh.sum[0] -= end;
-                sh.sum[Sh::kParts] = end;
+                sh.sum[tail_part] -= end;
+                sh.sum[parts] = end;
             }
         }
         __syncthreads();
-        pick(Sh::kParts, part_vectors, weigh);
+        pick(parts, part_vectors, weigh);
     }
     __device__ __forceinline__ uint64_t weigh_kept(float l, uint32_t i, uint64_t cut) const
     {
@@ -668,6 +708,38 @@ struct SampleGroup {
         });
         __syncthreads();
         return close_list(in.n, in.before_n, in.before_w);
+    }
+
+    // The row's cuts, and where its draw is made from the list, the first z listed.  Without a
+    // cut the list has to reach min-p's: a margin of 0.01 in z, far more than the weights' error.
+    __device__ __forceinline__ bool cuts() const { return s.k < a.V || s.p24 < kAllP; }
+    __device__ __forceinline__ float near_z() const
+    {
+        return cuts() ? kNearZ : __builtin_fmaxf(__builtin_log2f((float)s.least) - 40.01f, kLastZ);
+    }
+    __device__ __forceinline__ void list_from(float z0)
+    {
+        auto want = [&](float l) { return (l - m) * s.c >= z0; };
+        x.each_vector([&](const Vec16& y, uint32_t v) { append_vector(y, v, want); });
+        append_tail(want);
+        __syncthreads();
+    }
+    // Cut and draw, near_z() on being listed.
+    __device__ __forceinline__ void draw_near()
+    {
+        bool done = draw_listed();
+        if (!done && cuts() && sh.count <= Sh::kList) {
+            clear_list();
+            x.each_again([&](float l, uint32_t i) {
+                if ((l - m) * s.c >= kFarZ) {
+                    const uint32_t at = atomicAdd(&sh.count, 1u);
+                    if (at < Sh::kList) sh.list_code[at] = code(l, i);
+                }
+            });
+            __syncthreads();
+            done = draw_listed();
+        }
+        if (!done) draw_dense();
     }
 
     // Cut and draw where too many entries are close to the largest: bins of z for the
@@ -720,15 +792,23 @@ struct SampleGroup {
     }
 };
 
-// z from which entries are listed at first: with a top-k cut, where it is expected (a
-// thousandth of the largest weight), then further down.
-constexpr float kNearZ = -10.0f, kFarZ = -24.0f;
+// What a row's settings and largest entry ask for.
+enum class SampleKind { kEmpty, kGreedy, kOdd, kPlain, kTopP, kListed };
+__device__ __forceinline__ SampleKind sample_kind(const SampleArgs& a, const SampleRow& s, float m)
+{
+    if (m == -__builtin_inff()) return SampleKind::kEmpty;
+    if (s.greedy) return SampleKind::kGreedy;
+    if (!(m < __builtin_inff() && s.c < __builtin_inff())) return SampleKind::kOdd;
+    if (s.k == a.V && s.p24 == kAllP) return s.least ? SampleKind::kListed : SampleKind::kPlain;
+    return s.k == a.V ? SampleKind::kTopP : SampleKind::kListed;
+}
 
 template <int D, int NT>
 __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_sample(SampleArgs a)
 {
     using R = Row<D, NT, 0>;
-    __shared__ SampleShared<NT> sh;
+    using Sh = SampleShared<NT>;
+    __shared__ Sh sh;
     for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         R x;
         x.open(a.logits, row, a.stride, a.V);
@@ -741,51 +821,160 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_sample(SampleArgs a)
         }
         const float m = uniform(group_max<R::NW>(x.max(), sh.f));
         if (R::NW == 1u) __syncthreads();
-        SampleGroup<D, NT> g{a, sh, x, s, row, m, 32u - (uint32_t)__builtin_clz(a.V)};
-        const bool cut = s.k < a.V || s.p24 < kAllP;
-        if (m == -__builtin_inff()) {
-            if (threadIdx.x == 0u) {
-                a.token[row] = -1;
-                if (a.logp) a.logp[row] = 0.0f;
-            }
-        } else if (s.greedy) {
+        SampleGroup<D, NT> g{a, sh, x, s, row, m, 32u - (uint32_t)__builtin_clz(a.V), 0u};
+        const SampleKind kind = sample_kind(a, s, m);
+        if (kind == SampleKind::kEmpty) {
+            if (threadIdx.x == 0u) g.answer(0xFFFFFFFFu, 0.0f);
+        } else if (kind == SampleKind::kGreedy) {
             uint32_t at = 0xFFFFFFFFu;
             x.each_and_tail([&](float l, uint32_t i) { at = l == m && i < at ? i : at; });
             if (at != 0xFFFFFFFFu) atomicMin(&sh.best, at);
             __syncthreads();
-            if (threadIdx.x == 0u) {
-                a.token[row] = (int32_t)sh.best;
-                if (a.logp) a.logp[row] = 0.0f;
-            }
-        } else if (!(m < __builtin_inff() && s.c < __builtin_inff())) {
+            if (threadIdx.x == 0u) g.answer(sh.best, 0.0f);
+        } else if (kind == SampleKind::kOdd) {
             g.draw_dense();
-        } else if (!cut && s.least == 0u) {
+        } else if (kind == SampleKind::kPlain) {
             double mine = 0.0;            // whole numbers, less than 2^53
             x.each([&](float l, uint32_t) { mine += (double)entry_weight32((l - m) * s.c); });
             g.draw((uint64_t)mine, [&](float l, uint32_t) { return entry_weight((l - m) * s.c); });
-        } else if (s.k == a.V && s.p24 < kAllP) {
-            g.draw_top_p();
+        } else if (kind == SampleKind::kTopP) {
+            g.bin_weights();
+            g.draw_top_p(&sh.part_w[0][0], Sh::kParts, x.seg * 64u * (R::NW / Sh::kParts), 0u);
         } else {
-            // without a cut the list has to reach min-p's: a margin of 0.01 in z, far more
-            // than the weights' error
-            const float least_z = __builtin_log2f((float)s.least) - 40.01f;
-            auto list = [&](float from) {
-                auto want = [&](float l) { return (l - m) * s.c >= from; };
-                x.each_vector([&](const Vec16& y, uint32_t v) { g.append_vector(y, v, want); });
-                g.append_tail(want);
-                __syncthreads();
-            };
-            bool done = false;
-#pragma unroll 1
-            for (uint32_t far = 0u; far < 2u && !done; ++far) {
-                if (far) g.clear_list();
-                list(!cut ? __builtin_fmaxf(least_z, kLastZ) : far ? kFarZ : kNearZ);
-                done = g.draw_listed();
-                if (!cut || sh.count > SampleShared<NT>::kList) break;
-            }
-            if (!done) g.draw_dense();
+            g.list_from(g.near_z());
+            g.draw_near();
         }
         __syncthreads();                  // the row's shared memory is used again
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: each is shared among workgroups, so that a single row's latency is that of a
+// chunk.  The first kernel finds the chunks' largest entries, the second weighs, bins or
+// lists them, the third makes the draws.  Three launches, because what one workgroup
+// tells another within a kernel has to pass the XCDs' separate L2 caches: with a counter by
+// which the last workgroup of a row went on to its draw, the write-backs of 448
+// workgroups took 64 rows of 50,001 from 69 to 119 us.
+constexpr uint32_t kSplitThreads = 1024u;
+
+template <int D>
+__global__ __launch_bounds__(kSplitThreads) void k_sample_top(SampleArgs a, SampleSplit p)
+{
+    using R = Row<D, (int)kSplitThreads, 0>;
+    __shared__ float sh[R::NW];
+    __shared__ uint32_t best;
+    const uint32_t row = blockIdx.y, from = blockIdx.x * p.chunk, group = row * p.chunks + blockIdx.x;
+    R x;
+    x.open(a.logits, row, a.stride, min(p.chunk, a.V - from), from);
+    if (threadIdx.x == 0u) best = 0xFFFFFFFFu;
+    const float m = uniform(group_max<R::NW>(x.max(), sh));
+    uint32_t at = 0xFFFFFFFFu;
+    x.each_and_tail([&](float l, uint32_t i) { at = l == m && i < at ? i : at; });
+    if (at != 0xFFFFFFFFu) atomicMin(&best, at);
+    __syncthreads();
+    if (threadIdx.x == 0u) {
+        p.top[group] = m;
+        p.top_at[group] = from + best;
+    }
+}
+
+// The row's largest entry, from its chunks': the first chunk that has it goes to `first`.
+__device__ __forceinline__ float split_top(const SampleSplit& p, uint32_t row, uint32_t& first)
+{
+    const uint32_t lane = threadIdx.x % 64u;
+    const float top = lane < p.chunks ? p.top[row * p.chunks + lane] : -__builtin_inff();
+    const float m = uniform(wave_max(top));
+    first = (uint32_t)__builtin_ctzll(__ballot(top == m));
+    return m;
+}
+
+template <int D>
+__global__ __launch_bounds__(kSplitThreads, 8) void k_sample_chunk(SampleArgs a, SampleSplit p)
+{
+    constexpr int NT = (int)kSplitThreads;
+    using R = Row<D, NT, 0>;
+    using Sh = SampleShared<NT>;
+    __shared__ Sh sh;
+    static_assert(Sh::kList == kSplitList && Sh::kUsedBins == kSplitBins);
+    const uint32_t row = blockIdx.y, from = blockIdx.x * p.chunk, group = row * p.chunks + blockIdx.x;
+    const SampleRow s = sample_row(a, row);
+    uint32_t first;
+    const float m = split_top(p, row, first);
+    const SampleKind kind = sample_kind(a, s, m);
+    if (kind == SampleKind::kEmpty || kind == SampleKind::kGreedy || kind == SampleKind::kOdd) return;
+    if (threadIdx.x == 0u) sh.count = 0u;
+    R x;
+    x.open(a.logits, row, a.stride, min(p.chunk, a.V - from), from);
+    SampleGroup<D, NT> part{a, sh, x, s, row, m, 32u - (uint32_t)__builtin_clz(a.V), from};
+    __syncthreads();
+    if (kind == SampleKind::kPlain) {
+        double mine = 0.0;
+        x.each_and_tail([&](float l, uint32_t) { mine += (double)entry_weight32((l - m) * s.c); });
+        const uint64_t w = wave_total((uint64_t)mine);
+        if (x.lane == 0u) sh.group[x.wave] = w;
+        __syncthreads();
+        if (threadIdx.x < 64u) {
+            const uint64_t all = wave_total(x.lane < R::NW ? sh.group[x.lane] : 0u);
+            if (x.lane == 0u) p.sum[group] = all;
+        }
+    } else if (kind == SampleKind::kTopP) {
+        part.bin_weights();
+        for (uint32_t j = threadIdx.x; j < Sh::kUsedBins; j += NT) {
+            uint64_t w = 0u;
+            for (uint32_t q = 0; q < Sh::kParts; ++q) w += sh.part_w[q][j];
+            p.part_w[(uint64_t)group * kSplitBins + j] = w;
+        }
+    } else {
+        part.list_from(part.near_z());
+        const uint32_t n = sh.count;
+        if (threadIdx.x == 0u) sh.few = atomicAdd(&p.count[row], n);
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < min(n, Sh::kList); j += NT)
+            if (sh.few + j < kSplitList) p.list[(uint64_t)row * kSplitList + sh.few + j] = sh.list_code[j];
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(kSplitThreads) void k_sample_draw(SampleArgs a, SampleSplit p)
+{
+    constexpr int NT = (int)kSplitThreads;
+    using R = Row<D, NT, 0>;
+    __shared__ SampleShared<NT> sh;
+    const uint32_t row = blockIdx.x, group0 = row * p.chunks;
+    const SampleRow s = sample_row(a, row);
+    uint32_t first;
+    const float m = split_top(p, row, first);
+    const SampleKind kind = sample_kind(a, s, m);
+    R x;
+    x.open(a.logits, row, a.stride, a.V);
+    SampleGroup<D, NT> g{a, sh, x, s, row, m, 32u - (uint32_t)__builtin_clz(a.V), 0u};
+    const uint32_t chunk_vectors = p.chunk / R::E, last = p.chunks - 1u;
+    uint32_t listed = 0u;
+    if (kind == SampleKind::kListed) {
+        listed = p.count[row];
+        for (uint32_t j = threadIdx.x; j < min(listed, kSplitList); j += NT) sh.list_code[j] = p.list[(uint64_t)row * kSplitList + j];
+    }
+    if (kind == SampleKind::kPlain)
+        for (uint32_t j = threadIdx.x; j < p.chunks; j += NT) sh.sum[j] = p.sum[group0 + j];
+    if (threadIdx.x == 0u) {
+        sh.count = listed;
+        sh.near = 0u;
+        sh.far = 0u;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0u && listed) p.count[row] = 0u;       // as a call finds it
+    if (kind == SampleKind::kEmpty) {
+        if (threadIdx.x == 0u) g.answer(0xFFFFFFFFu, 0.0f);
+    } else if (kind == SampleKind::kGreedy) {
+        if (threadIdx.x == 0u) g.answer(p.top_at[group0 + first], 0.0f);
+    } else if (kind == SampleKind::kOdd) {
+        g.draw_dense();
+    } else if (kind == SampleKind::kPlain) {
+        g.pick_parts(p.chunks, chunk_vectors, last, [&](float l, uint32_t) { return entry_weight((l - m) * s.c); });
+    } else if (kind == SampleKind::kTopP) {
+        g.draw_top_p(p.part_w + (uint64_t)group0 * kSplitBins, p.chunks, chunk_vectors, last);
+    } else {
+        g.draw_near();
     }
 }
 
