@@ -112,7 +112,7 @@ uint32_t tiny_grid(const rlsim_head* h, uint32_t rows, uint32_t vocab)
 }
 
 // The workspace of the calls that share rows, and its parts.
-constexpr uint64_t kSplitGroupBytes = 4u + 4u + 8u + 8u * kSplitBins, kSplitRowBytes = 8u * kSplitList + 4u;
+constexpr uint64_t kSplitGroupBytes = 8u + 8u * kSplitBins + 4u * 4u, kSplitRowBytes = 8u * kSplitList;
 uint64_t split_bytes(uint32_t rows) { return kSplitGroups * kSplitGroupBytes + rows * kSplitRowBytes; }
 SampleSplit sample_split(const rlsim_head* h)
 {
@@ -129,6 +129,8 @@ SampleSplit sample_split(const rlsim_head* h)
     p.top_at = reinterpret_cast<uint32_t*>(at);
     at += 4u * kSplitGroups;
     p.count = reinterpret_cast<uint32_t*>(at);
+    at += 4u * kSplitGroups;
+    p.list_z = reinterpret_cast<float*>(at);
     return p;
 }
 
@@ -146,6 +148,7 @@ void launch_sample(const rlsim_head* h, const SampleArgs& a)
         const uint32_t strip = 64u * Elem<D>::kPerVec, strips = (a.V + strip - 1u) / strip;
         p.chunk = (strips + shared_by - 1u) / shared_by * strip;
         p.chunks = (a.V + p.chunk - 1u) / p.chunk;
+        p.room = kSplitList / p.chunks;
         const dim3 grid(p.chunks, a.rows), block(kSplitThreads);
         hipLaunchKernelGGL(k_sample_top<D>, grid, block, 0, h->stream, a, p);
         hipLaunchKernelGGL(k_sample_chunk<D>, grid, block, 0, h->stream, a, p);
@@ -215,10 +218,6 @@ int rlsim_head_create(uint32_t max_rows, uint32_t max_vocab, void* stream, rlsim
     h->split_rows = std::min(max_rows, kSplitGroups / 2u);
     const size_t bytes = split_bytes(h->split_rows);
     e = hipMalloc(reinterpret_cast<void**>(&h->work), bytes);
-    if (e == hipSuccess) {
-        e = hipMemsetAsync(h->work, 0, bytes, static_cast<hipStream_t>(stream));   // a call finds its counters at 0
-        if (e == hipSuccess) e = hipStreamSynchronize(static_cast<hipStream_t>(stream));
-    }
     if (e != hipSuccess) {
         const int code = e == hipErrorOutOfMemory ? RLSIM_ENOMEM : RLSIM_EDEVICE;
         if (h->work) (void)hipFree(h->work);

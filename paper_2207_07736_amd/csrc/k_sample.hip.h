@@ -54,8 +54,10 @@ struct SampleSplit {
     uint32_t* top_at;             // [groups] the first one's index
     uint64_t* sum;                // [groups] weight
     uint64_t* part_w;             // [groups][kSplitBins] weights by bins of z
-    uint64_t* list;               // [rows][kSplitList] codes
-    uint32_t* count;              // [rows] entries listed, 0 between calls
+    uint64_t* list;               // [rows][chunks][room] codes
+    uint32_t room;                // kSplitList / chunks
+    uint32_t* count;              // [groups] entries listed; above `room`: not all of them
+    float* list_z;                // [groups] all with z above this are listed
 };
 
 // A row's settings.  T <= 0 or NaN: the first of the largest entries.
@@ -216,7 +218,7 @@ struct SampleShared {
     static constexpr uint32_t kList = NT == 64 ? 256u : NT == 256 ? 1024u : 3072u;
     // bins of z: -kPerZ z, 0 .. 41 kPerZ, padded to a multiple of 64; in longer rows finer
     // ones, so that the bin of a cut fits the list
-    static constexpr uint32_t kPerZ = NT == 1024 ? 16u : 8u;
+    static constexpr uint32_t kPerZ = NT == 1024 ? 16u : NT == 256 ? 8u : 4u;
     static constexpr uint32_t kUsedBins = 41u * kPerZ + 1u, kBins = (kUsedBins + 63u) / 64u * 64u;
     static constexpr uint32_t kParts = NT == 1024 ? 8u : NW;      // of a row, with bins of their own
     float f[NW];
@@ -358,9 +360,9 @@ __device__ __forceinline__ void find_listed(Sh& sh, Among in, uint32_t listed, C
     __syncthreads();
 }
 
-// z from which entries are listed at first: with a top-k cut, where it is expected (a
-// thousandth of the largest weight), then further down.
-constexpr float kNearZ = -10.0f, kFarZ = -24.0f;
+// z from which a row's entries are listed at first with a top-k cut, where it is expected: at
+// a thousandth of the largest weight.
+constexpr float kNearZ = -10.0f;
 
 template <int D, int NT>
 struct SampleGroup {
@@ -441,14 +443,23 @@ struct SampleGroup {
         upto += before;
         if (upto > target && upto - own <= target) {
             uint64_t t = upto - own;
-            for (uint32_t i = v0 * E; i < v1 * E; ++i) {
-                const float l = x.entry(i);
-                t += weigh(l, i);
-                if (t > target) {
-                    answer(i, sample_logp(l, m, s.T, whole));
-                    break;
+            uint32_t at = 0u;
+            float found = 0.0f;
+            bool done = false;
+            for (uint32_t v = v0; v < v1 && !done; ++v) {
+                const Vec16 y = x.vector(v);
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) {
+                    const float l = El::get(y, e);
+                    t += weigh(l, v * E + e);
+                    if (!done && t > target) {
+                        at = v * E + e;
+                        found = l;
+                        done = true;
+                    }
                 }
             }
+            answer(at, sample_logp(found, m, s.T, whole));
         }
     }
 
@@ -724,20 +735,53 @@ struct SampleGroup {
         append_tail(want);
         __syncthreads();
     }
+    // The z, a multiple of -1/2, from which to list a row's (a chunk's) entries: down to where
+    // the largest k are among them (then `enough` is set), if `room` takes that many, else
+    // as far as it takes them.  Counts go to sh.n.
+    static constexpr uint32_t kDepths = 128u;         // down to kLastZ and beyond
+    __device__ __forceinline__ float list_depth(uint32_t room, bool& enough)
+    {
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < kDepths; j += NT) sh.n[j] = 0u;
+        __syncthreads();
+        auto count = [&](float l) {
+            const float zi = (l - m) * s.c;
+            if (zi > kLastZ) atomicAdd(&sh.n[(uint32_t)(zi * -2.0f)], 1u);
+        };
+        x.each([&](float l, uint32_t) { count(l); });
+        if (x.wave == 0u) count(x.last);
+        __syncthreads();
+        // entries in the depths up to this lane's two
+        const uint32_t here = sh.n[2u * x.lane], next = sh.n[2u * x.lane + 1u];
+        const uint32_t upto1 = wave_scan(here + next), upto0 = upto1 - next;
+        const uint64_t room0 = __ballot(upto0 <= room), room1 = __ballot(upto1 <= room);
+        const uint64_t k0 = __ballot(upto0 >= s.k), k1 = __ballot(upto1 >= s.k);
+        // depths (of 2 lanes) that fit, a first part of all; the first that reaches k
+        const uint32_t fit = (uint32_t)(__builtin_popcountll(room0) + __builtin_popcountll(room1));
+        const uint32_t f0 = k0 ? 2u * (uint32_t)__builtin_ctzll(k0) : kDepths, f1 = k1 ? 2u * (uint32_t)__builtin_ctzll(k1) + 1u : kDepths;
+        const uint32_t need = min(f0, f1) + 1u;       // depths that hold the first k
+        enough = need <= fit || fit == kDepths;
+        return -0.5f * (float)min(need, fit);         // entries with z > this (none: 0)
+    }
+    __device__ __forceinline__ void list_above(float z0)
+    {
+        auto want = [&](float l) { return (l - m) * s.c > z0; };
+        x.each_vector([&](const Vec16& y, uint32_t v) { append_vector(y, v, want); });
+        append_tail(want);
+        __syncthreads();
+    }
     // Cut and draw, near_z() on being listed.
     __device__ __forceinline__ void draw_near()
     {
         bool done = draw_listed();
-        if (!done && cuts() && sh.count <= Sh::kList) {
-            clear_list();
-            x.each_again([&](float l, uint32_t i) {
-                if ((l - m) * s.c >= kFarZ) {
-                    const uint32_t at = atomicAdd(&sh.count, 1u);
-                    if (at < Sh::kList) sh.list_code[at] = code(l, i);
-                }
-            });
-            __syncthreads();
-            done = draw_listed();
+        if (!done && s.k < a.V) {
+            bool enough;
+            const float z0 = list_depth(Sh::kList, enough);
+            if (enough) {
+                clear_list();
+                list_above(z0);
+                done = draw_listed();
+            }
         }
         if (!done) draw_dense();
     }
@@ -925,12 +969,20 @@ __global__ __launch_bounds__(kSplitThreads, 8) void k_sample_chunk(SampleArgs a,
             p.part_w[(uint64_t)group * kSplitBins + j] = w;
         }
     } else {
-        part.list_from(part.near_z());
+        bool enough = true;
+        float z0 = 0.0f;
+        if (s.k < a.V) {
+            z0 = part.list_depth(p.room, enough);
+            part.list_above(z0);
+        } else {
+            part.list_from(part.near_z());
+        }
         const uint32_t n = sh.count;
-        if (threadIdx.x == 0u) sh.few = atomicAdd(&p.count[row], n);
-        __syncthreads();
-        for (uint32_t j = threadIdx.x; j < min(n, Sh::kList); j += NT)
-            if (sh.few + j < kSplitList) p.list[(uint64_t)row * kSplitList + sh.few + j] = sh.list_code[j];
+        for (uint32_t j = threadIdx.x; j < min(n, p.room); j += NT) p.list[(uint64_t)group * p.room + j] = sh.list_code[j];
+        if (threadIdx.x == 0u) {
+            p.count[group] = n;
+            p.list_z[group] = enough ? -__builtin_inff() : z0;
+        }
     }
 }
 
@@ -949,20 +1001,29 @@ __global__ __launch_bounds__(kSplitThreads) void k_sample_draw(SampleArgs a, Sam
     x.open(a.logits, row, a.stride, a.V);
     SampleGroup<D, NT> g{a, sh, x, s, row, m, 32u - (uint32_t)__builtin_clz(a.V), 0u};
     const uint32_t chunk_vectors = p.chunk / R::E, last = p.chunks - 1u;
-    uint32_t listed = 0u;
-    if (kind == SampleKind::kListed) {
-        listed = p.count[row];
-        for (uint32_t j = threadIdx.x; j < min(listed, kSplitList); j += NT) sh.list_code[j] = p.list[(uint64_t)row * kSplitList + j];
-    }
     if (kind == SampleKind::kPlain)
         for (uint32_t j = threadIdx.x; j < p.chunks; j += NT) sh.sum[j] = p.sum[group0 + j];
     if (threadIdx.x == 0u) {
-        sh.count = listed;
+        sh.count = 0u;
         sh.near = 0u;
         sh.far = 0u;
     }
     __syncthreads();
-    if (threadIdx.x == 0u && listed) p.count[row] = 0u;       // as a call finds it
+    if (kind == SampleKind::kListed) {
+        // the chunks' lists down to where all of them reach; too long a one shows in the count
+        const uint32_t lane = threadIdx.x % 64u, count = lane < p.chunks ? p.count[group0 + lane] : 0u;
+        const float z0 = uniform(wave_max(lane < p.chunks ? p.list_z[group0 + lane] : -__builtin_inff()));
+        const bool whole = __ballot(count > p.room) == 0ull;
+        for (uint32_t j = threadIdx.x; j < p.chunks * p.room; j += NT) {
+            const uint32_t q = j / p.room;
+            if (j - q * p.room >= min(p.count[group0 + q], p.room)) continue;
+            const uint64_t code = p.list[(uint64_t)group0 * p.room + j];
+            if (g.z(rank_logit<D>(code, g.ibits)) > z0) sh.list_code[atomicAdd(&sh.count, 1u)] = code;
+        }
+        __syncthreads();
+        if (!whole && threadIdx.x == 0u) sh.count = kSplitList + 1u;
+        __syncthreads();
+    }
     if (kind == SampleKind::kEmpty) {
         if (threadIdx.x == 0u) g.answer(0xFFFFFFFFu, 0.0f);
     } else if (kind == SampleKind::kGreedy) {
