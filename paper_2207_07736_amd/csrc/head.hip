@@ -93,23 +93,18 @@ uint32_t head_grid(const rlsim_head* h, uint32_t items, uint32_t threads)
             hipLaunchKernelGGL((KERNEL<D, 1024, 0>), dim3(grid), dim3(1024), shared, stream, args);                          \
     } while (0)
 
-#define HEAD_TINY(KERNEL, D, vocab, grid, stream, args)                                                                      \
+// Rows of up to kHeadTinyVocab entries: FEW has a thread to a row, TINY some lanes.
+#define HEAD_TINY(FEW, TINY, D, h, a)                                                                                        \
     do {                                                                                                                     \
-        if (vocab <= 2u) hipLaunchKernelGGL((KERNEL<D, 2>), dim3(grid), dim3(256), 0, stream, args);                         \
-        else if (vocab <= 4u) hipLaunchKernelGGL((KERNEL<D, 4>), dim3(grid), dim3(256), 0, stream, args);                    \
-        else if (vocab <= 8u) hipLaunchKernelGGL((KERNEL<D, 8>), dim3(grid), dim3(256), 0, stream, args);                    \
-        else if (vocab <= 16u) hipLaunchKernelGGL((KERNEL<D, 16>), dim3(grid), dim3(256), 0, stream, args);                  \
-        else if (vocab <= 32u) hipLaunchKernelGGL((KERNEL<D, 32>), dim3(grid), dim3(256), 0, stream, args);                  \
-        else hipLaunchKernelGGL((KERNEL<D, 64>), dim3(grid), dim3(256), 0, stream, args);                                    \
+        const uint32_t lanes = (a).V <= 8u ? 1u : (a).V <= 16u ? 16u : (a).V <= 32u ? 32u : 64u;                             \
+        const dim3 grid(head_grid(h, ((a).rows + 256u / lanes - 1u) / (256u / lanes), 256u)), block(256);                    \
+        if ((a).V <= 2u) hipLaunchKernelGGL((FEW<D, 2>), grid, block, 0, (h)->stream, a);                                    \
+        else if ((a).V <= 4u) hipLaunchKernelGGL((FEW<D, 4>), grid, block, 0, (h)->stream, a);                               \
+        else if ((a).V <= 8u) hipLaunchKernelGGL((FEW<D, 8>), grid, block, 0, (h)->stream, a);                               \
+        else if ((a).V <= 16u) hipLaunchKernelGGL((TINY<D, 16>), grid, block, 0, (h)->stream, a);                            \
+        else if ((a).V <= 32u) hipLaunchKernelGGL((TINY<D, 32>), grid, block, 0, (h)->stream, a);                            \
+        else hipLaunchKernelGGL((TINY<D, 64>), grid, block, 0, (h)->stream, a);                                              \
     } while (0)
-
-uint32_t tiny_grid(const rlsim_head* h, uint32_t rows, uint32_t vocab)
-{
-    uint32_t lanes = 2u;
-    while (lanes < vocab) lanes *= 2u;
-    const uint32_t per_group = 256u / lanes;
-    return head_grid(h, (rows + per_group - 1u) / per_group, 256u);
-}
 
 // The workspace of the calls that share rows, and its parts.
 constexpr uint64_t kSplitGroupBytes = 8u + 8u * kSplitBins + 4u * 4u, kSplitRowBytes = 8u * kSplitList;
@@ -138,8 +133,7 @@ template <int D>
 void launch_sample(const rlsim_head* h, const SampleArgs& a)
 {
     if (a.V <= kHeadTinyVocab) {
-        const uint32_t grid = tiny_grid(h, a.rows, a.V);
-        HEAD_TINY(k_sample_tiny, D, a.V, grid, h->stream, a);
+        HEAD_TINY(k_sample_few, k_sample_tiny, D, h, a);
         return;
     }
     const uint32_t shared_by = a.rows <= h->split_rows ? sample_chunks(a.rows, a.V, Elem<D>::kBytes, h->cus) : 1u;
@@ -166,8 +160,7 @@ template <int D>
 void launch_distill(const rlsim_head* h, const DistillArgs& a)
 {
     if (a.V <= kHeadTinyVocab) {
-        const uint32_t grid = tiny_grid(h, a.rows, a.V);
-        HEAD_TINY(k_distill_tiny, D, a.V, grid, h->stream, a);
+        HEAD_TINY(k_distill_few, k_distill_tiny, D, h, a);
         return;
     }
     const HeadForm form = head_form(a.V, Elem<D>::kBytes);

@@ -6,7 +6,7 @@
 
 namespace rlsim_dev {
 
-// Rows of up to 64 entries: a power of two of lanes to a row, one entry a lane.
+// Rows of up to 64 entries: one thread to a row for up to 8, else one lane to an entry.
 constexpr uint32_t kHeadTinyVocab = 64u;
 
 // Threads to a row and strips of 64 16-byte vectors a wave of them holds in

@@ -15,7 +15,8 @@
 // stands in an earlier slot.  A row without any teacher mass has loss 0 and gradient 0
 // whatever its logits; so has the gradient of a row of weight 0.
 //
-// k_distill_tiny: rows of up to 64 entries, a power of two of lanes to a row.
+// k_distill_few, k_distill_tiny: rows of up to 8 entries, one thread to a row, and of up to
+// 64, 16 to 64 lanes to a row.
 // k_distill: longer rows, one workgroup to a row, held in registers where it fits
 // (Row), so that loss and gradient cost one read and one write of it.  The gradient
 // may overwrite the logits: a thread writes only what it has read, and the listed
@@ -144,6 +145,71 @@ __device__ __forceinline__ GradScale grad_scale(const DistillArgs& a, const Stud
     g.listed = g.weighted * inv;
     g.other = g.weighted * (s.share * inv - (p_rest == 0.0f || s.sum == 0.0 ? 0.0f : p_rest / (float)s.sum));
     return g;
+}
+
+// ---------------------------------------------------------------------------
+template <int D, int N>
+__global__ __launch_bounds__(256) void k_distill_few(DistillArgs a)
+{
+    using El = Elem<D>;
+    const float none = -__builtin_inff();
+    for (uint32_t row = blockIdx.x * 256u + threadIdx.x; row < a.rows; row += gridDim.x * 256u) {
+        const typename El::Word* const logits = static_cast<const typename El::Word*>(a.logits) + (uint64_t)row * a.stride;
+        float s[N], t[N], e_t[N], e_s[N];
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+            s[e] = e < a.V ? El::one(logits[e]) : none;
+            t[e] = none;
+        }
+        const float weight = a.weight ? a.weight[row] : 1.0f;
+        const float rest = a.rest ? rest_value(a, row) : none;
+        uint32_t listed = 0u;             // a bit for each entry; the first slot that names it counts
+        for (uint32_t j = 0; j < a.k; ++j) {
+            const Slot slot = load_slot(a, row, j);
+#pragma unroll
+            for (uint32_t e = 0; e < N; ++e) t[e] = slot.entry == e && !(listed >> e & 1u) ? slot.t : t[e];
+            listed |= slot.entry != kNoEntry ? 1u << slot.entry : 0u;
+        }
+        float top_t = none, m = none, mu = none;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+            top_t = __builtin_fmaxf(top_t, t[e]);
+            m = __builtin_fmaxf(m, s[e]);
+            mu = __builtin_fmaxf(mu, a.rest && (listed >> e & 1u) ? none : s[e]);
+        }
+        m = m == none ? 0.0f : m;
+        mu = mu == none ? 0.0f : mu;
+        const double mt = __builtin_fmax((double)top_t * a.inv_tau, (double)rest), x_rest = (double)rest - mt;
+        const bool empty = mt == -__builtin_inf();
+        const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
+        float sum = 0.0f, apart = 0.0f, sum_t = e_rest;
+        double d = 0.0;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+            const bool in = listed >> e & 1u;
+            const double x = (double)t[e] * a.inv_tau - mt;
+            e_t[e] = in ? exp_slot(x) : 0.0f;
+            sum_t += e_t[e];
+            if (in) d += excess(e_t[e], x, log_part(a, s[e], m));
+            e_s[e] = e >= a.V ? 0.0f : exp_slot(log_part(a, s[e], a.rest && in ? m : mu));
+            (a.rest && in ? apart : sum) += e_s[e];
+        }
+        const Student st = student_row(a, m, mu, sum, apart);
+        if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log32()));
+        if (a.loss) a.loss[row] = empty ? 0.0f : row_loss(a, st, d, sum_t, Log32());
+        if (a.grad) {
+            const float inv_t = 1.0f / sum_t;
+            const GradScale g = grad_scale(a, st, weight, a.rest ? e_rest * inv_t : 0.0f);
+            typename El::Word* const grad = static_cast<typename El::Word*>(a.grad) + (uint64_t)row * a.grad_stride;
+#pragma unroll
+            for (uint32_t e = 0; e < N; ++e) {
+                const bool in = listed >> e & 1u;
+                float ds = e_s[e] * (a.rest && in ? g.listed : g.other) - (in ? e_t[e] * inv_t * g.weighted : 0.0f);
+                if (empty || weight == 0.0f) ds = 0.0f;
+                if (e < a.V) grad[e] = El::word(ds);
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------

@@ -14,8 +14,8 @@
 // floor(u 2^24) W' / 2^24 (rounded down), W' the kept sum.  The
 // log-probability is (l - m) / T - ln(W' / 2^40).
 //
-// k_sample_tiny: rows of up to 64 entries, a power of two of lanes to a row; ranks
-// by comparing every pair of a row's lanes.
+// k_sample_few, k_sample_tiny: rows of up to 8 entries, one thread to a row, and of up to
+// 64, 16 to 64 lanes to a row; ranks by comparing every pair of entries.
 // k_sample: longer rows, one workgroup to a row, held in registers where it fits
 // (Row).  The end of the kept part is found without sorting: the entries' weights
 // and counts are binned by z in steps of 1/8, the bin in which the cut lies is
@@ -147,6 +147,69 @@ __device__ __forceinline__ float sample_logp(float l, float m, float T, uint64_t
 {
     const float above = l == m ? 0.0f : (l - m) / T;
     return above - __builtin_logf((float)whole * 0x1p-40f);
+}
+
+// ---------------------------------------------------------------------------
+template <int D, int N>
+__global__ __launch_bounds__(256) void k_sample_few(SampleArgs a)
+{
+    using El = Elem<D>;
+    const float none = -__builtin_inff();
+    for (uint32_t row = blockIdx.x * 256u + threadIdx.x; row < a.rows; row += gridDim.x * 256u) {
+        const typename El::Word* const p = static_cast<const typename El::Word*>(a.logits) + (uint64_t)row * a.stride;
+        float l[N], m = none;
+        uint64_t w[N], whole = 0u;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+            l[e] = e < a.V ? El::one(p[e]) : none;
+            l[e] = l[e] == l[e] ? l[e] : none;
+            m = __builtin_fmaxf(m, l[e]);
+        }
+        const SampleRow s = sample_row(a, row);
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) w[e] = l[e] > none ? entry_weight(entry_z(l[e], m, s.c)) : 0u;
+        if (s.k < a.V || s.p24 < kAllP || s.greedy) {
+            uint32_t rank[N];
+            uint64_t before[N], all = 0u;         // the entries ahead of each: how many, and their weight
+#pragma unroll
+            for (uint32_t e = 0; e < N; ++e) {
+                rank[e] = 0u;
+                before[e] = 0u;
+#pragma unroll
+                for (uint32_t j = 0; j < N; ++j) {
+                    const bool ahead = l[j] > l[e] || (l[j] == l[e] && j < e);
+                    rank[e] += ahead ? 1u : 0u;
+                    before[e] += ahead ? w[j] : 0u;
+                }
+                all += rank[e] < s.k ? w[e] : 0u;
+            }
+            const uint64_t target = share24(all, s.p24);
+#pragma unroll
+            for (uint32_t e = 0; e < N; ++e) {
+                const bool keep = rank[e] == 0u || (!s.greedy && rank[e] < s.k && (s.p24 == kAllP || before[e] < target));
+                w[e] = keep ? w[e] : 0u;
+            }
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+            w[e] = w[e] >= s.least ? w[e] : 0u;
+            whole += w[e];
+        }
+        const uint64_t target = share24(whole, s.u24);
+        uint64_t running = 0u;
+        int32_t token = -1;
+        float found = m;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+            running += w[e];
+            if (token < 0 && running > target) {
+                token = (int32_t)e;
+                found = l[e];
+            }
+        }
+        a.token[row] = token;
+        if (a.logp) a.logp[row] = s.greedy || token < 0 ? 0.0f : sample_logp(found, m, s.T, whole);
+    }
 }
 
 // ---------------------------------------------------------------------------

@@ -86,8 +86,10 @@ class Head:
         self.h = None
         self._dtypes = {torch.float32: RLSIM_F32, torch.bfloat16: RLSIM_BF16, torch.float16: RLSIM_F16}
         self._index = {torch.int32: 4, torch.int64: 8}
-        self._torch = torch
+        self._torch, self._tensor, self._empty = torch, torch.Tensor, torch.empty
+        self._f32, self._i32 = torch.float32, torch.int32
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._ordinal = self.device.index
         self.max_rows, self.max_vocab = int(max_rows), int(max_vocab)
         self.h = rlsim_head_create(max_rows, max_vocab, stream)
 
@@ -103,23 +105,35 @@ class Head:
             pass
 
     def _rows(self, name, t, rows=None, columns=None):
-        """A 2-d tensor whose rows are consecutive elements, and its row stride."""
-        if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (columns is not None and t.shape[1] != columns):
+        """The address of a 2-d tensor whose rows are consecutive elements, its shape and
+        its row stride."""
+        shape = t.shape
+        if len(shape) != 2 or (rows is not None and shape[0] != rows) or (columns is not None and shape[1] != columns):
             raise ValueError(f"{name} must be 2-d" + ("" if rows is None else f", [{rows}, {columns or 'k'}]"))
-        if t.device != self.device:
+        if t.get_device() != self._ordinal:
             raise ValueError(f"{name} must be on {self.device}")
-        stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-        if t.shape[1] > 1 and t.stride(1) != 1 or stride < t.shape[1]:
+        n, width = shape
+        if t.is_contiguous():
+            return t.data_ptr(), n, width, width
+        stride, step = t.stride()
+        stride = stride if n > 1 else width
+        if (width > 1 and step != 1) or stride < width:
             raise ValueError(f"{name} must hold each row in consecutive elements, rows apart")
-        return t.data_ptr(), stride
+        return t.data_ptr(), n, width, stride
 
     def _vector(self, name, t, rows, dtype):
         """The address of a [rows] tensor, None for None."""
         if t is None:
             return None
-        if t.dtype != dtype or t.dim() != 1 or t.shape[0] != rows or (rows > 1 and t.stride(0) != 1) or t.device != self.device:
+        if t.dtype != dtype or t.shape != (rows,) or not t.is_contiguous() or t.get_device() != self._ordinal:
             raise ValueError(f"{name} must be {dtype}, [{rows}], contiguous, on {self.device}")
         return t.data_ptr()
+
+    def _setting(self, name, value, rows, dtype):
+        """A setting as a number for the call and an address of [rows] numbers, one of them."""
+        if isinstance(value, self._tensor):
+            return 0, self._vector(name, value, rows, dtype)
+        return value, None
 
     def _dtype(self, name, t):
         try:
@@ -132,41 +146,23 @@ class Head:
         numbers ``u`` [rows] (float32).  Each setting is a number, or a [rows] tensor
         (float32; top_k: int32).  Returns the int32 tokens, or with ``logp`` also
         their float32 log-probabilities among the entries that the filters keep."""
-        torch = self._torch
-        a = rlsim_sample()
-        a.dtype = self._dtype("logits", logits)
-        a.logits, a.row_stride = self._rows("logits", logits)
-        rows, a.vocab = logits.shape
-        a.rows = rows
+        dtype = self._dtype("logits", logits)
+        data, rows, vocab, stride = self._rows("logits", logits)
         if u is None:
             raise ValueError("u is needed")
-        a.u = self._vector("u", u, rows, torch.float32)
-        if torch.is_tensor(temperature):
-            a.temperature_rows = self._vector("temperature", temperature, rows, torch.float32)
-        else:
-            a.temperature = temperature
-        if torch.is_tensor(top_k):
-            a.top_k_rows = self._vector("top_k", top_k, rows, torch.int32)
-        else:
-            if top_k < 0 or top_k > 0xFFFFFFFF:
-                raise ValueError("top_k must be >= 0")
-            a.top_k = top_k
-        if torch.is_tensor(top_p):
-            a.top_p_rows = self._vector("top_p", top_p, rows, torch.float32)
-        else:
-            a.top_p = top_p
-        if torch.is_tensor(min_p):
-            a.min_p_rows = self._vector("min_p", min_p, rows, torch.float32)
-        else:
-            a.min_p = min_p
-        token = torch.empty(rows, dtype=torch.int32, device=self.device)
-        a.token = token.data_ptr()
-        p = None
-        if logp:
-            p = torch.empty(rows, dtype=torch.float32, device=self.device)
-            a.logp = p.data_ptr()
-        rlsim_head_sample(self.h, a)
-        return (token, p) if logp else token
+        f32 = self._f32
+        T, T_rows = self._setting("temperature", temperature, rows, f32)
+        k, k_rows = self._setting("top_k", top_k, rows, self._i32)
+        p, p_rows = self._setting("top_p", top_p, rows, f32)
+        m, m_rows = self._setting("min_p", min_p, rows, f32)
+        if not 0 <= k <= 0xFFFFFFFF:
+            raise ValueError("top_k must be >= 0")
+        token = self._empty(rows, dtype=self._i32, device=self.device)
+        lp = self._empty(rows, dtype=f32, device=self.device) if logp else None
+        rlsim_head_sample(self.h, rlsim_sample(dtype, data, rows, vocab, stride, self._vector("u", u, rows, f32), T, k, p, m,
+                                               T_rows, k_rows, p_rows, m_rows, token.data_ptr(),
+                                               lp.data_ptr() if logp else None))
+        return (token, lp) if logp else token
 
     def distill(self, logits, teacher, index, temperature: float = 1.0, rest=None, weight=None, loss: bool = True, grad=True):
         """Distil rows of student ``logits`` [rows, vocab] from a teacher's top logits
@@ -176,36 +172,25 @@ class Head:
         [rows] and the gradient of sum(weight * loss) in the logits' type; ``loss``
         or ``grad`` False leaves that one out.  ``grad`` may be a tensor to write to,
         the logits themselves among them."""
-        torch = self._torch
-        a = rlsim_distill()
-        a.dtype = self._dtype("logits", logits)
-        a.logits, a.row_stride = self._rows("logits", logits)
-        rows, a.vocab = logits.shape
-        a.rows = rows
-        a.teacher_dtype = self._dtype("teacher", teacher)
-        a.teacher, a.teacher_stride = self._rows("teacher", teacher, rows)
+        dtype = self._dtype("logits", logits)
+        data, rows, vocab, stride = self._rows("logits", logits)
+        t_dtype = self._dtype("teacher", teacher)
+        t_data, _, k, t_stride = self._rows("teacher", teacher, rows)
         if index.dtype not in self._index:
             raise ValueError("index must be int32 or int64")
-        a.k = teacher.shape[1]
-        a.index_bytes = self._index[index.dtype]
-        a.index, a.index_stride = self._rows("index", index, rows, a.k)
-        a.temperature = temperature
-        a.rest = self._vector("rest", rest, rows, torch.float32)
-        a.weight = self._vector("weight", weight, rows, torch.float32)
-        losses = None
-        if loss:
-            losses = torch.empty(rows, dtype=torch.float32, device=self.device)
-            a.loss = losses.data_ptr()
-        out = None
+        i_data, _, _, i_stride = self._rows("index", index, rows, k)
+        losses = self._empty(rows, dtype=self._f32, device=self.device) if loss else None
+        out, g_data, g_stride = None, None, 0
         if grad is not False:
-            if grad is True:
-                out = torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
-            else:
-                out = grad
-                if out.dtype != logits.dtype:
-                    raise ValueError("grad must have the logits' type")
-            a.grad, a.grad_stride = self._rows("grad", out, rows, logits.shape[1])
-        rlsim_head_distill(self.h, a)
+            out = self._empty((rows, vocab), dtype=logits.dtype, device=self.device) if grad is True else grad
+            if out.dtype != logits.dtype:
+                raise ValueError("grad must have the logits' type")
+            g_data, _, _, g_stride = self._rows("grad", out, rows, vocab)
+        rlsim_head_distill(self.h, rlsim_distill(dtype, data, rows, vocab, stride, t_dtype, t_data, t_stride,
+                                                 self._index[index.dtype], i_data, i_stride, k, temperature,
+                                                 self._vector("rest", rest, rows, self._f32),
+                                                 self._vector("weight", weight, rows, self._f32),
+                                                 losses.data_ptr() if loss else None, g_data, g_stride))
         if loss and out is not None:
             return losses, out
         return losses if loss else out
