@@ -56,6 +56,8 @@ struct HeadDevice {
     }
 };
 
+constexpr uint64_t kLastLevelBytes = 256ull << 20;
+
 bool known_dtype(int d) { return d == RLSIM_F32 || d == RLSIM_BF16 || d == RLSIM_F16; }
 uint32_t dtype_bytes(int d) { return d == RLSIM_F32 ? 4u : 2u; }
 bool aligned(const void* p, uint32_t bytes) { return (uintptr_t)p % bytes == 0u; }
@@ -109,6 +111,21 @@ uint32_t head_grid(const rlsim_head* h, uint32_t items, uint32_t threads)
 // The workspace of the calls that share rows, and its parts.
 constexpr uint64_t kSplitGroupBytes = 8u + 8u * kSplitBins + 4u * 4u, kSplitRowBytes = 8u * kSplitList;
 uint64_t split_bytes(uint32_t rows) { return kSplitGroups * kSplitGroupBytes + rows * kSplitRowBytes; }
+DistillSplit distill_split(const rlsim_head* h)
+{
+    static_assert(kSplitRowBytes >= 8u * kHeadMaxTeacher);
+    static_assert(kSplitGroups * kSplitGroupBytes >= kDistillSplitGroups * 12u);
+    DistillSplit p{};
+    char* at = h->work;
+    p.sum = reinterpret_cast<double*>(at);
+    at += 8u * kDistillSplitGroups;
+    p.mu = reinterpret_cast<float*>(at);
+    at += 4u * kDistillSplitGroups;
+    p.entry = reinterpret_cast<uint32_t*>(at);
+    at += 4ull * kHeadMaxTeacher * h->split_rows;
+    p.logit = reinterpret_cast<float*>(at);
+    return p;
+}
 SampleSplit sample_split(const rlsim_head* h)
 {
     SampleSplit p{};
@@ -163,6 +180,17 @@ void launch_distill(const rlsim_head* h, const DistillArgs& a)
         HEAD_TINY(k_distill_few, k_distill_tiny, D, h, a);
         return;
     }
+    const uint32_t shared_by = a.rows <= h->split_rows ? distill_chunks(a.rows, a.V, Elem<D>::kBytes, h->cus) : 1u;
+    if (shared_by > 1u && a.rows * shared_by <= kDistillSplitGroups) {
+        DistillSplit p = distill_split(h);
+        const uint32_t strip = 64u * Elem<D>::kPerVec, strips = (a.V + strip - 1u) / strip;
+        p.chunk = (strips + shared_by - 1u) / shared_by * strip;
+        p.chunks = (a.V + p.chunk - 1u) / p.chunk;
+        const dim3 grid(p.chunks, a.rows), block(kDistillSplitThreads);
+        hipLaunchKernelGGL(k_distill_chunk<D>, grid, block, p.chunk / 8u + 8u * a.k, h->stream, a, p);
+        hipLaunchKernelGGL(k_distill_join<D>, a.grad ? grid : dim3(1, a.rows), block, 12u * a.k, h->stream, a, p);
+        return;
+    }
     const HeadForm form = head_form(a.V, Elem<D>::kBytes);
     const uint32_t grid = head_grid(h, a.rows, form.threads);
     const uint32_t shared = distill_shared_bytes(a.k, a.V);
@@ -174,8 +202,12 @@ template <int D>
 hipError_t allow_shared()
 {
     const int bytes = (int)distill_shared_bytes(kHeadMaxTeacher, kHeadMaxVocab);
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(k_distill<D, 1024, 0>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    const void* const kernels[] = {reinterpret_cast<const void*>(k_distill<D, 1024, 0>),
+                                   reinterpret_cast<const void*>(k_distill_chunk<D>)};
+    hipError_t e = hipSuccess;
+    for (const void* k : kernels)
+        if (e == hipSuccess) e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e;
 }
 
 // The bytes that `rows` rows of `row` bytes take, `stride` bytes apart.
@@ -323,6 +355,7 @@ int rlsim_head_distill(rlsim_head_t* h, const rlsim_distill* d)
     a.loss = d->loss;
     a.grad = d->grad;
     a.grad_stride = d->grad_stride;
+    a.past_cache = d->grad && (uint64_t)d->rows * d->vocab * dtype_bytes(d->dtype) > kLastLevelBytes ? 1u : 0u;
     if (d->dtype == RLSIM_F32) launch_distill<kHeadF32>(h, a);
     else if (d->dtype == RLSIM_BF16) launch_distill<kHeadBF16>(h, a);
     else launch_distill<kHeadF16>(h, a);

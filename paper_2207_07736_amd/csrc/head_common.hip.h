@@ -21,6 +21,7 @@ template <> struct Elem<kHeadF32> {
     static constexpr uint32_t kNegInf = 0xFF800000u;             // a word of -inf entries
     static constexpr uint32_t kZeroBits = 0u;                    // of an entry as a float
     struct __attribute__((packed, aligned(4))) Run { uint32_t w[4]; };
+    typedef uint32_t Packed __attribute__((ext_vector_type(4), aligned(4)));
     using Word = uint32_t;
     __device__ static float get(const Vec16& v, uint32_t e) { return __builtin_bit_cast(float, v.w[e]); }
     __device__ static Vec16 with_neg_inf(Vec16 v, uint32_t e) { v.w[e] = kNegInf; return v; }
@@ -36,6 +37,7 @@ template <> struct Elem<kHeadBF16> {
     static constexpr uint32_t kNegInf = 0xFF80FF80u;
     static constexpr uint32_t kZeroBits = 16u;
     struct __attribute__((packed, aligned(2))) Run { uint32_t w[4]; };
+    typedef uint32_t Packed __attribute__((ext_vector_type(4), aligned(2)));
     using Word = uint16_t;
     __device__ static float get(const Vec16& v, uint32_t e)
     {
@@ -63,6 +65,7 @@ template <> struct Elem<kHeadF16> {
     static constexpr uint32_t kNegInf = 0xFC00FC00u;
     static constexpr uint32_t kZeroBits = 13u;
     struct __attribute__((packed, aligned(2))) Run { uint32_t w[4]; };
+    typedef uint32_t Packed __attribute__((ext_vector_type(4), aligned(2)));
     using Word = uint16_t;
     __device__ static float get(const Vec16& v, uint32_t e)
     {

@@ -39,4 +39,13 @@ inline uint32_t sample_chunks(uint32_t rows, uint32_t vocab, uint32_t elem_bytes
     return chunks < 2u ? 1u : chunks < 32u ? chunks : 32u;
 }
 
+// The same for the distillation kernel.
+inline uint32_t distill_chunks(uint32_t rows, uint32_t vocab, uint32_t elem_bytes, uint32_t cus)
+{
+    const uint32_t vectors = vocab / (16u / elem_bytes);
+    const uint32_t by_rows = 2u * cus / rows, by_size = vectors / 512u;
+    const uint32_t chunks = by_rows < by_size ? by_rows : by_size;
+    return chunks < 2u ? 1u : chunks < 64u ? chunks : 64u;
+}
+
 }  // namespace rlsim_dev

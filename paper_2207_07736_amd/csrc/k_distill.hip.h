@@ -44,9 +44,24 @@ struct DistillArgs {
     float* loss;                  // [rows] or null
     void* grad;                   // or null
     uint64_t grad_stride;
+    uint32_t past_cache;          // the gradient is larger than the last-level cache
 };
 
 constexpr uint32_t kNoEntry = 0xFFFFFFFFu;
+constexpr float kLowest = -3.40282347e38f;
+
+// A call of few rows shares each among several workgroups, a chunk of `chunk` entries (a
+// multiple of 64 vectors) to each; what the first kernel hands on, by workgroup
+// (row * chunks + chunk) or by slot (row * k + slot).
+constexpr uint32_t kDistillSplitGroups = 1024u;   // most workgroups of such a call
+constexpr uint32_t kDistillSplitChunks = 64u;     // most chunks of a row
+struct DistillSplit {
+    uint32_t chunk, chunks;
+    float* mu;                    // [groups] largest entry of the chunk's sum
+    double* sum;                  // [groups]
+    uint32_t* entry;              // [rows][k]
+    float* logit;                 // [rows][k]
+};
 
 // A teacher slot: its entry (kNoEntry: left out) and its logit.
 struct Slot { uint32_t entry; float t; };
@@ -280,80 +295,105 @@ __global__ __launch_bounds__(256) void k_distill_tiny(DistillArgs a)
 // then k entries, k teacher logits (then probabilities) and k student logits.
 inline __host__ __device__ uint32_t distill_shared_bytes(uint32_t k, uint32_t V) { return (V + 31u) / 32u * 4u + 12u * k; }
 
+template <int NW>
+struct DistillShared {
+    float max[3][NW];
+    double sum[4][NW];
+    uint32_t again, mass;                 // whether a slot repeats an earlier one's entry; any has mass
+};
+
+// A row, or a chunk of one `from` entries behind its start, as a workgroup's kernel works on
+// it; entry, prob and logit hold the row's slots in shared memory.
 template <int D, int NT, int NV>
-__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs a)
-{
+struct DistillGroup {
     using R = Row<D, NT, NV>;
     using El = Elem<D>;
-    constexpr uint32_t E = R::E;
-    constexpr int NW = NT / 64;
-    __shared__ float sh_max[3][NW];
-    __shared__ double sh_sum[4][NW];
-    __shared__ uint32_t again, mass;      // whether a slot repeats an earlier one's entry; any has mass
-    extern __shared__ uint32_t bits[];
-    const uint32_t words = (a.V + 31u) / 32u;
-    uint32_t* const entry = bits + words;
-    float* const prob = reinterpret_cast<float*>(entry + a.k);          // t, then p
-    float* const logit = prob + a.k;                                    // the student's
-    const uint32_t tid = threadIdx.x;
-    const float none = -__builtin_inff();
-    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        R x;
-        x.open(a.logits, row, a.stride, a.V);
-        char* const grad = a.grad ? static_cast<char*>(a.grad) + row * a.grad_stride * El::kBytes : nullptr;
-        auto store = [&](uint32_t i, const Vec16& v) {
-            typename El::Run r;
-            for (uint32_t j = 0; j < 4u; ++j) r.w[j] = v.w[j];
-            if (i < x.vectors) reinterpret_cast<typename El::Run*>(grad)[i] = r;
-        };
-        auto store_one = [&](uint32_t i, float v) { reinterpret_cast<typename El::Word*>(grad)[i] = El::word(v); };
-        const float weight = uniform(a.weight ? a.weight[row] : 1.0f);
-        const float rest = uniform(a.rest ? rest_value(a, row) : none);
-        for (uint32_t j = tid; j < a.k; j += NT) {
-            const Slot s = load_slot(a, row, j);
-            entry[j] = s.entry;
-            prob[j] = s.t;
-            if (s.entry != kNoEntry) logit[j] = x.entry(s.entry);
-        }
-        for (uint32_t j = tid; j < words; j += NT) bits[j] = 0u;
+    static constexpr uint32_t E = R::E;
+    static constexpr int NW = NT / 64;
+
+    const DistillArgs& a;
+    DistillShared<NW>& sh;
+    R& x;
+    const uint32_t row, from, length;
+    uint32_t* const bits;                 // of the chunk's entries: listed
+    uint32_t* const entry;                // kNoEntry: left out
+    float* const prob;                    // teacher's logit, then exponential
+    float* const logit;                   // the student's
+    float weight, rest;
+
+    __device__ __forceinline__ void read_scalars()
+    {
+        weight = uniform(a.weight ? a.weight[row] : 1.0f);
+        rest = uniform(a.rest ? rest_value(a, row) : -__builtin_inff());
+    }
+    __device__ __forceinline__ char* grad() const
+    {
+        return static_cast<char*>(a.grad) + ((uint64_t)row * a.grad_stride + from) * El::kBytes;
+    }
+    // Gradients larger than the last-level cache go past it: 2,048 x 131,072 bf16 in 292
+    // instead of 312 us.
+    __device__ __forceinline__ void store(uint32_t i, const Vec16& v) const
+    {
+        if (i >= x.vectors) return;
+        const typename El::Packed w = {v.w[0], v.w[1], v.w[2], v.w[3]};
+        typename El::Packed* const to = reinterpret_cast<typename El::Packed*>(grad()) + i;
+        if (a.past_cache) __builtin_nontemporal_store(w, to);
+        else *to = w;
+    }
+    __device__ __forceinline__ void store_one(uint32_t i, float v) const
+    {
+        reinterpret_cast<typename El::Word*>(grad())[i] = El::word(v);
+    }
+    __device__ __forceinline__ void store_zeros() const
+    {
+        for (uint32_t v = 0; v < x.seg; ++v)
+            if (x.any(v)) store(x.index(v), Vec16{{0u, 0u, 0u, 0u}});
+        if (threadIdx.x < x.tail) store_one(x.vectors * E + threadIdx.x, 0.0f);
+    }
+
+    // Mark the chunk's listed entries; a slot that repeats an earlier one's is left out.
+    // Returns whether a slot has mass.  Slots outside the chunk are kNoEntry here.
+    __device__ __forceinline__ bool mark_listed()
+    {
+        const uint32_t tid = threadIdx.x;
+        const float none = -__builtin_inff();
+        for (uint32_t j = tid; j < (length + 31u) / 32u; j += NT) bits[j] = 0u;
         if (tid == 0u) {
-            again = 0u;
-            mass = 0u;
+            sh.again = 0u;
+            sh.mass = 0u;
         }
         __syncthreads();
         for (uint32_t j = tid; j < a.k; j += NT) {
-            const uint32_t i = entry[j];
-            if (i == kNoEntry) continue;
-            if (atomicOr(&bits[i / 32u], 1u << (i % 32u)) >> (i % 32u) & 1u) again = 1u;
-            if (prob[j] != none) mass = 1u;
+            if (entry[j] == kNoEntry) continue;
+            const uint32_t i = entry[j] - from;
+            if (atomicOr(&bits[i / 32u], 1u << (i % 32u)) >> (i % 32u) & 1u) sh.again = 1u;
+            if (prob[j] != none) sh.mass = 1u;
         }
         __syncthreads();
-        bool empty = mass == 0u && rest == none;
-        if (again) {                      // leave out the slots that repeat an earlier one's entry
-            uint32_t gone = 0u, left = 0u;            // a bit for each of this thread's slots
-            for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) {
-                bool repeats = false;
-                for (uint32_t i = 0; i < j; ++i) repeats = repeats || entry[i] == entry[j];
-                gone |= repeats ? b : 0u;
-                left |= !repeats && entry[j] != kNoEntry && prob[j] != none ? 1u : 0u;
-            }
-            __syncthreads();
-            for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1)
-                if (gone & b) entry[j] = kNoEntry;
-            empty = __syncthreads_or((int)left) == 0 && rest == none;
+        if (sh.again == 0u) return sh.mass != 0u;
+        uint32_t gone = 0u, left = 0u;    // a bit for each of this thread's slots
+        for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) {
+            bool repeats = false;
+            for (uint32_t i = 0; i < j; ++i) repeats = repeats || entry[i] == entry[j];
+            gone |= repeats ? b : 0u;
+            left |= !repeats && entry[j] != kNoEntry && prob[j] != none ? 1u : 0u;
         }
-        if (empty || (weight == 0.0f && !a.loss)) {
-            if (a.loss && tid == 0u) a.loss[row] = 0.0f;
-            if (grad) {
-                for (uint32_t v = 0; v < x.seg; ++v)
-                    if (x.any(v)) store(x.index(v), Vec16{{0u, 0u, 0u, 0u}});
-                if (tid < x.tail) store_one(x.vectors * E + tid, 0.0f);
-            }
-            __syncthreads();
-            continue;
-        }
-        // the student's row; with a rest, without the listed entries
-        auto unlisted = [&](const Vec16& y, uint32_t i) {
+        __syncthreads();
+        for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1)
+            if (gone & b) entry[j] = kNoEntry;
+        return __syncthreads_or((int)left) != 0;
+    }
+
+    // One pass: this thread's largest entry and the exponentials' sum against it, which
+    // shrinks as a larger one comes; with a rest, without the listed entries.  It starts
+    // from the lowest value, so that a row of -inf has a sum of 0.  A vector is added by
+    // pairs: short chains of roundings.
+    __device__ __forceinline__ void add_row(float& largest, float& sum)
+    {
+        const uint32_t at = x.vectors * E + x.lane;
+        if (a.rest && x.lane < x.tail && (bits[at / 32u] >> (at % 32u) & 1u)) x.last = -__builtin_inff();
+        float mine = kLowest, total = 0.0f;
+        x.each_vector([&](const Vec16& y, uint32_t i) {
             Vec16 v = y;
             const uint32_t first = i * E;
             const uint32_t b = a.rest && i < x.vectors ? bits[first / 32u] >> (first % 32u) & ((1u << E) - 1u) : 0u;
@@ -361,21 +401,6 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs 
 #pragma unroll
                 for (uint32_t e = 0; e < E; ++e) v = b >> e & 1u ? El::with_neg_inf(v, e) : v;
             }
-            return v;
-        };
-        const uint32_t at = x.vectors * E + x.lane;
-        if (a.rest && x.lane < x.tail && (bits[at / 32u] >> (at % 32u) & 1u)) x.last = none;
-        // One pass: each thread's largest entry and the exponentials' sum against it, which
-        // shrinks as a larger one comes.  It starts from the type's lowest value, so that a
-        // row of -inf has a sum of 0.  A vector is added by pairs: short chains of roundings.
-        const float lowest = -3.40282347e38f;
-        float mine = lowest, sum = 0.0f;
-        auto add = [&](float top, float shrink, float terms) {
-            mine = top;
-            sum = __builtin_fmaf(sum, shrink, terms);
-        };
-        x.each_vector([&](const Vec16& y, uint32_t i) {
-            const Vec16 v = unlisted(y, i);
             float s[E], top = mine;
 #pragma unroll
             for (uint32_t e = 0; e < E; ++e) {
@@ -388,14 +413,24 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs 
             for (uint32_t n = E / 2u; n >= 1u; n /= 2u)
 #pragma unroll
                 for (uint32_t e = 0; e < n; ++e) s[e] += s[e + n];
-            add(top, exp_entry(a, mine, top), s[0]);
+            total = __builtin_fmaf(total, exp_entry(a, mine, top), s[0]);
+            mine = top;
         });
         if (x.wave == 0u) {
             const float top = __builtin_fmaxf(mine, x.last);
-            add(top, exp_entry(a, mine, top), exp_entry(a, x.last, top));
+            total = __builtin_fmaf(total, exp_entry(a, mine, top), exp_entry(a, x.last, top));
+            mine = top;
         }
+        largest = mine;
+        sum = total;
+    }
+
+    // Loss (where `owner`) and gradient, from each thread's largest entry and sum.
+    __device__ __forceinline__ void finish(float mine, double sum, bool owner)
+    {
+        const uint32_t tid = threadIdx.x;
         // the largest values of the row, the listed entries and the teacher's
-        float top_l = lowest, top_t = none;
+        float top_l = kLowest, top_t = -__builtin_inff();
         for (uint32_t j = tid; j < a.k; j += NT) {
             if (entry[j] == kNoEntry) continue;
             top_l = __builtin_fmaxf(top_l, logit[j]);
@@ -406,20 +441,20 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs 
         top_t = wave_max(top_t);
         if (NW > 1) {
             if (x.lane == 0u) {
-                sh_max[0][x.wave] = mu;
-                sh_max[1][x.wave] = top_l;
-                sh_max[2][x.wave] = top_t;
+                sh.max[0][x.wave] = mu;
+                sh.max[1][x.wave] = top_l;
+                sh.max[2][x.wave] = top_t;
             }
             __syncthreads();
             const uint32_t q = min(x.lane, (uint32_t)NW - 1u);
-            mu = wave_max(sh_max[0][q]);
-            top_l = wave_max(sh_max[1][q]);
-            top_t = wave_max(sh_max[2][q]);
+            mu = wave_max(sh.max[0][q]);
+            top_l = wave_max(sh.max[1][q]);
+            top_t = wave_max(sh.max[2][q]);
         }
         const float m = a.rest ? __builtin_fmaxf(mu, top_l) : mu;
         const double mt = uniform(__builtin_fmax((double)top_t * a.inv_tau, (double)rest));
         // the sums, and the excesses of the loss
-        double part = (double)(sum * exp_entry(a, mine, mu)), listed = 0.0, sum_t = 0.0, d = 0.0;
+        double part = sum * (double)exp_entry(a, mine, mu), listed = 0.0, sum_t = 0.0, d = 0.0;
         for (uint32_t j = tid; j < a.k; j += NT) {
             if (entry[j] == kNoEntry) continue;
             const double t = (double)prob[j] * a.inv_tau - mt, y = log_part(a, logit[j], m);
@@ -435,24 +470,24 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs 
         d = wave_total(d);
         if (NW > 1) {
             if (x.lane == 0u) {
-                sh_sum[0][x.wave] = part;
-                sh_sum[1][x.wave] = listed;
-                sh_sum[2][x.wave] = sum_t;
-                sh_sum[3][x.wave] = d;
+                sh.sum[0][x.wave] = part;
+                sh.sum[1][x.wave] = listed;
+                sh.sum[2][x.wave] = sum_t;
+                sh.sum[3][x.wave] = d;
             }
             __syncthreads();
             const bool in = x.lane < (uint32_t)NW;
-            part = wave_total(in ? sh_sum[0][x.lane] : 0.0);
-            listed = wave_total(in ? sh_sum[1][x.lane] : 0.0);
-            sum_t = wave_total(in ? sh_sum[2][x.lane] : 0.0);
-            d = wave_total(in ? sh_sum[3][x.lane] : 0.0);
+            part = wave_total(in ? sh.sum[0][x.lane] : 0.0);
+            listed = wave_total(in ? sh.sum[1][x.lane] : 0.0);
+            sum_t = wave_total(in ? sh.sum[2][x.lane] : 0.0);
+            d = wave_total(in ? sh.sum[3][x.lane] : 0.0);
         }
         const double x_rest = (double)rest - mt;
         const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
         sum_t += (double)e_rest;
         const float inv_t = uniform(1.0f / (float)sum_t), p_rest = a.rest ? e_rest * inv_t : 0.0f;
         const Student st = student_row(a, m, mu, part, listed);
-        if (grad) {
+        if (a.grad) {
             const GradScale g = grad_scale(a, st, weight, p_rest);
             const bool zero = weight == 0.0f;
             const float scale = uniform(g.other);
@@ -464,17 +499,138 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs 
                 store(i, El::pack(f));
             });
             if (tid < x.tail) store_one(x.vectors * E + tid, other(x.last));
-            __syncthreads();              // the listed entries over what the row's pass wrote
-            for (uint32_t j = tid; j < a.k; j += NT)
-                if (entry[j] != kNoEntry)
-                    store_one(entry[j], zero ? 0.0f : exp_slot(log_part(a, logit[j], m)) * g.listed - prob[j] * inv_t * g.weighted);
+            __syncthreads();              // the listed entries over what the pass wrote
+            for (uint32_t j = tid; j < a.k; j += NT) {
+                const uint32_t i = entry[j] - from;       // (kNoEntry and others' entries: past the chunk)
+                if (entry[j] != kNoEntry && i < length)
+                    store_one(i, zero ? 0.0f : exp_slot(log_part(a, logit[j], m)) * g.listed - prob[j] * inv_t * g.weighted);
+            }
         }
-        if (a.loss && tid == 0u) {
+        if (a.loss && owner && tid == 0u) {       // last: the logarithms take many registers
             if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log64()));
             a.loss[row] = row_loss(a, st, d, sum_t, Log64());
         }
+    }
+};
+
+template <int D, int NT, int NV>
+__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs a)
+{
+    using G = DistillGroup<D, NT, NV>;
+    __shared__ DistillShared<G::NW> sh;
+    extern __shared__ uint32_t bits[];
+    uint32_t* const entry = bits + (a.V + 31u) / 32u;
+    float* const prob = reinterpret_cast<float*>(entry + a.k);
+    float* const logit = prob + a.k;
+    const uint32_t tid = threadIdx.x;
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        typename G::R x;
+        x.open(a.logits, row, a.stride, a.V);
+        G g{a, sh, x, row, 0u, a.V, bits, entry, prob, logit, 0.0f, 0.0f};
+        g.read_scalars();
+        for (uint32_t j = tid; j < a.k; j += NT) {
+            const Slot s = load_slot(a, row, j);
+            entry[j] = s.entry;
+            prob[j] = s.t;
+            if (s.entry != kNoEntry) logit[j] = x.entry(s.entry);
+        }
+        const bool empty = !g.mark_listed() && g.rest == -__builtin_inff();
+        if (empty || (g.weight == 0.0f && !a.loss)) {
+            if (a.loss && tid == 0u) a.loss[row] = 0.0f;
+            if (a.grad) g.store_zeros();
+        } else {
+            float mine, sum;
+            g.add_row(mine, sum);
+            g.finish(mine, (double)sum, true);
+        }
         __syncthreads();                  // the row's shared memory is used again
     }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: each is shared among workgroups, a chunk of its entries to each.  The first
+// kernel sums the chunks and takes the student's logits at the listed entries, which a
+// gradient in place overwrites in the second; that one joins the chunks' sums, each
+// workgroup for itself, and writes its chunk's gradient.
+constexpr int kDistillSplitThreads = 256;
+
+template <int D>
+__global__ __launch_bounds__(kDistillSplitThreads) void k_distill_chunk(DistillArgs a, DistillSplit p)
+{
+    constexpr int NT = kDistillSplitThreads;
+    using G = DistillGroup<D, NT, 0>;
+    __shared__ DistillShared<G::NW> sh;
+    extern __shared__ uint32_t bits[];
+    uint32_t* const entry = bits + p.chunk / 32u;
+    float* const prob = reinterpret_cast<float*>(entry + a.k);
+    const uint32_t row = blockIdx.y, from = blockIdx.x * p.chunk, length = min(p.chunk, a.V - from), tid = threadIdx.x;
+    typename G::R x;
+    x.open(a.logits, row, a.stride, length, from);
+    G g{a, sh, x, row, from, length, bits, entry, prob, prob, 0.0f, 0.0f};
+    uint32_t* const entries = p.entry + (uint64_t)row * a.k;
+    for (uint32_t j = tid; j < a.k; j += NT) {
+        const uint32_t i = load_slot(a, row, j).entry;
+        entry[j] = i != kNoEntry && i - from < length ? i : kNoEntry;
+        prob[j] = 0.0f;
+        if (i == kNoEntry && blockIdx.x == 0u) entries[j] = kNoEntry;
+    }
+    __syncthreads();
+    // which slots are this chunk's, as some of them are left out
+    uint32_t own = 0u;
+    for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) own |= entry[j] != kNoEntry ? b : 0u;
+    (void)g.mark_listed();
+    for (uint32_t j = tid, b = 1u; j < a.k; j += NT, b <<= 1) {
+        if (!(own & b)) continue;
+        entries[j] = entry[j];
+        if (entry[j] != kNoEntry) p.logit[(uint64_t)row * a.k + j] = x.entry(entry[j] - from);
+    }
+    float mine, sum;
+    g.add_row(mine, sum);
+    const float mu = group_max<G::NW>(mine, sh.max[0]);
+    double part = wave_total((double)sum * (double)exp_entry(a, mine, mu));
+    if (x.lane == 0u) sh.sum[0][x.wave] = part;
+    __syncthreads();
+    part = wave_total(x.lane < (uint32_t)G::NW ? sh.sum[0][x.lane] : 0.0);
+    if (tid == 0u) {
+        p.mu[row * p.chunks + blockIdx.x] = mu;
+        p.sum[row * p.chunks + blockIdx.x] = part;
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(kDistillSplitThreads) void k_distill_join(DistillArgs a, DistillSplit p)
+{
+    constexpr int NT = kDistillSplitThreads;
+    using G = DistillGroup<D, NT, 0>;
+    __shared__ DistillShared<G::NW> sh;
+    extern __shared__ uint32_t entry[];
+    float* const prob = reinterpret_cast<float*>(entry + a.k);
+    float* const logit = prob + a.k;
+    const uint32_t row = blockIdx.y, from = blockIdx.x * p.chunk, length = min(p.chunk, a.V - from), tid = threadIdx.x;
+    typename G::R x;
+    x.open(a.logits, row, a.stride, length, from);
+    G g{a, sh, x, row, from, length, nullptr, entry, prob, logit, 0.0f, 0.0f};
+    g.read_scalars();
+    int mass = 0;
+    for (uint32_t j = tid; j < a.k; j += NT) {
+        const uint32_t i = p.entry[(uint64_t)row * a.k + j];
+        entry[j] = i;
+        if (i == kNoEntry) continue;
+        prob[j] = load_slot(a, row, j).t;
+        logit[j] = p.logit[(uint64_t)row * a.k + j];
+        mass |= prob[j] != -__builtin_inff() ? 1 : 0;
+    }
+    const bool empty = __syncthreads_or(mass) == 0 && g.rest == -__builtin_inff();
+    const bool owner = blockIdx.x == 0u;
+    if (empty || (g.weight == 0.0f && !a.loss)) {
+        if (a.loss && owner && tid == 0u) a.loss[row] = 0.0f;
+        if (a.grad) g.store_zeros();
+        return;
+    }
+    const bool in = x.lane < p.chunks;
+    const float mu_c = in ? p.mu[row * p.chunks + x.lane] : kLowest, mu = wave_max(mu_c);
+    const double sum = wave_total(in ? p.sum[row * p.chunks + x.lane] * (double)exp_slot(log_part(a, mu_c, mu)) : 0.0);
+    g.finish(mu, tid == 0u ? sum : 0.0, owner);
 }
 
 }  // namespace rlsim_dev

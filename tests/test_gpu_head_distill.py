@@ -210,6 +210,39 @@ def test_a_row_does_not_depend_on_its_batch(head):
         assert torch.equal(whole[0], again[0]) and torch.equal(whole[1], again[1])
 
 
+@pytest.mark.parametrize("V,k", ((65, 9), (700, 9), (5003, 33), (20011, 64), (70001, 20), (150001, 100)))
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_many_rows(head, V, k, dtype):
+    """Calls of more rows than workgroups can share: rows picked from all over the batch
+    against the plain ones, and against calls of few rows within both calls' bounds."""
+    rng = np.random.default_rng(V)
+    rows = 700
+    s, t, index, rest = _case(rng, 7, V, k, dtype)
+    turn = torch.arange(rows, device="cuda") % 7
+    weight = torch.from_numpy(rng.uniform(0.5, 2, rows).astype(np.float32)).cuda()
+    weight[350] = 0.0
+    r = torch.from_numpy(rest).cuda()
+    index[3, 1] = index[3, 0]
+    index[4] = -1
+    r[4] = -math.inf
+    rest[4] = -math.inf
+    loss, grad = head.distill(s[turn], t[turn], index[turn], 2.0, r[turn], weight)
+    assert not grad[350].any()
+    sh, th, ih = s.float().cpu().numpy(), t.float().cpu().numpy(), index.cpu().numpy()
+    for row in (0, 1, 2, 3, 4, 355, 356, 511, 512, 513, 697, 698, 699):
+        j = row % 7
+        w = float(weight[row])
+        slots = list(zip(ih[j].tolist(), th[j].tolist()))
+        want, g = ref.distill_row(sh[j], slots, 2.0, float(rest[j]), w)
+        with np.errstate(all="ignore"):
+            tl, tg = ref.distill_tolerance(sh[j], slots, 2.0, float(rest[j]), w, BITS[s.dtype])
+        _same(loss[row].cpu().numpy(), want, tl, f"loss {row}")
+        _same(grad[row].float().cpu().numpy(), g, tg, f"gradient {row}")
+    in_place = s[turn]
+    again = head.distill(in_place, t[turn], index[turn], 2.0, r[turn], weight, grad=in_place)
+    assert torch.equal(again[0], loss) and torch.equal(again[1], grad)
+
+
 def test_the_loss_moves_as_the_gradient_says(head):
     """Central differences of the kernel's own losses, step h along a direction d of entries
     within [-1, 1].  At tau = 1 the loss is a log-sum-exp less a linear part (with a rest:
