@@ -80,21 +80,6 @@ uint32_t head_grid(const rlsim_head* h, uint32_t items, uint32_t threads)
     return std::min(items, h->cus * (threads >= 1024u ? 2u : 2048u / threads));
 }
 
-// One template argument list for each element type and form.
-#define HEAD_FORMS(KERNEL, D, form, grid, shared, stream, args)                                                              \
-    do {                                                                                                                     \
-        if (form.threads == 64u && form.strips == 2u)                                                                        \
-            hipLaunchKernelGGL((KERNEL<D, 64, 2>), dim3(grid), dim3(64), shared, stream, args);                              \
-        else if (form.threads == 64u)                                                                                        \
-            hipLaunchKernelGGL((KERNEL<D, 64, 4>), dim3(grid), dim3(64), shared, stream, args);                              \
-        else if (form.threads == 256u && form.strips == 4u)                                                                  \
-            hipLaunchKernelGGL((KERNEL<D, 256, 4>), dim3(grid), dim3(256), shared, stream, args);                            \
-        else if (form.threads == 256u)                                                                                       \
-            hipLaunchKernelGGL((KERNEL<D, 256, 8>), dim3(grid), dim3(256), shared, stream, args);                            \
-        else                                                                                                                 \
-            hipLaunchKernelGGL((KERNEL<D, 1024, 0>), dim3(grid), dim3(1024), shared, stream, args);                          \
-    } while (0)
-
 // Rows of up to kHeadTinyVocab entries: FEW has a thread to a row, TINY some lanes.
 #define HEAD_TINY(FEW, TINY, D, h, a)                                                                                        \
     do {                                                                                                                     \
@@ -166,7 +151,7 @@ void launch_sample(const rlsim_head* h, const SampleArgs& a)
         hipLaunchKernelGGL(k_sample_draw<D>, dim3(a.rows), block, 0, h->stream, a, p);
         return;
     }
-    const uint32_t threads = head_threads(a.V, Elem<D>::kBytes);
+    const uint32_t threads = sample_threads(a.V, Elem<D>::kBytes);
     const dim3 grid(head_grid(h, a.rows, threads)), block(threads);
     if (threads == 64u) hipLaunchKernelGGL((k_sample<D, 64>), grid, block, 0, h->stream, a);
     else if (threads == 256u) hipLaunchKernelGGL((k_sample<D, 256>), grid, block, 0, h->stream, a);
@@ -191,10 +176,16 @@ void launch_distill(const rlsim_head* h, const DistillArgs& a)
         hipLaunchKernelGGL(k_distill_join<D>, a.grad ? grid : dim3(1, a.rows), block, 12u * a.k, h->stream, a, p);
         return;
     }
-    const HeadForm form = head_form(a.V, Elem<D>::kBytes);
+    const HeadForm form = distill_form(a.rows, a.V, Elem<D>::kBytes, a.grad != nullptr, h->cus);
     const uint32_t grid = head_grid(h, a.rows, form.threads);
     const uint32_t shared = distill_shared_bytes(a.k, a.V);
-    HEAD_FORMS(k_distill, D, form, grid, shared, h->stream, a);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(form.threads), shared, h->stream, a); };
+    if (form.threads == 64u && form.strips == 2u) launch(k_distill<D, 64, 2>);
+    else if (form.threads == 64u) launch(k_distill<D, 64, 4>);
+    else if (form.strips == 4u) launch(k_distill<D, 256, 4>);
+    else if (form.strips == 8u) launch(k_distill<D, 256, 8>);
+    else if (form.threads == 256u) launch(k_distill<D, 256, 0>);
+    else launch(k_distill<D, 1024, 0>);
 }
 
 // A kernel may use more than 64 KB of dynamic shared memory only once it is told so.
@@ -203,6 +194,7 @@ hipError_t allow_shared()
 {
     const int bytes = (int)distill_shared_bytes(kHeadMaxTeacher, kHeadMaxVocab);
     const void* const kernels[] = {reinterpret_cast<const void*>(k_distill<D, 1024, 0>),
+                                   reinterpret_cast<const void*>(k_distill<D, 256, 0>),
                                    reinterpret_cast<const void*>(k_distill_chunk<D>)};
     hipError_t e = hipSuccess;
     for (const void* k : kernels)

@@ -472,14 +472,12 @@ struct SampleGroup {
     __device__ __forceinline__ void pick(uint32_t parts, uint32_t vectors, F weigh)
     {
         const uint64_t end = x.lane < x.tail ? weigh(x.last, x.vectors * E + x.lane) : 0u;
-        uint64_t whole = 0u;
-        for (uint32_t j = 0; j <= parts; ++j) whole += sh.sum[j];
-        whole = uniform(whole);
+        const uint64_t mine = x.lane <= parts ? sh.sum[x.lane] : 0u, running = wave_scan(mine);
+        const uint64_t whole = lane_u64(running, 63);
         const uint64_t target = share24(whole, s.u24);
-        uint64_t before = 0u;
-        uint32_t part = 0u;
-        while (part < parts && before + sh.sum[part] <= target) before += sh.sum[part++];
-        part = uniform(part);
+        const int part_lane = (int)__builtin_ctzll(__ballot(running > target));       // the last one's passes it
+        const uint32_t part = (uint32_t)part_lane;
+        uint64_t before = lane_u64(running, part_lane) - lane_u64(mine, part_lane);
         if (part == parts) {              // the tail's lanes
             if (x.wave == 0u) {
                 const uint64_t upto = before + wave_scan(end);
@@ -501,7 +499,8 @@ struct SampleGroup {
         if (NW > 1u) {
             if (x.lane == 63u) sh.group[x.wave] = upto;
             __syncthreads();
-            for (uint32_t j = 0; j < x.wave; ++j) before += sh.group[j];
+            const uint64_t upto_wave = wave_scan(x.lane < NW ? sh.group[x.lane] : 0u);
+            if (x.wave) before += lane_u64(upto_wave, (int)x.wave - 1);
         }
         upto += before;
         if (upto > target && upto - own <= target) {
@@ -685,43 +684,58 @@ struct SampleGroup {
         if (threadIdx.x < 64u) find_bin<Sh::kBins>(sh, sh.n, sh.w, true, target);     // (counts are not looked at)
         __syncthreads();
         const uint32_t b = sh.found;
-        const uint64_t before_w = sh.before_w;
-        // bin_of(z) == b: the bins' ends are exact in fp32
-        const float upper = -(float)b / (float)Sh::kPerZ, lower = -(float)(b + 1u) / (float)Sh::kPerZ;
-        auto in_bin = [&](float l) {
+        uint64_t before_w = sh.before_w;
+        // Where min-p's end lies, a margin of 0.01 in z to both sides, far more than the weights'
+        // error: bins [b0, b1] have to be looked into, those before are kept.  If they end
+        // before the cut's bin, top-p cuts nothing off.
+        uint32_t b0 = b, b1 = b;
+        if (s.least) {
+            const float least_z = __builtin_log2f((float)s.least) - 40.0f;
+            b0 = min(b, bin_of(__builtin_fminf(least_z + 0.01f, 0.0f)));
+            b1 = min(b, bin_of(__builtin_fmaxf(least_z - 0.01f, kLastZ)));
+        }
+        const bool by_top_p = b1 == b;
+        for (uint32_t j = b0; j < b; ++j) before_w -= sh.w[j];
+        // the bins' ends are exact in fp32
+        const float upper = -(float)b0 / (float)Sh::kPerZ, lower = -(float)(b1 + 1u) / (float)Sh::kPerZ;
+        auto in_bins = [&](float l) {
             const float zi = (l - m) * s.c;
             return zi <= upper && zi > lower;
         };
-        x.each_vector([&](const Vec16& y, uint32_t v) { append_vector(y, v, in_bin); });
-        append_tail(in_bin);
+        x.each_vector([&](const Vec16& y, uint32_t v) { append_vector(y, v, in_bins); });
+        append_tail(in_bins);
         __syncthreads();
         const uint32_t n = sh.count;
         const bool listed = n <= Sh::kList;
-        const Among in = listed ? close_list(n, 0u, before_w) : narrow_to_list(b, n, 0u, before_w, true, target);
-        find_listed<NT>(sh, in, in.n, [&](uint32_t j) { return sh.list_code[j]; }, [&](uint32_t j) { return listed_weight(j); },
-                        true, target);
-        const uint64_t cut = sh.cut;
+        uint64_t cut = ~0ull;
+        if (by_top_p) {
+            const Among in = listed ? close_list(n, 0u, before_w) : narrow_to_list(b0, b1, n, 0u, before_w, true, target);
+            find_listed<NT>(sh, in, in.n, [&](uint32_t j) { return sh.list_code[j]; }, [&](uint32_t j) { return listed_weight(j); },
+                            true, target);
+            cut = sh.cut;
+        }
         auto weigh = [&](float l, uint32_t i) { return weigh_kept(l, i, cut); };
-        if (!listed || s.least) {
+        if (!listed) {
             uint64_t mine = 0u;
             x.each_again_vectors([&](float l, uint32_t i) { mine += weigh(l, i); });
             draw(mine, weigh);
             return;
         }
-        // a part's kept weight: the bins before the cut's, and what of that one is kept
+        // a part's kept weight: the bins before, and what of the listed ones is kept
         for (uint32_t q = x.wave; q < parts; q += NW) {
             uint64_t w = 0u;
-            for (uint32_t j = x.lane; j < b; j += 64u) w += part_w[q * Sh::kUsedBins + j];
+            for (uint32_t j = x.lane; j < b0; j += 64u) w += part_w[q * Sh::kUsedBins + j];
             w = wave_total(w);
             if (x.lane == 0u) sh.sum[q] = w;
         }
         __syncthreads();
-        for (uint32_t j = threadIdx.x; j < in.n; j += NT)
-            if (sh.list_code[j] <= cut) {
+        for (uint32_t j = threadIdx.x; j < n; j += NT) {
+            const uint64_t w = listed_weight(j);
+            if (sh.list_code[j] <= cut && w >= s.least) {
                 const uint32_t v = (uint32_t)(sh.list_code[j] & ((1ull << ibits) - 1u)) / E;
-                atomicAdd((unsigned long long*)&sh.sum[v < x.vectors ? v / part_vectors : tail_part],
-                          (unsigned long long)listed_weight(j));
+                atomicAdd((unsigned long long*)&sh.sum[v < x.vectors ? v / part_vectors : tail_part], (unsigned long long)w);
             }
+        }
         __syncthreads();
         pick_parts(parts, part_vectors, tail_part, weigh);
     }
@@ -755,15 +769,15 @@ struct SampleGroup {
             if (zi >= kLastZ) f(l, i, zi);
         });
     }
-    // Where a bin of z holds more entries than the list: narrow them by their codes until
+    // Where bins b0 to b1 of z hold more entries than the list: narrow them by their codes until
     // the list takes what is left, and list it.
-    __device__ __forceinline__ Among narrow_to_list(uint32_t bin, uint32_t n, uint64_t before_n, uint64_t before_w, bool by_weight,
+    __device__ __forceinline__ Among narrow_to_list(uint32_t b0, uint32_t b1, uint32_t n, uint64_t before_n, uint64_t before_w, bool by_weight,
                                                     uint64_t target)
     {
         Among in{0u, 0u, 64u, n, before_n, before_w};
         auto visit = [&](auto f) {
             each_live([&](float l, uint32_t i, float zi) {
-                if (bin_of(zi) == bin) f(code(l, i), entry_weight(zi));
+                if (bin_of(zi) >= b0 && bin_of(zi) <= b1) f(code(l, i), entry_weight(zi));
             });
         };
         if (n > Sh::kList) {              // the range of the bin's codes
@@ -886,7 +900,7 @@ struct SampleGroup {
             if (threadIdx.x < 64u) find_bin<Sh::kBins>(sh, sh.n, sh.w, by_weight != 0u, target);
             __syncthreads();
             const uint32_t bin = sh.found;
-            const Among in = narrow_to_list(bin, sh.n[bin], sh.before_n, sh.before_w, by_weight != 0u, target);
+            const Among in = narrow_to_list(bin, bin, sh.n[bin], sh.before_n, sh.before_w, by_weight != 0u, target);
             find_listed<NT>(sh, in, in.n, [&](uint32_t j) { return sh.list_code[j]; },
                             [&](uint32_t j) { return listed_weight(j); }, by_weight != 0u, target);
             cut = sh.cut;
