@@ -695,7 +695,8 @@ struct SampleGroup {
             b1 = min(b, bin_of(__builtin_fmaxf(least_z - 0.01f, kLastZ)));
         }
         const bool by_top_p = b1 == b;
-        for (uint32_t j = b0; j < b; ++j) before_w -= sh.w[j];
+        if (by_top_p)
+            for (uint32_t j = b0; j < b; ++j) before_w -= sh.w[j];
         // the bins' ends are exact in fp32
         const float upper = -(float)b0 / (float)Sh::kPerZ, lower = -(float)(b1 + 1u) / (float)Sh::kPerZ;
         auto in_bins = [&](float l) {
