@@ -74,17 +74,16 @@ const char* check_rows(const rlsim_head* h, int dtype, const void* logits, uint3
     return nullptr;
 }
 
-// Workgroups of a kernel that goes through `items` rows (or groups of rows).
-uint32_t head_grid(const rlsim_head* h, uint32_t items, uint32_t threads)
-{
-    return std::min(items, h->cus * (threads >= 1024u ? 2u : 2048u / threads));
-}
+// Workgroups of a kernel for `items` rows (or groups of rows): one each, as far as a launch
+// holds fewer than 2^32 threads.  (Fewer that go through several rows each, as many as fit
+// the GPU: 20,000 x 8,000 bf16 distilled in 226 us instead of 199.)
+uint32_t head_grid(uint32_t items) { return std::min(items, 1u << 21); }
 
 // Rows of up to kHeadTinyVocab entries: FEW has a thread to a row, TINY some lanes.
 #define HEAD_TINY(FEW, TINY, D, h, a)                                                                                        \
     do {                                                                                                                     \
         const uint32_t lanes = (a).V <= 8u ? 1u : (a).V <= 16u ? 16u : (a).V <= 32u ? 32u : 64u;                             \
-        const dim3 grid(head_grid(h, ((a).rows + 256u / lanes - 1u) / (256u / lanes), 256u)), block(256);                    \
+        const dim3 grid(head_grid(((a).rows + 256u / lanes - 1u) / (256u / lanes))), block(256);                            \
         if ((a).V <= 2u) hipLaunchKernelGGL((FEW<D, 2>), grid, block, 0, (h)->stream, a);                                    \
         else if ((a).V <= 4u) hipLaunchKernelGGL((FEW<D, 4>), grid, block, 0, (h)->stream, a);                               \
         else if ((a).V <= 8u) hipLaunchKernelGGL((FEW<D, 8>), grid, block, 0, (h)->stream, a);                               \
@@ -152,7 +151,7 @@ void launch_sample(const rlsim_head* h, const SampleArgs& a)
         return;
     }
     const uint32_t threads = sample_threads(a.V, Elem<D>::kBytes);
-    const dim3 grid(head_grid(h, a.rows, threads)), block(threads);
+    const dim3 grid(head_grid(a.rows)), block(threads);
     if (threads == 64u) hipLaunchKernelGGL((k_sample<D, 64>), grid, block, 0, h->stream, a);
     else if (threads == 256u) hipLaunchKernelGGL((k_sample<D, 256>), grid, block, 0, h->stream, a);
     else hipLaunchKernelGGL((k_sample<D, 1024>), grid, block, 0, h->stream, a);
@@ -177,7 +176,7 @@ void launch_distill(const rlsim_head* h, const DistillArgs& a)
         return;
     }
     const HeadForm form = distill_form(a.rows, a.V, Elem<D>::kBytes, a.grad != nullptr, h->cus);
-    const uint32_t grid = head_grid(h, a.rows, form.threads);
+    const uint32_t grid = head_grid(a.rows);
     const uint32_t shared = distill_shared_bytes(a.k, a.V);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(form.threads), shared, h->stream, a); };
     if (form.threads == 64u && form.strips == 2u) launch(k_distill<D, 64, 2>);
@@ -232,9 +231,9 @@ int rlsim_head_create(uint32_t max_rows, uint32_t max_vocab, void* stream, rlsim
     if (e != hipSuccess) return head_fail(nullptr, RLSIM_EDEVICE, "rlsim_head_create: %s", hipGetErrorString(e));
     rlsim_head* h = new (std::nothrow) rlsim_head;
     if (!h) return head_fail(nullptr, RLSIM_ENOMEM, "rlsim_head_create: host allocation failed");
-    h->split_rows = std::min(max_rows, kSplitGroups / 2u);
-    const size_t bytes = split_bytes(h->split_rows);
-    e = hipMalloc(reinterpret_cast<void**>(&h->work), bytes);
+    // rows too short to be shared need no workspace (fp32 distillation shares the shortest)
+    h->split_rows = distill_chunks(1u, max_vocab, 4u, 256u) > 1u ? std::min(max_rows, kSplitGroups / 2u) : 0u;
+    if (h->split_rows) e = hipMalloc(reinterpret_cast<void**>(&h->work), split_bytes(h->split_rows));
     if (e != hipSuccess) {
         const int code = e == hipErrorOutOfMemory ? RLSIM_ENOMEM : RLSIM_EDEVICE;
         if (h->work) (void)hipFree(h->work);

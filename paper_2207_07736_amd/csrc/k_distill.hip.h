@@ -199,15 +199,29 @@ __global__ __launch_bounds__(256) void k_distill_few(DistillArgs a)
         const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
         float sum = 0.0f, apart = 0.0f, sum_t = e_rest;
         double d = 0.0;
+        if (a.rest) {
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) {
-            const bool in = listed >> e & 1u;
-            const double x = (double)t[e] * a.inv_tau - mt;
-            e_t[e] = in ? exp_slot(x) : 0.0f;
-            sum_t += e_t[e];
-            if (in) d += excess(e_t[e], x, log_part(a, s[e], m));
-            e_s[e] = e >= a.V ? 0.0f : exp_slot(log_part(a, s[e], a.rest && in ? m : mu));
-            (a.rest && in ? apart : sum) += e_s[e];
+            for (uint32_t e = 0; e < N; ++e) {
+                const bool in = listed >> e & 1u;
+                const double x = (double)t[e] * a.inv_tau - mt;
+                e_t[e] = in ? exp_slot(x) : 0.0f;
+                if (in) d += excess(e_t[e], x, log_part(a, s[e], m));
+                e_s[e] = e >= a.V ? 0.0f : exp_slot(log_part(a, s[e], in ? m : mu));
+                (in ? apart : sum) += e_s[e];
+                sum_t += e_t[e];
+            }
+        } else {                          // the logits' differences alone: fp32 holds them
+            float excesses = 0.0f;
+#pragma unroll
+            for (uint32_t e = 0; e < N; ++e) {
+                const bool in = listed >> e & 1u;
+                e_t[e] = in ? exp_entry(a, t[e], top_t) : 0.0f;
+                e_s[e] = e >= a.V ? 0.0f : exp_entry(a, s[e], m);
+                if (e_t[e] != 0.0f) excesses += e_t[e] * (((t[e] - top_t) - (s[e] - m)) * (float)a.inv_tau);
+                sum += e_s[e];
+                sum_t += e_t[e];
+            }
+            d = (double)excesses;
         }
         const Student st = student_row(a, m, mu, sum, apart);
         if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log32()));

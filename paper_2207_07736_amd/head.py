@@ -63,11 +63,15 @@ def rlsim_head_create(max_rows: int, max_vocab: int, stream=None) -> ctypes.c_vo
 
 
 def rlsim_head_sample(h, args: rlsim_sample) -> None:
-    _check_head(lib.rlsim_head_sample(h, ctypes.byref(args)), h)
+    rc = lib.rlsim_head_sample(h, ctypes.byref(args))
+    if rc:
+        _check_head(rc, h)
 
 
 def rlsim_head_distill(h, args: rlsim_distill) -> None:
-    _check_head(lib.rlsim_head_distill(h, ctypes.byref(args)), h)
+    rc = lib.rlsim_head_distill(h, ctypes.byref(args))
+    if rc:
+        _check_head(rc, h)
 
 
 def rlsim_head_destroy(h) -> None:
