@@ -56,7 +56,7 @@ struct SampleSplit {
     uint64_t* part_w;             // [groups][kSplitBins] weights by bins of z
     uint64_t* list;               // [rows][chunks][room] codes
     uint32_t room;                // kSplitList / chunks
-    uint32_t* count;              // [groups] entries listed; above `room`: not all of them
+    uint32_t* count;              // [groups] entries listed
     float* list_z;                // [groups] all with z above this are listed
 };
 
@@ -102,7 +102,8 @@ __device__ __forceinline__ float entry_z(float l, float m, float c) { return l =
 // 2^40 2^z as a whole number: 2^f on [-1/2, 1/2] in fp32, Horner form with one
 // rounding per operation (relative error 1.9e-7), truncated to 24 bits and shifted by the
 // whole part of z.  Coefficients scaled by 2^40, so that P 2^n is the weight before its
-// fraction is cut off; it needs at most 24 bits, so fp32 holds it too.
+// fraction is cut off; it needs at most 24 bits, so fp32 holds it too.  (entry_weight32
+// leaves the fraction on: every use of it cuts it off.)
 // z + 1.5 2^23 rounds z to the whole number n that its low bits then show.  At -41, to
 // which the maximum raises all below it and NaN, P 2^n is less than 1.
 __device__ __forceinline__ float entry_weight32(float z)
@@ -115,10 +116,9 @@ __device__ __forceinline__ float entry_weight32(float z)
     P = P * f + 0x1.ebf9bcp+37f;
     P = P * f + 0x1.62e42ap+39f;
     P = P * f + 0x1p40f;
-    return __builtin_truncf(__builtin_bit_cast(float, __builtin_bit_cast(uint32_t, P)
-                                                          + (__builtin_bit_cast(uint32_t, y) << 23)));
+    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, P) + (__builtin_bit_cast(uint32_t, y) << 23));
 }
-__device__ __forceinline__ uint64_t whole_weight(float w)        // w < 2^41, a whole number
+__device__ __forceinline__ uint64_t whole_weight(float w)        // w < 2^41, without its fraction
 {
     const float high = __builtin_truncf(w * 0x1p-32f);
     return (uint64_t)(uint32_t)high << 32 | (uint32_t)__builtin_fmaf(high, -0x1p32f, w);
@@ -423,8 +423,8 @@ __device__ __forceinline__ void find_listed(Sh& sh, Among in, uint32_t listed, C
     __syncthreads();
 }
 
-// z from which a row's entries are listed at first with a top-k cut, where it is expected: at
-// a thousandth of the largest weight.
+// z from which a row's entries are listed at first, where a top-k cut is expected: at a
+// thousandth of the largest weight.
 constexpr float kNearZ = -10.0f;
 
 template <int D, int NT>
@@ -600,12 +600,12 @@ struct SampleGroup {
         return Among{(uint64_t)first << ibits, 0u, max(bits, 8u), n, before_n, before_w};
     }
 
-    // Cut and draw from the list; top-p is not the first cut.  False: the list does not
+    // Cut, by top-k at first, and draw from the list.  False: the list does not
     // reach the cut.
     __device__ __forceinline__ bool draw_listed()
     {
         const uint32_t listed = sh.count;
-        if (listed > Sh::kList || listed == 0u || (s.k < a.V && listed < s.k)) return false;
+        if (listed > Sh::kList || listed < s.k) return false;
         const Among rank = close_list(listed, 0u, 0u);
         uint64_t whole = 0u, weight = 0u;
         auto code = [&](uint32_t j) { return sh.list_code[j]; };
@@ -614,9 +614,7 @@ struct SampleGroup {
         // top-k, then top-p: one piece of code for both
         for (uint32_t by_weight = 0u; by_weight < 2u; ++by_weight) {
             uint64_t target = s.k;
-            if (by_weight == 0u) {
-                if (s.k == a.V) continue;
-            } else {
+            if (by_weight) {
                 if (s.p24 == kAllP) continue;
                 target = share24(whole, s.p24);
                 target = target ? target : 1u;
@@ -671,8 +669,10 @@ struct SampleGroup {
     {
         for (uint32_t j = threadIdx.x; j < Sh::kBins; j += NT) {
             uint64_t w = 0u;
-            if (j < Sh::kUsedBins)
+            if (j < Sh::kUsedBins) {
+#pragma unroll 8
                 for (uint32_t q = 0; q < parts; ++q) w += part_w[q * Sh::kUsedBins + j];
+            }
             sh.w[j] = w;
         }
         __syncthreads();
@@ -725,6 +725,7 @@ struct SampleGroup {
         // a part's kept weight: the bins before, and what of the listed ones is kept
         for (uint32_t q = x.wave; q < parts; q += NW) {
             uint64_t w = 0u;
+#pragma unroll 8
             for (uint32_t j = x.lane; j < b0; j += 64u) w += part_w[q * Sh::kUsedBins + j];
             w = wave_total(w);
             if (x.lane == 0u) sh.sum[q] = w;
@@ -799,12 +800,34 @@ struct SampleGroup {
         return close_list(in.n, in.before_n, in.before_w);
     }
 
-    // The row's cuts, and where its draw is made from the list, the first z listed.  Without a
-    // cut the list has to reach min-p's: a margin of 0.01 in z, far more than the weights' error.
-    __device__ __forceinline__ bool cuts() const { return s.k < a.V || s.p24 < kAllP; }
-    __device__ __forceinline__ float near_z() const
+    // Without a top-k or top-p cut: an entry's weight, if min-p keeps it, and this thread's sum of
+    // them, whole numbers less than 2^53.  With min-p few entries come near it: the others
+    // are told by their z, with a margin of 0.01, far more than the weights' error.
+    __device__ __forceinline__ uint64_t weigh_uncut(float l) const
     {
-        return cuts() ? kNearZ : __builtin_fmaxf(__builtin_log2f((float)s.least) - 40.01f, kLastZ);
+        const uint64_t w = entry_weight((l - m) * s.c);
+        return w >= s.least ? w : 0u;
+    }
+    __device__ __forceinline__ double sum_uncut(bool tail) const
+    {
+        double sum = 0.0;
+        if (s.least == 0u) {
+            auto add = [&](float l, uint32_t) { sum += (double)__builtin_truncf(entry_weight32((l - m) * s.c)); };
+            if (tail) x.each_and_tail(add);
+            else x.each(add);
+        } else {
+            const float least = (float)s.least, near = __builtin_log2f(least) - 40.01f;
+            auto add = [&](float l, uint32_t) {
+                const float zi = (l - m) * s.c;
+                if (zi >= near) {
+                    const float w = __builtin_truncf(entry_weight32(zi));
+                    sum += w >= least ? (double)w : 0.0;
+                }
+            };
+            if (tail) x.each_and_tail(add);
+            else x.each(add);
+        }
+        return sum;
     }
     __device__ __forceinline__ void list_from(float z0)
     {
@@ -839,7 +862,7 @@ struct SampleGroup {
         const uint32_t f0 = k0 ? 2u * (uint32_t)__builtin_ctzll(k0) : kDepths, f1 = k1 ? 2u * (uint32_t)__builtin_ctzll(k1) + 1u : kDepths;
         const uint32_t need = min(f0, f1) + 1u;       // depths that hold the first k
         enough = need <= fit || fit == kDepths;
-        return -0.5f * (float)min(need, fit);         // entries with z > this (none: 0)
+        return __builtin_fmaxf(-0.5f * (float)min(need, fit), kLastZ);        // entries with z > this (none: 0)
     }
     __device__ __forceinline__ void list_above(float z0)
     {
@@ -848,11 +871,11 @@ struct SampleGroup {
         append_tail(want);
         __syncthreads();
     }
-    // Cut and draw, near_z() on being listed.
+    // Cut and draw, the entries from kNearZ on being listed.
     __device__ __forceinline__ void draw_near()
     {
         bool done = draw_listed();
-        if (!done && s.k < a.V) {
+        if (!done) {
             bool enough;
             const float z0 = list_depth(Sh::kList, enough);
             if (enough) {
@@ -915,14 +938,14 @@ struct SampleGroup {
 };
 
 // What a row's settings and largest entry ask for.
-enum class SampleKind { kEmpty, kGreedy, kOdd, kPlain, kTopP, kListed };
+enum class SampleKind { kEmpty, kGreedy, kOdd, kUncut, kTopP, kTopK };
 __device__ __forceinline__ SampleKind sample_kind(const SampleArgs& a, const SampleRow& s, float m)
 {
     if (m == -__builtin_inff()) return SampleKind::kEmpty;
     if (s.greedy) return SampleKind::kGreedy;
     if (!(m < __builtin_inff() && s.c < __builtin_inff())) return SampleKind::kOdd;
-    if (s.k == a.V && s.p24 == kAllP) return s.least ? SampleKind::kListed : SampleKind::kPlain;
-    return s.k == a.V ? SampleKind::kTopP : SampleKind::kListed;
+    if (s.k < a.V) return SampleKind::kTopK;
+    return s.p24 < kAllP ? SampleKind::kTopP : SampleKind::kUncut;
 }
 
 template <int D, int NT>
@@ -955,15 +978,13 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_sample(SampleArgs a)
             if (threadIdx.x == 0u) g.answer(sh.best, 0.0f);
         } else if (kind == SampleKind::kOdd) {
             g.draw_dense();
-        } else if (kind == SampleKind::kPlain) {
-            double mine = 0.0;            // whole numbers, less than 2^53
-            x.each([&](float l, uint32_t) { mine += (double)entry_weight32((l - m) * s.c); });
-            g.draw((uint64_t)mine, [&](float l, uint32_t) { return entry_weight((l - m) * s.c); });
+        } else if (kind == SampleKind::kUncut) {
+            g.draw((uint64_t)g.sum_uncut(false), [&](float l, uint32_t) { return g.weigh_uncut(l); });
         } else if (kind == SampleKind::kTopP) {
             g.bin_weights();
             g.draw_top_p(&sh.part_w[0][0], Sh::kParts, x.seg * 64u * (R::NW / Sh::kParts), 0u);
         } else {
-            g.list_from(g.near_z());
+            g.list_from(kNearZ);
             g.draw_near();
         }
         __syncthreads();                  // the row's shared memory is used again
@@ -1029,10 +1050,8 @@ __global__ __launch_bounds__(kSplitThreads, 8) void k_sample_chunk(SampleArgs a,
     x.open(a.logits, row, a.stride, min(p.chunk, a.V - from), from);
     SampleGroup<D, NT> part{a, sh, x, s, row, m, 32u - (uint32_t)__builtin_clz(a.V), from};
     __syncthreads();
-    if (kind == SampleKind::kPlain) {
-        double mine = 0.0;
-        x.each_and_tail([&](float l, uint32_t) { mine += (double)entry_weight32((l - m) * s.c); });
-        const uint64_t w = wave_total((uint64_t)mine);
+    if (kind == SampleKind::kUncut) {
+        const uint64_t w = wave_total((uint64_t)part.sum_uncut(true));
         if (x.lane == 0u) sh.group[x.wave] = w;
         __syncthreads();
         if (threadIdx.x < 64u) {
@@ -1047,16 +1066,11 @@ __global__ __launch_bounds__(kSplitThreads, 8) void k_sample_chunk(SampleArgs a,
             p.part_w[(uint64_t)group * kSplitBins + j] = w;
         }
     } else {
-        bool enough = true;
-        float z0 = 0.0f;
-        if (s.k < a.V) {
-            z0 = part.list_depth(p.room, enough);
-            part.list_above(z0);
-        } else {
-            part.list_from(part.near_z());
-        }
-        const uint32_t n = sh.count;
-        for (uint32_t j = threadIdx.x; j < min(n, p.room); j += NT) p.list[(uint64_t)group * p.room + j] = sh.list_code[j];
+        bool enough;
+        const float z0 = part.list_depth(p.room, enough);
+        part.list_above(z0);
+        const uint32_t n = min(sh.count, p.room);             // (list_depth keeps within it)
+        for (uint32_t j = threadIdx.x; j < n; j += NT) p.list[(uint64_t)group * p.room + j] = sh.list_code[j];
         if (threadIdx.x == 0u) {
             p.count[group] = n;
             p.list_z[group] = enough ? -__builtin_inff() : z0;
@@ -1079,7 +1093,7 @@ __global__ __launch_bounds__(kSplitThreads) void k_sample_draw(SampleArgs a, Sam
     x.open(a.logits, row, a.stride, a.V);
     SampleGroup<D, NT> g{a, sh, x, s, row, m, 32u - (uint32_t)__builtin_clz(a.V), 0u};
     const uint32_t chunk_vectors = p.chunk / R::E, last = p.chunks - 1u;
-    if (kind == SampleKind::kPlain)
+    if (kind == SampleKind::kUncut)
         for (uint32_t j = threadIdx.x; j < p.chunks; j += NT) sh.sum[j] = p.sum[group0 + j];
     if (threadIdx.x == 0u) {
         sh.count = 0u;
@@ -1087,19 +1101,16 @@ __global__ __launch_bounds__(kSplitThreads) void k_sample_draw(SampleArgs a, Sam
         sh.far = 0u;
     }
     __syncthreads();
-    if (kind == SampleKind::kListed) {
-        // the chunks' lists down to where all of them reach; too long a one shows in the count
-        const uint32_t lane = threadIdx.x % 64u, count = lane < p.chunks ? p.count[group0 + lane] : 0u;
+    if (kind == SampleKind::kTopK) {
+        // the chunks' lists down to where all of them reach
+        const uint32_t lane = threadIdx.x % 64u;
         const float z0 = uniform(wave_max(lane < p.chunks ? p.list_z[group0 + lane] : -__builtin_inff()));
-        const bool whole = __ballot(count > p.room) == 0ull;
         for (uint32_t j = threadIdx.x; j < p.chunks * p.room; j += NT) {
             const uint32_t q = j / p.room;
-            if (j - q * p.room >= min(p.count[group0 + q], p.room)) continue;
+            if (j - q * p.room >= p.count[group0 + q]) continue;
             const uint64_t code = p.list[(uint64_t)group0 * p.room + j];
             if (g.z(rank_logit<D>(code, g.ibits)) > z0) sh.list_code[atomicAdd(&sh.count, 1u)] = code;
         }
-        __syncthreads();
-        if (!whole && threadIdx.x == 0u) sh.count = kSplitList + 1u;
         __syncthreads();
     }
     if (kind == SampleKind::kEmpty) {
@@ -1108,8 +1119,8 @@ __global__ __launch_bounds__(kSplitThreads) void k_sample_draw(SampleArgs a, Sam
         if (threadIdx.x == 0u) g.answer(p.top_at[group0 + first], 0.0f);
     } else if (kind == SampleKind::kOdd) {
         g.draw_dense();
-    } else if (kind == SampleKind::kPlain) {
-        g.pick_parts(p.chunks, chunk_vectors, last, [&](float l, uint32_t) { return entry_weight((l - m) * s.c); });
+    } else if (kind == SampleKind::kUncut) {
+        g.pick_parts(p.chunks, chunk_vectors, last, [&](float l, uint32_t) { return g.weigh_uncut(l); });
     } else if (kind == SampleKind::kTopP) {
         g.draw_top_p(p.part_w + (uint64_t)group0 * kSplitBins, p.chunks, chunk_vectors, last);
     } else {

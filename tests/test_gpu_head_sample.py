@@ -128,6 +128,24 @@ def test_cuts_among_many_close_entries(head, V, flat, dtype):
         _check(head, logits, _u(rng, 4), **settings)
 
 
+@pytest.mark.parametrize("V", (40000, 131072))
+def test_fewer_live_entries_than_top_k(head, V):
+    """Sharp rows in which fewer than k entries weigh anything, and many lie just past the
+    weights' end: all that weigh are kept, whatever the others' number."""
+    rng = np.random.default_rng(V + 3)
+    x = np.full((6, V), -30.0, np.float32) + rng.uniform(0, 1, (6, V)).astype(np.float32)
+    for r, n in enumerate((1, 3, 30, 100, 250, 299)):
+        x[r, rng.permutation(V)[:n]] = rng.uniform(-8, 0, n).astype(np.float32)
+    for rows in (6, 600):
+        logits = torch.from_numpy(np.tile(x, (rows // 6, 1))).cuda()
+        u = _u(rng, rows)
+        for settings in (dict(top_k=300), dict(top_k=300, top_p=0.0), dict(top_k=300, top_p=0.9), dict(top_k=900, min_p=0.01)):
+            got = head.sample(logits, torch.from_numpy(u).cuda(), **settings).cpu().numpy()
+            for r in (*range(6), rows - 1):
+                assert got[r] == ref.sample_row(x[r % 6], u[r], settings.get("T", 1.0), settings["top_k"],
+                                                settings.get("top_p", 1.0), settings.get("min_p", 0.0))[0]
+
+
 def test_uniform_numbers_at_the_ends(head):
     rng = np.random.default_rng(5)
     u = np.array([0.0, 1 - 2.0 ** -24, 1.0, 2.0, -1.0, np.nan, 0.5, 2.0 ** -25], dtype=np.float32)
