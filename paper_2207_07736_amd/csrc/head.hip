@@ -152,9 +152,11 @@ void launch_sample(const rlsim_head* h, const SampleArgs& a)
     }
     const uint32_t threads = sample_threads(a.V, Elem<D>::kBytes);
     const dim3 grid(head_grid(a.rows)), block(threads);
-    if (threads == 64u) hipLaunchKernelGGL((k_sample<D, 64>), grid, block, 0, h->stream, a);
-    else if (threads == 256u) hipLaunchKernelGGL((k_sample<D, 256>), grid, block, 0, h->stream, a);
-    else hipLaunchKernelGGL((k_sample<D, 1024>), grid, block, 0, h->stream, a);
+    const bool cuts = a.top_k_rows || a.top_p_rows || (a.top_k && a.top_k < a.V) || a.top_p < 1.0f;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, h->stream, a); };
+    if (threads == 64u) cuts ? launch(k_sample<D, 64, true>) : launch(k_sample<D, 64, false>);
+    else if (threads == 256u) cuts ? launch(k_sample<D, 256, true>) : launch(k_sample<D, 256, false>);
+    else cuts ? launch(k_sample<D, 1024, true>) : launch(k_sample<D, 1024, false>);
 }
 
 template <int D>

@@ -829,6 +829,17 @@ struct SampleGroup {
         }
         return sum;
     }
+    // The draw without cuts from a row whose largest entry or scale is infinite.
+    __device__ __forceinline__ void draw_odd()
+    {
+        auto weigh = [&](float l, uint32_t) {
+            const uint64_t w = entry_weight(z(l));
+            return w >= s.least ? w : 0u;
+        };
+        uint64_t mine = 0u;
+        x.each_again_vectors([&](float l, uint32_t i) { mine += weigh(l, i); });
+        draw(mine, weigh);
+    }
     __device__ __forceinline__ void list_from(float z0)
     {
         auto want = [&](float l) { return (l - m) * s.c >= z0; };
@@ -948,7 +959,10 @@ __device__ __forceinline__ SampleKind sample_kind(const SampleArgs& a, const Sam
     return s.p24 < kAllP ? SampleKind::kTopP : SampleKind::kUncut;
 }
 
-template <int D, int NT>
+// CUTS: a row of the call may have a top-k or top-p cut.  Without them the kernel is small
+// (512 rows of 151,001 bf16 in 66 instead of 78 us); with all of it 64 registers do not hold
+// the state of two workgroups of 1,024 threads to a CU, and 41 go to scratch memory.
+template <int D, int NT, bool CUTS>
 __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_sample(SampleArgs a)
 {
     using R = Row<D, NT, 0>;
@@ -977,15 +991,18 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_sample(SampleArgs a)
             __syncthreads();
             if (threadIdx.x == 0u) g.answer(sh.best, 0.0f);
         } else if (kind == SampleKind::kOdd) {
-            g.draw_dense();
-        } else if (kind == SampleKind::kUncut) {
+            if constexpr (CUTS) g.draw_dense();
+            else g.draw_odd();
+        } else if (!CUTS || kind == SampleKind::kUncut) {
             g.draw((uint64_t)g.sum_uncut(false), [&](float l, uint32_t) { return g.weigh_uncut(l); });
-        } else if (kind == SampleKind::kTopP) {
-            g.bin_weights();
-            g.draw_top_p(&sh.part_w[0][0], Sh::kParts, x.seg * 64u * (R::NW / Sh::kParts), 0u);
-        } else {
-            g.list_from(kNearZ);
-            g.draw_near();
+        } else if constexpr (CUTS) {
+            if (kind == SampleKind::kTopP) {
+                g.bin_weights();
+                g.draw_top_p(&sh.part_w[0][0], Sh::kParts, x.seg * 64u * (R::NW / Sh::kParts), 0u);
+            } else {
+                g.list_from(kNearZ);
+                g.draw_near();
+            }
         }
         __syncthreads();                  // the row's shared memory is used again
     }
