@@ -220,9 +220,10 @@ const char* rlsim_last_error(const rlsim_t* h);
  *
  * A row is `vocab` consecutive logits (actions, or tokens) of RLSIM_F32,
  * RLSIM_BF16 or RLSIM_F16, aligned to the element; rows start row_stride elements
- * apart.  A handle serves calls of up to max_rows rows of up to max_vocab
- * logits on its stream; every buffer is a DEVICE pointer that the caller owns.
- * Calls allocate nothing and do not synchronise, so they can be captured. */
+ * apart, at most 2^32 (as all strides here).  A handle serves calls of up to
+ * max_rows rows of up to max_vocab logits on its stream; every buffer is a DEVICE
+ * pointer that the caller owns.  Calls allocate nothing and do not synchronise, so
+ * they can be captured (rlsim_head_create allocates the handle's workspace). */
 typedef struct rlsim_head rlsim_head_t;       /* opaque handle */
 
 /* Errors: EINVAL (out NULL, max_rows not in [1, 2^30], max_vocab not in
@@ -252,7 +253,7 @@ typedef struct {
     int dtype;
     const void* logits;
     uint32_t rows, vocab;
-    uint64_t row_stride;                      /* elements, >= vocab */
+    uint64_t row_stride;                      /* elements, in [vocab, 2^32] */
     const float* u;                           /* [rows] uniform numbers in [0, 1) */
     float temperature;
     uint32_t top_k;

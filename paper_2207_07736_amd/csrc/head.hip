@@ -57,6 +57,7 @@ struct HeadDevice {
 };
 
 constexpr uint64_t kLastLevelBytes = 256ull << 20;
+constexpr uint64_t kMaxStride = 1ull << 32;       // elements: 2^30 rows end below 2^64 bytes
 
 bool known_dtype(int d) { return d == RLSIM_F32 || d == RLSIM_BF16 || d == RLSIM_F16; }
 uint32_t dtype_bytes(int d) { return d == RLSIM_F32 ? 4u : 2u; }
@@ -69,7 +70,7 @@ const char* check_rows(const rlsim_head* h, int dtype, const void* logits, uint3
     if (!logits) return "logits is NULL";
     if (rows == 0u || rows > h->max_rows) return "rows must be in [1, max_rows]";
     if (vocab == 0u || vocab > h->max_vocab) return "vocab must be in [1, max_vocab]";
-    if (stride < vocab || stride > 1ull << 40) return "the row stride must be in [vocab, 2^40]";
+    if (stride < vocab || stride > kMaxStride) return "the row stride must be in [vocab, 2^32]";
     if (!aligned(logits, dtype_bytes(dtype))) return "logits must be aligned to its element size";
     return nullptr;
 }
@@ -186,7 +187,7 @@ void launch_distill(const rlsim_head* h, const DistillArgs& a)
     else if (form.strips == 4u) launch(k_distill<D, 256, 4>);
     else if (form.strips == 8u) launch(k_distill<D, 256, 8>);
     else if (form.threads == 256u) launch(k_distill<D, 256, 0>);
-    else launch(k_distill<D, 1024, 0>);
+    else launch(k_distill<D, 512, 0>);
 }
 
 // A kernel may use more than 64 KB of dynamic shared memory only once it is told so.
@@ -194,7 +195,7 @@ template <int D>
 hipError_t allow_shared()
 {
     const int bytes = (int)distill_shared_bytes(kHeadMaxTeacher, kHeadMaxVocab);
-    const void* const kernels[] = {reinterpret_cast<const void*>(k_distill<D, 1024, 0>),
+    const void* const kernels[] = {reinterpret_cast<const void*>(k_distill<D, 512, 0>),
                                    reinterpret_cast<const void*>(k_distill<D, 256, 0>),
                                    reinterpret_cast<const void*>(k_distill_chunk<D>)};
     hipError_t e = hipSuccess;
@@ -306,8 +307,8 @@ int rlsim_head_distill(rlsim_head_t* h, const rlsim_distill* d)
     if (!d->teacher || !d->index) return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: teacher or index is NULL");
     if (!aligned(d->teacher, dtype_bytes(d->teacher_dtype)) || !aligned(d->index, (uint32_t)d->index_bytes))
         return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: teacher or index is not aligned to its element size");
-    if (d->teacher_stride < d->k || d->index_stride < d->k || d->teacher_stride > 1ull << 40 || d->index_stride > 1ull << 40)
-        return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: teacher and index strides must be in [k, 2^40]");
+    if (d->teacher_stride < d->k || d->index_stride < d->k || d->teacher_stride > kMaxStride || d->index_stride > kMaxStride)
+        return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: teacher and index strides must be in [k, 2^32]");
     // 1 / temperature and its product with log2(e) have to be finite and not 0
     if (!(d->temperature >= 0x1.0p-60f && d->temperature <= 0x1.0p60f))
         return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: temperature must be in [2^-60, 2^60]");
@@ -318,8 +319,8 @@ int rlsim_head_distill(rlsim_head_t* h, const rlsim_distill* d)
     if (d->grad) {
         const uint32_t bytes = dtype_bytes(d->dtype);
         if (!aligned(d->grad, bytes)) return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: grad is not aligned to its element size");
-        if (d->grad_stride < d->vocab || d->grad_stride > 1ull << 40)
-            return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: grad_stride must be in [vocab, 2^40]");
+        if (d->grad_stride < d->vocab || d->grad_stride > kMaxStride)
+            return head_fail(h, RLSIM_EINVAL, "rlsim_head_distill: grad_stride must be in [vocab, 2^32]");
         const bool in_place = d->grad == d->logits && d->grad_stride == d->row_stride;
         const Span g = span(d->grad, d->rows, d->grad_stride * bytes, (uint64_t)d->vocab * bytes);
         const Span l = span(d->logits, d->rows, d->row_stride * bytes, (uint64_t)d->vocab * bytes);

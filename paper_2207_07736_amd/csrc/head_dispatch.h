@@ -13,11 +13,12 @@ constexpr uint32_t kHeadTinyVocab = 64u;
 // of them holds in registers (0: the row is read again for the gradient), for rows
 // of more entries.  Long rows take 256 threads, several workgroups to a CU, as long
 // as the rows at work, some six to a CU, stay in the 256 MB last-level cache between their
-// two reads; 1,024 threads, two to a CU, beyond.  256 / 1,024 threads, us:
-//   600 x 20,011 bf16         24 /  35      4,000 x 50,001 bf16        260 / 305
-//   1,024 x 50,001 bf16       55 /  73      2,000 x 50,001 f32         264 / 222
-//   600 x 100,000 bf16        71 /  75      2,048 x 131,072 bf16       345 / 306
-//   losses alone: 600 x 50,001 f16 23 / 34, 2,048 x 131,072 bf16 113 / 137
+// two reads; 512 threads, two to a CU, beyond.  256 / 512 / 1,024 threads, us:
+//   600 x 20,011 bf16        24 /   - /  35      4,000 x 50,001 bf16      260 /   - / 305
+//   1,024 x 50,001 bf16      55 /   - /  73      2,000 x 50,001 f32       264 / 231 / 230
+//   600 x 100,000 bf16       71 /   - /  75      2,048 x 131,072 bf16     345 / 287 / 305
+//   losses alone: 600 x 50,001 f16 23 / - / 34, 2,048 x 131,072 bf16 113 / - / 137
+// (1,024 threads, two to a CU, leave 64 registers a thread, which are too few.)
 struct HeadForm { uint32_t threads, strips; };
 inline HeadForm distill_form(uint32_t rows, uint32_t vocab, uint32_t elem_bytes, bool grad, uint32_t cus)
 {
@@ -27,7 +28,7 @@ inline HeadForm distill_form(uint32_t rows, uint32_t vocab, uint32_t elem_bytes,
     if (vectors <= 256u * 4u) return {256u, 4u};
     if (vectors <= 256u * 8u) return {256u, 8u};
     const uint64_t at_work = rows < 6u * cus ? rows : 6u * cus;
-    return {!grad || at_work * vocab * elem_bytes <= 160000000ull ? 256u : 1024u, 0u};
+    return {!grad || at_work * vocab * elem_bytes <= 160000000ull ? 256u : 512u, 0u};
 }
 
 // Threads to a row of the sampling kernel, for rows of more entries than the tiny form's.

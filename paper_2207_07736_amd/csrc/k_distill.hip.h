@@ -528,7 +528,7 @@ struct DistillGroup {
 };
 
 template <int D, int NT, int NV>
-__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_distill(DistillArgs a)
+__global__ __launch_bounds__(NT, 4) void k_distill(DistillArgs a)
 {
     using G = DistillGroup<D, NT, NV>;
     __shared__ DistillShared<G::NW> sh;

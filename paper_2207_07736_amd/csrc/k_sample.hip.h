@@ -386,14 +386,19 @@ __device__ __forceinline__ void find_listed(Sh& sh, Among in, uint32_t listed, C
     auto visit = [&](auto f) {
         for (uint32_t j = threadIdx.x; j < listed; j += NT) f(code_of(j), weight_of(j));
     };
-    while (in.n > kFew) narrow<NT>(sh, in, visit, by_weight, target);
+    // (with a shift of 0 one entry is left: the loop ends and the list holds what it gets even
+    // if another kernel changes the logits meanwhile)
+    while (in.n > kFew && in.shift) narrow<NT>(sh, in, visit, by_weight, target);
+    in.n = min(in.n, kFew);
     if (threadIdx.x == 0u) sh.few = 0u;
     __syncthreads();
     visit([&](uint64_t code, uint64_t w) {
         if (in.holds(code)) {
             const uint32_t at = atomicAdd(&sh.few, 1u);
-            sh.few_code[at] = code;
-            sh.few_w[at] = w;
+            if (at < kFew) {
+                sh.few_code[at] = code;
+                sh.few_w[at] = w;
+            }
         }
     });
     __syncthreads();
@@ -475,7 +480,8 @@ struct SampleGroup {
         const uint64_t mine = x.lane <= parts ? sh.sum[x.lane] : 0u, running = wave_scan(mine);
         const uint64_t whole = lane_u64(running, 63);
         const uint64_t target = share24(whole, s.u24);
-        const int part_lane = (int)__builtin_ctzll(__ballot(running > target));       // the last one's passes it
+        const uint64_t past = __ballot(running > target);     // the last one's passes it
+        const int part_lane = past ? (int)__builtin_ctzll(past) : (int)parts;
         const uint32_t part = (uint32_t)part_lane;
         uint64_t before = lane_u64(running, part_lane) - lane_u64(mine, part_lane);
         if (part == parts) {              // the tail's lanes
@@ -791,10 +797,14 @@ struct SampleGroup {
             });
             in = range(far, near, n, before_n, before_w);
         }
-        while (in.n > Sh::kList) narrow<NT>(sh, in, visit, by_weight, target);
+        while (in.n > Sh::kList && in.shift) narrow<NT>(sh, in, visit, by_weight, target);
+        in.n = min(in.n, Sh::kList);
         clear_list();
         visit([&](uint64_t c, uint64_t) {
-            if (in.holds(c)) sh.list_code[atomicAdd(&sh.count, 1u)] = c;
+            if (in.holds(c)) {
+                const uint32_t at = atomicAdd(&sh.count, 1u);
+                if (at < Sh::kList) sh.list_code[at] = c;
+            }
         });
         __syncthreads();
         return close_list(in.n, in.before_n, in.before_w);

@@ -34,15 +34,15 @@ int main()
                     for (bool grad : {false, true}) {
                         const HeadForm f = distill_form(rows, vocab, bytes, grad, cus);
                         CHECK(f.strips == 0u || f.threads * f.strips >= vectors);
-                        CHECK(f.threads != 1024u || grad);
+                        CHECK(f.threads != 512u || grad);
                     }
                 }
     // few long rows are shared, many are not
     CHECK(sample_chunks(1, 131072, 2, 256) == 16u && sample_chunks(512, 131072, 2, 256) == 1u);
     CHECK(distill_chunks(8, 262144, 4, 256) == 64u && distill_chunks(512, 262144, 4, 256) == 1u);
     CHECK(sample_chunks(1, 1000, 2, 256) == 1u && distill_chunks(1, 1000, 4, 256) == 1u);
-    // 1,024 threads only where the rows at work pass the last-level cache
-    CHECK(distill_form(2048, 131072, 2, true, 256).threads == 1024u && distill_form(2048, 131072, 2, false, 256).threads == 256u);
+    // 512 threads only where the rows at work pass the last-level cache
+    CHECK(distill_form(2048, 131072, 2, true, 256).threads == 512u && distill_form(2048, 131072, 2, false, 256).threads == 256u);
     CHECK(distill_form(600, 100000, 2, true, 256).threads == 256u && distill_form(4000, 50001, 2, true, 256).threads == 256u);
     printf("head dispatch: OK\n");
     return 0;
