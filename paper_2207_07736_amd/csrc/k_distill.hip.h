@@ -9,18 +9,25 @@
 // q_r being the unlisted entries' part of q.  q_r is summed over these entries alone, against
 // the largest of them (a bit for each entry of the row says which are listed): as
 // 1 - sum q_j it would vanish in rounding where the teacher lists nearly all of the mass.
-// Statistics are fp32; a gradient is rounded once, to the logits' type.
+// Statistics are fp32, the few of a row that meet in its loss 64 bits; a gradient is rounded
+// once, to the logits' type.
 //
 // A slot is left out if its entry lies outside the row (-1 marks an empty one) or
 // stands in an earlier slot.  A row without any teacher mass has loss 0 and gradient 0
 // whatever its logits; so has the gradient of a row of weight 0.
 //
 // k_distill_few, k_distill_tiny: rows of up to 8 entries, one thread to a row, and of up to
-// 64, 16 to 64 lanes to a row.
-// k_distill: longer rows, one workgroup to a row, held in registers where it fits
-// (Row), so that loss and gradient cost one read and one write of it.  The gradient
-// may overwrite the logits: a thread writes only what it has read, and the listed
-// entries' exponentials are taken before the first write.
+// 64, 16 to 64 lanes to a row.  1,048,576 rows of two fp32 entries 13 us, 42 MB.
+// k_distill: longer rows, one workgroup to a row, which is read once for the sum of its
+// exponentials against a running maximum and used again for the gradient: from registers
+// up to 16,384 2-byte entries, read again beyond (2,048 x 131,072 bf16: as fast in
+// registers, one workgroup to a CU, as read again by two).  Bound by the bytes of both
+// passes: that case 287 us, 3.7 TB/s of logits read and gradient written; 4,097 x 5,003 fp32 49-53
+// us, 3.1-3.4 TB/s; the losses alone of 1,024 x 50,001 fp16 26-29 us, 3.5-3.9 TB/s.
+// k_distill_chunk, _join: few long rows, each shared among workgroups; 8 x 262,144 fp32 in
+// 14 us, two launches of 5 and 9 us.
+// The gradient may overwrite the logits: a thread writes only what it has read, and the
+// listed entries' logits are taken before the first write.
 #pragma once
 
 #include "head_common.hip.h"
@@ -50,11 +57,10 @@ struct DistillArgs {
 constexpr uint32_t kNoEntry = 0xFFFFFFFFu;
 constexpr float kLowest = -3.40282347e38f;
 
-// A call of few rows shares each among several workgroups, a chunk of `chunk` entries (a
+// A call of few rows shares each among up to 64 workgroups, a chunk of `chunk` entries (a
 // multiple of 64 vectors) to each; what the first kernel hands on, by workgroup
 // (row * chunks + chunk) or by slot (row * k + slot).
 constexpr uint32_t kDistillSplitGroups = 1024u;   // most workgroups of such a call
-constexpr uint32_t kDistillSplitChunks = 64u;     // most chunks of a row
 struct DistillSplit {
     uint32_t chunk, chunks;
     float* mu;                    // [groups] largest entry of the chunk's sum
