@@ -156,15 +156,19 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const Student& s
 }
 
 // What a row's gradient is made of: listed entries e^((s - m) / tau) listed - p weighted,
-// others e^((s - mu) / tau) other.
-struct GradScale { float weighted, listed, other; };
-__device__ __forceinline__ GradScale grad_scale(const DistillArgs& a, const Student& s, float weight, float p_rest)
+// others e^((s - mu) / tau) other.  Both are differences that nearly cancel where the student
+// follows its teacher, so longer rows, whose sums have 64 bits, take them with Real = double:
+// four roundings of the factors to fp32 were 2e-6 of the gradient of a row whose first entry
+// holds 0.83 of the student and 0.88 of the teacher.
+template <class Real> struct GradScale { Real weighted, listed, other; };
+template <class Real>
+__device__ __forceinline__ GradScale<Real> grad_scale(const DistillArgs& a, const Student& s, float weight, Real p_rest)
 {
-    GradScale g;
-    g.weighted = a.tau * weight;
-    const float inv = s.whole == 0.0 ? 0.0f : 1.0f / (float)s.whole;     // a row of -inf: q = 0
+    GradScale<Real> g;
+    g.weighted = (Real)a.tau * (Real)weight;
+    const Real inv = s.whole == 0.0 ? (Real)0 : (Real)1 / (Real)s.whole;     // a row of -inf: q = 0
     g.listed = g.weighted * inv;
-    g.other = g.weighted * (s.share * inv - (p_rest == 0.0f || s.sum == 0.0 ? 0.0f : p_rest / (float)s.sum));
+    g.other = g.weighted * ((Real)s.share * inv - (p_rest == (Real)0 || s.sum == 0.0 ? (Real)0 : p_rest / (Real)s.sum));
     return g;
 }
 
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(256) void k_distill_few(DistillArgs a)
         if (a.loss) a.loss[row] = empty ? 0.0f : row_loss(a, st, d, sum_t, Log32());
         if (a.grad) {
             const float inv_t = 1.0f / sum_t;
-            const GradScale g = grad_scale(a, st, weight, a.rest ? e_rest * inv_t : 0.0f);
+            const GradScale<float> g = grad_scale(a, st, weight, a.rest ? e_rest * inv_t : 0.0f);
             typename El::Word* const grad = static_cast<typename El::Word*>(a.grad) + (uint64_t)row * a.grad_stride;
 #pragma unroll
             for (uint32_t e = 0; e < N; ++e) {
@@ -302,7 +306,7 @@ __global__ __launch_bounds__(256) void k_distill_tiny(DistillArgs a)
         if (!live_row) continue;
         if (a.loss && e == 0u) a.loss[row] = empty ? 0.0f : row_loss(a, st, d, sum_t, Log32());
         if (a.grad && e < a.V) {
-            const GradScale g = grad_scale(a, st, weight, p_rest);
+            const GradScale<float> g = grad_scale(a, st, weight, p_rest);
             float ds = es * (apart ? g.listed : g.other) - (listed ? p * g.weighted : 0.0f);
             if (empty || weight == 0.0f) ds = 0.0f;
             static_cast<typename El::Word*>(a.grad)[(uint64_t)row * a.grad_stride + e] = El::word(ds);
@@ -505,12 +509,16 @@ struct DistillGroup {
         const double x_rest = (double)rest - mt;
         const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
         sum_t += (double)e_rest;
-        const float inv_t = uniform(1.0f / (float)sum_t), p_rest = a.rest ? e_rest * inv_t : 0.0f;
         const Student st = student_row(a, m, mu, part, listed);
         if (a.grad) {
-            const GradScale g = grad_scale(a, st, weight, p_rest);
+            const double inv_t = 1.0 / sum_t;
+            const GradScale<double> g = grad_scale(a, st, weight, a.rest ? (double)e_rest * inv_t : 0.0);
             const bool zero = weight == 0.0f;
-            const float scale = uniform(g.other);
+            const float scale = uniform((float)g.other);
+            // in scalar registers, of which one wave's forms have fewer to spare: as many waves
+            // to a SIMD as with fp32 factors
+            const double to_listed = NW > 1 ? uniform(g.listed) : g.listed;
+            const double to_prob = NW > 1 ? uniform(inv_t * g.weighted) : inv_t * g.weighted;
             auto other = [&](float s) { return zero ? 0.0f : exp_entry(a, s, mu) * scale; };
             x.each_vector([&](const Vec16& y, uint32_t i) {
                 float f[E];
@@ -523,7 +531,8 @@ struct DistillGroup {
             for (uint32_t j = tid; j < a.k; j += NT) {
                 const uint32_t i = entry[j] - from;       // (kNoEntry and others' entries: past the chunk)
                 if (entry[j] != kNoEntry && i < length)
-                    store_one(i, zero ? 0.0f : exp_slot(log_part(a, logit[j], m)) * g.listed - prob[j] * inv_t * g.weighted);
+                    store_one(i, zero ? 0.0f : (float)((double)exp_slot(log_part(a, logit[j], m)) * to_listed
+                                                       - (double)prob[j] * to_prob));
             }
         }
         if (a.loss && owner && tid == 0u) {       // last: the logarithms take many registers

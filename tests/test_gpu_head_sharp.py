@@ -1,0 +1,48 @@
+"""Distilling rows that one entry dominates on the GPU: loss and gradient lie within bounds
+that fp32 statistics would miss (head_sharp.py), in every form for rows of more than 64
+entries.  A row of up to 64 has fp32 sums."""
+import numpy as np
+import pytest
+
+import head_sharp as sharp
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+DTYPES = {"f32": (torch.float32, 24), "bf16": (torch.bfloat16, 8), "f16": (torch.float16, 11)}
+ADDS = 66                                 # the longest thread's: 131,072 fp32 entries on 512 threads
+
+
+@pytest.fixture(scope="module")
+def head():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2207_07736_amd as p
+    h = p.Head(1024, 1 << 18)
+    yield h
+    h.close()
+
+
+@pytest.mark.parametrize("rows", (6, 700))
+@pytest.mark.parametrize("V,k,tau", ((70, 5, 1.0), (700, 9, 1.0), (2500, 20, 0.7), (5003, 33, 2.0), (20011, 64, 0.7), (70001, 9, 1.3),
+                                     (131072, 100, 2.0)))
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_student_near_a_sharp_teacher(head, dtype, V, k, tau, rows):
+    kind, bits = DTYPES[dtype]
+    rng = np.random.default_rng(V)
+    s, t, top, rest = sharp.case(rng, 6, V, k, tau)
+    dev = lambda v: torch.from_numpy(v).cuda()  # noqa: E731
+    s, t, top, rest = dev(s).to(kind), dev(t).to(kind), dev(top), dev(rest)
+    weight = dev(rng.uniform(0.5, 3.0, 6).astype(np.float32))
+    turn = torch.arange(rows, device="cuda") % 6
+    loss, grad = head.distill(s[turn], t[turn], top[turn], tau, rest[turn], weight[turn])
+    tau = float(np.float32(tau))
+    pick = sorted({*range(6), rows - 1, rows // 2})
+    loss, grad = loss[pick].cpu().numpy(), grad[pick].float().cpu().numpy()
+    s, t, top, rest, weight = (v.cpu().numpy() for v in (s.float(), t.float(), top, rest, weight))
+    for at, r in enumerate(pick):
+        j = r % 6
+        want, g, loss_bound, grad_bound = sharp.bounds(s[j], t[j], top[j], tau, float(rest[j]), float(weight[j]), bits, ADDS)
+        assert abs(float(loss[at]) - want) <= loss_bound, (r, float(loss[at]), want, loss_bound)
+        off = np.abs(grad[at] - g) - grad_bound
+        assert off.max() <= 0, (r, int(off.argmax()), grad[at][off.argmax()], g[off.argmax()], grad_bound[off.argmax()])
