@@ -9,8 +9,8 @@
 // q_r being the unlisted entries' part of q.  q_r is summed over these entries alone, against
 // the largest of them (a bit for each entry of the row says which are listed): as
 // 1 - sum q_j it would vanish in rounding where the teacher lists nearly all of the mass.
-// Statistics are fp32, the few of a row that meet in its loss 64 bits; a gradient is rounded
-// once, to the logits' type.
+// Statistics are fp32; in rows of more than 64 entries the few that meet in a row's loss and in
+// its gradient's factors are 64 bits.  A gradient is rounded once, to the logits' type.
 //
 // A slot is left out if its entry lies outside the row (-1 marks an empty one) or
 // stands in an earlier slot.  A row without any teacher mass has loss 0 and gradient 0
@@ -103,22 +103,42 @@ __device__ __forceinline__ float exp_slot(double x)
     return __builtin_ldexpf(__builtin_amdgcn_exp2f((float)(z - n)), (int)n);
 }
 
-struct Log32 {
-    __device__ double operator()(double x) const { return (double)__builtin_logf((float)x); }
+// A row's logarithms and, of a whole part of its sums, exponentials (x <= 0): of fp32 for rows
+// of up to 64 entries, whose sums are fp32 too, else of 64 bits.
+struct Stat32 {
+    __device__ static double log(double x) { return (double)__builtin_logf((float)x); }
+    __device__ static double exp(double x) { return (double)exp_slot(x); }
 };
-struct Log64 {
-    __device__ double operator()(double x) const { return ::log(x); }
+struct Stat64 {
+    __device__ static double log(double x) { return ::log(x); }
+    // the power series of e^(f ln 2 / 64), |f| <= 1/2, up to the third power, to the 64th: 2.3e-9,
+    // with few constants, each of which takes two registers.  0 where fp32 has 0, so that a
+    // mass too small for it counts as none.
+    __device__ static double exp(double x)
+    {
+        const double z = x * 1.4426950408889634;
+        if (z < -150.0) return 0.0;
+        const double n = __builtin_rint(z), y = (z - n) * (0.6931471805599453 / 64.0);
+        double e = __builtin_fma(y, 1.0 / 6.0, 0.5);
+        e = __builtin_fma(e, y, 1.0);
+        e = __builtin_fma(e, y, 1.0);
+#pragma unroll
+        for (int square = 0; square < 6; ++square) e *= e;
+        return __builtin_ldexp(e, (int)n);
+    }
 };
 
 // The loss is ln(sum of student exponentials / sum of teacher ones) plus the mean over p of
 // (t - mt) / tau - (s - m) / tau, the logits against their largest.  It is small where
 // the student follows its teacher, so what is left of it after the cancellation needs
-// more than fp32: differences, and in longer rows sums and logarithms, are in 64
-// bits, which for a few values a row costs nothing beside the row.
+// more than fp32: differences, and in longer rows sums, logarithms and the exponentials that
+// stand for many entries (the teacher's rest, the student's unlisted part; rounded to fp32 each
+// showed as 2^-25 tau^2 in the loss), are in 64 bits, which for a few values a row costs nothing
+// beside the row.
 // e (x - y) with 0 for e = 0
-__device__ __forceinline__ double excess(float e, double x, double y)
+__device__ __forceinline__ double excess(double e, double x, double y)
 {
-    return e == 0.0f ? 0.0 : (double)e * (x - y);
+    return e == 0.0 ? 0.0 : e * (x - y);
 }
 
 // A student's row: the largest logit m, and mu and sum, the largest of the pass's entries
@@ -128,31 +148,31 @@ __device__ __forceinline__ double excess(float e, double x, double y)
 struct Student {
     float m, mu;
     double sum, whole;
-    float share;                                  // e^((mu - m) / tau)
+    double share;                                 // e^((mu - m) / tau)
 };
 // ln of an entry's part of `whole`, and (log_rest) of the unlisted entries'
 __device__ __forceinline__ double log_part(const DistillArgs& a, float logit, float m)
 {
     return ((double)logit - (double)m) * a.inv_tau;
 }
-__device__ __forceinline__ Student student_row(const DistillArgs& a, float m, float mu, double sum, double listed)
+__device__ __forceinline__ Student student_row(float m, float mu, double sum, double share, double listed)
 {
-    Student s{m, mu, sum, 0.0, 0.0f};
-    s.share = sum == 0.0 ? 0.0f : exp_slot(log_part(a, mu, m));
+    Student s{m, mu, sum, 0.0, 0.0};
+    s.share = sum == 0.0 ? 0.0 : share;
     s.whole = listed + sum * s.share;
     return s;
 }
-template <class Log>
-__device__ __forceinline__ double log_rest(const DistillArgs& a, const Student& s, Log log)
+template <class Stat>
+__device__ __forceinline__ double log_rest(const DistillArgs& a, const Student& s)
 {
-    return s.sum == 0.0 ? -__builtin_inf() : log_part(a, s.mu, s.m) + log(s.sum);
+    return s.sum == 0.0 ? -__builtin_inf() : log_part(a, s.mu, s.m) + Stat::log(s.sum);
 }
 // `excesses`: their sum over the teacher's values, whose exponentials sum to sum_t
-template <class Log>
-__device__ __forceinline__ float row_loss(const DistillArgs& a, const Student& s, double excesses, double sum_t, Log log)
+template <class Stat>
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const Student& s, double excesses, double sum_t)
 {
     const double mean = excesses / sum_t;         // +inf where q = 0 < p
-    return a.tau * a.tau * (float)(s.whole == 0.0 ? mean : mean + log(s.whole / sum_t));
+    return a.tau * a.tau * (float)(s.whole == 0.0 ? mean : mean + Stat::log(s.whole / sum_t));
 }
 
 // What a row's gradient is made of: listed entries e^((s - m) / tau) listed - p weighted,
@@ -233,9 +253,9 @@ __global__ __launch_bounds__(256) void k_distill_few(DistillArgs a)
             }
             d = (double)excesses;
         }
-        const Student st = student_row(a, m, mu, sum, apart);
-        if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log32()));
-        if (a.loss) a.loss[row] = empty ? 0.0f : row_loss(a, st, d, sum_t, Log32());
+        const Student st = student_row(m, mu, sum, Stat32::exp(log_part(a, mu, m)), apart);
+        if (a.rest) d += excess(e_rest, x_rest, log_rest<Stat32>(a, st));
+        if (a.loss) a.loss[row] = empty ? 0.0f : row_loss<Stat32>(a, st, d, sum_t);
         if (a.grad) {
             const float inv_t = 1.0f / sum_t;
             const GradScale<float> g = grad_scale(a, st, weight, a.rest ? e_rest * inv_t : 0.0f);
@@ -300,11 +320,11 @@ __global__ __launch_bounds__(256) void k_distill_tiny(DistillArgs a)
         const float p = et / sum_t, p_rest = a.rest ? e_rest / sum_t : 0.0f;
         const float es = e >= a.V ? 0.0f : apart ? exp_slot(log_part(a, s, m)) : exp_entry(a, s, mu);
         const float sum = row_total(apart ? 0.0f : es);
-        const Student st = student_row(a, m, mu, sum, row_total(apart ? es : 0.0f));
+        const Student st = student_row(m, mu, sum, Stat32::exp(log_part(a, mu, m)), row_total(apart ? es : 0.0f));
         double d = row_total(listed ? (float)excess(et, x, log_part(a, s, m)) : 0.0f);
-        if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log32()));
+        if (a.rest) d += excess(e_rest, x_rest, log_rest<Stat32>(a, st));
         if (!live_row) continue;
-        if (a.loss && e == 0u) a.loss[row] = empty ? 0.0f : row_loss(a, st, d, sum_t, Log32());
+        if (a.loss && e == 0u) a.loss[row] = empty ? 0.0f : row_loss<Stat32>(a, st, d, sum_t);
         if (a.grad && e < a.V) {
             const GradScale<float> g = grad_scale(a, st, weight, p_rest);
             float ds = es * (apart ? g.listed : g.other) - (listed ? p * g.weighted : 0.0f);
@@ -477,6 +497,8 @@ struct DistillGroup {
         }
         const float m = a.rest ? __builtin_fmaxf(mu, top_l) : mu;
         const double mt = uniform(__builtin_fmax((double)top_t * a.inv_tau, (double)rest));
+        const double x_rest = (double)rest - mt, e_rest = uniform(a.rest ? Stat64::exp(x_rest) : 0.0);
+        const double share = uniform(Stat64::exp(log_part(a, mu, m)));
         // the sums, and the excesses of the loss
         double part = sum * (double)exp_entry(a, mine, mu), listed = 0.0, sum_t = 0.0, d = 0.0;
         for (uint32_t j = tid; j < a.k; j += NT) {
@@ -506,13 +528,11 @@ struct DistillGroup {
             sum_t = wave_total(in ? sh.sum[2][x.lane] : 0.0);
             d = wave_total(in ? sh.sum[3][x.lane] : 0.0);
         }
-        const double x_rest = (double)rest - mt;
-        const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
-        sum_t += (double)e_rest;
-        const Student st = student_row(a, m, mu, part, listed);
+        sum_t += e_rest;
+        const Student st = student_row(m, mu, part, share, listed);
         if (a.grad) {
             const double inv_t = 1.0 / sum_t;
-            const GradScale<double> g = grad_scale(a, st, weight, a.rest ? (double)e_rest * inv_t : 0.0);
+            const GradScale<double> g = grad_scale(a, st, weight, a.rest ? e_rest * inv_t : 0.0);
             const bool zero = weight == 0.0f;
             const float scale = uniform((float)g.other);
             // in scalar registers, of which one wave's forms have fewer to spare: as many waves
@@ -536,8 +556,8 @@ struct DistillGroup {
             }
         }
         if (a.loss && owner && tid == 0u) {       // last: the logarithms take many registers
-            if (a.rest) d += excess(e_rest, x_rest, log_rest(a, st, Log64()));
-            a.loss[row] = row_loss(a, st, d, sum_t, Log64());
+            if (a.rest) d += excess(e_rest, x_rest, log_rest<Stat64>(a, st));
+            a.loss[row] = row_loss<Stat64>(a, st, d, sum_t);
         }
     }
 };

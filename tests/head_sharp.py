@@ -82,3 +82,32 @@ def fp32_row(s, t, top, tau, rest, weight):
     weighted = f(tau) * f(weight)
     inv_t, listed = f(1) / sum_t, weighted * (f(1) / whole)
     return float(loss), float(f(e_s[top[0]] * listed) - f(f(e_t[0] * inv_t) * weighted))
+
+
+def even_case(rng, rows, V, tau, kind):
+    """One listed entry, and all others equal: their exponentials against their own largest are
+    1, their sum is exact, and so is the listed entry's e^0 on both sides.  What is left to be
+    off is e^((mu - m) / tau) and e^(rest - t / tau), one each.  `kind` rounds to the logits'
+    type.  Returns logits [rows, V], teacher [rows, 1], index [rows, 1] and rest, about a
+    thousandth from the student's own."""
+    at = rng.integers(0, V, rows)
+    g = rng.uniform(0.1, 2.0, rows)
+    low = kind((5.25 - tau * (np.log(V - 1.0) + g)).astype(np.float32))
+    s = np.repeat(low[:, None], V, axis=1)
+    s[np.arange(rows), at] = 5.25
+    t = np.full((rows, 1), 4.5, np.float32)
+    rest = 4.5 / tau + (low.astype(np.float64) - 5.25) / tau + np.log(V - 1.0) + 1e-3 * rng.standard_normal(rows)
+    return s, t, at[:, None], rest.astype(np.float32)
+
+
+def even_bounds(s, t, top, tau, rest, weight, bits):
+    """As bounds(): the two exponentials within 3e-9 of themselves, each a part of its sum, so
+    6e-9 (D + 1) tau^2, D the rest's |x - y| against the mean's."""
+    loss, grad = ref.distill_row(s, [(int(top[0]), float(t[0]))], tau, rest, weight)
+    x = s.astype(np.float64) / tau
+    q = np.exp(x - x.max())
+    q /= q.sum()
+    D = abs((float(t[0]) / tau - rest) - (x[top[0]] - (x[top[0] - 1] + np.log(len(s) - 1.0))))
+    # an unlisted entry: its factor's rounding, and its product's
+    grad_bound = tau * abs(weight) * 2e-8 * q + np.abs(grad) * (2 * U + 2.0 ** -bits) + (2.0 ** -25 if bits == 11 else 0.0)
+    return loss, grad, tau * tau * 6e-9 * (D + 1) + 2 * U * loss, grad_bound

@@ -46,3 +46,23 @@ def test_a_student_near_a_sharp_teacher(head, dtype, V, k, tau, rows):
         assert abs(float(loss[at]) - want) <= loss_bound, (r, float(loss[at]), want, loss_bound)
         off = np.abs(grad[at] - g) - grad_bound
         assert off.max() <= 0, (r, int(off.argmax()), grad[at][off.argmax()], g[off.argmax()], grad_bound[off.argmax()])
+
+
+@pytest.mark.parametrize("rows", (24, 700))
+@pytest.mark.parametrize("V,tau", ((70, 1.0), (700, 1.0), (2500, 0.7), (5003, 2.0), (20011, 0.7), (70001, 1.3), (131072, 2.0)))
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_rest_near_the_students(head, dtype, V, tau, rows):
+    kind, bits = DTYPES[dtype]
+    rng = np.random.default_rng(V + 1)
+    s, t, top, rest = sharp.even_case(rng, 24, V, tau, lambda v: torch.from_numpy(v).to(kind).float().numpy())
+    dev = lambda v: torch.from_numpy(v).cuda()  # noqa: E731
+    weight = dev(rng.uniform(0.5, 3.0, 24).astype(np.float32))
+    turn = torch.arange(rows, device="cuda") % 24
+    loss, grad = head.distill(dev(s).to(kind)[turn], dev(t).to(kind)[turn], dev(top)[turn], tau, dev(rest)[turn], weight[turn])
+    tau = float(np.float32(tau))
+    loss, grad, weight = loss.cpu().numpy(), grad[:24].float().cpu().numpy(), weight.cpu().numpy()
+    for r in range(24):
+        want, g, loss_bound, grad_bound = sharp.even_bounds(s[r], t[r], top[r], tau, float(rest[r]), float(weight[r]), bits)
+        assert abs(float(loss[r]) - want) <= loss_bound, (r, float(loss[r]), want, loss_bound)
+        off = np.abs(grad[r] - g) - grad_bound
+        assert off.max() <= 0, (r, int(off.argmax()), grad[r][off.argmax()], g[off.argmax()], grad_bound[off.argmax()])
