@@ -83,7 +83,8 @@ class Head:
     """Owning wrapper of one head handle: operators on rows of logits for up to
     ``max_rows`` rows of up to ``max_vocab`` entries.  Tensors are on the device the
     handle was created on, and are used on the handle's stream: work that makes or
-    frees them elsewhere has to be ordered with it."""
+    frees them elsewhere has to be ordered with it (``distill_loss`` orders itself).  That
+    holds for the returned tensors too, which torch allocates for its current stream."""
 
     def __init__(self, max_rows: int, max_vocab: int, stream=None):
         import torch
@@ -95,6 +96,10 @@ class Head:
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._ordinal = self.device.index
         self.max_rows, self.max_vocab = int(max_rows), int(max_vocab)
+        if stream is None or not hasattr(stream, "cuda_stream"):
+            stream = (torch.cuda.ExternalStream(int(stream), device=self.device) if stream
+                      else torch.cuda.default_stream(self.device))
+        self._stream = stream
         self.h = rlsim_head_create(max_rows, max_vocab, stream)
 
     def close(self):
@@ -176,6 +181,10 @@ class Head:
         [rows] and the gradient of sum(weight * loss) in the logits' type; ``loss``
         or ``grad`` False leaves that one out.  ``grad`` may be a tensor to write to,
         the logits themselves among them."""
+        return self._distill(rlsim_head_distill, logits, teacher, index, temperature, rest, weight, loss, grad)
+
+    def _distill(self, launch, logits, teacher, index, temperature, rest, weight, loss, grad):
+        """distill, its marshalled call made by launch(handle, arguments)."""
         dtype = self._dtype("logits", logits)
         data, rows, vocab, stride = self._rows("logits", logits)
         t_dtype = self._dtype("teacher", teacher)
@@ -190,19 +199,32 @@ class Head:
             if out.dtype != logits.dtype:
                 raise ValueError("grad must have the logits' type")
             g_data, _, _, g_stride = self._rows("grad", out, rows, vocab)
-        rlsim_head_distill(self.h, rlsim_distill(dtype, data, rows, vocab, stride, t_dtype, t_data, t_stride,
-                                                 self._index[index.dtype], i_data, i_stride, k, temperature,
-                                                 self._vector("rest", rest, rows, self._f32),
-                                                 self._vector("weight", weight, rows, self._f32),
-                                                 losses.data_ptr() if loss else None, g_data, g_stride))
+        launch(self.h, rlsim_distill(dtype, data, rows, vocab, stride, t_dtype, t_data, t_stride,
+                                     self._index[index.dtype], i_data, i_stride, k, temperature,
+                                     self._vector("rest", rest, rows, self._f32), self._vector("weight", weight, rows, self._f32),
+                                     losses.data_ptr() if loss else None, g_data, g_stride))
         if loss and out is not None:
             return losses, out
         return losses if loss else out
 
     def distill_loss(self, logits, teacher, index, temperature: float = 1.0, rest=None):
         """The losses of ``distill`` [rows], differentiable with respect to ``logits``
-        (the teacher is a constant)."""
+        (the teacher is a constant).  Forward and backward are in order with the current
+        stream, whichever the handle's is."""
         return _distill_function(self._torch).apply(self, logits, teacher, index, temperature, rest)
+
+    def _launch_in_order(self, h, args):
+        """Launch after what the current stream has been given, and before what it will be.
+        Autograd makes, uses and frees tensors on the current stream inside its backward
+        pass, where a caller can order nothing.  With both waits a tensor freed on the
+        current stream is not written to again before the kernel is done with it."""
+        current = self._torch.cuda.current_stream(self.device)
+        elsewhere = current.cuda_stream != self._stream.cuda_stream
+        if elsewhere:
+            self._stream.wait_stream(current)
+        rlsim_head_distill(h, args)
+        if elsewhere:
+            current.wait_stream(self._stream)
 
 
 _function = None
@@ -218,14 +240,14 @@ def _distill_function(torch):
             def forward(ctx, head, logits, teacher, index, temperature, rest):
                 ctx.head, ctx.temperature = head, temperature
                 ctx.save_for_backward(logits, teacher, index, *(() if rest is None else (rest,)))
-                return head.distill(logits, teacher, index, temperature, rest, grad=False)
+                return head._distill(head._launch_in_order, logits, teacher, index, temperature, rest, None, True, False)
 
             @staticmethod
             @torch.autograd.function.once_differentiable
             def backward(ctx, g):
                 logits, teacher, index, *rest = ctx.saved_tensors
-                out = ctx.head.distill(logits, teacher, index, ctx.temperature, rest[0] if rest else None,
-                                       weight=g.contiguous(), loss=False)
+                out = ctx.head._distill(ctx.head._launch_in_order, logits, teacher, index, ctx.temperature,
+                                        rest[0] if rest else None, g.contiguous(), False, True)
                 return None, out, None, None, None, None
 
         _function = DistillLoss

@@ -1,0 +1,83 @@
+"""The Python binding of the output head without a device: torch's streams and the library's
+launches are recorded, tensors are the CPU's, and no kernel runs."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2207_07736_amd as p  # noqa: E402
+from paper_2207_07736_amd import head as binding  # noqa: E402
+
+
+class Stream:
+    def __init__(self, name, address, log):
+        self.name, self.cuda_stream, self.log = name, address, log
+
+    def wait_stream(self, other):
+        self.log.append((self.name, "waits for", other.name))
+
+
+@pytest.fixture
+def device(monkeypatch):
+    """A log of launches and waits, streams to launch on, and the current one by name."""
+    class Device:
+        log, args, heads, current = [], [], [], "default"
+
+    d = Device()
+    d.streams = {name: Stream(name, at, d.log) for name, at in (("default", 0), ("own", 64), ("other", 128))}
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: d.streams[d.current])
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: d.streams["default"])
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda at, device=None: next(s for s in d.streams.values() if s.cuda_stream == at))
+    monkeypatch.setattr(binding, "rlsim_head_create", lambda *a: 1)
+    monkeypatch.setattr(binding, "rlsim_head_destroy", lambda h: None)
+
+    def launched(name):
+        def f(h, args):
+            d.log.append(name)
+            d.args.append(args)
+        return f
+
+    monkeypatch.setattr(binding, "rlsim_head_distill", launched("distill"))
+    monkeypatch.setattr(binding, "rlsim_head_sample", launched("sample"))
+
+    def head(stream=None):
+        h = p.Head(8, 16, stream=stream)
+        h.device, h._ordinal = torch.device("cpu"), -1
+        d.heads.append(h)
+        return h
+
+    d.head = head
+    yield d
+    for h in d.heads:                     # no handle is left for the real library to free
+        h.h = None
+
+
+def _teacher(rows=4):
+    return torch.zeros(rows, 3), torch.zeros(rows, 3, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("own", ("default", "own"))
+@pytest.mark.parametrize("current", ("default", "own", "other"))
+@pytest.mark.parametrize("raw", (False, True))
+def test_distill_loss_is_in_order_with_the_current_stream(device, own, current, raw):
+    """Off the handle's stream, forward and backward launch between two waits: the handle's stream
+    for the current one, then the current one for the handle's.  On it, they only launch."""
+    stream = device.streams[own]
+    head = device.head(None if own == "default" and not raw else stream.cuda_stream if raw else stream)
+    device.current = current
+    leaf = torch.zeros(4, 10, requires_grad=True)
+    loss = head.distill_loss(leaf, *_teacher())
+    want = ["distill"] if own == current else [(own, "waits for", current), "distill", (current, "waits for", own)]
+    assert device.log == want
+    device.log.clear()
+    loss.mean().backward()
+    assert device.log == want
+    assert leaf.grad.shape == leaf.shape
+
+
+def test_calls_without_a_graph_only_launch(device):
+    """sample and distill are ordered by the caller: they take no part in torch's streams."""
+    head = device.head(device.streams["own"])
+    head.distill(torch.zeros(4, 10), *_teacher())
+    head.sample(torch.zeros(4, 10), torch.zeros(4))
+    assert device.log == ["distill", "sample"]
