@@ -92,6 +92,7 @@ class Head:
         self._dtypes = {torch.float32: RLSIM_F32, torch.bfloat16: RLSIM_BF16, torch.float16: RLSIM_F16}
         self._index = {torch.int32: 4, torch.int64: 8}
         self._torch, self._tensor, self._empty = torch, torch.Tensor, torch.empty
+        self._written = torch.autograd.graph.increment_version
         self._f32, self._i32 = torch.float32, torch.int32
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._ordinal = self.device.index
@@ -180,7 +181,7 @@ class Head:
         exp(t / temperature) over what it does not list.  Returns the float32 losses
         [rows] and the gradient of sum(weight * loss) in the logits' type; ``loss``
         or ``grad`` False leaves that one out.  ``grad`` may be a tensor to write to,
-        the logits themselves among them."""
+        the logits themselves among them; autograd takes that for any other write in place."""
         return self._distill(rlsim_head_distill, logits, teacher, index, temperature, rest, weight, loss, grad)
 
     def _distill(self, launch, logits, teacher, index, temperature, rest, weight, loss, grad):
@@ -203,6 +204,8 @@ class Head:
                                      self._index[index.dtype], i_data, i_stride, k, temperature,
                                      self._vector("rest", rest, rows, self._f32), self._vector("weight", weight, rows, self._f32),
                                      losses.data_ptr() if loss else None, g_data, g_stride))
+        if out is not None and out is grad:
+            self._written(out)                    # autograd cannot see a write through an address
         if loss and out is not None:
             return losses, out
         return losses if loss else out

@@ -81,3 +81,26 @@ def test_calls_without_a_graph_only_launch(device):
     head.distill(torch.zeros(4, 10), *_teacher())
     head.sample(torch.zeros(4, 10), torch.zeros(4))
     assert device.log == ["distill", "sample"]
+
+
+def test_a_gradient_written_in_place_is_seen_by_autograd(device):
+    """What is written through an address raises the tensor's version, so that a graph which
+    saved the tensor refuses to use the overwritten values; other tensors' versions stay."""
+    head = device.head()
+    leaf = torch.ones(4, 10, requires_grad=True)
+    logits = leaf * 2.0
+    other = (logits * logits).sum()                  # saves the logits
+    out = head.distill(logits.detach(), *_teacher(), grad=logits.detach(), loss=False)
+    assert out.data_ptr() == logits.data_ptr()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        other.backward()
+    logits = leaf * 2.0
+    other = (logits * logits).sum()
+    teacher, index = _teacher()
+    before = logits._version, teacher._version, index._version
+    mine = torch.zeros(4, 10)
+    head.distill(logits.detach(), teacher, index, grad=mine)
+    head.distill(logits.detach(), teacher, index)
+    head.sample(logits.detach(), torch.zeros(4))
+    assert (logits._version, teacher._version, index._version) == before and mine._version == 1
+    other.backward()
