@@ -81,7 +81,7 @@ def rlsim_head_destroy(h) -> None:
 
 class Head:
     """Owning wrapper of one head handle: operators on rows of logits for up to
-    ``max_rows`` rows of up to ``max_vocab`` entries.  Tensors are on the device the
+    ``max_rows`` rows (none among them) of up to ``max_vocab`` entries.  Tensors are on the device the
     handle was created on, and are used on the handle's stream: work that makes or
     frees them elsewhere has to be ordered with it (``distill_loss`` orders itself).  That
     holds for the returned tensors too, which torch allocates for its current stream."""
@@ -169,9 +169,10 @@ class Head:
             raise ValueError("top_k must be >= 0")
         token = self._empty(rows, dtype=self._i32, device=self.device)
         lp = self._empty(rows, dtype=f32, device=self.device) if logp else None
-        rlsim_head_sample(self.h, rlsim_sample(dtype, data, rows, vocab, stride, self._vector("u", u, rows, f32), T, k, p, m,
-                                               T_rows, k_rows, p_rows, m_rows, token.data_ptr(),
-                                               lp.data_ptr() if logp else None))
+        args = rlsim_sample(dtype, data, rows, vocab, stride, self._vector("u", u, rows, f32), T, k, p, m,
+                            T_rows, k_rows, p_rows, m_rows, token.data_ptr(), lp.data_ptr() if logp else None)
+        if rows:                                  # an empty batch asks nothing of the device
+            rlsim_head_sample(self.h, args)
         return (token, lp) if logp else token
 
     def distill(self, logits, teacher, index, temperature: float = 1.0, rest=None, weight=None, loss: bool = True, grad=True):
@@ -200,10 +201,12 @@ class Head:
             if out.dtype != logits.dtype:
                 raise ValueError("grad must have the logits' type")
             g_data, _, _, g_stride = self._rows("grad", out, rows, vocab)
-        launch(self.h, rlsim_distill(dtype, data, rows, vocab, stride, t_dtype, t_data, t_stride,
-                                     self._index[index.dtype], i_data, i_stride, k, temperature,
-                                     self._vector("rest", rest, rows, self._f32), self._vector("weight", weight, rows, self._f32),
-                                     losses.data_ptr() if loss else None, g_data, g_stride))
+        args = rlsim_distill(dtype, data, rows, vocab, stride, t_dtype, t_data, t_stride,
+                             self._index[index.dtype], i_data, i_stride, k, temperature,
+                             self._vector("rest", rest, rows, self._f32), self._vector("weight", weight, rows, self._f32),
+                             losses.data_ptr() if loss else None, g_data, g_stride)
+        if rows:                                  # an empty batch asks nothing of the device
+            launch(self.h, args)
         if out is not None and out is grad:
             self._written(out)                    # autograd cannot see a write through an address
         if loss and out is not None:

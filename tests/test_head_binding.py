@@ -104,3 +104,30 @@ def test_a_gradient_written_in_place_is_seen_by_autograd(device):
     head.sample(logits.detach(), torch.zeros(4))
     assert (logits._version, teacher._version, index._version) == before and mine._version == 1
     other.backward()
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16, torch.float16))
+def test_no_rows(device, dtype):
+    """An empty batch gives empty tensors, by no launch; its arguments are checked all the same."""
+    head = device.head()
+    logits, u = torch.zeros(0, 10, dtype=dtype), torch.zeros(0)
+    teacher, index = _teacher(0)
+    token = head.sample(logits, u, temperature=u, top_k=5)
+    assert token.shape == (0,) and token.dtype == torch.int32
+    token, logp = head.sample(logits, u, logp=True)
+    assert token.shape == logp.shape == (0,) and logp.dtype == torch.float32
+    loss, grad = head.distill(logits, teacher, index, rest=u, weight=u)
+    assert loss.shape == (0,) and loss.dtype == torch.float32 and grad.shape == (0, 10) and grad.dtype == dtype
+    out = torch.zeros(0, 10, dtype=dtype)
+    assert head.distill(logits, teacher, index, grad=out, loss=False) is out
+    assert head.distill(logits, teacher, index, grad=False).shape == (0,)
+    leaf = logits.clone().requires_grad_()
+    head.distill_loss(leaf, teacher, index).sum().backward()
+    assert leaf.grad.shape == (0, 10)
+    assert device.args == []
+    for bad in (dict(u=torch.zeros(1)), dict(logits=logits.double()), dict(logits=torch.zeros(0)), dict(top_k=-1)):
+        with pytest.raises(ValueError):
+            head.sample(**{**dict(logits=logits, u=u), **bad})
+    for bad in (dict(teacher=torch.zeros(1, 3)), dict(index=index.float()), dict(rest=torch.zeros(1)), dict(grad=torch.zeros(1, 10))):
+        with pytest.raises(ValueError):
+            head.distill(**{**dict(logits=logits, teacher=teacher, index=index), **bad})
