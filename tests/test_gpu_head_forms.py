@@ -161,3 +161,63 @@ def test_rows_in_smaller_batches(head, V, k, dtype):
             for loss, grad in ((part[0][row - a], part[1][row - a]), (whole[0][row], whole[1][row])):
                 _same(loss.cpu().numpy(), want, loss_bound, f"loss {row}")
                 _same(grad.float().cpu().numpy(), g, grad_bound, f"gradient {row}")
+
+
+@pytest.mark.parametrize("rows", (2, ROWS))
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+def test_the_longest_rows(rows, dtype):
+    """2^20 entries, and as many teacher slots as a call takes."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2207_07736_amd as p
+    V, k = 1 << 20, 1024
+    h = p.Head(ROWS, V)
+    try:
+        rng = np.random.default_rng(rows)
+        s, t, index, rest = _case(rng, 2, V, k, dtype)
+        turn = torch.arange(rows, device="cuda") % 2
+        loss, grad = h.distill(s[turn], t[turn], index[turn], 2.0, torch.from_numpy(rest).cuda()[turn])
+        u = _u(rng, rows)
+        tokens = [h.sample(s[turn], torch.from_numpy(u).cuda(), **settings).cpu().numpy()
+                  for settings in (dict(), dict(top_p=0.9), dict(top_k=1000, min_p=0.01))]
+        sh, th, ih = s.float().cpu().numpy(), t.float().cpu().numpy(), index.cpu().numpy()
+        for row in (0, rows - 1):
+            j = row % 2
+            want, g, loss_bound, grad_bound = _bounds(sh[j], th[j], ih[j], float(rest[j]), 2.0, dtype)
+            _same(loss[row].cpu().numpy(), want, loss_bound, f"loss {row}")
+            _same(grad[row].float().cpu().numpy(), g, grad_bound, f"gradient {row}")
+            for token, settings in zip(tokens, (dict(), dict(top_p=0.9), dict(top_k=1000, min_p=0.01))):
+                assert token[row] == ref.sample_row(sh[j], u[row], **settings)[0], settings
+    finally:
+        h.close()
+
+
+# more rows than a launch has workgroups (or groups of rows) for: each goes through several
+@pytest.mark.parametrize("V,rows", ((2, 1 << 29), (9, 1 << 25), (65, 1 << 21), (2100, 1 << 21)))
+def test_more_rows_than_a_launch_has_workgroups(V, rows):
+    """The first and the last rows are those of a call of their own."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2207_07736_amd as p
+    rows, some = rows + 321, 1000
+    h = p.Head(rows, V)
+    try:
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(V)
+        logits = torch.empty((rows, V), dtype=torch.bfloat16, device="cuda").normal_(0.0, 2.0, generator=gen)
+        u = torch.rand(rows, generator=gen, device="cuda")
+        k = min(V, 3)
+        teacher = torch.empty((rows, k), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+        index = torch.randint(0, V, (rows, k), dtype=torch.int32, generator=gen, device="cuda")
+        rest = torch.zeros(rows, device="cuda")
+        for settings in (dict(), dict(top_k=2, top_p=0.8), dict(top_p=0.9)):
+            whole = h.sample(logits, u, **settings)
+            for a in (0, rows - some):
+                assert torch.equal(whole[a:a + some], h.sample(logits[a:a + some], u[a:a + some], **settings))
+            del whole
+        want = [h.distill(logits[a:a + some], teacher[a:a + some], index[a:a + some], rest=rest[a:a + some]) for a in (0, rows - some)]
+        loss, grad = h.distill(logits, teacher, index, rest=rest, grad=logits)
+        for a, (one, g) in zip((0, rows - some), want):
+            assert torch.equal(loss[a:a + some], one) and torch.equal(grad[a:a + some], g)
+    finally:
+        h.close()
