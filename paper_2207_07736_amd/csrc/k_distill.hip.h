@@ -9,8 +9,9 @@
 // q_r being the unlisted entries' part of q.  q_r is summed over these entries alone, against
 // the largest of them (a bit for each entry of the row says which are listed): as
 // 1 - sum q_j it would vanish in rounding where the teacher lists nearly all of the mass.
-// Statistics are fp32; in rows of more than 64 entries the few that meet in a row's loss and in
-// its gradient's factors are 64 bits.  A gradient is rounded once, to the logits' type.
+// Exponentials are fp32; the sums and differences that meet in a row's loss are 64 bits, and in
+// rows of more than 64 entries so are its gradient's factors.  A gradient is rounded once, to
+// the logits' type.
 //
 // A slot is left out if its entry lies outside the row (-1 marks an empty one) or
 // stands in an earlier slot.  A row without any teacher mass has loss 0 and gradient 0
@@ -103,38 +104,43 @@ __device__ __forceinline__ float exp_slot(double x)
     return __builtin_ldexpf(__builtin_amdgcn_exp2f((float)(z - n)), (int)n);
 }
 
-// A row's logarithms and, of a whole part of its sums, exponentials (x <= 0): of fp32 for rows
-// of up to 64 entries, whose sums are fp32 too, else of 64 bits.
-struct Stat32 {
-    __device__ static double log(double x) { return (double)__builtin_logf((float)x); }
-    __device__ static double exp(double x) { return (double)exp_slot(x); }
-};
-struct Stat64 {
-    __device__ static double log(double x) { return ::log(x); }
-    // the power series of e^(f ln 2 / 64), |f| <= 1/2, up to the third power, to the 64th: 2.3e-9,
-    // with few constants, each of which takes two registers.  0 where fp32 has 0, so that a
-    // mass too small for it counts as none.
-    __device__ static double exp(double x)
-    {
-        const double z = x * 1.4426950408889634;
-        if (z < -150.0) return 0.0;
-        const double n = __builtin_rint(z), y = (z - n) * (0.6931471805599453 / 64.0);
-        double e = __builtin_fma(y, 1.0 / 6.0, 0.5);
-        e = __builtin_fma(e, y, 1.0);
-        e = __builtin_fma(e, y, 1.0);
+// e^x, x <= 0, for what stands for many entries: the power series of e^(f ln 2 / 64), |f| <= 1/2,
+// up to the third power, to the 64th: 2.3e-9, with few constants, each of which takes two
+// registers.  0 where fp32 has 0, so that a mass too small for it counts as none.
+__device__ __forceinline__ double exp_part(double x)
+{
+    const double z = x * 1.4426950408889634;
+    if (z < -150.0) return 0.0;
+    const double n = __builtin_rint(z), y = (z - n) * (0.6931471805599453 / 64.0);
+    double e = __builtin_fma(y, 1.0 / 6.0, 0.5);
+    e = __builtin_fma(e, y, 1.0);
+    e = __builtin_fma(e, y, 1.0);
 #pragma unroll
-        for (int square = 0; square < 6; ++square) e *= e;
-        return __builtin_ldexp(e, (int)n);
+    for (int square = 0; square < 6; ++square) e *= e;
+    return __builtin_ldexp(e, (int)n);
+}
+
+// A row's logarithms: in short rows of x rounded to fp32, with what was rounded off to first
+// order, in longer ones of 64 bits.
+struct Log32 {
+    __device__ static double of(double x)
+    {
+        const float f = (float)x;
+        return (double)__builtin_logf(f) + (x - (double)f) * (double)(1.0f / f);
     }
+};
+struct Log64 {
+    __device__ static double of(double x) { return ::log(x); }
 };
 
 // The loss is ln(sum of student exponentials / sum of teacher ones) plus the mean over p of
 // (t - mt) / tau - (s - m) / tau, the logits against their largest.  It is small where
 // the student follows its teacher, so what is left of it after the cancellation needs
-// more than fp32: differences, and in longer rows sums, logarithms and the exponentials that
+// more than fp32: differences, sums and logarithms, and in longer rows the exponentials that
 // stand for many entries (the teacher's rest, the student's unlisted part; rounded to fp32 each
 // showed as 2^-25 tau^2 in the loss), are in 64 bits, which for a few values a row costs nothing
-// beside the row.
+// beside the row.  (Fp32 sums and logarithms of short rows: 1,048,576 rows of two fp32 entries
+// 13.3 instead of 13.6 us, losses 4.5e-7 off instead of 1.4e-7.)
 // e (x - y) with 0 for e = 0
 __device__ __forceinline__ double excess(double e, double x, double y)
 {
@@ -162,17 +168,17 @@ __device__ __forceinline__ Student student_row(float m, float mu, double sum, do
     s.whole = listed + sum * s.share;
     return s;
 }
-template <class Stat>
+template <class Log>
 __device__ __forceinline__ double log_rest(const DistillArgs& a, const Student& s)
 {
-    return s.sum == 0.0 ? -__builtin_inf() : log_part(a, s.mu, s.m) + Stat::log(s.sum);
+    return s.sum == 0.0 ? -__builtin_inf() : log_part(a, s.mu, s.m) + Log::of(s.sum);
 }
 // `excesses`: their sum over the teacher's values, whose exponentials sum to sum_t
-template <class Stat>
+template <class Log>
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const Student& s, double excesses, double sum_t)
 {
     const double mean = excesses / sum_t;         // +inf where q = 0 < p
-    return a.tau * a.tau * (float)(s.whole == 0.0 ? mean : mean + Stat::log(s.whole / sum_t));
+    return a.tau * a.tau * (float)(s.whole == 0.0 ? mean : mean + Log::of(s.whole / sum_t));
 }
 
 // What a row's gradient is made of: listed entries e^((s - m) / tau) listed - p weighted,
@@ -226,8 +232,8 @@ __global__ __launch_bounds__(256) void k_distill_few(DistillArgs a)
         mu = mu == none ? 0.0f : mu;
         const double mt = __builtin_fmax((double)top_t * a.inv_tau, (double)rest), x_rest = (double)rest - mt;
         const bool empty = mt == -__builtin_inf();
-        const float e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
-        float sum = 0.0f, apart = 0.0f, sum_t = e_rest;
+        const double e_rest = a.rest ? (double)exp_slot(x_rest) : 0.0;
+        double sum = 0.0, apart = 0.0, sum_t = e_rest;
         double d = 0.0;
         if (a.rest) {
 #pragma unroll
@@ -237,10 +243,12 @@ __global__ __launch_bounds__(256) void k_distill_few(DistillArgs a)
                 e_t[e] = in ? exp_slot(x) : 0.0f;
                 if (in) d += excess(e_t[e], x, log_part(a, s[e], m));
                 e_s[e] = e >= a.V ? 0.0f : exp_slot(log_part(a, s[e], in ? m : mu));
-                (in ? apart : sum) += e_s[e];
-                sum_t += e_t[e];
+                (in ? apart : sum) += (double)e_s[e];
+                sum_t += (double)e_t[e];
             }
-        } else {                          // the logits' differences alone: fp32 holds them
+        } else {
+            // The logits' differences alone, in fp32: at most 12 roundings, so off by no more than
+            // 2^-20 (|x| + |y|) of an entry's part, x and y its distances from the largest.
             float excesses = 0.0f;
 #pragma unroll
             for (uint32_t e = 0; e < N; ++e) {
@@ -248,17 +256,17 @@ __global__ __launch_bounds__(256) void k_distill_few(DistillArgs a)
                 e_t[e] = in ? exp_entry(a, t[e], top_t) : 0.0f;
                 e_s[e] = e >= a.V ? 0.0f : exp_entry(a, s[e], m);
                 if (e_t[e] != 0.0f) excesses += e_t[e] * (((t[e] - top_t) - (s[e] - m)) * (float)a.inv_tau);
-                sum += e_s[e];
-                sum_t += e_t[e];
+                sum += (double)e_s[e];
+                sum_t += (double)e_t[e];
             }
             d = (double)excesses;
         }
-        const Student st = student_row(m, mu, sum, Stat32::exp(log_part(a, mu, m)), apart);
-        if (a.rest) d += excess(e_rest, x_rest, log_rest<Stat32>(a, st));
-        if (a.loss) a.loss[row] = empty ? 0.0f : row_loss<Stat32>(a, st, d, sum_t);
+        const Student st = student_row(m, mu, sum, a.rest ? (double)exp_slot(log_part(a, mu, m)) : 1.0, apart);
+        if (a.rest) d += excess(e_rest, x_rest, log_rest<Log32>(a, st));
+        if (a.loss) a.loss[row] = empty ? 0.0f : row_loss<Log32>(a, st, d, sum_t);
         if (a.grad) {
-            const float inv_t = 1.0f / sum_t;
-            const GradScale<float> g = grad_scale(a, st, weight, a.rest ? e_rest * inv_t : 0.0f);
+            const float inv_t = 1.0f / (float)sum_t;
+            const GradScale<float> g = grad_scale(a, st, weight, a.rest ? (float)e_rest * inv_t : 0.0f);
             typename El::Word* const grad = static_cast<typename El::Word*>(a.grad) + (uint64_t)row * a.grad_stride;
 #pragma unroll
             for (uint32_t e = 0; e < N; ++e) {
@@ -284,9 +292,14 @@ __global__ __launch_bounds__(256) void k_distill_tiny(DistillArgs a)
         for (int off = G / 2; off >= 1; off /= 2) x = __builtin_fmaxf(x, __shfl_xor(x, off, G));
         return x;
     };
-    auto row_total = [](float x) {
+    auto row_total = [](double x) {       // rotations within 16 lanes, then across them
+        auto turned = [&](uint64_t y) { return __builtin_bit_cast(double, y); };
+        x += turned(dpp_u64<0x128, 0xf>(__builtin_bit_cast(uint64_t, x)));
+        x += turned(dpp_u64<0x124, 0xf>(__builtin_bit_cast(uint64_t, x)));
+        x += turned(dpp_u64<0x122, 0xf>(__builtin_bit_cast(uint64_t, x)));
+        x += turned(dpp_u64<0x121, 0xf>(__builtin_bit_cast(uint64_t, x)));
 #pragma unroll
-        for (int off = G / 2; off >= 1; off /= 2) x += __shfl_xor(x, off, G);
+        for (int off = 16; off < G; off *= 2) x += __shfl_xor(x, off, G);
         return x;
     };
     for (uint32_t first = blockIdx.x * per_group; first < a.rows; first += gridDim.x * per_group) {
@@ -315,16 +328,16 @@ __global__ __launch_bounds__(256) void k_distill_tiny(DistillArgs a)
         const float m = m0 == none ? 0.0f : m0, mu = mu0 == none ? 0.0f : mu0;
         const bool empty = mt == -__builtin_inf();
         const double x = (double)t * a.inv_tau - mt, x_rest = (double)rest - mt;
-        const float et = listed ? exp_slot(x) : 0.0f, e_rest = a.rest ? exp_slot(x_rest) : 0.0f;
-        const float sum_t = row_total(et) + e_rest;
-        const float p = et / sum_t, p_rest = a.rest ? e_rest / sum_t : 0.0f;
+        const float et = listed ? exp_slot(x) : 0.0f;
+        const double e_rest = a.rest ? (double)exp_slot(x_rest) : 0.0, sum_t = row_total((double)et) + e_rest;
+        const float inv_t = 1.0f / (float)sum_t, p = et * inv_t, p_rest = a.rest ? (float)e_rest * inv_t : 0.0f;
         const float es = e >= a.V ? 0.0f : apart ? exp_slot(log_part(a, s, m)) : exp_entry(a, s, mu);
-        const float sum = row_total(apart ? 0.0f : es);
-        const Student st = student_row(m, mu, sum, Stat32::exp(log_part(a, mu, m)), row_total(apart ? es : 0.0f));
-        double d = row_total(listed ? (float)excess(et, x, log_part(a, s, m)) : 0.0f);
-        if (a.rest) d += excess(e_rest, x_rest, log_rest<Stat32>(a, st));
+        const double sum = row_total(apart ? 0.0 : (double)es);
+        const Student st = student_row(m, mu, sum, a.rest ? (double)exp_slot(log_part(a, mu, m)) : 1.0, row_total(apart ? (double)es : 0.0));
+        double d = row_total(listed ? excess(et, x, log_part(a, s, m)) : 0.0);
+        if (a.rest) d += excess(e_rest, x_rest, log_rest<Log32>(a, st));
         if (!live_row) continue;
-        if (a.loss && e == 0u) a.loss[row] = empty ? 0.0f : row_loss<Stat32>(a, st, d, sum_t);
+        if (a.loss && e == 0u) a.loss[row] = empty ? 0.0f : row_loss<Log32>(a, st, d, sum_t);
         if (a.grad && e < a.V) {
             const GradScale<float> g = grad_scale(a, st, weight, p_rest);
             float ds = es * (apart ? g.listed : g.other) - (listed ? p * g.weighted : 0.0f);
@@ -497,8 +510,8 @@ struct DistillGroup {
         }
         const float m = a.rest ? __builtin_fmaxf(mu, top_l) : mu;
         const double mt = uniform(__builtin_fmax((double)top_t * a.inv_tau, (double)rest));
-        const double x_rest = (double)rest - mt, e_rest = uniform(a.rest ? Stat64::exp(x_rest) : 0.0);
-        const double share = uniform(Stat64::exp(log_part(a, mu, m)));
+        const double x_rest = (double)rest - mt, e_rest = uniform(a.rest ? exp_part(x_rest) : 0.0);
+        const double share = uniform(exp_part(log_part(a, mu, m)));
         // the sums, and the excesses of the loss
         double part = sum * (double)exp_entry(a, mine, mu), listed = 0.0, sum_t = 0.0, d = 0.0;
         for (uint32_t j = tid; j < a.k; j += NT) {
@@ -556,8 +569,8 @@ struct DistillGroup {
             }
         }
         if (a.loss && owner && tid == 0u) {       // last: the logarithms take many registers
-            if (a.rest) d += excess(e_rest, x_rest, log_rest<Stat64>(a, st));
-            a.loss[row] = row_loss<Stat64>(a, st, d, sum_t);
+            if (a.rest) d += excess(e_rest, x_rest, log_rest<Log64>(a, st));
+            a.loss[row] = row_loss<Log64>(a, st, d, sum_t);
         }
     }
 };

@@ -21,18 +21,21 @@ U = 2.0 ** -24
 
 def case(rng, rows, V, k, tau):
     """Student and teacher logits [rows, V] in fp32, each row's large entry first of its k
-    listed ones, and the teacher's rest in fp32."""
+    listed ones, and the teacher's rest in fp32 (None where every entry is listed)."""
     s = (rng.standard_normal((rows, V)) - tau * (np.log(V) + 9.0)).astype(np.float32)
     at = rng.integers(0, V, rows)
     s[np.arange(rows), at] = 5.25
     t = (s + 0.2 * tau * rng.standard_normal((rows, V))).astype(np.float32)
     t[np.arange(rows), at] = 4.5
     top = np.argsort(-t, axis=1, kind="stable")[:, :k]
+    listed = np.take_along_axis(t, top, axis=1)
+    if k == V:
+        return s, listed, top, None
     left = t.astype(np.float64) / tau
     np.put_along_axis(left, top, -np.inf, axis=1)
     most = left.max(axis=1, keepdims=True)
     rest = (most[:, 0] + np.log(np.exp(left - most).sum(axis=1))).astype(np.float32)
-    return s, np.take_along_axis(t, top, axis=1), top, rest
+    return s, listed, top, rest
 
 
 def bounds(s, t, top, tau, rest, weight, bits, adds):
@@ -40,22 +43,23 @@ def bounds(s, t, top, tau, rest, weight, bits, adds):
     slots = list(zip(top.tolist(), t.tolist()))
     loss, grad = ref.distill_row(s, slots, tau, rest, weight)
     x = s.astype(np.float64) / tau
-    values = np.append(t.astype(np.float64) / tau, rest)
+    values = t.astype(np.float64) / tau if rest is None else np.append(t.astype(np.float64) / tau, rest)
     q = np.exp(x - x.max())
     q /= q.sum()
     p = np.exp(values - values.max())
     p /= p.sum()
     other = np.ones(len(s), dtype=bool)
     other[top] = False
-    qs = np.append(q[top], q[other].sum())
+    qs = q[top] if rest is None else np.append(q[top], q[other].sum())
     R = max(1.0 - q.max(), 1.0 - p.max())
     X = max(np.ptp(x), np.ptp(values))
     E = (3 * X + 10 + 3 * adds) * U
     D = np.abs(np.log(p) - np.log(qs)).max()
     loss_bound = tau * tau * R * E * (D + 3) + U * loss * 2
     mine = np.zeros(len(s))                                  # p, and p_r q_i / q_r
-    mine[top] = p[:-1]
-    mine[other] = p[-1] * q[other] / qs[-1]
+    mine[top] = p[:len(top)]
+    if rest is not None:
+        mine[other] = p[-1] * q[other] / qs[-1]
     big = np.zeros(len(s), dtype=bool)
     big[top[0]] = True
     grad_bound = tau * abs(weight) * np.where(big, 4 * R * E, (q + mine) * 2 * E)

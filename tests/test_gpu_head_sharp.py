@@ -1,6 +1,6 @@
 """Distilling rows that one entry dominates on the GPU: loss and gradient lie within bounds
 that fp32 statistics would miss (head_sharp.py), in every form for rows of more than 64
-entries.  A row of up to 64 has fp32 sums."""
+entries; of shorter rows, whose gradients have fp32 factors, the losses do."""
 import numpy as np
 import pytest
 
@@ -66,3 +66,22 @@ def test_a_rest_near_the_students(head, dtype, V, tau, rows):
         assert abs(float(loss[r]) - want) <= loss_bound, (r, float(loss[r]), want, loss_bound)
         off = np.abs(grad[r] - g) - grad_bound
         assert off.max() <= 0, (r, int(off.argmax()), grad[r][off.argmax()], g[off.argmax()], grad_bound[off.argmax()])
+
+
+@pytest.mark.parametrize("rows", (24, 3000))
+@pytest.mark.parametrize("V,k,tau", ((2, 1, 1.0), (2, 2, 2.0), (4, 2, 1.0), (4, 4, 0.7), (8, 3, 2.0), (8, 8, 1.0), (13, 5, 1.0), (16, 16, 2.0),
+                                     (30, 8, 0.7), (55, 14, 1.0), (64, 64, 2.0)))
+def test_losses_of_short_rows(head, V, k, tau, rows):
+    import paper_2207_07736_amd as p
+    rng = np.random.default_rng(V + k)
+    s, t, top, rest = sharp.case(rng, 24, V, k, tau)
+    dev = lambda v: None if v is None else torch.from_numpy(v).cuda()[torch.arange(rows, device="cuda") % 24]  # noqa: E731
+    h = p.Head(rows, V)
+    try:
+        loss = h.distill(dev(s), dev(t), dev(top), tau, dev(rest), grad=False)[:24].cpu().numpy()
+    finally:
+        h.close()
+    tau = float(np.float32(tau))
+    for r in range(24):
+        want, _, bound, _ = sharp.bounds(s[r], t[r], top[r], tau, None if rest is None else float(rest[r]), 1.0, 24, 8)
+        assert abs(float(loss[r]) - want) <= bound, (r, float(loss[r]), want, bound)
