@@ -216,14 +216,22 @@ const char* rlsim_last_error(const rlsim_t* h);
 /* ------------------------------------------------------------------------
  * The output head: operators on rows of logits, for policies other than the one
  * built into rlsim_step_fused (the inference half of the data-collection loop,
- * Background, "RL Training") and for what a learner does with the rows.
+ * Background, "RL Training") and for what a learner does with the rows.  The
+ * simulators choose their actions themselves: rlsim_step_fused takes none drawn here.
  *
  * A row is `vocab` consecutive logits (actions, or tokens) of RLSIM_F32,
  * RLSIM_BF16 or RLSIM_F16, aligned to the element; rows start row_stride elements
  * apart, at most 2^32 (as all strides here).  A handle serves calls of up to
  * max_rows rows of up to max_vocab logits on its stream; every buffer is a DEVICE
- * pointer that the caller owns.  Calls allocate nothing and do not synchronise, so
- * they can be captured (rlsim_head_create allocates the handle's workspace). */
+ * pointer that the caller owns; outputs overlap no input but where stated.  Calls
+ * allocate nothing and do not synchronise, so they can be captured
+ * (rlsim_head_create allocates the handle's workspace).
+ *
+ * Calls of few long rows hand partial results from launch to launch in that
+ * workspace, whose address a graph keeps.  So all calls of a handle, and all replays of
+ * graphs that hold some, have to be ordered with one another, as they are on one
+ * stream; graphs that may run at the same time need a handle each; and no graph is
+ * replayed after rlsim_head_destroy. */
 typedef struct rlsim_head rlsim_head_t;       /* opaque handle */
 
 /* Errors: EINVAL (out NULL, max_rows not in [1, 2^30], max_vocab not in
@@ -286,7 +294,10 @@ int rlsim_head_sample(rlsim_head_t* h, const rlsim_sample* s);
  * whatever its student logits, and a row of weight 0 gradient 0.  A
  * student logit of -inf has q = 0: loss +inf where p > 0.  A NaN in a row that
  * counts gives NaN.  Teacher values are finite or -inf.
- * Statistics are fp32; the gradient is rounded once to the logits' type. */
+ * Exponentials and a thread's sum of them are fp32; what meets in a row's loss (and, in
+ * rows of more than 64, in its gradient's factors) is 64 bits; the gradient is rounded
+ * once to the logits' type.  Few long rows are summed in chunks, so a row's last bits can
+ * depend on how many rows the call has (a draw of rlsim_head_sample cannot). */
 typedef struct {
     int dtype;                                /* of logits and grad */
     const void* logits;

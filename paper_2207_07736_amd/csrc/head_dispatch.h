@@ -13,7 +13,9 @@ constexpr uint32_t kHeadTinyVocab = 64u;
 // of them holds in registers (0: the row is read again for the gradient), for rows
 // of more entries.  Long rows take 256 threads, several workgroups to a CU, as long
 // as the rows at work, some six to a CU, stay in the 256 MB last-level cache between their
-// two reads; 512 threads, two to a CU, beyond.  256 / 512 / 1,024 threads, us:
+// two reads; 512 threads, two to a CU, beyond.  256 / 512 / 1,024 threads, us, of one
+// batch again and again (batches in turn, which the cache does not hold, take 70 instead of 55
+// us at 1,024 rows and 84 instead of 71 at 600 x 100,000):
 //   600 x 20,011 bf16        24 /   - /  35      4,000 x 50,001 bf16      260 /   - / 305
 //   1,024 x 50,001 bf16      55 /   - /  73      2,000 x 50,001 f32       264 / 231 / 230
 //   600 x 100,000 bf16       71 /   - /  75      2,048 x 131,072 bf16     345 / 287 / 305

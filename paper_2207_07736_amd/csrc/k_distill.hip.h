@@ -9,7 +9,7 @@
 // q_r being the unlisted entries' part of q.  q_r is summed over these entries alone, against
 // the largest of them (a bit for each entry of the row says which are listed): as
 // 1 - sum q_j it would vanish in rounding where the teacher lists nearly all of the mass.
-// Exponentials are fp32; the sums and differences that meet in a row's loss are 64 bits, and in
+// Exponentials and a thread's sum of them are fp32; what meets in a row's loss is 64 bits, and in
 // rows of more than 64 entries so are its gradient's factors.  A gradient is rounded once, to
 // the logits' type.
 //
@@ -23,8 +23,8 @@
 // exponentials against a running maximum and used again for the gradient: from registers
 // up to 16,384 2-byte entries, read again beyond (2,048 x 131,072 bf16: as fast in
 // registers, one workgroup to a CU, as read again by two).  Bound by the bytes of both
-// passes: that case 287 us, 3.7 TB/s of logits read and gradient written; 4,097 x 5,003 fp32 49-53
-// us, 3.1-3.4 TB/s; the losses alone of 1,024 x 50,001 fp16 26-29 us, 3.5-3.9 TB/s.
+// passes: that case 285-292 us, 3.7 TB/s of logits read and gradient written; 4,097 x 5,003 fp32
+// 50-55 us, 3.0-3.3 TB/s; the losses alone of 1,024 x 50,001 fp16 26-29 us, 3.5-3.9 TB/s.
 // k_distill_chunk, _join: few long rows, each shared among workgroups; 8 x 262,144 fp32 in
 // 14 us, two launches of 5 and 9 us.
 // The gradient may overwrite the logits: a thread writes only what it has read, and the

@@ -981,7 +981,8 @@ __device__ __forceinline__ SampleKind sample_kind(const SampleArgs& a, const Sam
 
 // CUTS: a row of the call may have a top-k or top-p cut.  Without them the kernel is small
 // (512 rows of 151,001 bf16 in 66 instead of 78 us); with all of it 64 registers do not hold
-// the state of two workgroups of 1,024 threads to a CU, and 41 go to scratch memory.
+// the state of two workgroups of 1,024 threads to a CU, and 41 (bf16; fp32 43, fp16 57) go to
+// scratch memory.
 template <int D, int NT, bool CUTS>
 __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_sample(SampleArgs a)
 {

@@ -84,7 +84,10 @@ class Head:
     ``max_rows`` rows (none among them) of up to ``max_vocab`` entries.  Tensors are on the device the
     handle was created on, and are used on the handle's stream: work that makes or
     frees them elsewhere has to be ordered with it (``distill_loss`` orders itself).  That
-    holds for the returned tensors too, which torch allocates for its current stream."""
+    holds for the returned tensors too, which torch allocates for its current stream.
+    All calls of a handle, and all replays of graphs that captured some, have to be
+    ordered with one another: graphs that may run at the same time need a Head each, and
+    none is replayed once its Head is closed."""
 
     def __init__(self, max_rows: int, max_vocab: int, stream=None):
         import torch
@@ -155,7 +158,8 @@ class Head:
         """Draw one entry of each row of ``logits`` [rows, vocab] from the uniform
         numbers ``u`` [rows] (float32).  Each setting is a number, or a [rows] tensor
         (float32; top_k: int32).  Returns the int32 tokens, or with ``logp`` also
-        their float32 log-probabilities among the entries that the filters keep."""
+        their float32 log-probabilities among the entries that the filters keep (numbers
+        without a gradient)."""
         dtype = self._dtype("logits", logits)
         data, rows, vocab, stride = self._rows("logits", logits)
         if u is None:
