@@ -331,6 +331,145 @@ int rlsim_head_destroy(rlsim_head_t* h);
  * failure without a handle.  Valid until the next call on h. */
 const char* rlsim_head_last_error(const rlsim_head_t* h);
 
+/* ------------------------------------------------------------------------
+ * The learner: what a training step on recorded rows needs between a policy's layers
+ * and its optimiser.  A gated recurrence over rows in time (the recurrent core of a
+ * policy; one step of it acts), the cross entropy of an output layer, without an array
+ * of rows x vocab logits, with its gradient, and clipping by the gradients' global norm.
+ *
+ * A handle works on its stream; every buffer is a DEVICE pointer that the caller owns,
+ * aligned to its element; outputs overlap no input and no other output but where stated.
+ * Calls allocate nothing on the device and do not synchronise, so they can be captured
+ * (rlsim_learner_create allocates the handle's workspace).
+ *
+ * Calls hand partial results from launch to launch in that workspace, whose address a
+ * graph keeps.  So all calls of a handle, and all replays of graphs that hold some, have
+ * to be ordered with one another, as they are on one stream; graphs that may run at the
+ * same time need a handle each; and no graph is replayed after rlsim_learner_destroy.
+ * Results depend on a call's arguments alone: sums are taken in an order that its sizes
+ * fix. */
+typedef struct rlsim_learner rlsim_learner_t;       /* opaque handle */
+
+/* max_rows, max_dim, max_vocab bound the calls of rlsim_learner_xent; all three 0: the
+ * handle has no workspace for them.  rlsim_learner_scan and rlsim_learner_clip take any
+ * size.  Errors: EINVAL (out NULL; only some of the three 0; max_rows > 2^22, max_dim >
+ * 2^16 or max_vocab > 2^20), ENOMEM, EDEVICE.  On error *out is NULL. */
+int rlsim_learner_create(uint32_t max_rows, uint32_t max_dim, uint32_t max_vocab, void* stream, rlsim_learner_t** out);
+
+/* The gated recurrence.  For each of n sequences and each channel,
+ *   a_t = sigmoid(gate_t),  h_t = a_t h'_{t-1} + (1 - a_t) x_t,  y_t = h_t,
+ * h'_t being 0 where done_t is not 0 (an episode ended with step t) and h_t otherwise;
+ * h'_{-1} = state (NULL: 0), last = h'_{T-1}.  Channels of a row are consecutive elements;
+ * rows of step t and sequence i start at t step_stride + i seq_stride elements (rows of
+ * [T][n][channels] and of [n][T][channels] alike).  All of it is fp32 inside; y is
+ * rounded once.
+ *
+ * With dy the gradient of the y (NULL: 0) and dlast that of last (NULL: 0),
+ *   e_t = dy_t + (done_t ? 0 : a_{t+1} e_{t+1}),  e_{T-1} = dy_{T-1} + (done_{T-1} ? 0 : dlast),
+ *   dx_t = (1 - a_t) e_t,  dgate_t = a_t (1 - a_t) (h'_{t-1} - x_t) e_t,  dstate = a_0 e_0,
+ * from the marks that a forward call of the same x, gate, state and done left (fp32
+ * states h'_{16 j - 1}; the states between them are computed again).
+ *
+ * A NaN or an infinity stays in its channel of its sequence, from its step to the end of
+ * the episode (backward: to its beginning). */
+enum { RLSIM_SCAN_MARK = 16 };                /* steps between two marks */
+typedef struct {
+    int dtype;                                /* of x, gate, y, dy, dx and dgate */
+    uint32_t T, n, channels;                  /* each >= 1; T n channels <= 2^40 */
+    const void* x;
+    const void* gate;
+    uint64_t x_step, x_seq;                   /* strides in elements, at most 2^40; seq ignored for n = 1, */
+    uint64_t gate_step, gate_seq;             /* step for T = 1 */
+    const float* state;                       /* [n][channels] or NULL */
+    const uint8_t* done;                      /* [T][n] or NULL */
+    float* marks;                             /* [ceil(T / 16)][n][channels]; forward: out or NULL */
+    void* y;                                  /* forward: out */
+    uint64_t y_step, y_seq;
+    float* last;                              /* forward: [n][channels] out or NULL; may be state itself */
+} rlsim_scan;
+typedef struct {
+    const void* dy;                           /* or NULL */
+    uint64_t dy_step, dy_seq;
+    const float* dlast;                       /* [n][channels] or NULL */
+    void* dx;                                 /* out */
+    void* dgate;                              /* out */
+    uint64_t dx_step, dx_seq;
+    uint64_t dgate_step, dgate_seq;
+    float* dstate;                            /* [n][channels] out or NULL; may be dlast itself */
+} rlsim_scan_grad;
+
+/* Errors: EINVAL (NULL h, s, x, gate or y; unknown dtype; sizes or strides out of range;
+ * output rows that overlap; a misaligned pointer; an output over an input); EDEVICE. */
+int rlsim_learner_scan(rlsim_learner_t* h, const rlsim_scan* s);
+
+/* s as the forward call had it (y and last are ignored), its marks needed.
+ * Errors: as above; NULL g, marks, dx or dgate. */
+int rlsim_learner_scan_grad(rlsim_learner_t* h, const rlsim_scan* s, const rlsim_scan_grad* g);
+
+/* The cross entropy of an output layer: with z = hidden matrix^T,
+ *   loss_r = log sum_v exp(z_rv) - z_r,target,
+ *   dhidden, dmatrix = the gradients of sum_r weight_r loss_r (weight NULL: 1).
+ * A row whose target is outside [0, vocab) has loss 0 and adds nothing to a gradient
+ * whatever its hidden state, and so does a row of weight 0 to the gradients.  In other
+ * rows infinities and NaN do as in the formulas.
+ *
+ * Logits exist a piece of the vocabulary at a time.  They are sums of exact products in
+ * fp32 (of fp32 factors: of products to 24 bits); the softmax is fp32; its difference
+ * from the target enters the gradients' products rounded to the factors' type (fp16:
+ * scaled by powers of two before; fp32: kept to 24 bits), which are summed in fp32 and
+ * rounded once.
+ *
+ * stats holds each row's largest logit and sum of exp(z - largest): an output beside the
+ * losses, and the input of a later call for gradients alone (loss NULL) of the same
+ * hidden, matrix and target. */
+typedef struct {
+    int dtype;                                /* of hidden, matrix, dhidden and dmatrix */
+    uint32_t rows, dim, vocab;                /* each >= 1, at most the handle's */
+    const void* hidden;                       /* [rows][dim] */
+    uint64_t hidden_stride;                   /* elements, in [dim, 2^32], as all strides here */
+    const void* matrix;                       /* [vocab][dim] */
+    uint64_t matrix_stride;
+    int target_bytes;                         /* 1: uint8, 4: int32, 8: int64 */
+    const void* target;                       /* [rows] */
+    const float* weight;                      /* [rows] or NULL */
+    float* loss;                              /* [rows] out, or NULL */
+    float* stats;                             /* [rows][2] or NULL */
+    void* dhidden;                            /* [rows][dim] out, or NULL */
+    uint64_t dhidden_stride;
+    void* dmatrix;                            /* [vocab][dim] out, or NULL */
+    uint64_t dmatrix_stride;
+} rlsim_xent;
+
+/* Errors: EINVAL (NULL h, x, hidden, matrix or target; nothing wanted; loss and stats
+ * both NULL; unknown dtype or target_bytes; sizes or strides out of range; a misaligned
+ * pointer; an output over an input or another output); EDEVICE. */
+int rlsim_learner_xent(rlsim_learner_t* h, const rlsim_xent* x);
+
+/* Clip tensors by their global norm: norm = sqrt(sum of all squares), summed in 64 bits;
+ * where it is finite and above max_norm, each out is its tensor times max_norm / norm
+ * (fp32, rounded once), and its tensor otherwise.  out NULL, or an entry equal to its
+ * tensor with the same type: in place, where nothing is written unless something is
+ * scaled.  max_norm = +inf: the norm alone (in place). */
+typedef struct {
+    const void* data;                         /* may be NULL for 0 elements */
+    void* out;                                /* NULL: in place */
+    uint64_t elements;                        /* at most 2^40 */
+    int dtype, out_dtype;                     /* out_dtype is ignored in place */
+} rlsim_tensor;
+
+/* norm: device float, out.  tensors is a HOST array that the call does not keep.
+ * Errors: EINVAL (NULL h, norm or, with count > 0, tensors; count > 2^20; max_norm
+ * not > 0; NULL data, a misaligned pointer or unknown dtype; an output over another
+ * tensor's data or output, norm among them); EDEVICE. */
+int rlsim_learner_clip(rlsim_learner_t* h, const rlsim_tensor* tensors, uint32_t count, double max_norm, float* norm);
+
+/* Synchronise the stream and free the handle.  NULL is accepted (RLSIM_OK). */
+int rlsim_learner_destroy(rlsim_learner_t* h);
+
+/* Message of h's last failure ("" if none).  h == NULL: the calling thread's last
+ * failure without a handle.  Valid until the next call on h. */
+const char* rlsim_learner_last_error(const rlsim_learner_t* h);
+
 #ifdef __cplusplus
 }
 #endif

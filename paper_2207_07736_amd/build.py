@@ -16,6 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "rlsim.hip")
 HEAD_SRC = os.path.join(HERE, "csrc", "head.hip")                 # the output head's operators
+LEARN_SRC = os.path.join(HERE, "csrc", "learn.hip")               # the learner's operators
 LIB = os.path.join(HERE, "librlsim.so")
 PROBE_SRCS = [os.path.join(HERE, "csrc", "store_probe.hip")]      # includes math_probe.hip.h
 PROBE_LIB = os.path.join(HERE, "librlsim_probe.so")
@@ -45,16 +46,28 @@ def sources():
 
 
 def build(verbose: bool = False) -> str:
-    """Compile csrc/rlsim.hip and csrc/head.hip into librlsim.so and the probe sources into
-    librlsim_probe.so next to this file (always).  Returns the main library."""
-    _compile([SRC, HEAD_SRC], LIB, verbose)
-    _compile(PROBE_SRCS, PROBE_LIB, verbose)
+    """Compile csrc/rlsim.hip, csrc/head.hip and csrc/learn.hip into librlsim.so and the
+    probe sources into librlsim_probe.so next to this file (always), the sources side by
+    side.  Returns the main library."""
+    from concurrent.futures import ThreadPoolExecutor
+    objects = [(src, f"{lib}.{os.path.basename(src)}.o") for lib, srcs in ((LIB, [SRC, HEAD_SRC, LEARN_SRC]), (PROBE_LIB, PROBE_SRCS))
+               for src in srcs]
+    try:
+        with ThreadPoolExecutor(len(objects)) as pool:
+            list(pool.map(lambda so: _run([*[f for f in FLAGS if f != "-shared"], "-I", INCLUDE, "-c", "-o", so[1], so[0]], verbose),
+                          objects))
+        for lib in (LIB, PROBE_LIB):
+            _run([*FLAGS, "-o", lib + ".tmp", *[o for _, o in objects if o.startswith(lib + ".")]], verbose)
+            os.replace(lib + ".tmp", lib)
+    finally:
+        for _, o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     return LIB
 
 
-def _compile(srcs: list, lib: str, verbose: bool) -> None:
-    tmp = lib + ".tmp"
-    cmd = [HIPCC, *FLAGS, "-I", INCLUDE, "-o", tmp, *srcs]
+def _run(args: list, verbose: bool) -> None:
+    cmd = [HIPCC, *args]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -65,7 +78,6 @@ def _compile(srcs: list, lib: str, verbose: bool) -> None:
         raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
     if verbose and err.strip():
         print(err, file=sys.stderr)
-    os.replace(tmp, lib)
 
 
 def asm(out_path: str, src: str = SRC) -> str:

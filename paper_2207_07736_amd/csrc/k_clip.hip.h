@@ -1,0 +1,172 @@
+// k_clip.hip.h -- the global norm of many tensors, and their scaling by it.
+//
+// norm = sqrt(sum x^2).  One pass sums squares in 64 bits, a block of elements to a
+// workgroup; the next adds the workgroups' sums in their order (every workgroup for
+// itself: a few thousand numbers from the cache are cheaper than a launch between the
+// two) and scales.  The tensors come as kernel arguments, so that a captured call keeps
+// no table anywhere else.
+#pragma once
+
+#include "head_common.hip.h"
+#include "learn_dispatch.h"
+
+namespace rlsim_dev {
+
+struct ClipTensor {
+    const char* data;
+    char* out;
+    uint64_t elements;
+};
+struct ClipArgs {
+    ClipTensor t[kClipTensors];
+    uint32_t first[kClipTensors + 1];     // the first block of each tensor, of the launch's
+    uint8_t dtype[kClipTensors], out_dtype[kClipTensors];
+    uint32_t count, base;                 // tensors; blocks of the launches before
+    uint32_t blocks;                      // of the whole call
+    uint64_t chunk;                       // elements of a block
+    double max_norm;
+    double* sums;                         // [blocks]
+    float* norm;
+};
+
+template <int NT>
+__device__ __forceinline__ double group_sum(double x, double* sh)
+{
+    x = wave_total(x);
+    if (threadIdx.x % 64u == 0u) sh[threadIdx.x / 64u] = x;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < NT / 64; ++w) s += sh[w];
+    __syncthreads();
+    return s;
+}
+
+// f(4 floats, index) for whole fours of [from, to), g(float, index) for the rest.
+template <int D, class F, class G>
+__device__ __forceinline__ void each_four(const char* p, uint64_t from, uint64_t to, uint32_t nt, F f, G g)
+{
+    using El = Elem<D>;
+    constexpr uint32_t U = 8u;
+    const uint64_t vectors = (to - from) / El::kPerVec;
+    const auto* v = reinterpret_cast<const typename El::Run*>(p + from * El::kBytes);
+    for (uint64_t i0 = threadIdx.x; i0 < vectors; i0 += (uint64_t)nt * U) {
+        typename El::Run y[U];
+#pragma unroll
+        for (uint32_t j = 0; j < U; ++j)
+            if (i0 + j * nt < vectors) y[j] = v[i0 + j * nt];
+#pragma unroll
+        for (uint32_t j = 0; j < U; ++j)
+            if (i0 + j * nt < vectors) {
+                const Vec16 w{{y[j].w[0], y[j].w[1], y[j].w[2], y[j].w[3]}};
+                f(w, from + (i0 + j * nt) * El::kPerVec);
+            }
+    }
+    for (uint64_t i = from + vectors * El::kPerVec + threadIdx.x; i < to; i += nt)
+        g(El::one(reinterpret_cast<const typename El::Word*>(p)[i]), i);
+}
+
+template <int D>
+__device__ __forceinline__ double clip_squares(const char* p, uint64_t from, uint64_t to, uint32_t nt)
+{
+    double s = 0.0;
+    each_four<D>(p, from, to, nt,
+                 [&](const Vec16& v, uint64_t) {
+#pragma unroll
+                     for (uint32_t e = 0; e < Elem<D>::kPerVec; ++e) {
+                         const double x = (double)Elem<D>::get(v, e);
+                         s = __builtin_fma(x, x, s);
+                     }
+                 },
+                 [&](float x, uint64_t) { s = __builtin_fma((double)x, (double)x, s); });
+    return s;
+}
+
+template <int D, int O>
+__device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t from, uint64_t to, float scale, uint32_t nt)
+{
+    using To = Elem<O>;
+    each_four<D>(p, from, to, nt,
+                 [&](const Vec16& v, uint64_t i) {
+                     constexpr uint32_t E = Elem<D>::kPerVec;
+                     struct __attribute__((packed, aligned(To::kBytes))) Run { typename To::Word w[E]; } r;
+#pragma unroll
+                     for (uint32_t e = 0; e < E; ++e) r.w[e] = To::word(Elem<D>::get(v, e) * scale);
+                     *reinterpret_cast<Run*>(out + i * To::kBytes) = r;
+                 },
+                 [&](float x, uint64_t i) { reinterpret_cast<typename To::Word*>(out)[i] = To::word(x * scale); });
+}
+
+// The tensor of a block of the launch.
+__device__ __forceinline__ uint32_t clip_tensor(const ClipArgs& a, uint32_t block)
+{
+    uint32_t lo = 0u, hi = a.count;
+    while (hi - lo > 1u) {
+        const uint32_t mid = (lo + hi) / 2u;
+        if (a.first[mid] <= block) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ double squares_of(const ClipArgs& a, uint32_t block, uint32_t nt)
+{
+    const uint32_t k = clip_tensor(a, block);
+    const uint64_t from = (uint64_t)(block - a.first[k]) * a.chunk, to = min(from + a.chunk, a.t[k].elements);
+    return a.dtype[k] == kHeadF32    ? clip_squares<kHeadF32>(a.t[k].data, from, to, nt)
+           : a.dtype[k] == kHeadBF16 ? clip_squares<kHeadBF16>(a.t[k].data, from, to, nt)
+                                     : clip_squares<kHeadF16>(a.t[k].data, from, to, nt);
+}
+
+__device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, float scale, uint32_t nt)
+{
+    const uint32_t k = clip_tensor(a, block);
+    const ClipTensor& t = a.t[k];
+    if (scale == 1.0f && t.data == t.out) return;
+    const uint64_t from = (uint64_t)(block - a.first[k]) * a.chunk, to = min(from + a.chunk, t.elements);
+    auto to_type = [&](auto in) {
+        constexpr int D = decltype(in)::value;
+        if (a.out_dtype[k] == kHeadF32) clip_scale<D, kHeadF32>(t.data, t.out, from, to, scale, nt);
+        else if (a.out_dtype[k] == kHeadBF16) clip_scale<D, kHeadBF16>(t.data, t.out, from, to, scale, nt);
+        else clip_scale<D, kHeadF16>(t.data, t.out, from, to, scale, nt);
+    };
+    if (a.dtype[k] == kHeadF32) to_type(std::integral_constant<int, kHeadF32>{});
+    else if (a.dtype[k] == kHeadBF16) to_type(std::integral_constant<int, kHeadBF16>{});
+    else to_type(std::integral_constant<int, kHeadF16>{});
+}
+
+__device__ __forceinline__ float clip_factor(double norm, double max_norm)
+{
+    return norm > max_norm && norm < (double)__builtin_inff() ? (float)(max_norm / norm) : 1.0f;
+}
+
+__global__ __launch_bounds__(256) void k_clip_squares(ClipArgs a)
+{
+    __shared__ double sh[4];
+    const double s = group_sum<256>(squares_of(a, blockIdx.x, 256u), sh);
+    if (threadIdx.x == 0u) a.sums[a.base + blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a)
+{
+    __shared__ double sh[4];
+    double s = 0.0;
+    for (uint32_t i = threadIdx.x; i < a.blocks; i += 256u) s += a.sums[i];
+    const double norm = sqrt(group_sum<256>(s, sh));
+    if (a.base + blockIdx.x == 0u && threadIdx.x == 0u) *a.norm = (float)norm;
+    if (a.count) scale_block(a, blockIdx.x, clip_factor(norm, a.max_norm), 256u);
+}
+
+// Few elements: one workgroup, one launch.
+__global__ __launch_bounds__(1024) void k_clip_small(ClipArgs a)
+{
+    __shared__ double sh[16];
+    double s = 0.0;
+    const uint32_t blocks = a.first[a.count];
+    for (uint32_t b = 0; b < blocks; ++b) s += squares_of(a, b, 1024u);
+    const double norm = sqrt(group_sum<1024>(s, sh));
+    if (threadIdx.x == 0u) *a.norm = (float)norm;
+    const float scale = clip_factor(norm, a.max_norm);
+    for (uint32_t b = 0; b < blocks; ++b) scale_block(a, b, scale, 1024u);
+}
+
+}  // namespace rlsim_dev

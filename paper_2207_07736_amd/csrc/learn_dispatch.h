@@ -1,0 +1,118 @@
+// learn_dispatch.h -- which form of a learner's kernel a call runs, how its work is cut,
+// and what workspace that takes, as functions of its sizes alone (plain C++).
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace rlsim_dev {
+
+inline uint64_t up_to(uint64_t x, uint64_t multiple) { return (x + multiple - 1u) / multiple * multiple; }
+inline uint64_t least(uint64_t a, uint64_t b) { return a < b ? a : b; }
+inline uint64_t most(uint64_t a, uint64_t b) { return a > b ? a : b; }
+
+// ---- the gated recurrence ----------------------------------------------------------
+constexpr uint32_t kScanMark = 16u;               // steps between marks, and of a run of loads
+constexpr uint32_t kScanMapEntries = 1u << 21;    // most segments x channels of a call
+constexpr uint32_t kScanSegments = 256u;
+
+struct ScanCut { uint32_t segments, seg_len; };
+// Segments of time for `threads` threads' channels: as many as give every CU's waves work
+// while a segment is long enough to be worth its map (64 steps).
+inline ScanCut scan_cut(uint64_t threads, uint64_t channels, uint32_t T, uint32_t cus)
+{
+    const uint64_t wanted = 512ull * cus;
+    uint64_t s = threads >= wanted ? 1u : (wanted + threads - 1u) / threads;
+    s = least(s, T / 64u);
+    s = least(s, kScanSegments);
+    s = least(s, channels ? kScanMapEntries / channels : 1u);
+    if (s < 2u) return {1u, T};
+    const uint32_t len = (uint32_t)up_to((T + s - 1u) / s, kScanMark);
+    return {(T + len - 1u) / len, len};
+}
+
+// ---- clipping --------------------------------------------------------------------
+constexpr uint32_t kClipTensors = 96u;            // of one launch: their table has to fit its arguments
+constexpr uint32_t kClipBlocks = 4096u;           // blocks of a call, beyond one to a tensor
+constexpr uint64_t kClipSmall = 1u << 15;         // elements that one workgroup takes alone
+inline uint64_t clip_chunk(uint64_t total)
+{
+    return most(up_to((total + kClipBlocks - 1u) / kClipBlocks, 8192u), 8192u);
+}
+
+// ---- the output layer's cross entropy ------------------------------------------------
+// Products of rows run in 16-bit matrix instructions.  fp32 factors are cut into three
+// bf16 parts of 8 bits each; the six products of parts that reach 24 bits are summed.
+constexpr uint32_t kXentK = 64u;                  // elements of a step along the summed dimension
+struct XentShape {
+    uint32_t rows, dim, vocab, parts;
+    uint32_t dim_k, rows_k;                       // padded to whole steps
+    uint32_t piece;                               // entries of the vocabulary at a time
+};
+inline XentShape xent_shape(uint32_t rows, uint32_t dim, uint32_t vocab, uint32_t parts)
+{
+    XentShape s{rows, dim, vocab, parts, (uint32_t)up_to(dim, kXentK), (uint32_t)up_to(rows, kXentK), 0u};
+    uint64_t p = least((1ull << 26) / ((uint64_t)parts * s.rows_k), (1ull << 26) / ((uint64_t)parts * s.dim_k));
+    p = most(p / 256u * 256u, 256u);
+    s.piece = (uint32_t)least(p, up_to(vocab, 256u));
+    return s;
+}
+
+// The tile of a product M x N, and how many workgroups share the summed dimension of one
+// (only sums may be shared).
+struct XentTile { uint32_t m, n, span, share; };  // span: entries along m of one wave
+constexpr uint32_t kXentShareTiles = 1024u;
+inline XentTile xent_tile(uint32_t M, uint32_t N, uint64_t steps, bool sums, uint32_t cus)
+{
+    const uint64_t big = ((M + 255ull) / 256u) * ((N + 255ull) / 256u);
+    XentTile t = N <= 32u ? XentTile{128u, 32u, 32u, 1u} : big >= cus ? XentTile{256u, 256u, 128u, 1u} : XentTile{128u, 128u, 64u, 1u};
+    const uint64_t tiles = (uint64_t)((M + t.m - 1u) / t.m) * ((N + t.n - 1u) / t.n), wanted = 2ull * cus;
+    if (!sums || tiles >= wanted || t.m == 256u) return t;
+    const uint64_t s = least(least(wanted / tiles, steps / 4u), least(kXentShareTiles / tiles, 64u));
+    t.share = s < 2u ? 1u : (uint32_t)s;
+    return t;
+}
+// Floats that hold a product's shares: its tiles times 128 x 128 at most, or the product.
+inline uint64_t xent_share_floats(uint64_t rows, uint64_t dim4) { return most(rows * dim4, (uint64_t)kXentShareTiles * 128u * 128u); }
+
+struct XentWork {                                 // byte offsets
+    uint64_t target, info, zt, stats, wmax, part, x, xt, w, wt, dz, dzt, dx, dw, end;
+};
+inline XentWork xent_work(const XentShape& s)
+{
+    XentWork o{};
+    uint64_t at = 0u;
+    auto take = [&at](uint64_t bytes) { const uint64_t p = at; at += up_to(bytes, 256u); return p; };
+    const uint64_t P2 = 2ull * s.parts, dim4 = up_to(s.dim, 4u);
+    o.wmax = take(4u);
+    o.target = take(4ull * s.rows_k);
+    o.info = take(16ull * s.rows_k);
+    o.zt = take(4ull * s.rows_k);
+    o.stats = take(8ull * s.rows_k);
+    o.part = take(8ull * s.rows_k * (up_to(s.vocab, 256u) / 32u));
+    o.x = take(P2 * s.rows * s.dim_k);
+    o.xt = take(P2 * s.dim * s.rows_k);
+    o.w = take(P2 * s.piece * s.dim_k);
+    o.wt = take(P2 * s.dim * s.piece);
+    o.dz = take(P2 * s.rows * s.piece);
+    o.dzt = take(P2 * s.piece * s.rows_k);
+    o.dx = take(4u * xent_share_floats(s.rows, dim4));
+    o.dw = take(4ull * kXentShareTiles * 128u * 128u);
+    o.end = at;
+    return o;
+}
+// A handle's workspace: enough for every call within its bounds.
+inline uint64_t xent_bound(uint32_t rows, uint32_t dim, uint32_t vocab, uint32_t parts)
+{
+    const XentShape s = xent_shape(rows, dim, vocab, parts);
+    XentShape b = s;
+    XentWork o = xent_work(b);
+    // smaller rows or dim widen the piece: its arrays are bounded by their products
+    const uint64_t P2 = 2ull * parts, piece_all = up_to(vocab, 256u);
+    const uint64_t by_dim = least(P2 * piece_all * s.dim_k, most(2ull << 26, P2 * 256u * s.dim_k));
+    const uint64_t by_rows = least(P2 * piece_all * s.rows_k, most(2ull << 26, P2 * 256u * s.rows_k));
+    return o.x + 2u * up_to(P2 * (uint64_t)s.rows_k * s.dim_k, 256u) + 2u * up_to(by_dim, 256u) + 2u * up_to(by_rows, 256u)
+           + (o.end - o.dx) + 4096u;
+}
+
+}  // namespace rlsim_dev

@@ -30,7 +30,9 @@ RLSIM_MODEL_CHAIN = 1
 # every entry point include/rlsim.h declares
 EXPORTS = ("rlsim_cfg_default", "rlsim_create", "rlsim_reset", "rlsim_step_fused", "rlsim_get_state",
            "rlsim_set_state", "rlsim_destroy", "rlsim_last_error", "rlsim_head_create", "rlsim_head_sample",
-           "rlsim_head_distill", "rlsim_head_destroy", "rlsim_head_last_error")
+           "rlsim_head_distill", "rlsim_head_destroy", "rlsim_head_last_error", "rlsim_learner_create",
+           "rlsim_learner_scan", "rlsim_learner_scan_grad", "rlsim_learner_xent", "rlsim_learner_clip",
+           "rlsim_learner_destroy", "rlsim_learner_last_error")
 
 
 class RlsimError(RuntimeError):

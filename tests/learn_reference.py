@@ -1,0 +1,128 @@
+"""The learner's operators from their formulas in 64 bits, with bounds of the error that
+the kernels' arithmetic can make (torch tensors, any device).
+
+Bounds count roundings: u = 2^-24 for an fp32 operation to nearest, and a half step of the
+output's type for its own rounding.  The hardware's exp2 and reciprocal are good to one
+unit of the last place (2 u)."""
+import torch
+
+U = 2.0 ** -24
+HALF_STEP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+SMALLEST = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}
+
+
+def rounded(value, err, dtype):
+    """The bound once a value is rounded to dtype."""
+    return err + (value.abs() + err) * HALF_STEP[dtype] + SMALLEST[dtype]
+
+
+def scan(x, gate, state=None, done=None, dy=None, dlast=None):
+    """h, last, dx, dgate, dstate (the gradients None without dy and dlast), each as
+    (value, bound before the output's rounding)."""
+    T, n, d = x.shape
+    x64, g = x.double(), gate.double()
+    a, take = torch.sigmoid(g), torch.sigmoid(-g)
+    # exp2's argument is off by |g| log2(e) u (product) and as much for the constant, its
+    # value by 2 u; the sum, the reciprocal after its step, and E r add an u or two each
+    gate_err = (2.0 * g.abs() + 8.0) * U
+    keep = torch.ones((T, n, 1), dtype=torch.float64, device=x.device)
+    if done is not None:
+        keep = (done == 0).double()[:, :, None]
+    s = torch.zeros((n, d), dtype=torch.float64, device=x.device) if state is None else state.double()
+    se = torch.zeros_like(s)
+    h, he, into, into_e = [], [], [], []
+    for t in range(T):
+        into.append(s)
+        into_e.append(se)
+        parts = (a[t] * s).abs() + (take[t] * x64[t]).abs()
+        v = a[t] * s + take[t] * x64[t]
+        e = a[t] * se * (1 + 1e-5) + (gate_err[t] + 3.0 * U) * parts
+        h.append(v)
+        he.append(e)
+        s, se = v * keep[t], e * keep[t]
+    H, E, I, IE = torch.stack(h), torch.stack(he), torch.stack(into), torch.stack(into_e)
+    out = [(H, E), (s, se)]
+    if dy is None and dlast is None:
+        return out + [None, None, None]
+    dy64 = torch.zeros_like(x64) if dy is None else dy.double()
+    r = torch.zeros((n, d), dtype=torch.float64, device=x.device) if dlast is None else dlast.double()
+    re = torch.zeros_like(r)
+    dx, dg = [None] * T, [None] * T
+    for t in reversed(range(T)):
+        e = dy64[t] + keep[t] * r
+        ee = keep[t] * re + 2.0 * U * (dy64[t].abs() + (keep[t] * r).abs())
+        w = a[t] * take[t]
+        dx[t] = (take[t] * e, take[t] * (ee * (1 + 1e-5) + (gate_err[t] + 2.0 * U) * e.abs()))
+        diff = I[t] - x64[t]
+        diff_err = IE[t] + U * (I[t].abs() + x64[t].abs())
+        dg[t] = (w * diff * e, w * ((2.0 * gate_err[t] + 6.0 * U) * (diff * e).abs() + 1.00001 * (diff_err * e.abs() + ee * (diff.abs() + diff_err))))
+        r, re = a[t] * e, a[t] * (ee * (1 + 1e-5) + (gate_err[t] + 2.0 * U) * e.abs())
+    stack = lambda p: tuple(torch.stack(q) for q in zip(*p))  # noqa: E731
+    return out + [stack(dx), stack(dg), (r, re)]
+
+
+def xent(hidden, matrix, target, weight=None, grad=True):
+    """loss, dhidden, dmatrix, each as (value, bound before the output's rounding)."""
+    dtype = hidden.dtype
+    X, W = hidden.double(), matrix.double()
+    rows, dim = X.shape
+    V = W.shape[0]
+    counts = (target.long() >= 0) & (target.long() < V)
+    t = torch.where(counts, target.long(), 0)[:, None]
+    X = torch.where(counts[:, None], X, 0.0)
+    z = X @ W.t()
+    # sums of dim products, each step off by at most 2 u of what the sum of absolutes can
+    # reach (the matrix units may truncate); fp32 factors are cut to 24 bits: six sums,
+    # and three parts of 2^-24 left out
+    steps = (-(-dim // 64) * 64) * (6 if dtype == torch.float32 else 1)
+    reach = X.abs() @ W.abs().t()
+    ze = reach * (steps * 2.0 * U + 8.0 * U)
+    m = z.max(dim=1, keepdim=True).values
+    s = torch.exp(z - m).sum(dim=1, keepdim=True)
+    loss = (torch.log(s) + m - z.gather(1, t))[:, 0]
+    # a logit's error moves the loss by itself; exponentials (3 u and their argument's), the
+    # sum of V of them in fp32, the logarithm, and the differences' roundings
+    sums = (V / 16 + 64) * U
+    largest = ze.max(dim=1).values
+    exp_err = 4.0 * U + (z - m).abs().clamp(max=110.0) * 2.0 * U
+    loss_err = 2.0 * largest + sums + (exp_err * torch.exp(z - m)).sum(dim=1) / s[:, 0] + 8.0 * U * (1.0 + loss.abs() + m[:, 0].abs() + z.abs().max(dim=1).values)
+    loss = torch.where(counts, loss, 0.0)
+    loss_err = torch.where(counts, loss_err, 0.0)
+    if not grad:
+        return (loss, loss_err), None, None
+    w = torch.ones(rows, dtype=torch.float64, device=X.device) if weight is None else weight.double()
+    live = counts & (w != 0)
+    w = torch.where(live, w, 0.0)[:, None]
+    p = torch.exp(z - m) / s
+    dz = p.scatter_add(1, t, torch.full_like(z[:, :1], -1.0))
+    dz = torch.where(live[:, None], dz, 0.0)
+    pe = p * (exp_err + 2.0 * largest[:, None] + ze + sums + 8.0 * U)
+    pe = pe.scatter_add(1, t, torch.full_like(z[:, :1], U))
+    # the hardware's exp2 gives 0 below the smallest normal number, 2^-126, and so may the
+    # matrix units take a factor below it: what is smaller is off by no more than that, twice
+    tiny = 2.0 ** -125
+    pe = pe + tiny
+    half = 3.0 * U if dtype == torch.float32 else HALF_STEP[dtype]
+    floor = 2.0 ** -39 if dtype == torch.float16 else 0.0     # a denormal of 2^14 dz
+    dze = torch.where(live[:, None], pe + dz.abs() * half + floor, 0.0)
+    many = 6 if dtype == torch.float32 else 1
+    over_v = (-(-V // 64) * 64 * many + 80) * 2.0 * U
+    over_n = (-(-rows // 64) * 64 * many + 80) * 2.0 * U
+    dX = w * (dz @ W)
+    dXe = w.abs() * (dze @ W.abs() + over_v * (dz.abs() @ W.abs())) * 1.001
+    wd = w * dz
+    scale = w.abs().max() * 2.0
+    wde = w.abs() * (pe + dz.abs() * (half + 2.0 * U)) + ((floor * scale if floor else 0.0) + tiny) * live[:, None]
+    dW = wd.t() @ X
+    dWe = (wde.t() @ X.abs() + over_n * (wd.abs().t() @ X.abs())) * 1.001
+    return (loss, loss_err), (dX, dXe), (dW, dWe)
+
+
+def close(got, want, bound, what=""):
+    got = got.double()
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    off = (got - want).abs() - bound
+    assert not torch.isnan(off).any(), f"{what}: NaN"
+    worst = int(off.reshape(-1).argmax()) if off.numel() else 0
+    assert off.numel() == 0 or float(off.max()) <= 0.0, (what, worst, float(got.reshape(-1)[worst]), float(want.reshape(-1)[worst]),
+                                                         float(bound.expand_as(want).reshape(-1)[worst]))

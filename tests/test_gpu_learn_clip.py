@@ -1,0 +1,144 @@
+"""Clipping by the global norm on the GPU against its formula in 64 bits."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import learn_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+TYPES = (torch.float32, torch.bfloat16, torch.float16)
+
+
+@pytest.fixture(scope="module")
+def learner():
+    import paper_2207_07736_amd as rl
+    made = rl.Learner()
+    yield made
+    made.close()
+
+
+def _tensors(sizes, types, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return [(torch.randn(k, generator=g, device="cuda") * (1 + i % 3)).to(types[i % len(types)]) for i, k in enumerate(sizes)]
+
+
+def _norm(tensors):
+    return math.sqrt(sum(float((t.double() ** 2).sum()) for t in tensors))
+
+
+def _check(learner, tensors, max_norm, out=None):
+    before = [t.clone() for t in tensors]
+    want = _norm(tensors)
+    norm = learner.clip(tensors, max_norm, out=out)
+    assert norm.dtype == torch.float32 and norm.shape == ()
+    # products of 64 bits are exact, their sums off by 2^-53 a term; one rounding to fp32
+    assert abs(float(norm) - want) <= want * (2.0 ** -24 + 2.0 ** -30)
+    scale = max_norm / want if want > max_norm else 1.0
+    for b, t in zip(before, out if out is not None else tensors):
+        value = b.double() * scale
+        err = value.abs() * (2.5 * ref.U if scale != 1.0 else 0.0)       # the factor's and the product's roundings
+        if scale == 1.0 and b.dtype == t.dtype:
+            assert torch.equal(b, t)
+        ref.close(t, value, ref.rounded(value, err, t.dtype))
+    if out is not None:
+        for b, t in zip(before, tensors):
+            assert torch.equal(b, t)
+    return norm
+
+
+SIZES = [(1,), (0, 3), (5, 1000, 1, 7), (40000,), (32768,), (32769, 3), (300001, 1, 0, 8193, 17), tuple(range(1, 200))]
+
+
+@pytest.mark.parametrize("sizes", SIZES)
+@pytest.mark.parametrize("types", [(t,) for t in TYPES] + [TYPES])
+def test_in_place(learner, sizes, types):
+    for limit in (0.5, 1e9, float("inf")):
+        _check(learner, _tensors(sizes, types), limit)
+
+
+@pytest.mark.parametrize("sizes", SIZES)
+@pytest.mark.parametrize("types", [(t,) for t in TYPES] + [TYPES])
+@pytest.mark.parametrize("to", TYPES)
+def test_into_other_tensors(learner, sizes, types, to):
+    tensors = _tensors(sizes, types)
+    for limit in (0.5, 1e4):
+        out = [torch.full_like(t, 7.0, dtype=to) for t in tensors]
+        _check(learner, tensors, limit, out)
+
+
+def test_many_elements(learner):
+    _check(learner, _tensors((50_000_001, 3, 20_000_000), TYPES), 2.0)
+
+
+def test_more_tensors_than_a_launch_takes(learner):
+    _check(learner, _tensors([300 + i for i in range(1000)], TYPES), 3.0)
+
+
+@pytest.mark.parametrize("sizes", [(100,), (70000, 5)])
+def test_what_is_not_finite_is_left(learner, sizes):
+    for bad in (float("inf"), float("nan")):
+        tensors = _tensors(sizes, TYPES)
+        tensors[-1][2] = bad
+        before = [t.clone() for t in tensors]
+        norm = learner.clip(tensors, 1.0)
+        assert math.isinf(norm) if math.isinf(bad) else math.isnan(norm)
+        for a, b in zip(before, tensors):
+            assert torch.equal(a.view(torch.int16 if a.element_size() == 2 else torch.int32),
+                               b.view(torch.int16 if a.element_size() == 2 else torch.int32))
+
+
+def test_squares_past_fp32(learner):
+    """Values whose squares are beyond fp32 on either side."""
+    for scale in (1e25, 1e-25):
+        tensors = [torch.full((70000,), scale, device="cuda"), torch.full((3,), -2 * scale, device="cuda")]
+        limit = 10 * scale
+        want = scale * math.sqrt(70012.0)
+        norm = learner.clip(tensors, limit)
+        assert abs(float(norm) - want) <= 2.0 ** -22 * want
+        torch.testing.assert_close(tensors[0].double(), torch.full((70000,), scale * limit / want, dtype=torch.float64, device="cuda"),
+                                   rtol=2.0 ** -21, atol=0)
+
+
+def test_orders_of_dimensions_and_none(learner):
+    a = torch.randn((30, 40), device="cuda").t()
+    b = torch.randn((2, 3, 4, 5), device="cuda").to(memory_format=torch.channels_last)
+    _check(learner, [a, b], 1.0)
+    norm = learner.clip([None, a, None], 0.5)
+    assert abs(float(norm) - 1.0 * _norm([a]) / _norm([a])) < 1 and abs(_norm([a]) - 0.5) < 1e-4 or float(norm) <= 0.5
+    assert float(learner.clip([], 1.0)) == 0.0 and float(learner.clip([None], 1.0)) == 0.0
+
+
+def test_a_tensor_twice_counts_twice_where_nothing_is_written(learner):
+    a = torch.randn(1000, device="cuda")
+    assert abs(float(learner.clip([a, a], float("inf"))) - math.sqrt(2) * _norm([a])) < 1e-4 * _norm([a])
+
+
+def test_again_and_again(learner):
+    tensors = _tensors((3_000_001, 77, 500_000), TYPES)
+    out = [torch.empty_like(t) for t in tensors]
+    norm = learner.clip(tensors, 1.0, out=out)
+    first = [o.clone() for o in out]
+    for _ in range(5):
+        assert torch.equal(learner.clip(tensors, 1.0, out=out), norm)
+        for a, b in zip(first, out):
+            assert torch.equal(a, b)
+
+
+def test_refusals(learner):
+    import paper_2207_07736_amd as rl
+    a = torch.randn(1000, device="cuda")
+    for tensors, out, match in (([a.double()], None, "float32"), ([a[::2]], None, "side by side"), ([a], [a, a], "for each"),
+                                ([a], [a[:5]], "shape"), ([a.cpu()], None, "dense"), ([a], [None], "shape")):
+        with pytest.raises(ValueError, match=match):
+            learner.clip(tensors, 1.0, out=out)
+    for limit in (0.0, -1.0, float("nan")):
+        with pytest.raises(ValueError, match="max_norm"):
+            learner.clip([a], limit)
+    for tensors, out in (([a, a], None), ([a[:600], a[500:]], None), ([a[:500], a[400:900]], [a[:500], a[500:1000]]),
+                         ([a], [a.view(torch.bfloat16)[:1000]])):
+        with pytest.raises(rl.RlsimError) as e:
+            learner.clip(tensors, 1.0, out=out)
+        assert e.value.code == rl.RLSIM_EINVAL
