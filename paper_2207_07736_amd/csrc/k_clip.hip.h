@@ -7,6 +7,8 @@
 // no table anywhere else.
 #pragma once
 
+#include <type_traits>
+
 #include "head_common.hip.h"
 #include "learn_dispatch.h"
 

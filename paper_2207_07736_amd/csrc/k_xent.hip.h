@@ -1,14 +1,17 @@
 // k_xent.hip.h -- the output layer's cross entropy: products of rows on the matrix cores
 // with what the loss does to each tile of logits while it is in registers.
 //
-// All four products are of one form, C[m][n] = sum_k A[m][k] B[n][k], both operands with k
-// in consecutive elements:
-//   logits     A = matrix   (vocabulary x dim),   B = hidden (rows x dim)
-//   dhidden    A = matrix^T (dim x piece),        B = dz     (rows x piece)
-//   dmatrix    A = hidden^T (dim x rows),         B = dz^T   (piece x rows)
+// All products are of one form, C[m][n] = sum_k A[m][k] B[n][k].  An operand lies in
+// memory with k in consecutive elements ("along") or with m or n so ("across"); those are
+// turned on their way from LDS to the matrix cores, by its transposing reads:
+//   logits     A = matrix (vocabulary x dim) along,   B = hidden (rows x dim) along
+//   dhidden    A = matrix (piece x dim) across,       B = dz     (rows x piece) along
+//   dmatrix    A = hidden (rows x dim) across,        B = dz     (rows x piece) across
 // A wave's tile of C has four consecutive m in a lane's registers, and n over its lanes:
 // a row's softmax sums run within a lane, and outputs leave as runs along the row.
 #pragma once
+
+#include <type_traits>
 
 #include "head_common.hip.h"
 #include "learn_dispatch.h"
@@ -19,6 +22,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 // What a row of the call needs in the gradient's tiles.
 struct XentRow {
@@ -32,7 +36,8 @@ struct XentGemm {
     uint64_t lda, ldb;                            // bytes between rows
     uint64_t part_a, part_b;                      // bytes between the parts of fp32 factors
     uint32_t M, N;
-    uint32_t steps, products;                     // steps of one product of parts, how many products
+    uint32_t K;                                   // the summed dimension.  From K to a whole step B is 0, and A is 0
+    uint32_t steps, products;                     // too (along) or its last row again; products of parts
     uint32_t tiles_m, tiles_n, share;             // share: workgroups to a tile
     uint32_t m0;                                  // logits: first entry of the piece
     uint32_t vocab;
@@ -42,9 +47,9 @@ struct XentGemm {
     uint32_t part0, rows_k;
     const XentRow* row;                           // logits, gradient
     const float* wmax;
-    char* dz;                                     // [parts][rows][piece]
-    char* dzt;                                    // [parts][piece][rows_k]
-    uint64_t dz_ld, dzt_ld, dz_part, dzt_part;    // bytes
+    char* dz;                                     // [parts][rows_k][piece], with the rows' weights
+    char* dz_plain;                               // fp16: without them, or null
+    uint64_t dz_ld, dz_part;                      // bytes
     float* sum;                                   // gradients' products: [share][N][sum_ld]
     uint64_t sum_ld, sum_share;                   // elements
     uint32_t add;                                 // to what is there
@@ -91,44 +96,149 @@ __device__ __forceinline__ float weight_scale(float wmax)
     return __builtin_bit_cast(float, (uint32_t)(min(max(253 - e, 1), 254)) << 23);
 }
 
-// This wave's loads have arrived (those into LDS are counted as loads, which a barrier
-// alone does not wait for), then the workgroup's.
-__device__ __forceinline__ void loads_and_group()
+// Lane l has entries 0 .. 3 of two blocks of 8, lane l + 32 entries 4 .. 7 of both: lane l
+// gets the first block whole, lane l + 32 the second.
+__device__ __forceinline__ u32x4 eight_of(const uint16_t (&w)[8])
 {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    const uint32_t a0 = w[0] | (uint32_t)w[1] << 16, a1 = w[2] | (uint32_t)w[3] << 16;
+    const uint32_t b0 = w[4] | (uint32_t)w[5] << 16, b1 = w[6] | (uint32_t)w[7] << 16;
+    const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
+    const auto s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+    return u32x4{s0[0], s1[0], s0[1], s1[1]};
 }
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
 
-// A gradient's last factor: of dhidden the row's weight (and 0 for rows that do not
-// count, whatever the product is), of fp16 what dz was scaled by.
+// A gradient's last factor: 0 for dhidden's rows that do not count, whatever the product
+// is; of fp16 what dz was scaled by, and the row's weight where dz is without it.
 template <int F>
 struct OutScale {
     float by = 1.0f;
     bool counts = true;
     __device__ __forceinline__ OutScale(const XentRow* row, const float* wmax, uint32_t n)
     {
-        const float down = F == kHeadF16 ? kDzDown : 1.0f;
-        if (row) {
-            counts = row[n].target >= 0;
-            by = row[n].weight * down;
-        } else if (F == kHeadF16) {
-            by = down / weight_scale(*wmax);
-        }
+        if (row) counts = row[n].target >= 0;
+        if (F == kHeadF16) by = row ? row[n].weight * kDzDown : kDzDown / weight_scale(*wmax);
     }
     __device__ __forceinline__ float operator()(float x) const { return counts ? x * by : 0.0f; }
 };
 
-// D: the type of the factors' (parts'), F: of the call (fp32: three parts).
-template <int D, int F, int BM, int BN, int WM, int WN, int EPI>
+// One operand of a tile: R rows of C (m or n), 32 k of them at a time in LDS.
+//
+// Along: a row is 64 bytes, 4 chunks of 16; chunk c of row r lies at place c ^ (r / 2) % 4
+// of it, so that 8 lanes that read one chunk of 8 rows meet all banks.
+// Across: row k is 2 R bytes; its blocks of 32 bytes lie at place b ^ turn(k), so that the 32
+// bytes of 4 rows k that 16 lanes turn, and those of the next 16 lanes, meet all banks.
+template <bool ACROSS, uint32_t R, uint32_t NW>
+struct Operand {
+    static constexpr uint32_t kBytes = R * 64u;                  // of LDS, for a step of 32 k
+    static constexpr uint32_t kParts = R / 16u;                  // that one wave loads at once; where there are fewer
+    static constexpr uint32_t kLoads = (kParts + NW - 1u) / NW;  // than waves, two load the same
+    static_assert(kParts % NW == 0u || NW % kParts == 0u);
+    static constexpr uint32_t kRowChunks = R / 8u;               // across: chunks of 16 bytes of a row k
+    uint32_t at[kLoads];                                         // bytes from the tile's first
+    uint32_t k[ACROSS ? kLoads : 1];
+
+    __device__ __forceinline__ static uint32_t turn(uint32_t k) { return ((k & 3u) ^ (k & 1u) << 2) & (R / 16u - 1u); }
+
+    // base: the tile's first row of C; rows: how many there are in all.  What lies behind
+    // the last one is taken from the last ones again.
+    __device__ __forceinline__ void open(uint32_t base, uint32_t rows, uint32_t ld, uint32_t wave, uint32_t lane)
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) {
+            const uint32_t place = (i * NW + wave) % kParts * 64u + lane;        // of 16 bytes in LDS
+            if (ACROSS) {
+                k[i] = place / kRowChunks;
+                const uint32_t c = place % kRowChunks ^ 2u * turn(k[i]);
+                const uint32_t last = (rows + 7u) / 8u - 1u;                     // chunk of a whole row
+                at[i] = min(base / 8u + c, last) * 16u;
+            } else {
+                const uint32_t r = place / 4u, c = place % 4u ^ r / 2u % 4u;
+                at[i] = (min(base + r, rows - 1u) - min(base, rows - 1u)) * ld + c * 16u;
+            }
+        }
+    }
+    __device__ __forceinline__ static uint64_t first(uint32_t base, uint32_t rows, uint64_t ld)
+    {
+        return ACROSS ? 0u : min(base, rows - 1u) * ld;
+    }
+    // 32 k from p on into LDS; across: of the first `left` of them, the last one again and again
+    __device__ __forceinline__ void fetch(const char* p, char* to, uint32_t ld, uint32_t left, uint32_t wave) const
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) {
+            const uint32_t off = ACROSS ? at[i] + min(k[i], left - 1u) * ld : at[i];
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + off),
+                                             (__attribute__((address_space(3))) void*)(to + (i * NW + wave) % kParts * 1024u), 16, 0, 0);
+        }
+    }
+};
+// The fragments of F blocks of 32 rows of C, for the 16 k of half `h` of a step.
+template <bool ACROSS, uint32_t R, uint32_t F>
+struct Fragments {
+    uint32_t at[F];
+    u32x4 v[2][F];
+    __device__ __forceinline__ void open(uint32_t base, uint32_t lane)
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < F; ++i) {
+            if (ACROSS) {
+                const uint32_t p = lane % 16u, k = 8u * (lane / 32u) + p / 4u;
+                const uint32_t block = (base + i * 32u) / 16u + lane / 16u % 2u;
+                at[i] = k * (R * 2u) + (block ^ Operand<true, R, 1u>::turn(k)) * 32u + p % 4u * 8u;
+            } else {
+                at[i] = (base + i * 32u + lane % 32u) * 64u + (lane / 32u ^ lane / 2u % 4u) * 16u;
+            }
+        }
+    }
+    template <uint32_t H>
+    __device__ __forceinline__ void read(const char* from)
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < F; ++i) {
+            if (ACROSS) {
+                typedef __attribute__((address_space(3))) i16x4* At;
+                const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(from + at[i] + H * (R * 32u)));
+                const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(from + at[i] + H * (R * 32u) + R * 8u));
+                const uint2 l = __builtin_bit_cast(uint2, lo), u = __builtin_bit_cast(uint2, hi);
+                v[H][i] = u32x4{l.x, l.y, u.x, u.y};
+            } else {
+                v[H][i] = *reinterpret_cast<const u32x4*>(from + (at[i] ^ H * 32u));
+            }
+        }
+    }
+};
+
+// At most N of this wave's loads are still under way; none of its reads of LDS is.  (The
+// builtin, not the instruction as text: the compiler counts them too.)
+template <int N>
+__device__ __forceinline__ void loads_left()
+{
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+}
+__device__ __forceinline__ void reads_done() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+// The workgroup's waves meet.  No access to memory moves over it; what is under way stays so.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// D: the type of the factors' (parts'), F: of the call (fp32: three parts); AA, BA: whether
+// A and B lie across.
+template <int D, int F, int BM, int BN, int WM, int WN, bool AA, bool BA, int EPI>
 __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
 {
     constexpr uint32_t NW = WM * WN;
     constexpr uint32_t FM = BM / WM / 32, FN = BN / WN / 32;
-    constexpr uint32_t LA = BM * 8 / (64 * NW), LB = BN * 8 / (64 * NW);   // loads of 16 bytes a thread
-    static_assert(LA * 64 * NW == BM * 8 && LB * 64 * NW == BN * 8);
-    __shared__ __attribute__((aligned(1024))) char sh[2][(BM + BN) * 128];
+    using OpA = Operand<AA, BM, NW>;
+    using OpB = Operand<BA, BN, NW>;
+    // Four steps' operands.  Arrays of their own, and a loop that names them: the compiler has
+    // to see that a read of one does not touch what loads under way write to another.
+    constexpr uint32_t kStage = OpA::kBytes + OpB::kBytes;
+    __shared__ __attribute__((aligned(1024))) char sh0[kStage], sh1[kStage], sh2[kStage], sh3[kStage];
 
     const uint32_t lane = threadIdx.x % 64u, wave = uniform(threadIdx.x / 64u);
     const uint32_t wm = wave / WN, wn = wave % WN;
@@ -147,20 +257,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     const uint32_t tn = band * G + in % width, tm = in / width;
     const uint32_t m_base = tm * BM, n_base = tn * BN;
 
-    // A row of 64 elements is 8 chunks of 16 bytes; chunk c of row r lies at place c ^ r % 8
-    // of the row in LDS, so that the lanes that read one chunk of 8 rows meet all banks.
-    // Rows behind the last one are the last one again (a tile may lie behind it whole).
-    const uint32_t m_from = min(m_base, a.M - 1u), n_from = min(n_base, a.N - 1u);
-    uint32_t at_a[LA], at_b[LB];
-    const uint32_t chunk = (lane % 8u ^ lane / 8u) * 16u;
-#pragma unroll
-    for (uint32_t i = 0; i < LA; ++i)
-        at_a[i] = (min(m_base + (i * NW + wave) * 8u + lane / 8u, a.M - 1u) - m_from) * (uint32_t)a.lda + chunk;
-#pragma unroll
-    for (uint32_t i = 0; i < LB; ++i)
-        at_b[i] = (min(n_base + (i * NW + wave) * 8u + lane / 8u, a.N - 1u) - n_from) * (uint32_t)a.ldb + chunk;
-    const char* const A0 = a.A + (uint64_t)m_from * a.lda;
-    const char* const B0 = a.B + (uint64_t)n_from * a.ldb;
+    OpA op_a;
+    OpB op_b;
+    const uint32_t lda = (uint32_t)a.lda, ldb = (uint32_t)a.ldb;
+    op_a.open(m_base, a.M, lda, wave, lane);
+    op_b.open(n_base, a.N, ldb, wave, lane);
+    const char* const A0 = a.A + OpA::first(m_base, a.M, a.lda);
+    const char* const B0 = a.B + OpB::first(n_base, a.N, a.ldb);
+    const uint64_t step_a = AA ? 32u * a.lda : 64u, step_b = BA ? 32u * a.ldb : 64u;
 
     // the parts of product p, small products first: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
     const uint32_t all = a.steps * a.products;
@@ -171,27 +275,23 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     auto locate = [&]() {
         const uint32_t i = a.products == 1u ? 0u : 0x001012u >> (4u * product) & 15u;
         const uint32_t j = a.products == 1u ? 0u : 0x010210u >> (4u * product) & 15u;
-        pa = A0 + i * a.part_a + step * 128u;
-        pb = B0 + j * a.part_b + step * 128u;
+        pa = A0 + i * a.part_a + step * step_a;
+        pb = B0 + j * a.part_b + step * step_b;
     };
     locate();
     auto fetch = [&](char* to) {
-#pragma unroll
-        for (uint32_t i = 0; i < LA; ++i)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pa + at_a[i]),
-                                             (__attribute__((address_space(3))) void*)(to + (i * NW + wave) * 1024u), 16, 0, 0);
-#pragma unroll
-        for (uint32_t i = 0; i < LB; ++i)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pb + at_b[i]),
-                                             (__attribute__((address_space(3))) void*)(to + BM * 128u + (i * NW + wave) * 1024u), 16, 0, 0);
-        pa += 128;
-        pb += 128;
+        const uint32_t left = a.K - step * 32u;
+        op_a.fetch(pa, to, lda, left, wave);
+        op_b.fetch(pb, to + OpA::kBytes, ldb, 32u, wave);
+        pa += step_a;
+        pb += step_b;
         if (++step == a.steps) {
             step = 0u;
             ++product;
             if (product < a.products) locate();
         }
     };
+    constexpr int kEach = OpA::kLoads + OpB::kLoads;
 
     f32x16 c[FM][FN];
 #pragma unroll
@@ -199,36 +299,71 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
 #pragma unroll
         for (uint32_t j = 0; j < FN; ++j) c[i][j] = f32x16{};
 
-    const uint32_t row_a = (wm * (BM / WM) + lane % 32u) * 128u, row_b = BM * 128u + (wn * (BN / WN) + lane % 32u) * 128u;
-    auto multiply = [&](const char* from) {
-#pragma unroll
-        for (uint32_t k = 0; k < 4u; ++k) {
-            const uint32_t place = ((2u * k + lane / 32u) ^ lane % 8u) * 16u;
-            u32x4 x[FM], y[FN];
-#pragma unroll
-            for (uint32_t i = 0; i < FM; ++i) x[i] = *reinterpret_cast<const u32x4*>(from + row_a + i * 4096u + place);
-#pragma unroll
-            for (uint32_t j = 0; j < FN; ++j) y[j] = *reinterpret_cast<const u32x4*>(from + row_b + j * 4096u + place);
-#pragma unroll
-            for (uint32_t i = 0; i < FM; ++i)
-#pragma unroll
-                for (uint32_t j = 0; j < FN; ++j) c[i][j] = Matrix<D>::mma(x[i], y[j], c[i][j]);
-        }
-    };
+    Fragments<AA, BM, FM> x;
+    Fragments<BA, BN, FN> y;
+    x.open(wm * (BM / WM), lane);
+    y.open(wn * (BN / WN), lane);
 
-    // One step is in registers' work while the next one's loads are under way.
+    // Four steps of 32 k are in LDS or under way.  While a half step of 16 k is multiplied,
+    // the next one's fragments are read; the workgroup meets once a step, after which the
+    // step just read may be overwritten and the next one, loaded three steps ago, read.
+    auto one_step = [&](auto steady, uint32_t t, char* now, char* next, char* ahead) {
+        constexpr bool kSteady = decltype(steady)::value;        // three more steps are to come
+        if (kSteady || t + 3u < last) fetch(ahead);
+        reads_done();                             // of the first half
+        x.template read<1>(now);
+        y.template read<1>(now + OpA::kBytes);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < FN; ++j) c[i][j] = Matrix<D>::mma(x.v[0][i], y.v[0][j], c[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (kSteady || t + 3u < last) loads_left<2 * kEach>();
+        else if (t + 2u < last) loads_left<kEach>();
+        else loads_left<0>();
+        reads_done();
+        meet();
+        if (kSteady || t + 1u < last) {
+            x.template read<0>(next);
+            y.template read<0>(next + OpA::kBytes);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < FN; ++j) c[i][j] = Matrix<D>::mma(x.v[1][i], y.v[1][j], c[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
     if (first < last) {
-        fetch(sh[0]);
+        fetch(sh0);
+        if (first + 2u < last) {
+            fetch(sh1);
+            fetch(sh2);
+            loads_left<2 * kEach>();
+        } else {
+            if (first + 1u < last) fetch(sh1);
+            loads_left<0>();
+        }
+        meet();
+        x.template read<0>(sh0);
+        y.template read<0>(sh0 + OpA::kBytes);
+        uint32_t t = first;
+        constexpr std::true_type steady{};
+        constexpr std::false_type ending{};
 #pragma unroll 1
-        for (uint32_t t = first; t < last; t += 2u) {
-            loads_and_group();
-            if (t + 1u < last) fetch(sh[1]);
-            multiply(sh[0]);
-            loads_and_group();
-            if (t + 1u < last) {
-                if (t + 2u < last) fetch(sh[0]);
-                multiply(sh[1]);
-            }
+        for (; t + 6u < last; t += 4u) {
+            one_step(steady, t, sh0, sh1, sh3);
+            one_step(steady, t + 1u, sh1, sh2, sh0);
+            one_step(steady, t + 2u, sh2, sh3, sh1);
+            one_step(steady, t + 3u, sh3, sh0, sh2);
+        }
+#pragma unroll 1
+        for (; t < last; t += 4u) {
+            one_step(ending, t, sh0, sh1, sh3);
+            if (t + 1u < last) one_step(ending, t + 1u, sh1, sh2, sh0);
+            if (t + 2u < last) one_step(ending, t + 2u, sh2, sh3, sh1);
+            if (t + 3u < last) one_step(ending, t + 3u, sh3, sh0, sh2);
         }
     }
 
@@ -268,38 +403,40 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
             for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
                 for (uint32_t q = 0; q < 4u; ++q) {
-                    const uint32_t m = m_wave + i * 32u + q * 8u;
-                    uint16_t w[3][4];
 #pragma unroll
                     for (uint32_t e = 0; e < 4u; ++e) {
-                        const uint32_t v = a.m0 + m + e;
+                        const uint32_t v = a.m0 + m_wave + i * 32u + q * 8u + e;
                         float p = exp_of(c[i][j][4u * q + e] - r.largest) * r.inv_sum;
                         if ((int32_t)v == r.target) p -= 1.0f;
-                        if (v >= a.vocab || r.target < 0) p = 0.0f;
-                        if (F == kHeadF32) {
-                            uint16_t x[3], y[3];
-                            cut3(p, x);
-                            cut3(p == 0.0f ? 0.0f : p * weight, y);
-#pragma unroll
-                            for (uint32_t s = 0; s < 3u; ++s) {
-                                w[s][e] = x[s];
-                                if (n < a.rows_k)
-                                    *reinterpret_cast<uint16_t*>(a.dzt + s * a.dzt_part + (m + e) * a.dzt_ld + 2u * n) = y[s];
-                            }
-                        } else {
-                            w[0][e] = Elem<D>::word(p * up);
-                            if (n < a.rows_k)
-                                *reinterpret_cast<uint16_t*>(a.dzt + (m + e) * a.dzt_ld + 2u * n) = Elem<D>::word(p == 0.0f ? 0.0f : p * weight);
-                        }
-                    }
-                    if (n < a.N) {
-#pragma unroll
-                        for (uint32_t s = 0; s < (F == kHeadF32 ? 3u : 1u); ++s) {
-                            struct alignas(8) Four { uint16_t w[4]; } four{{w[s][0], w[s][1], w[s][2], w[s][3]}};
-                            *reinterpret_cast<Four*>(a.dz + s * a.dz_part + n * a.dz_ld + 2u * m) = four;
-                        }
+                        c[i][j][4u * q + e] = v >= a.vocab || r.target < 0 ? 0.0f : p;
                     }
                 }
+            if (n < a.rows_k) {
+                char* const to = a.dz + n * a.dz_ld;
+#pragma unroll
+                for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+                    for (uint32_t q = 0; q < 4u; q += 2u) {
+                        uint16_t w[3][8], plain[8];
+#pragma unroll
+                        for (uint32_t e = 0; e < 8u; ++e) {
+                            const float p = c[i][j][4u * q + e];
+                            const float pw = p == 0.0f ? 0.0f : p * weight;
+                            uint16_t cut[3];
+                            if (F == kHeadF32) cut3(pw, cut);
+                            else cut[0] = Elem<D>::word(pw);
+#pragma unroll
+                            for (uint32_t s = 0; s < (F == kHeadF32 ? 3u : 1u); ++s) w[s][e] = cut[s];
+                            plain[e] = F == kHeadF16 ? Elem<D>::word(p * up) : (uint16_t)0;
+                        }
+                        const uint64_t m = m_base + wm * (BM / WM) + i * 32u + (q + lane / 32u) * 8u;
+#pragma unroll
+                        for (uint32_t s = 0; s < (F == kHeadF32 ? 3u : 1u); ++s)
+                            *reinterpret_cast<u32x4*>(to + s * a.dz_part + 2u * m) = eight_of(w[s]);
+                        if (F == kHeadF16 && a.dz_plain)
+                            *reinterpret_cast<u32x4*>(a.dz_plain + n * a.dz_ld + 2u * m) = eight_of(plain);
+                    }
+            }
         }
         if (EPI == kXentSum) {
 #pragma unroll
@@ -416,48 +553,49 @@ __global__ __launch_bounds__(256) void k_xent_join(XentJoin a)
     }
 }
 
-// Rows as the products read them: whole steps wide, fp32 in three parts, and transposed.
+// Rows as the products read them: whole steps wide, fp32 in three parts; rows that do not
+// count are 0 where they are told.
 struct XentLay {
     const char* from;                             // [R][C]
     uint64_t ld;                                  // bytes
-    uint32_t R, C;
-    char* straight;                               // [parts][R][straight_ld], or null
-    uint64_t straight_ld, straight_part;          // bytes
-    uint32_t wide;                                // elements of a straight row
-    char* across;                                 // [parts][C][across_ld], or null
-    uint64_t across_ld, across_part;
-    uint32_t tall;                                // elements of a transposed row
-    const XentRow* row;                           // rows that do not count are 0 across
+    uint32_t R, C, wide;                          // wide: elements of a row of the copy, a multiple of 8
+    char* to;                                     // [parts][R][wide]
+    uint64_t part;                                // bytes
+    const XentRow* row;                           // or null
 };
 template <int F>
 __global__ __launch_bounds__(256) void k_xent_lay(XentLay a)
 {
     using El = Elem<F>;
     constexpr uint32_t P = F == kHeadF32 ? 3u : 1u;
-    __shared__ uint16_t tile[P][64][66];
-    const uint32_t c0 = blockIdx.x * 64u, r0 = blockIdx.y * 64u;
-    const uint32_t x = threadIdx.x % 64u;
-    for (uint32_t y = threadIdx.x / 64u; y < 64u; y += 4u) {
-        const uint32_t r = r0 + y, c = c0 + x;
-        uint16_t w[3] = {0, 0, 0};
-        if (r < a.R && c < a.C) {
-            const auto word = reinterpret_cast<const typename El::Word*>(a.from + r * a.ld)[c];
-            if (F == kHeadF32) cut3(El::one(word), w);
-            else w[0] = (uint16_t)word;
+    const uint32_t per = a.wide / 8u;
+    const uint64_t all = (uint64_t)a.R * per;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256u) {
+        const uint32_t r = (uint32_t)(i / per), c = (uint32_t)(i % per) * 8u;
+        uint16_t w[P][8] = {};
+        if (!a.row || a.row[r].target >= 0) {
+            struct __attribute__((packed, aligned(El::kBytes))) Eight { typename El::Word w[8]; } x{};
+            const auto* from = reinterpret_cast<const typename El::Word*>(a.from + r * a.ld) + c;
+            if (c + 8u <= a.C) {
+                x = *reinterpret_cast<const Eight*>(from);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 7u; ++e)
+                    if (c + e < a.C) x.w[e] = from[e];
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 8u; ++e) {
+                uint16_t cut[3] = {(uint16_t)x.w[e], 0, 0};
+                if (F == kHeadF32) cut3(El::one(x.w[e]), cut);
+#pragma unroll
+                for (uint32_t p = 0; p < P; ++p) w[p][e] = cut[p];
+            }
         }
-        if (a.straight && r < a.R && c < a.wide)
-            for (uint32_t p = 0; p < P; ++p)
-                *reinterpret_cast<uint16_t*>(a.straight + p * a.straight_part + r * a.straight_ld + 2ull * c) = w[p];
-        const bool counts = !a.row || (r < a.R && a.row[r].target >= 0);
-        for (uint32_t p = 0; p < P; ++p) tile[p][y][x] = counts ? w[p] : (uint16_t)0;
-    }
-    if (!a.across) return;
-    __syncthreads();
-    for (uint32_t y = threadIdx.x / 64u; y < 64u; y += 4u) {
-        const uint32_t c = c0 + y, r = r0 + x;
-        if (c < a.C && r < a.tall)
-            for (uint32_t p = 0; p < P; ++p)
-                *reinterpret_cast<uint16_t*>(a.across + p * a.across_part + c * a.across_ld + 2ull * r) = tile[p][x][y];
+#pragma unroll
+        for (uint32_t p = 0; p < P; ++p)
+            *reinterpret_cast<u32x4*>(a.to + p * a.part + i * 16u) =
+                u32x4{w[p][0] | (uint32_t)w[p][1] << 16, w[p][2] | (uint32_t)w[p][3] << 16,
+                      w[p][4] | (uint32_t)w[p][5] << 16, w[p][6] | (uint32_t)w[p][7] << 16};
     }
 }
 

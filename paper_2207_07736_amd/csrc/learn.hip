@@ -197,23 +197,24 @@ ScanArgs scan_args(const rlsim_scan& s)
 }
 
 // ---- the output layer's cross entropy ------------------------------------------------
-template <int D, int F, int EPI>
+template <int D, int F, bool AA, bool BA, int EPI>
 void launch_gemm(const rlsim_learner* h, XentGemm a, const XentTile& t)
 {
     a.tiles_m = (a.M + t.m - 1u) / t.m;
     a.tiles_n = ((EPI == kXentDz ? a.rows_k : a.N) + t.n - 1u) / t.n;
     a.share = t.share;
+    a.steps = (a.K + kXentK - 1u) / kXentK;
     const dim3 grid(a.tiles_m * a.tiles_n, t.share);
-    if (t.n == 32u) hipLaunchKernelGGL((k_xent_gemm<D, F, 128, 32, 4, 1, EPI>), grid, dim3(256), 0, h->stream, a);
-    else if (t.m == 128u) hipLaunchKernelGGL((k_xent_gemm<D, F, 128, 128, 2, 2, EPI>), grid, dim3(256), 0, h->stream, a);
-    else hipLaunchKernelGGL((k_xent_gemm<D, F, 256, 256, 2, 4, EPI>), grid, dim3(512), 0, h->stream, a);
+    if (t.n == 32u) hipLaunchKernelGGL((k_xent_gemm<D, F, 128, 32, 4, 1, AA, BA, EPI>), grid, dim3(256), 0, h->stream, a);
+    else if (t.m == 128u) hipLaunchKernelGGL((k_xent_gemm<D, F, 128, 128, 2, 2, AA, BA, EPI>), grid, dim3(256), 0, h->stream, a);
+    else hipLaunchKernelGGL((k_xent_gemm<D, F, 256, 256, 2, 4, AA, BA, EPI>), grid, dim3(512), 0, h->stream, a);
 }
 
 template <int F>
 void launch_lay(const rlsim_learner* h, const XentLay& a)
 {
-    const uint32_t wide = std::max(a.straight ? a.wide : 0u, a.C), tall = std::max(a.across ? a.tall : 0u, a.R);
-    hipLaunchKernelGGL(k_xent_lay<F>, dim3((wide + 63u) / 64u, (tall + 63u) / 64u), dim3(256), 0, h->stream, a);
+    const uint64_t all = (uint64_t)a.R * (a.wide / 8u);
+    hipLaunchKernelGGL(k_xent_lay<F>, dim3((uint32_t)std::min<uint64_t>((all + 255u) / 256u, 1u << 22)), dim3(256), 0, h->stream, a);
 }
 
 template <int F>
@@ -249,7 +250,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
 
     XentGemm z{};                                 // the logits' product
     z.products = P == 1u ? 1u : 6u;
-    z.steps = s.dim_k / kXentK;
+    z.K = s.dim_k;
     z.vocab = x.vocab;
     z.N = x.rows;
     z.rows_k = s.rows_k;
@@ -262,48 +263,24 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         z.B = static_cast<const char*>(x.hidden);
         z.ldb = x.hidden_stride * e;
     } else {
-        XentLay l{};
-        l.from = static_cast<const char*>(x.hidden);
-        l.ld = x.hidden_stride * e;
-        l.R = x.rows;
-        l.C = x.dim;
-        l.straight = w + o.x;
-        l.straight_ld = 2ull * s.dim_k;
-        l.straight_part = l.straight_ld * x.rows;
-        l.wide = s.dim_k;
-        launch_lay<F>(h, l);
-        z.B = l.straight;
-        z.ldb = l.straight_ld;
-        z.part_b = l.straight_part;
+        launch_lay<F>(h, XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, w + o.x,
+                                 2ull * s.dim_k * x.rows, nullptr});
+        z.B = w + o.x;
+        z.ldb = 2ull * s.dim_k;
+        z.part_b = z.ldb * x.rows;
     }
     const bool direct = P == 1u && as_they_are(x.matrix, x.matrix_stride, x.dim);
     z.lda = direct ? x.matrix_stride * e : 2ull * s.dim_k;
     const char* const matrix = static_cast<const char*>(x.matrix);
 
-    // The piece of the vocabulary from v0: its rows for the products, and transposed.
-    auto piece = [&](uint32_t v0, uint32_t count, bool straight, bool across) {
+    // The piece of the vocabulary from v0, as the products read it.
+    auto piece = [&](uint32_t v0, uint32_t count) {
         z.m0 = v0;
         z.M = count;
-        XentLay l{};
-        l.from = matrix + (uint64_t)v0 * x.matrix_stride * e;
-        l.ld = x.matrix_stride * e;
-        l.R = count;
-        l.C = x.dim;
-        if (straight) {
-            l.straight = w + o.w;
-            l.straight_ld = 2ull * s.dim_k;
-            l.straight_part = l.straight_ld * s.piece;
-            l.wide = s.dim_k;
-        }
-        if (across) {
-            l.across = w + o.wt;
-            l.across_ld = 2ull * s.piece;
-            l.across_part = l.across_ld * x.dim;
-            l.tall = (uint32_t)up_to(count, kXentK);
-        }
-        if (straight || across) launch_lay<F>(h, l);
-        z.A = direct ? l.from : w + o.w;
-        z.part_a = direct ? 0u : 2ull * s.dim_k * s.piece;
+        const char* const from = matrix + (uint64_t)v0 * x.matrix_stride * e;
+        z.A = direct ? from : w + o.w;
+        z.part_a = 2ull * s.dim_k * s.piece;
+        if (!direct) launch_lay<F>(h, XentLay{from, x.matrix_stride * e, count, x.dim, s.dim_k, w + o.w, z.part_a, nullptr});
     };
 
     XentJoin j{};
@@ -320,10 +297,10 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         const uint32_t width = direct ? x.vocab : s.piece;
         for (uint32_t v0 = 0u; v0 < x.vocab; v0 += width) {
             const uint32_t count = std::min(width, x.vocab - v0);
-            piece(v0, count, !direct, false);
+            piece(v0, count);
             z.part0 = j.parts;
             const XentTile t = xent_tile(count, x.rows, 0u, false, h->cus);
-            launch_gemm<D, F, kXentLoss>(h, z, t);
+            launch_gemm<D, F, false, false, kXentLoss>(h, z, t);
             j.parts += (count + t.m - 1u) / t.m * (t.m / t.span);
         }
         j.part = part;
@@ -331,69 +308,56 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     hipLaunchKernelGGL(k_xent_join, dim3((x.rows + 15u) / 16u), dim3(256), 0, h->stream, j);
     if (!grad) return;
 
-    XentLay l{};
-    if (x.dmatrix) {
-        l.from = static_cast<const char*>(x.hidden);
-        l.ld = x.hidden_stride * e;
-        l.R = x.rows;
-        l.C = x.dim;
-        l.across = w + o.xt;
-        l.across_ld = 2ull * s.rows_k;
-        l.across_part = l.across_ld * x.dim;
-        l.tall = s.rows_k;
-        l.row = row;
-        launch_lay<F>(h, l);
-    }
+    if (x.dmatrix)
+        launch_lay<F>(h, XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, w + o.xm,
+                                 2ull * s.dim_k * x.rows, row});
     const uint64_t dim4 = up_to(x.dim, 4u);
+    const bool plain = F == kHeadF16 && x.weight && x.dhidden;
     z.dz = w + o.dz;
+    z.dz_plain = plain ? w + o.dz_plain : nullptr;
     z.dz_ld = 2ull * s.piece;
-    z.dz_part = z.dz_ld * x.rows;
-    z.dzt = w + o.dzt;
-    z.dzt_ld = 2ull * s.rows_k;
-    z.dzt_part = z.dzt_ld * s.piece;
+    z.dz_part = z.dz_ld * s.rows_k;
     XentGemm gx{}, gw{};                          // dhidden's and dmatrix's products
     gx.products = gw.products = z.products;
     gx.M = gw.M = x.dim;
     gx.sum_ld = gw.sum_ld = dim4;
     gx.wmax = gw.wmax = wmax;
-    gx.A = w + o.wt;
-    gx.lda = 2ull * s.piece;
-    gx.part_a = gx.lda * x.dim;
-    gx.B = z.dz;
-    gx.ldb = z.dz_ld;
-    gx.part_b = z.dz_part;
+    gx.lda = z.lda;
+    gx.B = plain ? z.dz_plain : z.dz;
+    gx.ldb = gw.ldb = z.dz_ld;
+    gx.part_b = gw.part_b = z.dz_part;
     gx.N = x.rows;
     gx.sum = reinterpret_cast<float*>(w + o.dx);
     gx.sum_share = x.rows * dim4;
-    gw.A = w + o.xt;
-    gw.lda = l.across_ld;
-    gw.part_a = l.across_part;
-    gw.B = z.dzt;
-    gw.ldb = z.dzt_ld;
-    gw.part_b = z.dzt_part;
-    gw.steps = s.rows_k / kXentK;
+    gw.A = w + o.xm;
+    gw.lda = 2ull * s.dim_k;
+    gw.part_a = gw.lda * x.rows;
+    gw.B = z.dz;
+    gw.K = x.rows;
     gw.sum = reinterpret_cast<float*>(w + o.dw);
     const XentTile tx = xent_tile(x.dim, x.rows, (uint64_t)s.piece / kXentK * z.products, true, h->cus);
     for (uint32_t v0 = 0u; v0 < x.vocab; v0 += s.piece) {
         const uint32_t count = std::min(s.piece, x.vocab - v0);
-        piece(v0, count, !direct, x.dhidden != nullptr);
-        launch_gemm<D, F, kXentDz>(h, z, xent_tile(count, x.rows, 0u, false, h->cus));
+        piece(v0, count);
+        launch_gemm<D, F, false, false, kXentDz>(h, z, xent_tile(count, x.rows, 0u, false, h->cus));
         if (x.dhidden) {
-            gx.steps = (uint32_t)up_to(count, kXentK) / kXentK;
+            gx.A = z.A;
+            gx.part_a = z.part_a;
+            gx.K = count;
             gx.add = v0 ? 1u : 0u;
-            launch_gemm<D, F, kXentSum>(h, gx, tx);
+            launch_gemm<D, F, true, false, kXentSum>(h, gx, tx);
         }
         if (x.dmatrix) {
-            const XentTile t = xent_tile(x.dim, count, (uint64_t)gw.steps * gw.products, true, h->cus);
+            const XentTile t = xent_tile(x.dim, count, up_to(x.rows, kXentK) / kXentK * gw.products, true, h->cus);
             gw.N = count;
             char* const out = static_cast<char*>(x.dmatrix) + (uint64_t)v0 * x.dmatrix_stride * e;
             if (t.share == 1u) {
                 gw.out = out;
                 gw.out_ld = x.dmatrix_stride * e;
-                launch_gemm<D, F, kXentOut>(h, gw, t);
+                launch_gemm<D, F, true, true, kXentOut>(h, gw, t);
             } else {
                 gw.sum_share = count * dim4;
-                launch_gemm<D, F, kXentSum>(h, gw, t);
+                launch_gemm<D, F, true, true, kXentSum>(h, gw, t);
                 launch_round<F>(h, XentRound{gw.sum, dim4, gw.sum_share, t.share, count, x.dim, nullptr, wmax, out, x.dmatrix_stride * e});
             }
         }
