@@ -36,8 +36,8 @@ struct XentGemm {
     uint64_t lda, ldb;                            // bytes between rows
     uint64_t part_a, part_b;                      // bytes between the parts of fp32 factors
     uint32_t M, N;
-    uint32_t K;                                   // the summed dimension.  From K to a whole step B is 0, and A is 0
-    uint32_t steps, products;                     // too (along) or its last row again; products of parts
+    uint32_t K;                                   // the summed dimension: from K to a whole step B is 0, and A is
+    uint32_t steps, products;                     // too, or as many rows as K says; products of parts
     uint32_t tiles_m, tiles_n, share;             // share: workgroups to a tile
     uint32_t m0;                                  // logits: first entry of the piece
     uint32_t vocab;
@@ -123,10 +123,12 @@ struct OutScale {
     __device__ __forceinline__ float operator()(float x) const { return counts ? x * by : 0.0f; }
 };
 
-// One operand of a tile: R rows of C (m or n), 32 k of them at a time in LDS.
+// One operand of a tile: R rows of C (m or n), 32 k of them at a time in LDS, which has 64
+// banks of 4 bytes.
 //
-// Along: a row is 64 bytes, 4 chunks of 16; chunk c of row r lies at place c ^ (r / 2) % 4
-// of it, so that 8 lanes that read one chunk of 8 rows meet all banks.
+// Along: a row is 64 bytes, 4 chunks of 16; chunk c of row r lies at place c ^ (r / 4) % 4
+// of it, so that 16 lanes that read one chunk of 16 rows meet all banks (by (r / 2) % 4, which
+// suits 32 banks, half of the reads' cycles were conflicts).
 // Across: row k is 2 R bytes; its blocks of 32 bytes lie at place b ^ turn(k), so that the 32
 // bytes of 4 rows k that 16 lanes turn, and those of the next 16 lanes, meet all banks.
 template <bool ACROSS, uint32_t R, uint32_t NW>
@@ -137,9 +139,12 @@ struct Operand {
     static_assert(kParts % NW == 0u || NW % kParts == 0u);
     static constexpr uint32_t kRowChunks = R / 8u;               // across: chunks of 16 bytes of a row k
     uint32_t at[kLoads];                                         // bytes from the tile's first
-    uint32_t k[ACROSS ? kLoads : 1];
 
     __device__ __forceinline__ static uint32_t turn(uint32_t k) { return ((k & 3u) ^ (k & 1u) << 2) & (R / 16u - 1u); }
+    __device__ __forceinline__ static uint32_t place(uint32_t i, uint32_t wave, uint32_t lane)    // of 16 bytes in LDS
+    {
+        return (i * NW + wave) % kParts * 64u + lane;
+    }
 
     // base: the tile's first row of C; rows: how many there are in all.  What lies behind
     // the last one is taken from the last ones again.
@@ -147,14 +152,13 @@ struct Operand {
     {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i) {
-            const uint32_t place = (i * NW + wave) % kParts * 64u + lane;        // of 16 bytes in LDS
+            const uint32_t p = place(i, wave, lane);
             if (ACROSS) {
-                k[i] = place / kRowChunks;
-                const uint32_t c = place % kRowChunks ^ 2u * turn(k[i]);
+                const uint32_t k = p / kRowChunks, c = p % kRowChunks ^ 2u * turn(k);
                 const uint32_t last = (rows + 7u) / 8u - 1u;                     // chunk of a whole row
-                at[i] = min(base / 8u + c, last) * 16u;
+                at[i] = min(base / 8u + c, last) * 16u + k * ld;
             } else {
-                const uint32_t r = place / 4u, c = place % 4u ^ r / 2u % 4u;
+                const uint32_t r = p / 4u, c = p % 4u ^ r / 4u % 4u;
                 at[i] = (min(base + r, rows - 1u) - min(base, rows - 1u)) * ld + c * 16u;
             }
         }
@@ -163,12 +167,18 @@ struct Operand {
     {
         return ACROSS ? 0u : min(base, rows - 1u) * ld;
     }
-    // 32 k from p on into LDS; across: of the first `left` of them, the last one again and again
-    __device__ __forceinline__ void fetch(const char* p, char* to, uint32_t ld, uint32_t left, uint32_t wave) const
+    // 32 k from p on into LDS.  CUT: across, of the first `left` of them, the last one again
+    // and again.
+    template <bool CUT>
+    __device__ __forceinline__ void fetch(const char* p, char* to, uint32_t ld, uint32_t left, uint32_t wave, uint32_t lane) const
     {
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; ++i) {
-            const uint32_t off = ACROSS ? at[i] + min(k[i], left - 1u) * ld : at[i];
+            uint32_t off = at[i];
+            if (ACROSS && CUT) {
+                const uint32_t k = place(i, wave, lane) / kRowChunks;
+                off -= (k - min(k, left - 1u)) * ld;
+            }
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + off),
                                              (__attribute__((address_space(3))) void*)(to + (i * NW + wave) % kParts * 1024u), 16, 0, 0);
         }
@@ -188,7 +198,7 @@ struct Fragments {
                 const uint32_t block = (base + i * 32u) / 16u + lane / 16u % 2u;
                 at[i] = k * (R * 2u) + (block ^ Operand<true, R, 1u>::turn(k)) * 32u + p % 4u * 8u;
             } else {
-                at[i] = (base + i * 32u + lane % 32u) * 64u + (lane / 32u ^ lane / 2u % 4u) * 16u;
+                at[i] = (base + i * 32u + lane % 32u) * 64u + (lane / 32u ^ lane / 4u % 4u) * 16u;
             }
         }
     }
@@ -218,6 +228,19 @@ __device__ __forceinline__ void loads_left()
     __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
 }
 __device__ __forceinline__ void reads_done() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+// The order of a half step's instructions: reads of LDS and loads between the matrix
+// instructions, whose 32 cycles hide their issue.
+template <int MMA, int READS, int LOADS>
+__device__ __forceinline__ void mix()
+{
+    constexpr int kPer = MMA > 2 ? (READS + MMA - 3) / (MMA - 2) : READS;
+#pragma unroll
+    for (int i = 0; i < MMA; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i * kPer < READS) __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);
+        if (i < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+    }
+}
 // The workgroup's waves meet.  No access to memory moves over it; what is under way stays so.
 __device__ __forceinline__ void meet()
 {
@@ -279,19 +302,22 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         pb = B0 + j * a.part_b + step * step_b;
     };
     locate();
-    auto fetch = [&](char* to) {
-        const uint32_t left = a.K - step * 32u;
-        op_a.fetch(pa, to, lda, left, wave);
-        op_b.fetch(pb, to + OpA::kBytes, ldb, 32u, wave);
+    // CUT: K may end within the step.
+    auto fetch = [&](auto cut, char* to) {
+        constexpr bool CUT = decltype(cut)::value;
+        const uint32_t left = CUT ? a.K - step * 32u : 32u;
+        op_a.template fetch<CUT>(pa, to, lda, left, wave, lane);
+        op_b.template fetch<false>(pb, to + OpA::kBytes, ldb, 32u, wave, lane);
         pa += step_a;
         pb += step_b;
-        if (++step == a.steps) {
+        ++step;
+        if (F == kHeadF32 && step == a.steps) {
             step = 0u;
             ++product;
             if (product < a.products) locate();
         }
     };
-    constexpr int kEach = OpA::kLoads + OpB::kLoads;
+    constexpr int kEach = OpA::kLoads + OpB::kLoads, kReads = FM * (AA ? 2u : 1u) + FN * (BA ? 2u : 1u);
 
     f32x16 c[FM][FN];
 #pragma unroll
@@ -309,15 +335,16 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     // step just read may be overwritten and the next one, loaded three steps ago, read.
     auto one_step = [&](auto steady, uint32_t t, char* now, char* next, char* ahead) {
         constexpr bool kSteady = decltype(steady)::value;        // three more steps are to come
-        if (kSteady || t + 3u < last) fetch(ahead);
         reads_done();                             // of the first half
+        if (kSteady) fetch(std::false_type{}, ahead);
+        else if (t + 3u < last) fetch(std::true_type{}, ahead);
         x.template read<1>(now);
         y.template read<1>(now + OpA::kBytes);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
             for (uint32_t j = 0; j < FN; ++j) c[i][j] = Matrix<D>::mma(x.v[0][i], y.v[0][j], c[i][j]);
+        mix<FM * FN, kReads, kSteady ? kEach : 0>();
         __builtin_amdgcn_sched_barrier(0);
         if (kSteady || t + 3u < last) loads_left<2 * kEach>();
         else if (t + 2u < last) loads_left<kEach>();
@@ -328,21 +355,21 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
             x.template read<0>(next);
             y.template read<0>(next + OpA::kBytes);
         }
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
             for (uint32_t j = 0; j < FN; ++j) c[i][j] = Matrix<D>::mma(x.v[1][i], y.v[1][j], c[i][j]);
+        mix<FM * FN, kReads, 0>();
         __builtin_amdgcn_sched_barrier(0);
     };
     if (first < last) {
-        fetch(sh0);
+        fetch(std::true_type{}, sh0);
         if (first + 2u < last) {
-            fetch(sh1);
-            fetch(sh2);
+            fetch(std::true_type{}, sh1);
+            fetch(std::true_type{}, sh2);
             loads_left<2 * kEach>();
         } else {
-            if (first + 1u < last) fetch(sh1);
+            if (first + 1u < last) fetch(std::true_type{}, sh1);
             loads_left<0>();
         }
         meet();
@@ -558,8 +585,8 @@ __global__ __launch_bounds__(256) void k_xent_join(XentJoin a)
 struct XentLay {
     const char* from;                             // [R][C]
     uint64_t ld;                                  // bytes
-    uint32_t R, C, wide;                          // wide: elements of a row of the copy, a multiple of 8
-    char* to;                                     // [parts][R][wide]
+    uint32_t R, C, wide, tall;                    // wide: elements of a row of the copy, a multiple of 8;
+    char* to;                                     // [parts][tall][wide], 0 behind R and C
     uint64_t part;                                // bytes
     const XentRow* row;                           // or null
 };
@@ -569,11 +596,11 @@ __global__ __launch_bounds__(256) void k_xent_lay(XentLay a)
     using El = Elem<F>;
     constexpr uint32_t P = F == kHeadF32 ? 3u : 1u;
     const uint32_t per = a.wide / 8u;
-    const uint64_t all = (uint64_t)a.R * per;
+    const uint64_t all = (uint64_t)a.tall * per;
     for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256u) {
         const uint32_t r = (uint32_t)(i / per), c = (uint32_t)(i % per) * 8u;
         uint16_t w[P][8] = {};
-        if (!a.row || a.row[r].target >= 0) {
+        if (r < a.R && (!a.row || a.row[r].target >= 0)) {
             struct __attribute__((packed, aligned(El::kBytes))) Eight { typename El::Word w[8]; } x{};
             const auto* from = reinterpret_cast<const typename El::Word*>(a.from + r * a.ld) + c;
             if (c + 8u <= a.C) {

@@ -213,7 +213,7 @@ void launch_gemm(const rlsim_learner* h, XentGemm a, const XentTile& t)
 template <int F>
 void launch_lay(const rlsim_learner* h, const XentLay& a)
 {
-    const uint64_t all = (uint64_t)a.R * (a.wide / 8u);
+    const uint64_t all = (uint64_t)a.tall * (a.wide / 8u);
     hipLaunchKernelGGL(k_xent_lay<F>, dim3((uint32_t)std::min<uint64_t>((all + 255u) / 256u, 1u << 22)), dim3(256), 0, h->stream, a);
 }
 
@@ -263,7 +263,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         z.B = static_cast<const char*>(x.hidden);
         z.ldb = x.hidden_stride * e;
     } else {
-        launch_lay<F>(h, XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, w + o.x,
+        launch_lay<F>(h, XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, x.rows, w + o.x,
                                  2ull * s.dim_k * x.rows, nullptr});
         z.B = w + o.x;
         z.ldb = 2ull * s.dim_k;
@@ -280,7 +280,8 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         const char* const from = matrix + (uint64_t)v0 * x.matrix_stride * e;
         z.A = direct ? from : w + o.w;
         z.part_a = 2ull * s.dim_k * s.piece;
-        if (!direct) launch_lay<F>(h, XentLay{from, x.matrix_stride * e, count, x.dim, s.dim_k, w + o.w, z.part_a, nullptr});
+        if (!direct) launch_lay<F>(h, XentLay{from, x.matrix_stride * e, count, x.dim, s.dim_k, (uint32_t)up_to(count, kXentK), w + o.w,
+                                              z.part_a, nullptr});
     };
 
     XentJoin j{};
@@ -309,8 +310,8 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     if (!grad) return;
 
     if (x.dmatrix)
-        launch_lay<F>(h, XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, w + o.xm,
-                                 2ull * s.dim_k * x.rows, row});
+        launch_lay<F>(h, XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, s.rows_k, w + o.xm,
+                                 2ull * s.dim_k * s.rows_k, row});
     const uint64_t dim4 = up_to(x.dim, 4u);
     const bool plain = F == kHeadF16 && x.weight && x.dhidden;
     z.dz = w + o.dz;
@@ -331,9 +332,9 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     gx.sum_share = x.rows * dim4;
     gw.A = w + o.xm;
     gw.lda = 2ull * s.dim_k;
-    gw.part_a = gw.lda * x.rows;
+    gw.part_a = gw.lda * s.rows_k;
     gw.B = z.dz;
-    gw.K = x.rows;
+    gw.K = s.rows_k;
     gw.sum = reinterpret_cast<float*>(w + o.dw);
     const XentTile tx = xent_tile(x.dim, x.rows, (uint64_t)s.piece / kXentK * z.products, true, h->cus);
     for (uint32_t v0 = 0u; v0 < x.vocab; v0 += s.piece) {
@@ -343,12 +344,12 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         if (x.dhidden) {
             gx.A = z.A;
             gx.part_a = z.part_a;
-            gx.K = count;
+            gx.K = direct ? count : (uint32_t)up_to(count, kXentK);
             gx.add = v0 ? 1u : 0u;
             launch_gemm<D, F, true, false, kXentSum>(h, gx, tx);
         }
         if (x.dmatrix) {
-            const XentTile t = xent_tile(x.dim, count, up_to(x.rows, kXentK) / kXentK * gw.products, true, h->cus);
+            const XentTile t = xent_tile(x.dim, count, s.rows_k / kXentK * gw.products, true, h->cus);
             gw.N = count;
             char* const out = static_cast<char*>(x.dmatrix) + (uint64_t)v0 * x.dmatrix_stride * e;
             if (t.share == 1u) {

@@ -91,7 +91,7 @@ inline XentWork xent_work(const XentShape& s)
     o.stats = take(8ull * s.rows_k);
     o.part = take(8ull * s.rows_k * (up_to(s.vocab, 256u) / 32u));
     o.x = take(P2 * s.rows * s.dim_k);
-    o.xm = take(P2 * s.rows * s.dim_k);
+    o.xm = take(P2 * s.rows_k * s.dim_k);
     o.w = take(P2 * s.piece * s.dim_k);
     o.dz = take(P2 * s.rows_k * s.piece);
     o.dz_plain = take(s.parts == 1u ? P2 * s.rows_k * s.piece : 0u);
