@@ -43,35 +43,37 @@ __device__ __forceinline__ double group_sum(double x, double* sh)
     return s;
 }
 
-// f(4 floats, index) for whole fours of [from, to), g(float, index) for the rest.
-template <int D, class F, class G>
-__device__ __forceinline__ void each_four(const char* p, uint64_t from, uint64_t to, uint32_t nt, F f, G g)
+// f(vector of 16 bytes, index) for the whole ones of [from, to), g(float, index) for the rest;
+// NT consecutive threads share them.
+template <int D, uint32_t NT, class F, class G>
+__device__ __forceinline__ void each_vector(const char* p, uint64_t from, uint64_t to, F f, G g)
 {
     using El = Elem<D>;
-    constexpr uint32_t U = 8u;
+    constexpr uint32_t U = NT == 64u ? 2u : 8u;
+    const uint32_t thread = threadIdx.x % NT;
     const uint64_t vectors = (to - from) / El::kPerVec;
     const auto* v = reinterpret_cast<const typename El::Run*>(p + from * El::kBytes);
-    for (uint64_t i0 = threadIdx.x; i0 < vectors; i0 += (uint64_t)nt * U) {
+    for (uint64_t i0 = thread; i0 < vectors; i0 += NT * U) {
         typename El::Run y[U];
 #pragma unroll
         for (uint32_t j = 0; j < U; ++j)
-            if (i0 + j * nt < vectors) y[j] = v[i0 + j * nt];
+            if (i0 + j * NT < vectors) y[j] = v[i0 + j * NT];
 #pragma unroll
         for (uint32_t j = 0; j < U; ++j)
-            if (i0 + j * nt < vectors) {
+            if (i0 + j * NT < vectors) {
                 const Vec16 w{{y[j].w[0], y[j].w[1], y[j].w[2], y[j].w[3]}};
-                f(w, from + (i0 + j * nt) * El::kPerVec);
+                f(w, from + (i0 + j * NT) * El::kPerVec);
             }
     }
-    for (uint64_t i = from + vectors * El::kPerVec + threadIdx.x; i < to; i += nt)
+    for (uint64_t i = from + vectors * El::kPerVec + thread; i < to; i += NT)
         g(El::one(reinterpret_cast<const typename El::Word*>(p)[i]), i);
 }
 
-template <int D>
-__device__ __forceinline__ double clip_squares(const char* p, uint64_t from, uint64_t to, uint32_t nt)
+template <int D, uint32_t NT>
+__device__ __forceinline__ double clip_squares(const char* p, uint64_t from, uint64_t to)
 {
     double s = 0.0;
-    each_four<D>(p, from, to, nt,
+    each_vector<D, NT>(p, from, to,
                  [&](const Vec16& v, uint64_t) {
 #pragma unroll
                      for (uint32_t e = 0; e < Elem<D>::kPerVec; ++e) {
@@ -83,11 +85,11 @@ __device__ __forceinline__ double clip_squares(const char* p, uint64_t from, uin
     return s;
 }
 
-template <int D, int O>
-__device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t from, uint64_t to, float scale, uint32_t nt)
+template <int D, int O, uint32_t NT>
+__device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t from, uint64_t to, float scale)
 {
     using To = Elem<O>;
-    each_four<D>(p, from, to, nt,
+    each_vector<D, NT>(p, from, to,
                  [&](const Vec16& v, uint64_t i) {
                      constexpr uint32_t E = Elem<D>::kPerVec;
                      struct __attribute__((packed, aligned(To::kBytes))) Run { typename To::Word w[E]; } r;
@@ -110,16 +112,18 @@ __device__ __forceinline__ uint32_t clip_tensor(const ClipArgs& a, uint32_t bloc
     return lo;
 }
 
-__device__ __forceinline__ double squares_of(const ClipArgs& a, uint32_t block, uint32_t nt)
+template <uint32_t NT>
+__device__ __forceinline__ double squares_of(const ClipArgs& a, uint32_t block)
 {
     const uint32_t k = clip_tensor(a, block);
     const uint64_t from = (uint64_t)(block - a.first[k]) * a.chunk, to = min(from + a.chunk, a.t[k].elements);
-    return a.dtype[k] == kHeadF32    ? clip_squares<kHeadF32>(a.t[k].data, from, to, nt)
-           : a.dtype[k] == kHeadBF16 ? clip_squares<kHeadBF16>(a.t[k].data, from, to, nt)
-                                     : clip_squares<kHeadF16>(a.t[k].data, from, to, nt);
+    return a.dtype[k] == kHeadF32    ? clip_squares<kHeadF32, NT>(a.t[k].data, from, to)
+           : a.dtype[k] == kHeadBF16 ? clip_squares<kHeadBF16, NT>(a.t[k].data, from, to)
+                                     : clip_squares<kHeadF16, NT>(a.t[k].data, from, to);
 }
 
-__device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, float scale, uint32_t nt)
+template <uint32_t NT>
+__device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, float scale)
 {
     const uint32_t k = clip_tensor(a, block);
     const ClipTensor& t = a.t[k];
@@ -127,9 +131,9 @@ __device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, f
     const uint64_t from = (uint64_t)(block - a.first[k]) * a.chunk, to = min(from + a.chunk, t.elements);
     auto to_type = [&](auto in) {
         constexpr int D = decltype(in)::value;
-        if (a.out_dtype[k] == kHeadF32) clip_scale<D, kHeadF32>(t.data, t.out, from, to, scale, nt);
-        else if (a.out_dtype[k] == kHeadBF16) clip_scale<D, kHeadBF16>(t.data, t.out, from, to, scale, nt);
-        else clip_scale<D, kHeadF16>(t.data, t.out, from, to, scale, nt);
+        if (a.out_dtype[k] == kHeadF32) clip_scale<D, kHeadF32, NT>(t.data, t.out, from, to, scale);
+        else if (a.out_dtype[k] == kHeadBF16) clip_scale<D, kHeadBF16, NT>(t.data, t.out, from, to, scale);
+        else clip_scale<D, kHeadF16, NT>(t.data, t.out, from, to, scale);
     };
     if (a.dtype[k] == kHeadF32) to_type(std::integral_constant<int, kHeadF32>{});
     else if (a.dtype[k] == kHeadBF16) to_type(std::integral_constant<int, kHeadBF16>{});
@@ -144,7 +148,7 @@ __device__ __forceinline__ float clip_factor(double norm, double max_norm)
 __global__ __launch_bounds__(256) void k_clip_squares(ClipArgs a)
 {
     __shared__ double sh[4];
-    const double s = group_sum<256>(squares_of(a, blockIdx.x, 256u), sh);
+    const double s = group_sum<256>(squares_of<256u>(a, blockIdx.x), sh);
     if (threadIdx.x == 0u) a.sums[a.base + blockIdx.x] = s;
 }
 
@@ -155,20 +159,20 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a)
     for (uint32_t i = threadIdx.x; i < a.blocks; i += 256u) s += a.sums[i];
     const double norm = sqrt(group_sum<256>(s, sh));
     if (a.base + blockIdx.x == 0u && threadIdx.x == 0u) *a.norm = (float)norm;
-    if (a.count) scale_block(a, blockIdx.x, clip_factor(norm, a.max_norm), 256u);
+    if (a.count) scale_block<256u>(a, a.first[a.count] - 1u - blockIdx.x, clip_factor(norm, a.max_norm));
 }
 
-// Few elements: one workgroup, one launch.
+// Few elements: one workgroup, one launch.  Its waves take blocks in turn.
 __global__ __launch_bounds__(1024) void k_clip_small(ClipArgs a)
 {
     __shared__ double sh[16];
     double s = 0.0;
-    const uint32_t blocks = a.first[a.count];
-    for (uint32_t b = 0; b < blocks; ++b) s += squares_of(a, b, 1024u);
+    const uint32_t blocks = a.first[a.count], wave = uniform(threadIdx.x / 64u);
+    for (uint32_t b = wave; b < blocks; b += 16u) s += squares_of<64u>(a, b);
     const double norm = sqrt(group_sum<1024>(s, sh));
     if (threadIdx.x == 0u) *a.norm = (float)norm;
     const float scale = clip_factor(norm, a.max_norm);
-    for (uint32_t b = 0; b < blocks; ++b) scale_block(a, b, scale, 1024u);
+    for (uint32_t b = wave; b < blocks; b += 16u) scale_block<64u>(a, b, scale);
 }
 
 }  // namespace rlsim_dev

@@ -3,12 +3,14 @@
 //   a_t = sigmoid(gate_t), h_t = a_t h'_{t-1} + (1 - a_t) x_t, h'_t = done_t ? 0 : h_t
 //
 // A step is an affine map of the state, so a stretch of steps is one too (two numbers a
-// channel).  Where there are channels enough, a thread goes through all steps of its few
+// channel).  Where there are channels enough, a thread goes through all steps of its two
 // channels; where there are not, time is cut into segments: one launch finds each
-// segment's map, the next joins the maps in front of a segment to its first state and goes
-// through its rows.  Backward is the same from the end.  No result depends on how the
+// segment's map, the next joins them to the state each segment starts from, and the third
+// goes through the rows.  Backward is the same from the end.  No result depends on how the
 // workgroups are placed or timed.
 #pragma once
+
+#include <type_traits>
 
 #include "head_common.hip.h"
 #include "learn_dispatch.h"
@@ -27,8 +29,9 @@ struct ScanArgs {
     float* marks;
     float* last;                 // forward: last; backward: dstate; or null
     float* map_a;                // [segments][n channels]: a segment's map, product and
-    float* map_b;                // sum
+    float* map_b;                // sum; once joined, the state that the segment starts from
     uint32_t T, n, channels, groups, segments, seg_len;
+    uint32_t backward;
 };
 
 // sigmoid(g) and 1 - sigmoid(g), each to a few units of the last place: the smaller of the
@@ -96,37 +99,59 @@ struct Lane {
     }
     __device__ __forceinline__ void put(float* p, const float (&f)[V]) const
     {
+        Channels<kHeadF32, V>::store(reinterpret_cast<char*>(p + flat), f, from);
+    }
+    __device__ __forceinline__ void get(const float* p, float (&f)[V]) const
+    {
+        Channels<kHeadF32, V> r;
+        r.load(reinterpret_cast<const char*>(p + flat));
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if ((uint32_t)i >= from) p[flat + i] = f[i];
+        for (int i = 0; i < V; ++i) f[i] = r.get(i);
     }
 };
 
-// Steps [t0, t1) forward for one thread, kScanMark at a time: the loads of a run are made
-// before its first step.  ROWS: y and the marks are written; else only the map is kept.
-template <int D, int V, bool ROWS>
+// The lane's offset in an array's row of one step: 32 bits, so that a step's address is one
+// uniform number and this, unless sequences lie further apart (WIDE).
+template <bool WIDE, int D, int V>
+__device__ __forceinline__ auto lane_offset(const Lane<V>& l, uint64_t seq_bytes)
+{
+    using Off = std::conditional_t<WIDE, uint64_t, uint32_t>;
+    return (Off)(l.seq * (Off)seq_bytes + (Off)l.c * Elem<D>::kBytes);
+}
+
+// The bits of U steps' done flags, from step t on (t1: the end).
+template <uint32_t U>
+__device__ __forceinline__ uint32_t ends_of(const ScanArgs& a, uint32_t t, uint32_t t1, uint32_t seq)
+{
+    uint32_t ends = 0u;
+    if (a.done) {
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint8_t* row = a.done + (uint64_t)min(t + u, t1 - 1u) * a.n;
+            ends |= (row[seq] ? 1u : 0u) << u;
+        }
+    }
+    return ends;
+}
+
+// Steps [t0, t1) forward for one thread, U at a time: the loads of a run are made before
+// its first step.  ROWS: y and the marks are written; else only the map is kept.
+template <int D, int V, uint32_t U, bool WIDE, bool ROWS>
 __device__ __forceinline__ void scan_forward(const ScanArgs& a, const Lane<V>& l, uint32_t t0, uint32_t t1, float (&h)[V],
                                              float (&prod)[V])
 {
-    constexpr uint32_t U = kScanMark;
-    const char* px = a.x + l.seq * a.x_seq + (uint64_t)l.c * Elem<D>::kBytes;
-    const char* pg = a.gate + l.seq * a.gate_seq + (uint64_t)l.c * Elem<D>::kBytes;
-    char* py = a.y + l.seq * a.y_seq + (uint64_t)l.c * Elem<D>::kBytes;
+    const auto ox = lane_offset<WIDE, D, V>(l, a.x_seq), og = lane_offset<WIDE, D, V>(l, a.gate_seq),
+               oy = lane_offset<WIDE, D, V>(l, a.y_seq);
     for (uint32_t t = t0; t < t1; t += U) {
         Channels<D, V> x[U], g[U];
-        uint32_t ends = 0u;
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
             const uint64_t at = min(t + u, t1 - 1u);
-            x[u].load(px + at * a.x_step);
-            g[u].load(pg + at * a.gate_step);
+            x[u].load(a.x + at * a.x_step + ox);
+            g[u].load(a.gate + at * a.gate_step + og);
         }
-        if (a.done) {
-#pragma unroll
-            for (uint32_t u = 0; u < U; ++u)
-                ends |= (a.done[(uint64_t)min(t + u, t1 - 1u) * a.n + l.seq] ? 1u : 0u) << u;
-        }
-        if (ROWS && a.marks) l.put(a.marks + (uint64_t)(t / U) * a.n * a.channels, h);
+        const uint32_t ends = ends_of<U>(a, t, t1, l.seq);
+        if (ROWS && a.marks && (U == kScanMark || t % kScanMark == 0u)) l.put(a.marks + (uint64_t)(t / kScanMark) * a.n * a.channels, h);
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
             if (t + u < t1) {
@@ -140,13 +165,13 @@ __device__ __forceinline__ void scan_forward(const ScanArgs& a, const Lane<V>& l
                     if (end) h[i] = 0.0f;
                     if (!ROWS) prod[i] = end ? 0.0f : prod[i] * k.a;
                 }
-                if (ROWS) Channels<D, V>::store(py + (uint64_t)(t + u) * a.y_step, out, l.from);
+                if (ROWS) Channels<D, V>::store(a.y + (uint64_t)(t + u) * a.y_step + oy, out, l.from);
             }
         }
     }
 }
 
-template <int D, int V>
+template <int D, int V, bool WIDE>
 __global__ __launch_bounds__(256) void k_scan_maps(ScanArgs a)
 {
     const uint64_t all = (uint64_t)a.n * a.groups, stride = (uint64_t)gridDim.x * 256u;
@@ -156,35 +181,77 @@ __global__ __launch_bounds__(256) void k_scan_maps(ScanArgs a)
         float h[V], prod[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) { h[i] = 0.0f; prod[i] = 1.0f; }
-        scan_forward<D, V, false>(a, l, t0, t1, h, prod);
+        scan_forward<D, V, kScanMark, WIDE, false>(a, l, t0, t1, h, prod);
         const uint64_t at = (uint64_t)s * a.n * a.channels;
         l.put(a.map_a + at, prod);
         l.put(a.map_b + at, h);
     }
 }
 
-template <int D, int V>
+// Segments' maps to the states they start from.  A workgroup has 16 channels; each of its 16
+// rows of threads joins a run of segments, the runs meet in LDS, and each row goes through
+// its run again from there.  Backward, segment 0 is the last.
+__global__ __launch_bounds__(256) void k_scan_join(ScanArgs a)
+{
+    __shared__ float sa[16][16], sb[16][16];
+    const uint64_t C = (uint64_t)a.n * a.channels;
+    const uint32_t x = threadIdx.x % 16u, y = threadIdx.x / 16u;
+    const uint64_t c = (uint64_t)blockIdx.x * 16u + x;
+    const uint32_t run = (a.segments + 15u) / 16u, j0 = min(y * run, a.segments), j1 = min(j0 + run, a.segments);
+    auto at = [&](uint32_t j) { return (uint64_t)(a.backward ? a.segments - 1u - j : j) * C + c; };
+    float A = 1.0f, B = 0.0f;
+    if (c < C) {
+#pragma unroll 4
+        for (uint32_t j = j0; j < j1; ++j) {
+            const float p = a.map_a[at(j)], q = a.map_b[at(j)];
+            B = __builtin_fmaf(p, B, q);
+            A *= p;
+        }
+    }
+    sa[y][x] = A;
+    sb[y][x] = B;
+    __syncthreads();
+    if (c >= C) return;
+    float h = a.state ? a.state[c] : 0.0f;
+    for (uint32_t k = 0; k < y; ++k) h = __builtin_fmaf(sa[k][x], h, sb[k][x]);
+#pragma unroll 4
+    for (uint32_t j = j0; j < j1; ++j) {
+        const float p = a.map_a[at(j)], q = a.map_b[at(j)];
+        a.map_b[at(j)] = h;
+        h = __builtin_fmaf(p, h, q);
+    }
+}
+
+// What a thread's segment starts from.
+template <int V>
+__device__ __forceinline__ void scan_start(const ScanArgs& a, const Lane<V>& l, uint32_t s, float (&h)[V])
+{
+    if (a.segments > 1u) {
+        l.get(a.map_b + (uint64_t)s * a.n * a.channels, h);
+    } else if (a.state) {
+        l.get(a.state, h);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = 0.0f;
+    }
+}
+
+template <int D, int V, uint32_t U, bool WIDE>
 __global__ __launch_bounds__(256) void k_scan_rows(ScanArgs a)
 {
     const uint64_t all = (uint64_t)a.n * a.groups, stride = (uint64_t)gridDim.x * 256u;
     const uint32_t s = blockIdx.y, t0 = s * a.seg_len, t1 = min(t0 + a.seg_len, a.T);
-    const uint64_t C = (uint64_t)a.n * a.channels;
     for (uint64_t q = (uint64_t)blockIdx.x * 256u + threadIdx.x; q < all; q += stride) {
         const Lane<V> l(a, q);
         float h[V], unused[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) { h[i] = a.state ? a.state[l.flat + i] : 0.0f; unused[i] = 0.0f; }
-#pragma unroll 8
-        for (uint32_t j = 0; j < s; ++j)
-#pragma unroll
-            for (int i = 0; i < V; ++i) h[i] = __builtin_fmaf(a.map_a[j * C + l.flat + i], h[i], a.map_b[j * C + l.flat + i]);
-        scan_forward<D, V, true>(a, l, t0, t1, h, unused);
+        scan_start(a, l, s, h);
+        scan_forward<D, V, U, WIDE, true>(a, l, t0, t1, h, unused);
         if (a.last && t1 == a.T) l.put(a.last, h);
     }
 }
 
 // Backward.  `R` is a_{t+1} e_{t+1} when step t is reached from the end.
-template <int D, int V>
+template <int D, int V, bool WIDE>
 __global__ __launch_bounds__(256) void k_scan_back_maps(ScanArgs a)
 {
     constexpr uint32_t U = kScanMark;
@@ -193,22 +260,20 @@ __global__ __launch_bounds__(256) void k_scan_back_maps(ScanArgs a)
     const uint64_t C = (uint64_t)a.n * a.channels;
     for (uint64_t q = (uint64_t)blockIdx.x * 256u + threadIdx.x; q < all; q += stride) {
         const Lane<V> l(a, q);
-        const char* pg = a.gate + l.seq * a.gate_seq + (uint64_t)l.c * Elem<D>::kBytes;
-        const char* pd = a.dy + l.seq * a.dy_seq + (uint64_t)l.c * Elem<D>::kBytes;
+        const auto og = lane_offset<WIDE, D, V>(l, a.gate_seq), od = lane_offset<WIDE, D, V>(l, a.dy_seq);
         float P[V], Q[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) { P[i] = 1.0f; Q[i] = 0.0f; }
         for (uint32_t left = t1 - t0; left != 0u;) {
             const uint32_t run = left % U ? left % U : U, t = t0 + left - run;
             Channels<D, V> g[U], d[U];
-            uint32_t ends = 0u;
 #pragma unroll
             for (uint32_t u = 0; u < U; ++u) {
                 const uint64_t at = t + min(u, run - 1u);
-                g[u].load(pg + at * a.gate_step);
-                if (a.dy) d[u].load(pd + at * a.dy_step);
-                if (a.done) ends |= (a.done[at * a.n + l.seq] ? 1u : 0u) << u;
+                g[u].load(a.gate + at * a.gate_step + og);
+                if (a.dy) d[u].load(a.dy + at * a.dy_step + od);
             }
+            const uint32_t ends = ends_of<U>(a, t, t + run, l.seq);
 #pragma unroll
             for (uint32_t k = 0; k < U; ++k) {
                 const uint32_t u = U - 1u - k;
@@ -230,8 +295,10 @@ __global__ __launch_bounds__(256) void k_scan_back_maps(ScanArgs a)
     }
 }
 
-template <int D, int V>
-__global__ __launch_bounds__(256) void k_scan_back_rows(ScanArgs a)
+// A run of steps behind a mark goes forward first: the states between, of which only
+// h'_{t-1} - x_t is kept, with both gates, so that these are found once.
+template <int D, int V, bool WIDE>
+__global__ __launch_bounds__(256, D == kHeadF32 ? 2 : 3) void k_scan_back_rows(ScanArgs a)
 {
     constexpr uint32_t U = kScanMark;
     const uint64_t all = (uint64_t)a.n * a.groups, stride = (uint64_t)gridDim.x * 256u;
@@ -239,42 +306,34 @@ __global__ __launch_bounds__(256) void k_scan_back_rows(ScanArgs a)
     const uint64_t C = (uint64_t)a.n * a.channels;
     for (uint64_t q = (uint64_t)blockIdx.x * 256u + threadIdx.x; q < all; q += stride) {
         const Lane<V> l(a, q);
-        const char* px = a.x + l.seq * a.x_seq + (uint64_t)l.c * Elem<D>::kBytes;
-        const char* pg = a.gate + l.seq * a.gate_seq + (uint64_t)l.c * Elem<D>::kBytes;
-        const char* pd = a.dy + l.seq * a.dy_seq + (uint64_t)l.c * Elem<D>::kBytes;
-        char* qx = a.y + l.seq * a.y_seq + (uint64_t)l.c * Elem<D>::kBytes;
-        char* qg = a.dgate + l.seq * a.dgate_seq + (uint64_t)l.c * Elem<D>::kBytes;
+        const auto ox = lane_offset<WIDE, D, V>(l, a.x_seq), og = lane_offset<WIDE, D, V>(l, a.gate_seq),
+                   od = lane_offset<WIDE, D, V>(l, a.dy_seq), odx = lane_offset<WIDE, D, V>(l, a.y_seq),
+                   odg = lane_offset<WIDE, D, V>(l, a.dgate_seq);
         float R[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) R[i] = a.state ? a.state[l.flat + i] : 0.0f;
-#pragma unroll 8
-        for (uint32_t j = a.segments - 1u; j > s; --j)
-#pragma unroll
-            for (int i = 0; i < V; ++i) R[i] = __builtin_fmaf(a.map_a[j * C + l.flat + i], R[i], a.map_b[j * C + l.flat + i]);
+        scan_start(a, l, s, R);
         // segments start at marks, so a run is what lies behind one mark
         for (uint32_t left = t1 - t0; left != 0u;) {
             const uint32_t run = left % U ? left % U : U, t = t0 + left - run;
             Channels<D, V> x[U], g[U], d[U];
-            uint32_t ends = 0u;
-            float h[U][V], m[V];
+            float m[V], diff[U][V];
+            Gate w[U][V];
 #pragma unroll
             for (uint32_t u = 0; u < U; ++u) {
                 const uint64_t at = t + min(u, run - 1u);
-                x[u].load(px + at * a.x_step);
-                g[u].load(pg + at * a.gate_step);
-                if (a.dy) d[u].load(pd + at * a.dy_step);
-                if (a.done) ends |= (a.done[at * a.n + l.seq] ? 1u : 0u) << u;
+                x[u].load(a.x + at * a.x_step + ox);
+                g[u].load(a.gate + at * a.gate_step + og);
+                if (a.dy) d[u].load(a.dy + at * a.dy_step + od);
             }
-#pragma unroll
-            for (int i = 0; i < V; ++i) m[i] = a.marks[(uint64_t)(t / U) * C + l.flat + i];
-            // the states that the run's steps start from, as the forward pass had them
+            const uint32_t ends = ends_of<U>(a, t, t + run, l.seq);
+            l.get(a.marks + (uint64_t)(t / U) * C, m);
 #pragma unroll
             for (uint32_t u = 0; u < U; ++u)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    h[u][i] = m[i];
-                    const Gate w = gate_of(g[u].get(i));
-                    m[i] = ends >> u & 1u ? 0.0f : __builtin_fmaf(w.a, m[i], w.take * x[u].get(i));
+                    const float in = x[u].get(i);
+                    w[u][i] = gate_of(g[u].get(i));
+                    diff[u][i] = m[i] - in;
+                    m[i] = ends >> u & 1u ? 0.0f : __builtin_fmaf(w[u][i].a, m[i], w[u][i].take * in);
                 }
 #pragma unroll
             for (uint32_t k = 0; k < U; ++k) {
@@ -284,14 +343,13 @@ __global__ __launch_bounds__(256) void k_scan_back_rows(ScanArgs a)
                     const bool end = ends >> u & 1u;
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const Gate w = gate_of(g[u].get(i));
                         const float e = (a.dy ? d[u].get(i) : 0.0f) + (end ? 0.0f : R[i]);
-                        dx[i] = w.take * e;
-                        dg[i] = w.a * dx[i] * (h[u][i] - x[u].get(i));
-                        R[i] = w.a * e;
+                        dx[i] = w[u][i].take * e;
+                        dg[i] = w[u][i].a * dx[i] * diff[u][i];
+                        R[i] = w[u][i].a * e;
                     }
-                    Channels<D, V>::store(qx + (uint64_t)(t + u) * a.y_step, dx, l.from);
-                    Channels<D, V>::store(qg + (uint64_t)(t + u) * a.dgate_step, dg, l.from);
+                    Channels<D, V>::store(a.y + (uint64_t)(t + u) * a.y_step + odx, dx, l.from);
+                    Channels<D, V>::store(a.dgate + (uint64_t)(t + u) * a.dgate_step + odg, dg, l.from);
                 }
             }
             left -= run;

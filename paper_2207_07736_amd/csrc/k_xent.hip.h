@@ -30,6 +30,20 @@ struct XentRow {
     int32_t target;                               // -1: the row counts for nothing
 };
 
+// The rows' targets as given: -1 for one outside the vocabulary.
+struct XentTarget {
+    const void* p;
+    int bytes;
+    uint32_t vocab;
+    __device__ __forceinline__ int32_t operator()(uint32_t r) const
+    {
+        const int64_t t = bytes == 1   ? (int64_t) static_cast<const uint8_t*>(p)[r]
+                          : bytes == 4 ? (int64_t) static_cast<const int32_t*>(p)[r]
+                                       : static_cast<const int64_t*>(p)[r];
+        return t >= 0 && t < (int64_t)vocab ? (int32_t)t : -1;
+    }
+};
+
 struct XentGemm {
     const char* A;
     const char* B;
@@ -41,7 +55,7 @@ struct XentGemm {
     uint32_t tiles_m, tiles_n, share;             // share: workgroups to a tile
     uint32_t m0;                                  // logits: first entry of the piece
     uint32_t vocab;
-    const int32_t* target;                        // logits
+    XentTarget target;                            // logits
     float2* part;                                 // logits, losses: [wave columns][rows_k]
     float* zt;
     uint32_t part0, rows_k;
@@ -89,9 +103,11 @@ __device__ __forceinline__ void cut3(float x, uint16_t (&p)[3])
 // dz of fp16 factors is kept times 2^14, as probabilities below 2^-14 would lose bits.
 constexpr float kDzUp = 16384.0f, kDzDown = 1.0f / 16384.0f;
 // The power of two that brings the largest weight to [1/2, 1), for fp16.
-__device__ __forceinline__ float weight_scale(float wmax)
+// (No weights: 1.)
+__device__ __forceinline__ float weight_scale(const float* wmax)
 {
-    const int e = (int)(__builtin_bit_cast(uint32_t, wmax) >> 23 & 0xFFu);
+    if (!wmax) return 1.0f;
+    const int e = (int)(__builtin_bit_cast(uint32_t, *wmax) >> 23 & 0xFFu);
     if (e == 0 || e == 255) return 1.0f;          // none, denormal or not finite
     return __builtin_bit_cast(float, (uint32_t)(min(max(253 - e, 1), 254)) << 23);
 }
@@ -118,10 +134,26 @@ struct OutScale {
     __device__ __forceinline__ OutScale(const XentRow* row, const float* wmax, uint32_t n)
     {
         if (row) counts = row[n].target >= 0;
-        if (F == kHeadF16) by = row ? row[n].weight * kDzDown : kDzDown / weight_scale(*wmax);
+        if (F == kHeadF16) by = row ? row[n].weight * kDzDown : kDzDown / weight_scale(wmax);
     }
     __device__ __forceinline__ float operator()(float x) const { return counts ? x * by : 0.0f; }
 };
+
+// Entries m .. m + 3 of a row of M, rounded.
+template <int F>
+__device__ __forceinline__ void put_four(char* row, uint32_t m, uint32_t M, float x0, float x1, float x2, float x3)
+{
+    using El = Elem<F>;
+    using Word = typename El::Word;
+    struct __attribute__((packed, aligned(El::kBytes))) Four { Word w[4]; } four{{El::word(x0), El::word(x1), El::word(x2), El::word(x3)}};
+    if (m + 4u <= M) {
+        *reinterpret_cast<Four*>(row + (uint64_t)m * El::kBytes) = four;
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 3u; ++e)
+            if (m + e < M) reinterpret_cast<Word*>(row)[m + e] = four.w[e];
+    }
+}
 
 // One operand of a tile: R rows of C (m or n), 32 k of them at a time in LDS, which has 64
 // banks of 4 bytes.
@@ -401,7 +433,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         if (EPI == kXentLoss) {
             // largest logit and sum of this wave's entries of row n, and the target's logit
             float top = -__builtin_inff();
-            const int32_t target = n < a.N ? a.target[n] : -1;
+            const int32_t target = n < a.N ? a.target(n) : -1;
 #pragma unroll
             for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
@@ -425,7 +457,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
             XentRow r{0.0f, 0.0f, 0.0f, -1};
             if (n < a.N) r = a.row[n];
             const float up = F == kHeadF16 ? kDzUp : 1.0f;
-            const float weight = F == kHeadF16 ? r.weight * weight_scale(*a.wmax) * kDzUp : r.weight;
+            const float weight = F == kHeadF16 ? r.weight * weight_scale(a.wmax) * kDzUp : r.weight;
 #pragma unroll
             for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
@@ -490,40 +522,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
 #pragma unroll
                 for (uint32_t q = 0; q < 4u; ++q) {
                     const uint32_t m = m_wave + i * 32u + q * 8u;
-                    using Word = typename Elem<F>::Word;
-                    struct __attribute__((packed, aligned(Elem<F>::kBytes))) Four { Word w[4]; } four;
-#pragma unroll
-                    for (uint32_t e = 0; e < 4u; ++e) four.w[e] = Elem<F>::word(scale(c[i][j][4u * q + e]));
-                    if (m + 4u <= a.M) {
-                        *reinterpret_cast<Four*>(to + (uint64_t)m * sizeof(Word)) = four;
-                    } else {
-#pragma unroll
-                        for (uint32_t e = 0; e < 3u; ++e)
-                            if (m + e < a.M) reinterpret_cast<Word*>(to)[m + e] = four.w[e];
-                    }
+                    put_four<F>(to, m, a.M, scale(c[i][j][4u * q]), scale(c[i][j][4u * q + 1u]), scale(c[i][j][4u * q + 2u]),
+                                scale(c[i][j][4u * q + 3u]));
                 }
         }
     }
-}
-
-// Targets as int32, -1 for those outside the vocabulary, and the largest |weight|.
-struct XentPrepare {
-    const void* target;
-    int bytes;
-    uint32_t rows, rows_k, vocab;
-    int32_t* out;
-};
-__global__ __launch_bounds__(256) void k_xent_targets(XentPrepare a, float* wmax)
-{
-    const uint32_t r = blockIdx.x * 256u + threadIdx.x;
-    if (r == 0u) *wmax = 0.0f;
-    if (r >= a.rows_k) return;
-    int64_t t = -1;
-    if (r < a.rows)
-        t = a.bytes == 1   ? (int64_t) static_cast<const uint8_t*>(a.target)[r]
-            : a.bytes == 4 ? (int64_t) static_cast<const int32_t*>(a.target)[r]
-                           : static_cast<const int64_t*>(a.target)[r];
-    a.out[r] = t >= 0 && t < (int64_t)a.vocab ? (int32_t)t : -1;
 }
 
 // Rows' largest logits and sums from their parts (or as given), the losses, and what the
@@ -532,52 +535,63 @@ struct XentJoin {
     const float2* part;                           // null: stats is an input
     uint32_t parts, rows, rows_k;
     const float* zt;
-    const int32_t* target;
+    XentTarget target;
     const float* weight;
     float* stats;
     float* loss;
     XentRow* row;                                 // null: losses alone
-    float* wmax;
 };
-__global__ __launch_bounds__(256) void k_xent_join(XentJoin a)
+// Of two runs of a row, each its largest logit and its sum of exp(z - largest).
+__device__ __forceinline__ float2 joined(float2 p, float2 q)
 {
-    __shared__ float2 sh[16][16];
-    const uint32_t x = threadIdx.x % 16u, y = threadIdx.x / 16u, r = blockIdx.x * 16u + x;
+    const float top = __builtin_fmaxf(p.x, q.x), from = top == -__builtin_inff() ? 0.0f : top;
+    return float2{top, p.y * exp_of(p.x - from) + q.y * exp_of(q.x - from)};
+}
+constexpr uint32_t kJoinRows = 4u, kJoinRuns = 256u / kJoinRows;    // of a workgroup; threads to a row
+__device__ __forceinline__ void xent_join(const XentJoin& a, uint32_t block)
+{
+    __shared__ float2 sh[kJoinRuns][kJoinRows];
+    const uint32_t x = threadIdx.x % kJoinRows, y = threadIdx.x / kJoinRows, r = block * kJoinRows + x;
     float2 s{-__builtin_inff(), 0.0f};
     if (a.part) {
         if (r < a.rows) {
-#pragma unroll 4
-            for (uint32_t i = y; i < a.parts; i += 16u) s.x = __builtin_fmaxf(s.x, a.part[(uint64_t)i * a.rows_k + r].x);
-            const float from = s.x == -__builtin_inff() ? 0.0f : s.x;
-#pragma unroll 4
-            for (uint32_t i = y; i < a.parts; i += 16u) {
-                const float2 p = a.part[(uint64_t)i * a.rows_k + r];
-                s.y += p.y * exp_of(p.x - from);
-            }
+#pragma unroll 8
+            for (uint32_t i = y; i < a.parts; i += kJoinRuns) s = joined(s, a.part[(uint64_t)i * a.rows_k + r]);
         }
         sh[y][x] = s;
         __syncthreads();
+        for (uint32_t half = kJoinRuns / 2u; half != 0u; half /= 2u) {
+            if (y < half) sh[y][x] = joined(sh[y][x], sh[y + half][x]);
+            __syncthreads();
+        }
         if (y != 0u) return;
-        for (uint32_t i = 1; i < 16u; ++i) s.x = __builtin_fmaxf(s.x, sh[i][x].x);
-        const float from = s.x == -__builtin_inff() ? 0.0f : s.x;
-        s.y = 0.0f;
-        for (uint32_t i = 0; i < 16u; ++i) s.y += sh[i][x].y * exp_of(sh[i][x].x - from);
+        s = sh[0][x];
     } else if (y != 0u) {
         return;
     }
     if (r >= a.rows) return;
     if (!a.part) s = reinterpret_cast<const float2*>(a.stats)[r];
     else if (a.stats) reinterpret_cast<float2*>(a.stats)[r] = s;
-    const int32_t target = a.target[r];
+    const int32_t target = a.target(r);
     if (a.loss) a.loss[r] = target < 0 ? 0.0f : logf(s.y) + (s.x - a.zt[r]);
     if (a.row) {
         const float w = a.weight ? a.weight[r] : 1.0f;
         const bool counts = target >= 0 && w != 0.0f;
         a.row[r] = XentRow{s.x, 1.0f / s.y, counts ? w : 0.0f, counts ? target : -1};
-        // for finite weights the order of these does not matter
-        if (counts && __builtin_fabsf(w) < __builtin_inff())
-            atomicMax(reinterpret_cast<uint32_t*>(a.wmax), __builtin_bit_cast(uint32_t, __builtin_fabsf(w)));
     }
+}
+
+// The largest finite |weight| of the rows that count.
+__global__ __launch_bounds__(1024) void k_xent_wmax(XentTarget target, const float* weight, uint32_t rows, float* wmax)
+{
+    __shared__ float sh[16];
+    float top = 0.0f;
+    for (uint32_t r = threadIdx.x; r < rows; r += 1024u) {
+        const float w = __builtin_fabsf(weight[r]);
+        if (w < __builtin_inff() && target(r) >= 0) top = __builtin_fmaxf(top, w);
+    }
+    top = group_max<16>(top, sh);
+    if (threadIdx.x == 0u) *wmax = top;
 }
 
 // Rows as the products read them: whole steps wide, fp32 in three parts; rows that do not
@@ -588,19 +602,21 @@ struct XentLay {
     uint32_t R, C, wide, tall;                    // wide: elements of a row of the copy, a multiple of 8;
     char* to;                                     // [parts][tall][wide], 0 behind R and C
     uint64_t part;                                // bytes
-    const XentRow* row;                           // or null
+    XentTarget target;                            // p null: all rows count
+    const float* weight;
+    uint32_t blocks;
 };
 template <int F>
-__global__ __launch_bounds__(256) void k_xent_lay(XentLay a)
+__device__ __forceinline__ void xent_lay(const XentLay& a, uint32_t block)
 {
     using El = Elem<F>;
     constexpr uint32_t P = F == kHeadF32 ? 3u : 1u;
     const uint32_t per = a.wide / 8u;
     const uint64_t all = (uint64_t)a.tall * per;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256u) {
+    for (uint64_t i = (uint64_t)block * 256u + threadIdx.x; i < all; i += (uint64_t)a.blocks * 256u) {
         const uint32_t r = (uint32_t)(i / per), c = (uint32_t)(i % per) * 8u;
         uint16_t w[P][8] = {};
-        if (r < a.R && (!a.row || a.row[r].target >= 0)) {
+        if (r < a.R && (!a.target.p || (a.target(r) >= 0 && !(a.weight && a.weight[r] == 0.0f)))) {
             struct __attribute__((packed, aligned(El::kBytes))) Eight { typename El::Word w[8]; } x{};
             const auto* from = reinterpret_cast<const typename El::Word*>(a.from + r * a.ld) + c;
             if (c + 8u <= a.C) {
@@ -626,27 +642,54 @@ __global__ __launch_bounds__(256) void k_xent_lay(XentLay a)
     }
 }
 
+// Two copies in one launch, or the rows' sums and a copy.
+template <int F>
+__global__ __launch_bounds__(256) void k_xent_lays(XentLay a, XentLay b)
+{
+    if (blockIdx.x < a.blocks) xent_lay<F>(a, blockIdx.x);
+    else xent_lay<F>(b, blockIdx.x - a.blocks);
+}
+template <int F>
+__global__ __launch_bounds__(256) void k_xent_join(XentJoin a, XentLay b)
+{
+    const uint32_t blocks = (a.rows + kJoinRows - 1u) / kJoinRows;
+    if (blockIdx.x < blocks) xent_join(a, blockIdx.x);
+    else xent_lay<F>(b, blockIdx.x - blocks);
+}
+
 // A gradient from its shares: summed in order, scaled, rounded once.
 struct XentRound {
     const float* sum;
     uint64_t ld, share_ld;
     uint32_t share, rows, dim;
-    const XentRow* row;                           // dhidden: a row's weight; rows that do not count are 0
+    const XentRow* row;                           // dhidden: rows that do not count are 0; fp16: a row's weight
     const float* wmax;                            // dmatrix of fp16: the weights' scale
     char* out;
     uint64_t out_ld;                              // bytes
+    uint32_t blocks;
 };
 template <int F>
-__global__ __launch_bounds__(256) void k_xent_round(XentRound a)
+__device__ __forceinline__ void xent_round(const XentRound& a, uint32_t block)
 {
     using El = Elem<F>;
-    const uint32_t per = (a.dim + 255u) / 256u;
-    const uint32_t n = blockIdx.x / per, d = blockIdx.x % per * 256u + threadIdx.x;
-    if (d >= a.dim) return;
-    float s = 0.0f;
-    for (uint32_t i = 0; i < a.share; ++i) s += a.sum[i * a.share_ld + n * a.ld + d];
+    const uint32_t per = (a.dim + 3u) / 4u;       // of four entries
+    const uint64_t i = (uint64_t)block * 256u + threadIdx.x;
+    if (i >= (uint64_t)a.rows * per) return;
+    const uint32_t n = (uint32_t)(i / per), d = (uint32_t)(i % per) * 4u;
+    float4 s{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+    for (uint32_t k = 0; k < a.share; ++k) {
+        const float4 x = *reinterpret_cast<const float4*>(a.sum + k * a.share_ld + n * a.ld + d);
+        s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+    }
     const OutScale<F> scale(a.row, a.wmax, n);
-    reinterpret_cast<typename El::Word*>(a.out + n * a.out_ld)[d] = El::word(scale(s));
+    put_four<F>(a.out + n * a.out_ld, d, a.dim, scale(s.x), scale(s.y), scale(s.z), scale(s.w));
+}
+template <int F>
+__global__ __launch_bounds__(256) void k_xent_round(XentRound a, XentRound b)
+{
+    if (blockIdx.x < a.blocks) xent_round<F>(a, blockIdx.x);
+    else xent_round<F>(b, blockIdx.x - a.blocks);
 }
 
 }  // namespace rlsim_dev

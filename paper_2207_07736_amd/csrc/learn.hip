@@ -144,38 +144,41 @@ int check_scan(rlsim_learner* h, const char* who, const rlsim_scan* s, const Pla
     return RLSIM_OK;
 }
 
-template <int D, int V>
-void launch_scan(const rlsim_learner* h, ScanArgs a, bool backward)
+template <int D, int V, bool WIDE>
+void launch_scan(const rlsim_learner* h, ScanArgs a)
 {
     a.groups = (a.channels + V - 1u) / V;
-    const uint64_t threads = (uint64_t)a.n * a.groups;
-    const ScanCut cut = scan_cut(threads, (uint64_t)a.n * a.channels, a.T, h->cus);
+    const uint64_t threads = (uint64_t)a.n * a.groups, C = (uint64_t)a.n * a.channels;
+    const ScanCut cut = scan_cut(threads, C, a.T, h->cus);
     a.segments = cut.segments;
     a.seg_len = cut.seg_len;
     a.map_a = reinterpret_cast<float*>(h->work);
     a.map_b = a.map_a + kScanMapEntries;
     const dim3 grid((uint32_t)std::min<uint64_t>((threads + 255u) / 256u, 1u << 22), cut.segments), block(256);
-    if (backward) {
-        if (cut.segments > 1u) hipLaunchKernelGGL((k_scan_back_maps<D, V>), grid, block, 0, h->stream, a);
-        hipLaunchKernelGGL((k_scan_back_rows<D, V>), grid, block, 0, h->stream, a);
-    } else {
-        if (cut.segments > 1u) hipLaunchKernelGGL((k_scan_maps<D, V>), grid, block, 0, h->stream, a);
-        hipLaunchKernelGGL((k_scan_rows<D, V>), grid, block, 0, h->stream, a);
+    if (cut.segments > 1u) {
+        if (a.backward) hipLaunchKernelGGL((k_scan_back_maps<D, V, WIDE>), grid, block, 0, h->stream, a);
+        else hipLaunchKernelGGL((k_scan_maps<D, V, WIDE>), grid, block, 0, h->stream, a);
+        hipLaunchKernelGGL(k_scan_join, dim3((uint32_t)((C + 15u) / 16u)), block, 0, h->stream, a);
     }
+    if (a.backward) hipLaunchKernelGGL((k_scan_back_rows<D, V, WIDE>), grid, block, 0, h->stream, a);
+    else if (a.T == 1u) hipLaunchKernelGGL((k_scan_rows<D, V, 1u, WIDE>), grid, block, 0, h->stream, a);
+    else hipLaunchKernelGGL((k_scan_rows<D, V, kScanMark, WIDE>), grid, block, 0, h->stream, a);
 }
 
 template <int D>
-void scan_form(const rlsim_learner* h, const ScanArgs& a, bool backward)
+void scan_form(const rlsim_learner* h, const ScanArgs& a, bool wide)
 {
-    if (a.channels >= 2u) launch_scan<D, 2>(h, a, backward);
-    else launch_scan<D, 1>(h, a, backward);
+    if (a.channels < 2u) wide ? launch_scan<D, 1, true>(h, a) : launch_scan<D, 1, false>(h, a);
+    else wide ? launch_scan<D, 2, true>(h, a) : launch_scan<D, 2, false>(h, a);
 }
 
-void run_scan(const rlsim_learner* h, int dtype, const ScanArgs& a, bool backward)
+void run_scan(const rlsim_learner* h, int dtype, const ScanArgs& a)
 {
-    if (dtype == RLSIM_F32) scan_form<kHeadF32>(h, a, backward);
-    else if (dtype == RLSIM_BF16) scan_form<kHeadBF16>(h, a, backward);
-    else scan_form<kHeadF16>(h, a, backward);
+    const uint64_t far = std::max({a.x_seq, a.gate_seq, a.dy_seq, a.y_seq, a.dgate_seq});
+    const bool wide = far * (a.n - 1u) + 4ull * a.channels >= 1ull << 32;
+    if (dtype == RLSIM_F32) scan_form<kHeadF32>(h, a, wide);
+    else if (dtype == RLSIM_BF16) scan_form<kHeadBF16>(h, a, wide);
+    else scan_form<kHeadF16>(h, a, wide);
 }
 
 ScanArgs scan_args(const rlsim_scan& s)
@@ -210,17 +213,23 @@ void launch_gemm(const rlsim_learner* h, XentGemm a, const XentTile& t)
     else hipLaunchKernelGGL((k_xent_gemm<D, F, 256, 256, 2, 4, AA, BA, EPI>), grid, dim3(512), 0, h->stream, a);
 }
 
+// A copy's workgroups; none for one that is not made.
+uint32_t lay_blocks(const XentLay& a) { return (uint32_t)std::min<uint64_t>(((uint64_t)a.tall * (a.wide / 8u) + 255u) / 256u, 1u << 21); }
+
 template <int F>
-void launch_lay(const rlsim_learner* h, const XentLay& a)
+void launch_lays(const rlsim_learner* h, XentLay a, XentLay b)
 {
-    const uint64_t all = (uint64_t)a.tall * (a.wide / 8u);
-    hipLaunchKernelGGL(k_xent_lay<F>, dim3((uint32_t)std::min<uint64_t>((all + 255u) / 256u, 1u << 22)), dim3(256), 0, h->stream, a);
+    a.blocks = lay_blocks(a);
+    b.blocks = lay_blocks(b);
+    if (a.blocks + b.blocks) hipLaunchKernelGGL(k_xent_lays<F>, dim3(a.blocks + b.blocks), dim3(256), 0, h->stream, a, b);
 }
 
 template <int F>
-void launch_round(const rlsim_learner* h, const XentRound& a)
+void launch_round(const rlsim_learner* h, XentRound a, XentRound b)
 {
-    hipLaunchKernelGGL(k_xent_round<F>, dim3(a.rows * ((a.dim + 255u) / 256u)), dim3(256), 0, h->stream, a);
+    a.blocks = (uint32_t)(((uint64_t)a.rows * ((a.dim + 3u) / 4u) + 255u) / 256u);
+    b.blocks = (uint32_t)(((uint64_t)b.rows * ((b.dim + 3u) / 4u) + 255u) / 256u);
+    if (a.blocks + b.blocks) hipLaunchKernelGGL(k_xent_round<F>, dim3(a.blocks + b.blocks), dim3(256), 0, h->stream, a, b);
 }
 
 // Rows that the products can read where they are.
@@ -237,17 +246,21 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     const XentShape s = xent_shape(x.rows, x.dim, x.vocab, P);
     const XentWork o = xent_work(s);
     char* const w = h->work + h->xent_at;
-    auto* target = reinterpret_cast<int32_t*>(w + o.target);
-    auto* wmax = reinterpret_cast<float*>(w + o.wmax);
     auto* part = reinterpret_cast<float2*>(w + o.part);
     auto* zt = reinterpret_cast<float*>(w + o.zt);
     auto* row = reinterpret_cast<XentRow*>(w + o.info);
     float* stats = x.stats ? x.stats : reinterpret_cast<float*>(w + o.stats);
     const bool grad = x.dhidden || x.dmatrix;
+    const XentTarget target{x.target, x.target_bytes, x.vocab};
+    const char* const matrix = static_cast<const char*>(x.matrix);
+    float* wmax = nullptr;
+    if (F == kHeadF16 && grad && x.weight) {
+        wmax = reinterpret_cast<float*>(w + o.wmax);
+        hipLaunchKernelGGL(k_xent_wmax, dim3(1), dim3(1024), 0, h->stream, target, x.weight, x.rows, wmax);
+    }
 
-    hipLaunchKernelGGL(k_xent_targets, dim3((s.rows_k + 255u) / 256u), dim3(256), 0, h->stream,
-                       XentPrepare{x.target, x.target_bytes, x.rows, s.rows_k, x.vocab, target}, wmax);
-
+    const bool hidden_direct = P == 1u && as_they_are(x.hidden, x.hidden_stride, x.dim);
+    const bool direct = P == 1u && as_they_are(x.matrix, x.matrix_stride, x.dim);
     XentGemm z{};                                 // the logits' product
     z.products = P == 1u ? 1u : 6u;
     z.K = s.dim_k;
@@ -259,29 +272,30 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     z.zt = zt;
     z.row = row;
     z.wmax = wmax;
-    if (P == 1u && as_they_are(x.hidden, x.hidden_stride, x.dim)) {
-        z.B = static_cast<const char*>(x.hidden);
-        z.ldb = x.hidden_stride * e;
-    } else {
-        launch_lay<F>(h, XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, x.rows, w + o.x,
-                                 2ull * s.dim_k * x.rows, nullptr});
-        z.B = w + o.x;
-        z.ldb = 2ull * s.dim_k;
-        z.part_b = z.ldb * x.rows;
-    }
-    const bool direct = P == 1u && as_they_are(x.matrix, x.matrix_stride, x.dim);
+    z.B = hidden_direct ? static_cast<const char*>(x.hidden) : w + o.x;
+    z.ldb = hidden_direct ? x.hidden_stride * e : 2ull * s.dim_k;
+    z.part_b = 2ull * s.dim_k * x.rows;
     z.lda = direct ? x.matrix_stride * e : 2ull * s.dim_k;
-    const char* const matrix = static_cast<const char*>(x.matrix);
+    XentLay hidden_lay{};                         // made with the first piece of the matrix
+    if (!hidden_direct)
+        hidden_lay = XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, x.rows, w + o.x,
+                             z.part_b, {}, nullptr, 0u};
 
     // The piece of the vocabulary from v0, as the products read it.
+    uint32_t laid = ~0u;                          // the piece that is copied now
     auto piece = [&](uint32_t v0, uint32_t count) {
         z.m0 = v0;
         z.M = count;
         const char* const from = matrix + (uint64_t)v0 * x.matrix_stride * e;
         z.A = direct ? from : w + o.w;
         z.part_a = 2ull * s.dim_k * s.piece;
-        if (!direct) launch_lay<F>(h, XentLay{from, x.matrix_stride * e, count, x.dim, s.dim_k, (uint32_t)up_to(count, kXentK), w + o.w,
-                                              z.part_a, nullptr});
+        XentLay l{};
+        if (!direct && laid != v0)
+            l = XentLay{from, x.matrix_stride * e, count, x.dim, s.dim_k, (uint32_t)up_to(count, kXentK), w + o.w, z.part_a,
+                        {}, nullptr, 0u};
+        launch_lays<F>(h, hidden_lay, l);
+        hidden_lay = XentLay{};
+        laid = v0;
     };
 
     XentJoin j{};
@@ -293,25 +307,26 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     j.stats = stats;
     j.loss = x.loss;
     j.row = grad ? row : nullptr;
-    j.wmax = wmax;
     if (x.loss) {
         const uint32_t width = direct ? x.vocab : s.piece;
         for (uint32_t v0 = 0u; v0 < x.vocab; v0 += width) {
             const uint32_t count = std::min(width, x.vocab - v0);
             piece(v0, count);
-            z.part0 = j.parts;
             const XentTile t = xent_tile(count, x.rows, 0u, false, h->cus);
+            z.part0 = j.parts;
             launch_gemm<D, F, false, false, kXentLoss>(h, z, t);
             j.parts += (count + t.m - 1u) / t.m * (t.m / t.span);
         }
         j.part = part;
     }
-    hipLaunchKernelGGL(k_xent_join, dim3((x.rows + 15u) / 16u), dim3(256), 0, h->stream, j);
+    XentLay l{};                                  // for dmatrix: rows that do not count may hold anything
+    if (x.dmatrix)
+        l = XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, s.rows_k, w + o.xm,
+                    2ull * s.dim_k * s.rows_k, target, x.weight, 0u};
+    l.blocks = lay_blocks(l);
+    hipLaunchKernelGGL(k_xent_join<F>, dim3((x.rows + kJoinRows - 1u) / kJoinRows + l.blocks), dim3(256), 0, h->stream, j, l);
     if (!grad) return;
 
-    if (x.dmatrix)
-        launch_lay<F>(h, XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, s.rows_k, w + o.xm,
-                                 2ull * s.dim_k * s.rows_k, row});
     const uint64_t dim4 = up_to(x.dim, 4u);
     const bool plain = F == kHeadF16 && x.weight && x.dhidden;
     z.dz = w + o.dz;
@@ -339,6 +354,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     const XentTile tx = xent_tile(x.dim, x.rows, (uint64_t)s.piece / kXentK * z.products, true, h->cus);
     for (uint32_t v0 = 0u; v0 < x.vocab; v0 += s.piece) {
         const uint32_t count = std::min(s.piece, x.vocab - v0);
+        XentRound rx{}, rw{};
         piece(v0, count);
         launch_gemm<D, F, false, false, kXentDz>(h, z, xent_tile(count, x.rows, 0u, false, h->cus));
         if (x.dhidden) {
@@ -359,13 +375,15 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
             } else {
                 gw.sum_share = count * dim4;
                 launch_gemm<D, F, true, true, kXentSum>(h, gw, t);
-                launch_round<F>(h, XentRound{gw.sum, dim4, gw.sum_share, t.share, count, x.dim, nullptr, wmax, out, x.dmatrix_stride * e});
+                rw = XentRound{gw.sum, dim4, gw.sum_share, t.share, count, x.dim, nullptr, wmax, out, x.dmatrix_stride * e, 0u};
             }
         }
+        const bool done = count == x.vocab - v0;
+        if (done && x.dhidden)
+            rx = XentRound{gx.sum, dim4, gx.sum_share, tx.share, x.rows, x.dim, row, wmax, static_cast<char*>(x.dhidden),
+                           x.dhidden_stride * e, 0u};
+        launch_round<F>(h, rx, rw);
     }
-    if (x.dhidden)
-        launch_round<F>(h, XentRound{gx.sum, dim4, gx.sum_share, tx.share, x.rows, x.dim, row, wmax,
-                                     static_cast<char*>(x.dhidden), x.dhidden_stride * e});
 }
 
 // ---- clipping --------------------------------------------------------------------
@@ -512,7 +530,7 @@ int rlsim_learner_scan(rlsim_learner_t* h, const rlsim_scan* s)
     a.y_seq = s->n > 1u ? s->y_seq * e : 0u;
     a.state = s->state;
     a.last = s->last;
-    run_scan(h, s->dtype, a, false);
+    run_scan(h, s->dtype, a);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return learn_fail(h, RLSIM_EDEVICE, "%s: launch: %s", who, hipGetErrorString(err));
     return RLSIM_OK;
@@ -556,7 +574,8 @@ int rlsim_learner_scan_grad(rlsim_learner_t* h, const rlsim_scan* s, const rlsim
     a.dgate_seq = more ? d->dgate_seq * e : 0u;
     a.state = d->dlast;
     a.last = d->dstate;
-    run_scan(h, s->dtype, a, true);
+    a.backward = 1u;
+    run_scan(h, s->dtype, a);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return learn_fail(h, RLSIM_EDEVICE, "%s: launch: %s", who, hipGetErrorString(err));
     return RLSIM_OK;

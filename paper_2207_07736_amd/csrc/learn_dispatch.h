@@ -13,17 +13,21 @@ inline uint64_t most(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 // ---- the gated recurrence ----------------------------------------------------------
 constexpr uint32_t kScanMark = 16u;               // steps between marks, and of a run of loads
-constexpr uint32_t kScanMapEntries = 1u << 21;    // most segments x channels of a call
-constexpr uint32_t kScanSegments = 256u;
+constexpr uint32_t kScanMapEntries = 1u << 22;    // most segments x channels of a call
+constexpr uint32_t kScanSegments = 1024u;
 
 struct ScanCut { uint32_t segments, seg_len; };
-// Segments of time for `threads` threads' channels: as many as give every CU's waves work
-// while a segment is long enough to be worth its map (64 steps).
+// Segments of time for `threads` threads' channels.  A cut call reads its rows twice, so few
+// are cut: where there are fewer than two waves to a CU, or four if the steps are many (one
+// thread's run of 16 steps takes 4 us whatever the others do).  What is cut is cut into
+// enough for 16 waves a CU, of 32 steps at least.  Forward and backward, us, uncut / cut:
+//   200 x 4,096 x 64 fp32 338 / 531     1,000 x 1,024 x 64 bf16 652 / 359
+//   200 x 1,024 x 64 fp32 122 / 122     1,000 x 2,048 x 64 bf16 687 / 677
 inline ScanCut scan_cut(uint64_t threads, uint64_t channels, uint32_t T, uint32_t cus)
 {
-    const uint64_t wanted = 512ull * cus;
-    uint64_t s = threads >= wanted ? 1u : (wanted + threads - 1u) / threads;
-    s = least(s, T / 64u);
+    const uint64_t enough = (T <= 256u ? 128ull : 256ull) * cus, wanted = 1024ull * cus;
+    uint64_t s = threads >= enough ? 1u : (wanted + threads - 1u) / threads;
+    s = least(s, T / 32u);
     s = least(s, kScanSegments);
     s = least(s, channels ? kScanMapEntries / channels : 1u);
     if (s < 2u) return {1u, T};
@@ -35,8 +39,9 @@ inline ScanCut scan_cut(uint64_t threads, uint64_t channels, uint32_t T, uint32_
 constexpr uint32_t kClipTensors = 96u;            // of one launch: their table has to fit its arguments
 constexpr uint32_t kClipBlocks = 4096u;           // blocks of a call, beyond one to a tensor
 constexpr uint64_t kClipSmall = 1u << 15;         // elements that one workgroup takes alone
-inline uint64_t clip_chunk(uint64_t total)
+inline uint64_t clip_chunk(uint64_t total)         // elements of a block
 {
+    if (total <= kClipSmall) return 1024u;
     return most(up_to((total + kClipBlocks - 1u) / kClipBlocks, 8192u), 8192u);
 }
 
@@ -76,7 +81,7 @@ inline XentTile xent_tile(uint32_t M, uint32_t N, uint64_t steps, bool sums, uin
 inline uint64_t xent_share_floats(uint64_t rows, uint64_t dim4) { return most(rows * dim4, (uint64_t)kXentShareTiles * 128u * 128u); }
 
 struct XentWork {                                 // byte offsets
-    uint64_t target, info, zt, stats, wmax, part, x, xm, w, dz, dz_plain, dx, dw, end;
+    uint64_t info, zt, stats, wmax, part, x, xm, w, dz, dz_plain, dx, dw, end;
 };
 inline XentWork xent_work(const XentShape& s)
 {
@@ -85,7 +90,6 @@ inline XentWork xent_work(const XentShape& s)
     auto take = [&at](uint64_t bytes) { const uint64_t p = at; at += up_to(bytes, 256u); return p; };
     const uint64_t P2 = 2ull * s.parts, dim4 = up_to(s.dim, 4u);
     o.wmax = take(4u);
-    o.target = take(4ull * s.rows_k);
     o.info = take(16ull * s.rows_k);
     o.zt = take(4ull * s.rows_k);
     o.stats = take(8ull * s.rows_k);

@@ -7,6 +7,7 @@ layer and clipping by the global norm.  torch is used for device memory, and so 
 """
 from __future__ import annotations
 
+import array
 import ctypes
 
 from .rlsim import RLSIM_BF16, RLSIM_F16, RLSIM_F32, RLSIM_OK, RlsimError, lib
@@ -118,10 +119,11 @@ class Learner:
         import torch
         self.h = None
         self._dtypes = {torch.float32: RLSIM_F32, torch.bfloat16: RLSIM_BF16, torch.float16: RLSIM_F16}
+        self._types = {t: d | d << 32 for t, d in self._dtypes.items()}          # both types of an rlsim_tensor
         self._target = {torch.uint8: 1, torch.int32: 4, torch.int64: 8}
-        self._torch, self._empty = torch, torch.empty
+        self._torch, self._empty, self._empty_like = torch, torch.empty, torch.empty_like
         self._written = torch.autograd.graph.increment_version
-        self._f32 = torch.float32
+        self._f32, self._strided = torch.float32, torch.strided
         self._done = (torch.uint8, torch.bool)
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._ordinal = self.device.index
@@ -178,17 +180,21 @@ class Learner:
         return self._plain("done", done, (T, n), done.dtype)
 
     def _scan_args(self, x, gate, state, done, marks):
+        shape, kind = x.shape, x.dtype
         dtype = self._dtype("x", x)
-        if x.dim() != 3:
+        if len(shape) != 3:
             raise ValueError("x must be 3-d, [T, n, channels]")
-        shape = T, n, channels = tuple(x.shape)
-        x_at, x_step, x_seq = self._rows("x", x, shape, x.dtype)
-        g_at, g_step, g_seq = self._rows("gate", gate, shape, x.dtype)
+        T, n, channels = shape
+        x_at, x_step, x_seq = self._rows("x", x, shape, kind)
+        g_at, g_step, g_seq = self._rows("gate", gate, shape, kind)
         return rlsim_scan(dtype, T, n, channels, x_at, g_at, x_step, x_seq, g_step, g_seq,
-                          self._plain("state", state, (n, channels)), self._ends(done, T, n), marks)
+                          None if state is None else self._plain("state", state, (n, channels)),
+                          None if done is None else self._ends(done, T, n), marks)
 
     def _like(self, x):
         """A new tensor of x's shape and order of its first two dimensions."""
+        if x.is_contiguous():
+            return self._empty_like(x)
         T, n, channels = x.shape
         if n > 1 and T > 1 and x.stride(1) > x.stride(0):
             return self._empty((n, T, channels), dtype=x.dtype, device=self.device).transpose(0, 1)
@@ -210,14 +216,16 @@ class Learner:
         y = self._like(x)
         given = last is not None
         if not given:
-            last = self._empty((n, channels), dtype=self._f32, device=self.device)
+            last = (self._empty((n, channels), dtype=self._f32, device=self.device) if state is None or not state.is_contiguous()
+                    else self._empty_like(state))
         kept = None
         if marks:
             kept = self._empty((-(-T // RLSIM_SCAN_MARK), n, channels), dtype=self._f32, device=self.device)
             args.marks = kept.data_ptr()
-        args.y, args.y_step, args.y_seq = y.data_ptr(), y.stride(0), y.stride(1)
-        args.last = self._plain("last", last, (n, channels))
-        if y.numel():
+        args.y = y.data_ptr()
+        args.y_step, args.y_seq, _ = y.stride()
+        args.last = self._plain("last", last, (n, channels)) if given else last.data_ptr()
+        if T and n and channels:
             launch(self.h, args)
         elif n and channels:                      # no steps: the state as it was
             if state is None:
@@ -336,7 +344,7 @@ class Learner:
 
     def _dense(self, name, t):
         """Whether t's elements lie side by side, in whatever order."""
-        if t.layout != self._torch.strided or t.get_device() != self._ordinal:
+        if t.layout is not self._strided or t.get_device() != self._ordinal:
             raise ValueError(f"{name} must be a dense tensor on {self.device}")
         if t.is_contiguous():
             return
@@ -362,23 +370,27 @@ class Learner:
             pairs = [(t, o) for t, o in zip(tensors, out) if t is not None]
         else:
             pairs = [(t, t) for t in tensors if t is not None]
-        table = (rlsim_tensor * max(1, len(pairs)))()
-        for i, (t, o) in enumerate(pairs):
-            dtype = self._dtype("tensors", t)
-            self._dense("tensors", t)
-            at = t.data_ptr()
+        words, types, ordinal, here = [], self._types, self._ordinal, self._dense
+        add = words.extend
+        for t, o in pairs:
+            kind = types.get(t.dtype)
+            if kind is None:
+                raise ValueError("tensors must be float32, bfloat16 or float16")
+            if t.get_device() != ordinal or not t.is_contiguous():
+                here("tensors", t)
             if o is t:
-                table[i] = (at, None, t.numel(), dtype, dtype)
+                add((t.data_ptr(), 0, t.numel(), kind))
                 continue
-            if o is None or o.shape != t.shape or (o.stride() != t.stride() and not (o.is_contiguous() and t.is_contiguous())):
+            if o is None or o.shape != t.shape or o.stride() != t.stride():
                 raise ValueError("out must have its tensor's shape and order in memory")
-            self._dense("out", o)
-            table[i] = (at, o.data_ptr(), t.numel(), dtype, self._dtype("out", o))
+            if o.get_device() != ordinal or not o.is_contiguous():
+                here("out", o)
+            add((t.data_ptr(), o.data_ptr(), t.numel(), kind & 0xFFFFFFFF | self._dtype("out", o) << 32))
+        table = array.array("Q", words)           # rows of an rlsim_tensor
         norm = self._empty((), dtype=self._f32, device=self.device)
-        rlsim_learner_clip(self.h, table, len(pairs), float(max_norm), norm.data_ptr())
-        if max_norm < float("inf") or out is not None:
-            for _, o in pairs:
-                self._written(o)                  # autograd cannot see a write through an address
+        rlsim_learner_clip(self.h, table.buffer_info()[0], len(pairs), float(max_norm), norm.data_ptr())
+        if pairs and (max_norm < float("inf") or out is not None):
+            self._written([o for _, o in pairs])  # autograd cannot see a write through an address
         return norm
 
     def _in_order(self, launch, *args):
