@@ -50,8 +50,8 @@ struct XentGemm {
     uint64_t lda, ldb;                            // bytes between rows
     uint64_t part_a, part_b;                      // bytes between the parts of fp32 factors
     uint32_t M, N;
-    uint32_t K;                                   // the summed dimension: from K to a whole step B is 0, and A is
-    uint32_t steps, products;                     // too, or as many rows as K says; products of parts
+    uint32_t K;                                   // the summed dimension; along operands may go on behind it (of
+    uint32_t steps, products;                     // fp32 they are 0 there), across ones end; products of parts
     uint32_t tiles_m, tiles_n, share;             // share: workgroups to a tile
     uint32_t m0;                                  // logits: first entry of the piece
     uint32_t vocab;
@@ -155,6 +155,19 @@ __device__ __forceinline__ void put_four(char* row, uint32_t m, uint32_t M, floa
     }
 }
 
+// Entries m .. m + 7 of a row of M, of 16 bits.
+__device__ __forceinline__ void put_eight(char* row, uint32_t m, uint32_t M, u32x4 w)
+{
+    typedef uint32_t Packed __attribute__((ext_vector_type(4), aligned(2)));
+    if (m + 8u <= M) {
+        *reinterpret_cast<Packed*>(row + 2ull * m) = w;
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 7u; ++e)
+            if (m + e < M) reinterpret_cast<uint16_t*>(row)[m + e] = (uint16_t)(w[e / 2u] >> 16u * (e % 2u));
+    }
+}
+
 // One operand of a tile: R rows of C (m or n), 32 k of them at a time in LDS, which has 64
 // banks of 4 bytes.
 //
@@ -199,8 +212,8 @@ struct Operand {
     {
         return ACROSS ? 0u : min(base, rows - 1u) * ld;
     }
-    // 32 k from p on into LDS.  CUT: across, of the first `left` of them, the last one again
-    // and again.
+    // 32 k from p on into LDS.  CUT: of the first `left` of them, a multiple of 8 along; what lies
+    // behind is the row's last chunk, or the last row k, again.
     template <bool CUT>
     __device__ __forceinline__ void fetch(const char* p, char* to, uint32_t ld, uint32_t left, uint32_t wave, uint32_t lane) const
     {
@@ -210,6 +223,10 @@ struct Operand {
             if (ACROSS && CUT) {
                 const uint32_t k = place(i, wave, lane) / kRowChunks;
                 off -= (k - min(k, left - 1u)) * ld;
+            }
+            if (!ACROSS && CUT) {
+                const uint32_t q = place(i, wave, lane), c = q % 4u ^ q / 4u / 4u % 4u;
+                off -= (c - min(c, (left + 7u) / 8u - 1u)) * 16u;
             }
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + off),
                                              (__attribute__((address_space(3))) void*)(to + (i * NW + wave) % kParts * 1024u), 16, 0, 0);
@@ -233,6 +250,15 @@ struct Fragments {
                 at[i] = (base + i * 32u + lane % 32u) * 64u + (lane / 32u ^ lane / 4u % 4u) * 16u;
             }
         }
+    }
+    // Along: 0 instead of what has k at or behind `left`, which lies in other rows.
+    template <uint32_t H>
+    __device__ __forceinline__ void cut(uint32_t left, uint32_t lane)
+    {
+        if (ACROSS || left >= 16u * H + 16u) return;
+#pragma unroll
+        for (uint32_t i = 0; i < F; ++i)
+            if (16u * H + lane / 32u * 8u >= left) v[H][i] = u32x4{0u, 0u, 0u, 0u};
     }
     template <uint32_t H>
     __device__ __forceinline__ void read(const char* from)
@@ -339,7 +365,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         constexpr bool CUT = decltype(cut)::value;
         const uint32_t left = CUT ? a.K - step * 32u : 32u;
         op_a.template fetch<CUT>(pa, to, lda, left, wave, lane);
-        op_b.template fetch<false>(pb, to + OpA::kBytes, ldb, 32u, wave, lane);
+        op_b.template fetch<CUT && !BA>(pb, to + OpA::kBytes, ldb, left, wave, lane);
         pa += step_a;
         pb += step_b;
         ++step;
@@ -365,6 +391,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     // Four steps of 32 k are in LDS or under way.  While a half step of 16 k is multiplied,
     // the next one's fragments are read; the workgroup meets once a step, after which the
     // step just read may be overwritten and the next one, loaded three steps ago, read.
+    auto cut = [&](auto half, uint32_t t) {       // (parts of fp32 are copies that end with whole steps)
+        constexpr uint32_t H = decltype(half)::value;
+        if (F == kHeadF32 || a.K >= t * 32u + 32u) return;
+        x.template cut<H>(a.K - t * 32u, lane);
+        y.template cut<H>(a.K - t * 32u, lane);
+    };
     auto one_step = [&](auto steady, uint32_t t, char* now, char* next, char* ahead) {
         constexpr bool kSteady = decltype(steady)::value;        // three more steps are to come
         reads_done();                             // of the first half
@@ -372,6 +404,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         else if (t + 3u < last) fetch(std::true_type{}, ahead);
         x.template read<1>(now);
         y.template read<1>(now + OpA::kBytes);
+        if (!kSteady) cut(std::integral_constant<uint32_t, 1u>{}, t);
 #pragma unroll
         for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
@@ -386,6 +419,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         if (kSteady || t + 1u < last) {
             x.template read<0>(next);
             y.template read<0>(next + OpA::kBytes);
+            if (!kSteady) cut(std::integral_constant<uint32_t, 0u>{}, t + 1u);
         }
 #pragma unroll
         for (uint32_t i = 0; i < FM; ++i)
@@ -407,6 +441,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         meet();
         x.template read<0>(sh0);
         y.template read<0>(sh0 + OpA::kBytes);
+        cut(std::integral_constant<uint32_t, 0u>{}, first);
         uint32_t t = first;
         constexpr std::true_type steady{};
         constexpr std::false_type ending{};
@@ -517,14 +552,24 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         if (EPI == kXentOut && n < a.N) {
             const OutScale<F> scale(a.out_row, a.wmax, n);
             char* const to = a.out + n * a.out_ld;
+            if (F == kHeadF32) {
 #pragma unroll
-            for (uint32_t i = 0; i < FM; ++i)
+                for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
-                for (uint32_t q = 0; q < 4u; ++q) {
-                    const uint32_t m = m_wave + i * 32u + q * 8u;
-                    put_four<F>(to, m, a.M, scale(c[i][j][4u * q]), scale(c[i][j][4u * q + 1u]), scale(c[i][j][4u * q + 2u]),
-                                scale(c[i][j][4u * q + 3u]));
-                }
+                    for (uint32_t q = 0; q < 4u; ++q)
+                        put_four<F>(to, m_wave + i * 32u + q * 8u, a.M, scale(c[i][j][4u * q]), scale(c[i][j][4u * q + 1u]),
+                                    scale(c[i][j][4u * q + 2u]), scale(c[i][j][4u * q + 3u]));
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+                    for (uint32_t q = 0; q < 4u; q += 2u) {
+                        uint16_t w[8];
+#pragma unroll
+                        for (uint32_t e = 0; e < 8u; ++e) w[e] = (uint16_t)Elem<F>::word(scale(c[i][j][4u * q + e]));
+                        put_eight(to, m_base + wm * (BM / WM) + i * 32u + (q + lane / 32u) * 8u, a.M, eight_of(w));
+                    }
+            }
         }
     }
 }
@@ -671,7 +716,6 @@ struct XentRound {
 template <int F>
 __device__ __forceinline__ void xent_round(const XentRound& a, uint32_t block)
 {
-    using El = Elem<F>;
     const uint32_t per = (a.dim + 3u) / 4u;       // of four entries
     const uint64_t i = (uint64_t)block * 256u + threadIdx.x;
     if (i >= (uint64_t)a.rows * per) return;

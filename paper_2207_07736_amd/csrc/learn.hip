@@ -235,7 +235,7 @@ void launch_round(const rlsim_learner* h, XentRound a, XentRound b)
 // Rows that the products can read where they are.
 bool as_they_are(const void* p, uint64_t stride, uint32_t dim)
 {
-    return dim % kXentK == 0u && on_boundary(p, 16u) && stride % 8u == 0u && stride <= 1u << 22;
+    return dim % 8u == 0u && on_boundary(p, 16u) && stride % 8u == 0u && stride <= 1u << 22;
 }
 
 template <int D, int F>
@@ -263,7 +263,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     const bool direct = P == 1u && as_they_are(x.matrix, x.matrix_stride, x.dim);
     XentGemm z{};                                 // the logits' product
     z.products = P == 1u ? 1u : 6u;
-    z.K = s.dim_k;
+    z.K = P == 1u ? x.dim : s.dim_k;
     z.vocab = x.vocab;
     z.N = x.rows;
     z.rows_k = s.rows_k;
@@ -312,7 +312,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         for (uint32_t v0 = 0u; v0 < x.vocab; v0 += width) {
             const uint32_t count = std::min(width, x.vocab - v0);
             piece(v0, count);
-            const XentTile t = xent_tile(count, x.rows, 0u, false, h->cus);
+            const XentTile t = xent_tile(count, x.rows, (uint64_t)s.dim_k / kXentK * z.products, false, h->cus);
             z.part0 = j.parts;
             launch_gemm<D, F, false, false, kXentLoss>(h, z, t);
             j.parts += (count + t.m - 1u) / t.m * (t.m / t.span);
@@ -356,7 +356,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         const uint32_t count = std::min(s.piece, x.vocab - v0);
         XentRound rx{}, rw{};
         piece(v0, count);
-        launch_gemm<D, F, false, false, kXentDz>(h, z, xent_tile(count, x.rows, 0u, false, h->cus));
+        launch_gemm<D, F, false, false, kXentDz>(h, z, xent_tile(count, x.rows, (uint64_t)s.dim_k / kXentK * z.products, false, h->cus));
         if (x.dhidden) {
             gx.A = z.A;
             gx.part_a = z.part_a;

@@ -70,7 +70,7 @@ constexpr uint32_t kXentShareTiles = 1024u;
 inline XentTile xent_tile(uint32_t M, uint32_t N, uint64_t steps, bool sums, uint32_t cus)
 {
     const uint64_t big = ((M + 255ull) / 256u) * ((N + 255ull) / 256u);
-    XentTile t = N <= 32u ? XentTile{128u, 32u, 32u, 1u} : big >= cus ? XentTile{256u, 256u, 128u, 1u} : XentTile{128u, 128u, 64u, 1u};
+    XentTile t = N <= 32u ? XentTile{128u, 32u, 32u, 1u} : big >= cus && steps >= 8u ? XentTile{256u, 256u, 128u, 1u} : XentTile{128u, 128u, 64u, 1u};
     const uint64_t tiles = (uint64_t)((M + t.m - 1u) / t.m) * ((N + t.n - 1u) / t.n), wanted = 2ull * cus;
     if (!sums || tiles >= wanted || t.m == 256u) return t;
     const uint64_t s = least(least(wanted / tiles, steps / 4u), least(kXentShareTiles / tiles, 64u));

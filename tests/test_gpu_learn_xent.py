@@ -39,14 +39,14 @@ def _check(learner, hidden, matrix, target, weight=None):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,dim,V", [(1, 1, 1), (1, 64, 2), (3, 5, 7), (7, 64, 300), (17, 100, 1000), (33, 33, 257),
+@pytest.mark.parametrize("rows,dim,V", [(1, 1, 1), (1, 64, 2), (3, 5, 7), (7, 64, 300), (17, 100, 1000), (33, 33, 257), (40, 8, 300), (300, 40, 520),
                                         (32, 128, 129), (64, 192, 64), (130, 65, 515), (257, 320, 777), (1000, 16, 2)])
 def test_sizes(learner, rows, dim, V, dtype):
     _check(learner, *_inputs(rows, dim, V, dtype, seed=rows + V))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,dim,V", [(2049, 1024, 8200), (2000, 1001, 20000), (5, 1024, 20000)])
+@pytest.mark.parametrize("rows,dim,V", [(2049, 1024, 8200), (2000, 1001, 20000), (5, 1024, 20000), (700, 1000, 9001)])
 def test_larger(learner, rows, dim, V, dtype):
     _check(learner, *_inputs(rows, dim, V, dtype, seed=1))
 
@@ -128,6 +128,18 @@ def test_padded_rows_may_hold_anything(learner, dtype):
     assert torch.isnan(loss[live]) and torch.isnan(dhidden[live]).all() and torch.isnan(dmatrix[:, :]).all()
     others = ~out & (torch.arange(60, device="cuda") != live) & (weight != 0)
     assert torch.equal(loss[others], want[0][others]) and torch.equal(dhidden[others], want[1][others])
+
+
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float16))
+def test_rows_that_end_within_a_step_keep_to_themselves(learner, dtype):
+    """Rows of 40 entries inside wider arrays of NaN: nothing behind a row's end is used."""
+    hidden, matrix, target, weight = _inputs(50, 40, 300, dtype)
+    wide_h = torch.full((50, 72), float("nan"), device="cuda", dtype=dtype)
+    wide_m = torch.full((300, 72), float("nan"), device="cuda", dtype=dtype)
+    wide_h[:, 8:48], wide_m[:, 8:48] = hidden, matrix
+    want = _check(learner, hidden, matrix, target, weight)
+    for a, b in zip(want, learner.cross_entropy(wide_h[:, 8:48], wide_m[:, 8:48], target, weight)):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("rows", (7, 100))

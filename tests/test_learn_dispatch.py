@@ -59,12 +59,12 @@ int main()
             uint64_t all = 0;
             for (uint32_t v0 = 0; v0 < v; v0 += s.piece) {
                 const uint32_t n = s.piece < v - v0 ? s.piece : v - v0;
-                const XentTile t = xent_tile(n, r, 0u, false, cus);
+                const XentTile t = xent_tile(n, r, s.dim_k / kXentK * (parts == 1u ? 1u : 6u), false, cus);
                 CHECK(t.share == 1u && t.m % t.span == 0u);
                 all += (n + t.m - 1u) / t.m * (t.m / t.span);
             }
             CHECK(8ull * all * s.rows_k <= o.x - o.part);
-            const XentTile t = xent_tile(v, r, 0u, false, cus);
+            const XentTile t = xent_tile(v, r, s.dim_k / kXentK * (parts == 1u ? 1u : 6u), false, cus);
             CHECK(8ull * ((v + t.m - 1u) / t.m * (t.m / t.span)) * s.rows_k <= o.x - o.part);
         }
     }
