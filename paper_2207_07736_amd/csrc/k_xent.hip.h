@@ -388,9 +388,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     x.open(wm * (BM / WM), lane);
     y.open(wn * (BN / WN), lane);
 
-    // Four steps of 32 k are in LDS or under way.  While a half step of 16 k is multiplied,
-    // the next one's fragments are read; the workgroup meets once a step, after which the
-    // step just read may be overwritten and the next one, loaded three steps ago, read.
+    // Up to four steps of 32 k are in LDS or under way.  While a half step of 16 k is
+    // multiplied, the next one's fragments are read; the workgroup meets once, in the middle
+    // of a step, after which the next one may be read.
     auto cut = [&](auto half, uint32_t t) {       // (parts of fp32 are copies that end with whole steps)
         constexpr uint32_t H = decltype(half)::value;
         if (F == kHeadF32 || a.K >= t * 32u + 32u) return;
@@ -400,8 +400,6 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     auto one_step = [&](auto steady, uint32_t t, char* now, char* next, char* ahead) {
         constexpr bool kSteady = decltype(steady)::value;        // three more steps are to come
         reads_done();                             // of the first half
-        if (kSteady) fetch(std::false_type{}, ahead);
-        else if (t + 3u < last) fetch(std::true_type{}, ahead);
         x.template read<1>(now);
         y.template read<1>(now + OpA::kBytes);
         if (!kSteady) cut(std::integral_constant<uint32_t, 1u>{}, t);
@@ -409,13 +407,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
             for (uint32_t j = 0; j < FN; ++j) c[i][j] = Matrix<D>::mma(x.v[0][i], y.v[0][j], c[i][j]);
-        mix<FM * FN, kReads, kSteady ? kEach : 0>();
+        mix<FM * FN, kReads, 0>();
         __builtin_amdgcn_sched_barrier(0);
-        if (kSteady || t + 3u < last) loads_left<2 * kEach>();
-        else if (t + 2u < last) loads_left<kEach>();
+        if (kSteady || t + 2u < last) loads_left<kEach>();       // the next step has arrived
         else loads_left<0>();
         reads_done();
         meet();
+        if (kSteady) fetch(std::false_type{}, ahead);
+        else if (t + 3u < last) fetch(std::true_type{}, ahead);
         if (kSteady || t + 1u < last) {
             x.template read<0>(next);
             y.template read<0>(next + OpA::kBytes);
@@ -425,7 +424,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
             for (uint32_t j = 0; j < FN; ++j) c[i][j] = Matrix<D>::mma(x.v[1][i], y.v[1][j], c[i][j]);
-        mix<FM * FN, kReads, 0>();
+        mix<FM * FN, kReads, kSteady ? kEach : 0>();
         __builtin_amdgcn_sched_barrier(0);
     };
     if (first < last) {
