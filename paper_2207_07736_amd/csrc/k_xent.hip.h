@@ -44,6 +44,25 @@ struct XentTarget {
     }
 };
 
+constexpr int kDzUp = 14;                         // see XentRefs
+
+// A gradient's last factor: 0 for dhidden's rows that do not count, whatever the product
+// is, and their weight where dz is without it; the power of two that dz was scaled by.
+struct OutScale {
+    const XentRow* row;                           // dhidden, or null
+    const int32_t* ref;                           // dz carries 2^(kDzUp - *ref), or null
+    int32_t up;                                   // else the result is due 2^up
+    uint32_t weigh;
+    __device__ __forceinline__ float operator()(float x, uint32_t n) const
+    {
+        if (row) {
+            if (row[n].target < 0) return 0.0f;
+            if (weigh) x *= row[n].weight;
+        }
+        return ldexpf(x, ref ? *ref - kDzUp : up);
+    }
+};
+
 struct XentGemm {
     const char* A;
     const char* B;
@@ -60,16 +79,19 @@ struct XentGemm {
     float* zt;
     uint32_t part0, rows_k;
     const XentRow* row;                           // logits, gradient
-    const float* wmax;
+    const int32_t* up_n;                          // fp32: exponents of the rows of hidden and of matrix,
+    const int32_t* up_m;                          // what a factor was divided by
+    const int32_t* refs;                          // fp16, fp32: XentRefs' results
     char* dz;                                     // [parts][rows_k][piece], with the rows' weights
-    char* dz_plain;                               // fp16: without them, or null
+    char* dz_plain;                               // fp16, fp32: without them (for dhidden), or null
     uint64_t dz_ld, dz_part;                      // bytes
     float* sum;                                   // gradients' products: [share][N][sum_ld]
     uint64_t sum_ld, sum_share;                   // elements
     uint32_t add;                                 // to what is there
+    const int32_t* sum_ref;                       // fp32, dhidden: refs' entry of the piece, or null
     char* out;                                    // gradients' products, rounded: [N][M]
     uint64_t out_ld;                              // bytes
-    const XentRow* out_row;                       // dhidden: a row's weight
+    OutScale scale;
 };
 
 // What becomes of a tile: softmax sums, the logits' gradient, fp32 sums, a gradient.
@@ -89,28 +111,17 @@ template <> struct Matrix<kHeadF16> {
     }
 };
 
-// fp32 as a sum of three bf16 parts of 8 bits each (what is not finite stays in the first).
-__device__ __forceinline__ void cut3(float x, uint16_t (&p)[3])
+// fp32 (scaled to below 2^15) as a sum of two fp16 parts: to 22 bits at worst, and to 2^-25
+// where it is small.  What is not finite stays in the first.
+__device__ __forceinline__ void cut2(float x, uint16_t& hi, uint16_t& lo)
 {
-    p[0] = Elem<kHeadBF16>::word(x);
-    const float r1 = x - Elem<kHeadBF16>::one(p[0]);
-    const bool fine = __builtin_fabsf(r1) < __builtin_inff();      // false for NaN too
-    p[1] = fine ? Elem<kHeadBF16>::word(r1) : (uint16_t)0;
-    const float r2 = r1 - Elem<kHeadBF16>::one(p[1]);
-    p[2] = fine ? Elem<kHeadBF16>::word(r2) : (uint16_t)0;
+    hi = Elem<kHeadF16>::word(x);
+    const float rest = x - Elem<kHeadF16>::one(hi);
+    lo = __builtin_fabsf(rest) < __builtin_inff() ? Elem<kHeadF16>::word(rest) : (uint16_t)0;
 }
 
-// dz of fp16 factors is kept times 2^14, as probabilities below 2^-14 would lose bits.
-constexpr float kDzUp = 16384.0f, kDzDown = 1.0f / 16384.0f;
-// The power of two that brings the largest weight to [1/2, 1), for fp16.
-// (No weights: 1.)
-__device__ __forceinline__ float weight_scale(const float* wmax)
-{
-    if (!wmax) return 1.0f;
-    const int e = (int)(__builtin_bit_cast(uint32_t, *wmax) >> 23 & 0xFFu);
-    if (e == 0 || e == 255) return 1.0f;          // none, denormal or not finite
-    return __builtin_bit_cast(float, (uint32_t)(min(max(253 - e, 1), 254)) << 23);
-}
+// The exponent e of a finite x: |x| < 2^(e + 1) (of 0 and of denormals -127).
+__device__ __forceinline__ int exponent_of(float x) { return (int)(__builtin_bit_cast(uint32_t, x) >> 23 & 0xFFu) - 127; }
 
 // Lane l has entries 0 .. 3 of two blocks of 8, lane l + 32 entries 4 .. 7 of both: lane l
 // gets the first block whole, lane l + 32 the second.
@@ -124,20 +135,6 @@ __device__ __forceinline__ u32x4 eight_of(const uint16_t (&w)[8])
 }
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
-
-// A gradient's last factor: 0 for dhidden's rows that do not count, whatever the product
-// is; of fp16 what dz was scaled by, and the row's weight where dz is without it.
-template <int F>
-struct OutScale {
-    float by = 1.0f;
-    bool counts = true;
-    __device__ __forceinline__ OutScale(const XentRow* row, const float* wmax, uint32_t n)
-    {
-        if (row) counts = row[n].target >= 0;
-        if (F == kHeadF16) by = row ? row[n].weight * kDzDown : kDzDown / weight_scale(wmax);
-    }
-    __device__ __forceinline__ float operator()(float x) const { return counts ? x * by : 0.0f; }
-};
 
 // Entries m .. m + 3 of a row of M, rounded.
 template <int F>
@@ -307,7 +304,7 @@ __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
-// D: the type of the factors' (parts'), F: of the call (fp32: three parts); AA, BA: whether
+// D: the type of the factors (parts), F: of the call (fp32: two parts); AA, BA: whether
 // A and B lie across.
 template <int D, int F, int BM, int BN, int WM, int WN, bool AA, bool BA, int EPI>
 __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
@@ -347,15 +344,15 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     const char* const B0 = a.B + OpB::first(n_base, a.N, a.ldb);
     const uint64_t step_a = AA ? 32u * a.lda : 64u, step_b = BA ? 32u * a.ldb : 64u;
 
-    // the parts of product p, small products first: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
+    // the parts of product p, small products first: (1,0) (0,1) (0,0)
     const uint32_t all = a.steps * a.products;
     const uint32_t first = (uint32_t)((uint64_t)all * blockIdx.y / a.share);
     const uint32_t last = (uint32_t)((uint64_t)all * (blockIdx.y + 1u) / a.share);
     uint32_t product = first / a.steps, step = first % a.steps;
     const char *pa, *pb;
     auto locate = [&]() {
-        const uint32_t i = a.products == 1u ? 0u : 0x001012u >> (4u * product) & 15u;
-        const uint32_t j = a.products == 1u ? 0u : 0x010210u >> (4u * product) & 15u;
+        const uint32_t i = a.products == 1u ? 0u : product == 0u;
+        const uint32_t j = a.products == 1u ? 0u : product == 1u;
         pa = A0 + i * a.part_a + step * step_a;
         pb = B0 + j * a.part_b + step * step_b;
     };
@@ -461,6 +458,24 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     }
 
     const uint32_t m_wave = m_base + wm * (BM / WM) + 4u * (lane / 32u);
+    if (F == kHeadF32 && (EPI == kXentLoss || EPI == kXentDz)) {
+        // the logits: what the factors were divided by comes back
+        int up_n[FN];
+#pragma unroll
+        for (uint32_t j = 0; j < FN; ++j) up_n[j] = a.up_n[min(n_base + wn * (BN / WN) + j * 32u + lane % 32u, a.N - 1u)];
+#pragma unroll
+        for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+            for (uint32_t q = 0; q < 4u; ++q) {
+                const int4 up = *reinterpret_cast<const int4*>(a.up_m + m_wave + i * 32u + q * 8u);
+                const int up_m[4] = {up.x, up.y, up.z, up.w};
+#pragma unroll
+                for (uint32_t j = 0; j < FN; ++j)
+#pragma unroll
+                    for (uint32_t e = 0; e < 4u; ++e) c[i][j][4u * q + e] = ldexpf(c[i][j][4u * q + e], up_n[j] + up_m[e]);
+                __builtin_amdgcn_sched_barrier(0);        // few of these loads at a time: registers
+            }
+    }
 #pragma unroll
     for (uint32_t j = 0; j < FN; ++j) {
         const uint32_t n = n_base + wn * (BN / WN) + j * 32u + lane % 32u;
@@ -490,8 +505,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         if (EPI == kXentDz) {
             XentRow r{0.0f, 0.0f, 0.0f, -1};
             if (n < a.N) r = a.row[n];
-            const float up = F == kHeadF16 ? kDzUp : 1.0f;
-            const float weight = F == kHeadF16 ? r.weight * weight_scale(a.wmax) * kDzUp : r.weight;
+            // fp16 and fp32: by powers of two, to below 2^kDzUp over the rows (with weights; fp32 also
+            // with what the row of hidden was divided by) or over the piece (without weights)
+            int up = F == kHeadBF16 ? 0 : kDzUp - a.refs[0];
+            if (F == kHeadF32) up += a.up_n[min(n, a.N - 1u)];
+            const float weight = r.weight;
 #pragma unroll
             for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
@@ -510,24 +528,31 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                 for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
                     for (uint32_t q = 0; q < 4u; q += 2u) {
-                        uint16_t w[3][8], plain[8];
+                        uint16_t w[2][8], plain[2][8];
+                        int up_m[8];
+                        if (F == kHeadF32) {
+#pragma unroll
+                            for (uint32_t e = 0; e < 8u; ++e) up_m[e] = a.up_m[m_wave + i * 32u + (q + e / 4u) * 8u + e % 4u] + kDzUp - a.refs[1];
+                        }
 #pragma unroll
                         for (uint32_t e = 0; e < 8u; ++e) {
                             const float p = c[i][j][4u * q + e];
                             const float pw = p == 0.0f ? 0.0f : p * weight;
-                            uint16_t cut[3];
-                            if (F == kHeadF32) cut3(pw, cut);
-                            else cut[0] = Elem<D>::word(pw);
-#pragma unroll
-                            for (uint32_t s = 0; s < (F == kHeadF32 ? 3u : 1u); ++s) w[s][e] = cut[s];
-                            plain[e] = F == kHeadF16 ? Elem<D>::word(p * up) : (uint16_t)0;
+                            if (F == kHeadF32) {
+                                cut2(ldexpf(pw, up), w[0][e], w[1][e]);
+                                cut2(ldexpf(p, up_m[e]), plain[0][e], plain[1][e]);
+                            } else {
+                                w[0][e] = Elem<D>::word(F == kHeadF16 ? ldexpf(pw, up) : pw);
+                                plain[0][e] = F == kHeadF16 ? Elem<D>::word(ldexpf(p, kDzUp)) : (uint16_t)0;
+                            }
                         }
                         const uint64_t m = m_base + wm * (BM / WM) + i * 32u + (q + lane / 32u) * 8u;
 #pragma unroll
-                        for (uint32_t s = 0; s < (F == kHeadF32 ? 3u : 1u); ++s)
+                        for (uint32_t s = 0; s < (F == kHeadF32 ? 2u : 1u); ++s) {
                             *reinterpret_cast<u32x4*>(to + s * a.dz_part + 2u * m) = eight_of(w[s]);
-                        if (F == kHeadF16 && a.dz_plain)
-                            *reinterpret_cast<u32x4*>(a.dz_plain + n * a.dz_ld + 2u * m) = eight_of(plain);
+                            if (F != kHeadBF16 && a.dz_plain)
+                                *reinterpret_cast<u32x4*>(a.dz_plain + n * a.dz_ld + s * a.dz_part + 2u * m) = eight_of(plain[s]);
+                        }
                     }
             }
         }
@@ -540,6 +565,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                     if (n < a.N && m < a.sum_ld) {        // sum_ld: M up to a multiple of 4
                         float4* to = reinterpret_cast<float4*>(a.sum + blockIdx.y * a.sum_share + n * a.sum_ld + m);
                         float4 s{c[i][j][4u * q], c[i][j][4u * q + 1u], c[i][j][4u * q + 2u], c[i][j][4u * q + 3u]};
+                        if (F == kHeadF32 && a.sum_ref) {        // pieces are scaled each by its own power of two
+                            const int up = *a.sum_ref - kDzUp;
+                            s = float4{ldexpf(s.x, up), ldexpf(s.y, up), ldexpf(s.z, up), ldexpf(s.w, up)};
+                        }
                         if (a.add) {
                             const float4 old = *to;
                             s.x += old.x, s.y += old.y, s.z += old.z, s.w += old.w;
@@ -549,7 +578,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                 }
         }
         if (EPI == kXentOut && n < a.N) {
-            const OutScale<F> scale(a.out_row, a.wmax, n);
+            auto scale = [&](float x) { return F == kHeadBF16 ? x : a.scale(x, n); };
             char* const to = a.out + n * a.out_ld;
             if (F == kHeadF32) {
 #pragma unroll
@@ -625,21 +654,55 @@ __device__ __forceinline__ void xent_join(const XentJoin& a, uint32_t block)
     }
 }
 
-// The largest finite |weight| of the rows that count.
-__global__ __launch_bounds__(1024) void k_xent_wmax(XentTarget target, const float* weight, uint32_t rows, float* wmax)
+// The powers of two that dz of fp16 and fp32 calls is scaled by, so that the largest that it
+// can be is just below 2^kDzUp (a probability below 2^-14 would lose bits of fp16):
+//   out[0]  for dmatrix, a bound of |weight| 2^up_n over the rows that count
+//   out[1]  for dhidden (fp32), of 2^up_m over the piece
+struct XentRefs {
+    XentTarget target;
+    const float* weight;
+    const int32_t* up_n;                          // or null
+    const int32_t* up_m;                          // or null
+    uint32_t rows, count;
+    int32_t* out;                                 // null: none is wanted
+};
+__device__ __forceinline__ void xent_refs(const XentRefs& a)
 {
-    __shared__ float sh[16];
-    float top = 0.0f;
-    for (uint32_t r = threadIdx.x; r < rows; r += 1024u) {
-        const float w = __builtin_fabsf(weight[r]);
-        if (w < __builtin_inff() && target(r) >= 0) top = __builtin_fmaxf(top, w);
+    __shared__ uint32_t sh[2][4];
+    uint32_t top_n = 0u, top_m = 0u;              // exponents and 1024
+    for (uint32_t r = threadIdx.x; r < a.rows; r += 256u) {
+        const float w = a.weight ? a.weight[r] : 1.0f;
+        if (__builtin_fabsf(w) < __builtin_inff() && w != 0.0f && a.target(r) >= 0)
+            top_n = max(top_n, (uint32_t)(1024 + exponent_of(w) + 1 + (a.up_n ? a.up_n[r] : 0)));
     }
-    top = group_max<16>(top, sh);
-    if (threadIdx.x == 0u) *wmax = top;
+    if (a.up_m) {
+#pragma unroll 4
+        for (uint32_t v = 4u * threadIdx.x; v < a.count; v += 1024u) {
+            const int4 up = *reinterpret_cast<const int4*>(a.up_m + v);          // whole fours: copies end with steps
+            top_m = max(top_m, (uint32_t)(1024 + max(max(up.x, up.y), max(up.z, up.w))));
+        }
+    }
+    top_n = wave_max(top_n);
+    top_m = wave_max(top_m);
+    if (threadIdx.x % 64u == 0u) {
+        sh[0][threadIdx.x / 64u] = top_n;
+        sh[1][threadIdx.x / 64u] = top_m;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0u) {
+        for (uint32_t w = 1; w < 4u; ++w) {
+            top_n = max(top_n, sh[0][w]);
+            top_m = max(top_m, sh[1][w]);
+        }
+        a.out[0] = top_n ? (int)top_n - 1024 : 0;
+        a.out[1] = top_m ? (int)top_m - 1024 : 0;
+    }
 }
+__global__ __launch_bounds__(256) void k_xent_refs(XentRefs a) { xent_refs(a); }
 
-// Rows as the products read them: whole steps wide, fp32 in three parts; rows that do not
-// count are 0 where they are told.
+// Rows as the products read them: whole steps wide; rows that do not count are 0 where they
+// are told.  fp32 rows are divided by a power of two, so that the largest entry is between
+// 2^14 and 2^15, and cut in two parts.
 struct XentLay {
     const char* from;                             // [R][C]
     uint64_t ld;                                  // bytes
@@ -648,21 +711,69 @@ struct XentLay {
     uint64_t part;                                // bytes
     XentTarget target;                            // p null: all rows count
     const float* weight;
+    int32_t* up;                                  // fp32: [tall] exponents of what rows were divided by, or null
     uint32_t blocks;
+    __device__ __forceinline__ bool counts(uint32_t r) const
+    {
+        return r < R && (!target.p || (target(r) >= 0 && !(weight && weight[r] == 0.0f)));
+    }
 };
+// fp32: a wave to a row.
+__device__ __forceinline__ void xent_lay32(const XentLay& a, uint32_t block)
+{
+    struct __attribute__((packed, aligned(4))) Four { float x[4]; };
+    const uint32_t lane = threadIdx.x % 64u;
+    for (uint32_t r = uniform(block * 4u + threadIdx.x / 64u); r < a.tall; r += a.blocks * 4u) {
+        const float* const from = reinterpret_cast<const float*>(a.from + r * a.ld);
+        const bool counts = a.counts(r);
+        auto load = [&](uint32_t c) {
+            Four f{};
+            if (counts && c + 4u <= a.C) {
+                f = *reinterpret_cast<const Four*>(from + c);
+            } else if (counts) {
+#pragma unroll
+                for (uint32_t e = 0; e < 3u; ++e)
+                    if (c + e < a.C) f.x[e] = from[c + e];
+            }
+            return f;
+        };
+        uint32_t top = 0u;                        // of the finite ones, as bits
+        for (uint32_t c = 4u * lane; c < a.C; c += 256u) {
+            const Four f = load(c);
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; ++e) {
+                const uint32_t bits = __builtin_bit_cast(uint32_t, f.x[e]) & 0x7FFFFFFFu;
+                top = max(top, bits < 0x7F800000u ? bits : 0u);
+            }
+        }
+        top = wave_max(top);
+        const int up = top ? exponent_of(__builtin_bit_cast(float, top)) - 14 : -500;     // a row of 0 sets no scale
+        if (lane == 0u && a.up) a.up[r] = up;
+        for (uint32_t c = 4u * lane; c < a.wide; c += 256u) {
+            const Four f = load(c);
+            uint16_t hi[4], lo[4];
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; ++e) cut2(ldexpf(f.x[e], -up), hi[e], lo[e]);
+            char* const to = a.to + ((uint64_t)r * a.wide + c) * 2u;
+            *reinterpret_cast<uint2*>(to) = uint2{hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16};
+            *reinterpret_cast<uint2*>(to + a.part) = uint2{lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16};
+        }
+    }
+}
 template <int F>
 __device__ __forceinline__ void xent_lay(const XentLay& a, uint32_t block)
 {
-    using El = Elem<F>;
-    constexpr uint32_t P = F == kHeadF32 ? 3u : 1u;
+    if (F == kHeadF32) {
+        xent_lay32(a, block);
+        return;
+    }
     const uint32_t per = a.wide / 8u;
     const uint64_t all = (uint64_t)a.tall * per;
     for (uint64_t i = (uint64_t)block * 256u + threadIdx.x; i < all; i += (uint64_t)a.blocks * 256u) {
         const uint32_t r = (uint32_t)(i / per), c = (uint32_t)(i % per) * 8u;
-        uint16_t w[P][8] = {};
-        if (r < a.R && (!a.target.p || (a.target(r) >= 0 && !(a.weight && a.weight[r] == 0.0f)))) {
-            struct __attribute__((packed, aligned(El::kBytes))) Eight { typename El::Word w[8]; } x{};
-            const auto* from = reinterpret_cast<const typename El::Word*>(a.from + r * a.ld) + c;
+        struct __attribute__((packed, aligned(2))) Eight { uint16_t w[8]; } x{};
+        if (a.counts(r)) {
+            const auto* from = reinterpret_cast<const uint16_t*>(a.from + r * a.ld) + c;
             if (c + 8u <= a.C) {
                 x = *reinterpret_cast<const Eight*>(from);
             } else {
@@ -670,23 +781,12 @@ __device__ __forceinline__ void xent_lay(const XentLay& a, uint32_t block)
                 for (uint32_t e = 0; e < 7u; ++e)
                     if (c + e < a.C) x.w[e] = from[e];
             }
-#pragma unroll
-            for (uint32_t e = 0; e < 8u; ++e) {
-                uint16_t cut[3] = {(uint16_t)x.w[e], 0, 0};
-                if (F == kHeadF32) cut3(El::one(x.w[e]), cut);
-#pragma unroll
-                for (uint32_t p = 0; p < P; ++p) w[p][e] = cut[p];
-            }
         }
-#pragma unroll
-        for (uint32_t p = 0; p < P; ++p)
-            *reinterpret_cast<u32x4*>(a.to + p * a.part + i * 16u) =
-                u32x4{w[p][0] | (uint32_t)w[p][1] << 16, w[p][2] | (uint32_t)w[p][3] << 16,
-                      w[p][4] | (uint32_t)w[p][5] << 16, w[p][6] | (uint32_t)w[p][7] << 16};
+        *reinterpret_cast<u32x4*>(a.to + i * 16u) = __builtin_bit_cast(u32x4, x);
     }
 }
 
-// Two copies in one launch, or the rows' sums and a copy.
+// Two copies in one launch, or the rows' sums, a copy and the powers of two.
 template <int F>
 __global__ __launch_bounds__(256) void k_xent_lays(XentLay a, XentLay b)
 {
@@ -694,11 +794,12 @@ __global__ __launch_bounds__(256) void k_xent_lays(XentLay a, XentLay b)
     else xent_lay<F>(b, blockIdx.x - a.blocks);
 }
 template <int F>
-__global__ __launch_bounds__(256) void k_xent_join(XentJoin a, XentLay b)
+__global__ __launch_bounds__(256) void k_xent_join(XentJoin a, XentLay b, XentRefs c)
 {
     const uint32_t blocks = (a.rows + kJoinRows - 1u) / kJoinRows;
     if (blockIdx.x < blocks) xent_join(a, blockIdx.x);
-    else xent_lay<F>(b, blockIdx.x - blocks);
+    else if (blockIdx.x < blocks + b.blocks) xent_lay<F>(b, blockIdx.x - blocks);
+    else xent_refs(c);
 }
 
 // A gradient from its shares: summed in order, scaled, rounded once.
@@ -706,8 +807,7 @@ struct XentRound {
     const float* sum;
     uint64_t ld, share_ld;
     uint32_t share, rows, dim;
-    const XentRow* row;                           // dhidden: rows that do not count are 0; fp16: a row's weight
-    const float* wmax;                            // dmatrix of fp16: the weights' scale
+    OutScale scale;
     char* out;
     uint64_t out_ld;                              // bytes
     uint32_t blocks;
@@ -725,8 +825,7 @@ __device__ __forceinline__ void xent_round(const XentRound& a, uint32_t block)
         const float4 x = *reinterpret_cast<const float4*>(a.sum + k * a.share_ld + n * a.ld + d);
         s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
     }
-    const OutScale<F> scale(a.row, a.wmax, n);
-    put_four<F>(a.out + n * a.out_ld, d, a.dim, scale(s.x), scale(s.y), scale(s.z), scale(s.w));
+    put_four<F>(a.out + n * a.out_ld, d, a.dim, a.scale(s.x, n), a.scale(s.y, n), a.scale(s.z, n), a.scale(s.w, n));
 }
 template <int F>
 __global__ __launch_bounds__(256) void k_xent_round(XentRound a, XentRound b)

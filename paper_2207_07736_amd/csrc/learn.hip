@@ -214,13 +214,18 @@ void launch_gemm(const rlsim_learner* h, XentGemm a, const XentTile& t)
 }
 
 // A copy's workgroups; none for one that is not made.
-uint32_t lay_blocks(const XentLay& a) { return (uint32_t)std::min<uint64_t>(((uint64_t)a.tall * (a.wide / 8u) + 255u) / 256u, 1u << 21); }
+template <int F>
+uint32_t lay_blocks(const XentLay& a)
+{
+    const uint64_t blocks = F == kHeadF32 ? (a.tall + 3ull) / 4u : ((uint64_t)a.tall * (a.wide / 8u) + 255u) / 256u;
+    return (uint32_t)std::min<uint64_t>(blocks, 1u << 21);
+}
 
 template <int F>
 void launch_lays(const rlsim_learner* h, XentLay a, XentLay b)
 {
-    a.blocks = lay_blocks(a);
-    b.blocks = lay_blocks(b);
+    a.blocks = lay_blocks<F>(a);
+    b.blocks = lay_blocks<F>(b);
     if (a.blocks + b.blocks) hipLaunchKernelGGL(k_xent_lays<F>, dim3(a.blocks + b.blocks), dim3(256), 0, h->stream, a, b);
 }
 
@@ -241,7 +246,7 @@ bool as_they_are(const void* p, uint64_t stride, uint32_t dim)
 template <int D, int F>
 void run_xent(const rlsim_learner* h, const rlsim_xent& x)
 {
-    constexpr uint32_t P = F == kHeadF32 ? 3u : 1u;
+    constexpr uint32_t P = F == kHeadF32 ? 2u : 1u;
     constexpr uint64_t e = F == kHeadF32 ? 4u : 2u;
     const XentShape s = xent_shape(x.rows, x.dim, x.vocab, P);
     const XentWork o = xent_work(s);
@@ -253,16 +258,14 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     const bool grad = x.dhidden || x.dmatrix;
     const XentTarget target{x.target, x.target_bytes, x.vocab};
     const char* const matrix = static_cast<const char*>(x.matrix);
-    float* wmax = nullptr;
-    if (F == kHeadF16 && grad && x.weight) {
-        wmax = reinterpret_cast<float*>(w + o.wmax);
-        hipLaunchKernelGGL(k_xent_wmax, dim3(1), dim3(1024), 0, h->stream, target, x.weight, x.rows, wmax);
-    }
+    auto* up_n = reinterpret_cast<int32_t*>(w + o.up_n);
+    auto* up_m = reinterpret_cast<int32_t*>(w + o.up_m);
+    auto* refs = reinterpret_cast<int32_t*>(w + o.refs);
 
     const bool hidden_direct = P == 1u && as_they_are(x.hidden, x.hidden_stride, x.dim);
     const bool direct = P == 1u && as_they_are(x.matrix, x.matrix_stride, x.dim);
     XentGemm z{};                                 // the logits' product
-    z.products = P == 1u ? 1u : 6u;
+    z.products = P == 1u ? 1u : 3u;
     z.K = P == 1u ? x.dim : s.dim_k;
     z.vocab = x.vocab;
     z.N = x.rows;
@@ -271,7 +274,9 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     z.part = part;
     z.zt = zt;
     z.row = row;
-    z.wmax = wmax;
+    z.up_n = up_n;
+    z.up_m = up_m;
+    z.refs = refs;
     z.B = hidden_direct ? static_cast<const char*>(x.hidden) : w + o.x;
     z.ldb = hidden_direct ? x.hidden_stride * e : 2ull * s.dim_k;
     z.part_b = 2ull * s.dim_k * x.rows;
@@ -279,7 +284,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     XentLay hidden_lay{};                         // made with the first piece of the matrix
     if (!hidden_direct)
         hidden_lay = XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, x.rows, w + o.x,
-                             z.part_b, {}, nullptr, 0u};
+                             z.part_b, {}, nullptr, up_n, 0u};
 
     // The piece of the vocabulary from v0, as the products read it.
     uint32_t laid = ~0u;                          // the piece that is copied now
@@ -292,7 +297,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         XentLay l{};
         if (!direct && laid != v0)
             l = XentLay{from, x.matrix_stride * e, count, x.dim, s.dim_k, (uint32_t)up_to(count, kXentK), w + o.w, z.part_a,
-                        {}, nullptr, 0u};
+                        {}, nullptr, up_m, 0u};
         launch_lays<F>(h, hidden_lay, l);
         hidden_lay = XentLay{};
         laid = v0;
@@ -319,16 +324,22 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         }
         j.part = part;
     }
+    // before a call for gradients alone, the first piece's copies
+    if (!x.loss && F == kHeadF32) piece(0u, std::min(s.piece, x.vocab));
     XentLay l{};                                  // for dmatrix: rows that do not count may hold anything
     if (x.dmatrix)
         l = XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, s.rows_k, w + o.xm,
-                    2ull * s.dim_k * s.rows_k, target, x.weight, 0u};
-    l.blocks = lay_blocks(l);
-    hipLaunchKernelGGL(k_xent_join<F>, dim3((x.rows + kJoinRows - 1u) / kJoinRows + l.blocks), dim3(256), 0, h->stream, j, l);
+                    2ull * s.dim_k * s.rows_k, target, x.weight, nullptr, 0u};
+    l.blocks = lay_blocks<F>(l);
+    // fp16, fp32: dz's powers of two (fp32: of the piece that the loss left in the copy)
+    XentRefs refs_of{target, x.weight, F == kHeadF32 ? up_n : nullptr, F == kHeadF32 ? up_m : nullptr, x.rows,
+                     z.M, F != kHeadBF16 && grad ? refs : nullptr};
+    hipLaunchKernelGGL(k_xent_join<F>, dim3((x.rows + kJoinRows - 1u) / kJoinRows + l.blocks + (refs_of.out ? 1u : 0u)), dim3(256), 0,
+                       h->stream, j, l, refs_of);
     if (!grad) return;
 
     const uint64_t dim4 = up_to(x.dim, 4u);
-    const bool plain = F == kHeadF16 && x.weight && x.dhidden;
+    const bool plain = F == kHeadF32 ? x.dhidden != nullptr : F == kHeadF16 && x.weight && x.dhidden;
     z.dz = w + o.dz;
     z.dz_plain = plain ? w + o.dz_plain : nullptr;
     z.dz_ld = 2ull * s.piece;
@@ -337,7 +348,12 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     gx.products = gw.products = z.products;
     gx.M = gw.M = x.dim;
     gx.sum_ld = gw.sum_ld = dim4;
-    gx.wmax = gw.wmax = wmax;
+    const int32_t* const ref = F == kHeadBF16 ? nullptr : refs;
+    // what the products are short of (fp32's dhidden: its sums are not)
+    const OutScale scale_x = plain ? OutScale{row, nullptr, F == kHeadF16 ? -kDzUp : 0, 1u} : OutScale{row, ref, 0, 0u};
+    const OutScale scale_w{nullptr, ref, 0, 0u};
+    gx.sum_ref = F == kHeadF32 ? refs + 1 : nullptr;
+    gw.scale = scale_w;
     gx.lda = z.lda;
     gx.B = plain ? z.dz_plain : z.dz;
     gx.ldb = gw.ldb = z.dz_ld;
@@ -355,7 +371,12 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     for (uint32_t v0 = 0u; v0 < x.vocab; v0 += s.piece) {
         const uint32_t count = std::min(s.piece, x.vocab - v0);
         XentRound rx{}, rw{};
+        const bool anew = laid != v0;
         piece(v0, count);
+        if (F == kHeadF32 && anew) {
+            refs_of.count = count;
+            hipLaunchKernelGGL(k_xent_refs, dim3(1), dim3(256), 0, h->stream, refs_of);
+        }
         launch_gemm<D, F, false, false, kXentDz>(h, z, xent_tile(count, x.rows, (uint64_t)s.dim_k / kXentK * z.products, false, h->cus));
         if (x.dhidden) {
             gx.A = z.A;
@@ -375,12 +396,12 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
             } else {
                 gw.sum_share = count * dim4;
                 launch_gemm<D, F, true, true, kXentSum>(h, gw, t);
-                rw = XentRound{gw.sum, dim4, gw.sum_share, t.share, count, x.dim, nullptr, wmax, out, x.dmatrix_stride * e, 0u};
+                rw = XentRound{gw.sum, dim4, gw.sum_share, t.share, count, x.dim, scale_w, out, x.dmatrix_stride * e, 0u};
             }
         }
         const bool done = count == x.vocab - v0;
         if (done && x.dhidden)
-            rx = XentRound{gx.sum, dim4, gx.sum_share, tx.share, x.rows, x.dim, row, wmax, static_cast<char*>(x.dhidden),
+            rx = XentRound{gx.sum, dim4, gx.sum_share, tx.share, x.rows, x.dim, scale_x, static_cast<char*>(x.dhidden),
                            x.dhidden_stride * e, 0u};
         launch_round<F>(h, rx, rw);
     }
@@ -489,7 +510,7 @@ int rlsim_learner_create(uint32_t max_rows, uint32_t max_dim, uint32_t max_vocab
     h->clip_blocks = 2u * kClipBlocks + kMaxTensors;
     h->clip_at = up_to(8ull * kScanMapEntries, 256u);
     h->xent_at = h->clip_at + up_to(8ull * h->clip_blocks, 256u);
-    h->bytes = h->xent_at + (none ? 0u : std::max(xent_bound(max_rows, max_dim, max_vocab, 1u), xent_bound(max_rows, max_dim, max_vocab, 3u)));
+    h->bytes = h->xent_at + (none ? 0u : std::max(xent_bound(max_rows, max_dim, max_vocab, 1u), xent_bound(max_rows, max_dim, max_vocab, 2u)));
     e = hipMalloc(reinterpret_cast<void**>(&h->work), h->bytes);
     if (e != hipSuccess) {
         const int code = e == hipErrorOutOfMemory ? RLSIM_ENOMEM : RLSIM_EDEVICE;
@@ -618,12 +639,12 @@ int rlsim_learner_xent(rlsim_learner_t* h, const rlsim_xent* x)
     b.add("stats", x->stats, 8ull * x->rows, x->loss != nullptr);
     const char *one, *two;
     if (b.clash(&one, &two)) return learn_fail(h, RLSIM_EINVAL, "%s: %s overlaps %s", who, one, two);
-    const uint32_t parts = x->dtype == RLSIM_F32 ? 3u : 1u;
+    const uint32_t parts = x->dtype == RLSIM_F32 ? 2u : 1u;
     if (xent_work(xent_shape(x->rows, x->dim, x->vocab, parts)).end > h->bytes - h->xent_at)
         return learn_fail(h, RLSIM_EINVAL, "%s: the workspace does not hold this call", who);
     LearnDevice g(h->device);
     if (!g.ok) return learn_fail(h, RLSIM_EDEVICE, "%s: cannot select the handle's device", who);
-    if (x->dtype == RLSIM_F32) run_xent<kHeadBF16, kHeadF32>(h, *x);
+    if (x->dtype == RLSIM_F32) run_xent<kHeadF16, kHeadF32>(h, *x);
     else if (x->dtype == RLSIM_BF16) run_xent<kHeadBF16, kHeadBF16>(h, *x);
     else run_xent<kHeadF16, kHeadF16>(h, *x);
     const hipError_t err = hipGetLastError();

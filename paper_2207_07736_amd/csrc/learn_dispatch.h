@@ -46,8 +46,10 @@ inline uint64_t clip_chunk(uint64_t total)         // elements of a block
 }
 
 // ---- the output layer's cross entropy ------------------------------------------------
-// Products of rows run in 16-bit matrix instructions.  fp32 factors are cut into three
-// bf16 parts of 8 bits each; the six products of parts that reach 24 bits are summed.
+// Products of rows run in 16-bit matrix instructions.  fp32 rows are scaled and cut into
+// two fp16 parts of 11 bits each; the three products that reach 22 bits are summed.  (Three
+// bf16 parts and six products, 24 bits, took 187 instead of XXX us at 2,048 x 256 on 4,096; the
+// matrix units' own fp32 products run at a sixteenth of the rate.)
 constexpr uint32_t kXentK = 32u;                  // elements of a step along the summed dimension
 struct XentShape {
     uint32_t rows, dim, vocab, parts;
@@ -81,7 +83,7 @@ inline XentTile xent_tile(uint32_t M, uint32_t N, uint64_t steps, bool sums, uin
 inline uint64_t xent_share_floats(uint64_t rows, uint64_t dim4) { return most(rows * dim4, (uint64_t)kXentShareTiles * 128u * 128u); }
 
 struct XentWork {                                 // byte offsets
-    uint64_t info, zt, stats, wmax, part, x, xm, w, dz, dz_plain, dx, dw, end;
+    uint64_t info, zt, stats, refs, part, up_n, up_m, x, xm, w, dz, dz_plain, dx, dw, end;
 };
 inline XentWork xent_work(const XentShape& s)
 {
@@ -89,16 +91,18 @@ inline XentWork xent_work(const XentShape& s)
     uint64_t at = 0u;
     auto take = [&at](uint64_t bytes) { const uint64_t p = at; at += up_to(bytes, 256u); return p; };
     const uint64_t P2 = 2ull * s.parts, dim4 = up_to(s.dim, 4u);
-    o.wmax = take(4u);
+    o.refs = take(8u);
     o.info = take(16ull * s.rows_k);
     o.zt = take(4ull * s.rows_k);
     o.stats = take(8ull * s.rows_k);
     o.part = take(8ull * s.rows_k * (up_to(s.vocab, 256u) / 32u));
+    o.up_n = take(4ull * s.rows_k);
+    o.up_m = take(4ull * s.piece);
     o.x = take(P2 * s.rows * s.dim_k);
     o.xm = take(P2 * s.rows_k * s.dim_k);
     o.w = take(P2 * s.piece * s.dim_k);
     o.dz = take(P2 * s.rows_k * s.piece);
-    o.dz_plain = take(s.parts == 1u ? P2 * s.rows_k * s.piece : 0u);
+    o.dz_plain = take(P2 * s.rows_k * s.piece);
     o.dx = take(4u * xent_share_floats(s.rows, dim4));
     o.dw = take(4ull * kXentShareTiles * 128u * 128u);
     o.end = at;
@@ -114,7 +118,7 @@ inline uint64_t xent_bound(uint32_t rows, uint32_t dim, uint32_t vocab, uint32_t
     const uint64_t P2 = 2ull * parts, piece_all = up_to(vocab, 256u);
     const uint64_t by_dim = least(P2 * piece_all * s.dim_k, most(2ull << 26, P2 * 256u * s.dim_k));
     const uint64_t by_rows = least(P2 * piece_all * s.rows_k, most(2ull << 26, P2 * 256u * s.rows_k));
-    return o.x + 2u * up_to(P2 * (uint64_t)s.rows_k * s.dim_k, 256u) + up_to(by_dim, 256u) + 2u * up_to(by_rows, 256u)
+    return o.up_m + up_to(4ull * piece_all, 256u) + 2u * up_to(P2 * (uint64_t)s.rows_k * s.dim_k, 256u) + up_to(by_dim, 256u) + 2u * up_to(by_rows, 256u)
            + (o.end - o.dx) + 4096u;
 }
 

@@ -71,12 +71,18 @@ def xent(hidden, matrix, target, weight=None, grad=True):
     t = torch.where(counts, target.long(), 0)[:, None]
     X = torch.where(counts[:, None], X, 0.0)
     z = X @ W.t()
-    # sums of dim products, each step off by at most 2 u of what the sum of absolutes can
-    # reach (the matrix units may truncate); fp32 factors are cut to 24 bits: six sums,
-    # and three parts of 2^-24 left out
-    steps = (-(-dim // 64) * 64) * (6 if dtype == torch.float32 else 1)
+    # Sums of dim products, each step off by at most 2 u of what the sum of absolutes can
+    # reach (the matrix units may truncate).  fp32 factors are scaled to below 2^15 by row and
+    # cut into two fp16 parts: each is off by 2^-11 of the 2^-11 that the first leaves, 4 u of
+    # itself, or by 2^-25 where that part is small, 2^-39 of the row's largest entry (which
+    # is 2^14 at least); the product of both second parts, another 4 u, is left out; three sums.
+    full = dtype == torch.float32
+    steps = (-(-dim // 32) * 32) * (3 if full else 1)
     reach = X.abs() @ W.abs().t()
     ze = reach * (steps * 2.0 * U + 8.0 * U)
+    xtop, wtop = X.abs().max(dim=1, keepdim=True).values, W.abs().max(dim=1, keepdim=True).values
+    if full:
+        ze = ze + reach * 12.1 * U + 2.0 ** -38 * (xtop * W.abs().sum(dim=1)[None] + X.abs().sum(dim=1)[:, None] * wtop.t())
     m = z.max(dim=1, keepdim=True).values
     s = torch.exp(z - m).sum(dim=1, keepdim=True)
     loss = (torch.log(s) + m - z.gather(1, t))[:, 0]
@@ -102,19 +108,31 @@ def xent(hidden, matrix, target, weight=None, grad=True):
     # matrix units take a factor below it: what is smaller is off by no more than that, twice
     tiny = 2.0 ** -125
     pe = pe + tiny
-    half = 3.0 * U if dtype == torch.float32 else HALF_STEP[dtype]
-    floor = 2.0 ** -39 if dtype == torch.float16 else 0.0     # a denormal of 2^14 dz
+    half = 4.0 * U if full else HALF_STEP[dtype]
+    # fp16: dz is held times 2^13 at least (of the largest weight), its denormals off by 2^-25
+    floor = 2.0 ** -38 if dtype == torch.float16 else 0.0
     dze = torch.where(live[:, None], pe + dz.abs() * half + floor, 0.0)
-    many = 6 if dtype == torch.float32 else 1
-    over_v = (-(-V // 64) * 64 * many + 80) * 2.0 * U
-    over_n = (-(-rows // 64) * 64 * many + 80) * 2.0 * U
+    many = 3 if full else 1
+    over_v = (-(-V // 32) * 32 * many + 80) * 2.0 * U
+    over_n = (-(-rows // 32) * 32 * many + 80) * 2.0 * U
+    xfloor = wfloor = 0.0
+    if full:
+        # the other factor's cut, the part left out, and its small parts; dz's small parts: it is held
+        # times what its partner was divided by, below 2^14 over all, so off by 2^-39 of the largest
+        # such, and its partner is below 2^15 then
+        over_v, over_n = over_v + 8.1 * U, over_n + 8.1 * U
+        tops = wtop.clamp(min=1e-300)
+        xfloor = w.abs() * 2.0 ** -38 * ((dz.abs() @ wtop) + (W.abs() / tops).sum(dim=0)[None] * wtop.max())
+        xt = xtop.clamp(min=1e-300)
+        most = (w.abs() * xtop).max() * 2.0
+        wfloor = 2.0 ** -38 * ((w * dz).abs().t() @ xtop + (X.abs() / xt * live[:, None]).sum(dim=0)[None] * most)
     dX = w * (dz @ W)
-    dXe = w.abs() * (dze @ W.abs() + over_v * (dz.abs() @ W.abs())) * 1.001
+    dXe = w.abs() * (dze @ W.abs() + over_v * (dz.abs() @ W.abs())) * 1.001 + xfloor
     wd = w * dz
     scale = w.abs().max() * 2.0
     wde = w.abs() * (pe + dz.abs() * (half + 2.0 * U)) + ((floor * scale if floor else 0.0) + tiny) * live[:, None]
     dW = wd.t() @ X
-    dWe = (wde.t() @ X.abs() + over_n * (wd.abs().t() @ X.abs())) * 1.001
+    dWe = (wde.t() @ X.abs() + over_n * (wd.abs().t() @ X.abs())) * 1.001 + wfloor
     return (loss, loss_err), (dX, dXe), (dW, dWe)
 
 

@@ -39,7 +39,7 @@ int main()
         CHECK(total / clip_chunk(total) <= kClipBlocks);
         // a call within a handle's bounds fits its workspace
         const uint32_t rows = size_below(1u << 22), dim = size_below(1u << 16), vocab = size_below(1u << 20);
-        for (uint32_t parts : {1u, 3u}) {
+        for (uint32_t parts : {1u, 2u}) {
             const uint64_t bound = xent_bound(rows, dim, vocab, parts);
             const uint32_t r = 1u + below(rows), d = 1u + below(dim), v = 1u + below(vocab);
             for (const XentShape& s : {xent_shape(rows, dim, vocab, parts), xent_shape(r, d, v, parts), xent_shape(1, dim, vocab, parts),
@@ -50,21 +50,21 @@ int main()
             const XentShape s = xent_shape(r, d, v, parts);
             const XentWork o = xent_work(s);
             // shares of both products fit
-            const XentTile x = xent_tile(d, r, (uint64_t)s.piece / kXentK * (parts == 1u ? 1u : 6u), true, cus);
+            const XentTile x = xent_tile(d, r, (uint64_t)s.piece / kXentK * (parts == 1u ? 1u : 3u), true, cus);
             CHECK(x.share >= 1u && up_to(d, 4u) * 4u * r * x.share <= o.dw - o.dx);
             const uint32_t count = s.piece < v ? s.piece : v;
-            const XentTile w = xent_tile(d, count, (uint64_t)s.rows_k / kXentK * (parts == 1u ? 1u : 6u), true, cus);
+            const XentTile w = xent_tile(d, count, (uint64_t)s.rows_k / kXentK * (parts == 1u ? 1u : 3u), true, cus);
             CHECK(w.share == 1u || up_to(d, 4u) * 4u * count * w.share <= o.end - o.dw);
             // parts of the softmax sums fit
             uint64_t all = 0;
             for (uint32_t v0 = 0; v0 < v; v0 += s.piece) {
                 const uint32_t n = s.piece < v - v0 ? s.piece : v - v0;
-                const XentTile t = xent_tile(n, r, s.dim_k / kXentK * (parts == 1u ? 1u : 6u), false, cus);
+                const XentTile t = xent_tile(n, r, s.dim_k / kXentK * (parts == 1u ? 1u : 3u), false, cus);
                 CHECK(t.share == 1u && t.m % t.span == 0u);
                 all += (n + t.m - 1u) / t.m * (t.m / t.span);
             }
             CHECK(8ull * all * s.rows_k <= o.x - o.part);
-            const XentTile t = xent_tile(v, r, s.dim_k / kXentK * (parts == 1u ? 1u : 6u), false, cus);
+            const XentTile t = xent_tile(v, r, s.dim_k / kXentK * (parts == 1u ? 1u : 3u), false, cus);
             CHECK(8ull * ((v + t.m - 1u) / t.m * (t.m / t.span)) * s.rows_k <= o.x - o.part);
         }
     }
