@@ -149,7 +149,8 @@ void launch_scan(const rlsim_learner* h, ScanArgs a)
 {
     a.groups = (a.channels + V - 1u) / V;
     const uint64_t threads = (uint64_t)a.n * a.groups, C = (uint64_t)a.n * a.channels;
-    const ScanCut cut = scan_cut(threads, C, a.T, h->cus);
+    // as their registers allow: k_scan_back_rows has 256 for fp32, 168 otherwise
+    const ScanCut cut = scan_cut(threads, C, a.T, h->cus, !a.backward ? 4u : D == kHeadF32 ? 2u : 3u);
     a.segments = cut.segments;
     a.seg_len = cut.seg_len;
     a.map_a = reinterpret_cast<float*>(h->work);

@@ -20,13 +20,15 @@ struct ScanCut { uint32_t segments, seg_len; };
 // Segments of time for `threads` threads' channels.  A cut call reads its rows twice, so few
 // are cut: where there are fewer than two waves to a CU, or four if the steps are many (one
 // thread's run of 16 steps takes 4 us whatever the others do).  What is cut is cut into
-// enough for 16 waves a CU, of 32 steps at least.  Forward and backward, us, uncut / cut:
+// segments of 32 steps at least, and no more workgroups than run at once: `per_cu` of 256
+// threads on each CU (1,024 x 37 x 336 fp16 backward 82 us with 800 workgroups where 768 run at
+// once, 37 x 320 with 768 of them 63).  Forward and backward, us, uncut / cut:
 //   200 x 4,096 x 64 fp32 338 / 531     1,000 x 1,024 x 64 bf16 652 / 359
 //   200 x 1,024 x 64 fp32 122 / 122     1,000 x 2,048 x 64 bf16 687 / 677
-inline ScanCut scan_cut(uint64_t threads, uint64_t channels, uint32_t T, uint32_t cus)
+inline ScanCut scan_cut(uint64_t threads, uint64_t channels, uint32_t T, uint32_t cus, uint32_t per_cu)
 {
-    const uint64_t enough = (T <= 256u ? 128ull : 256ull) * cus, wanted = 1024ull * cus;
-    uint64_t s = threads >= enough ? 1u : (wanted + threads - 1u) / threads;
+    const uint64_t enough = (T <= 256u ? 128ull : 256ull) * cus, groups = (threads + 255u) / 256u;
+    uint64_t s = threads >= enough ? 1u : most((uint64_t)per_cu * cus / groups, 1u);
     s = least(s, T / 32u);
     s = least(s, kScanSegments);
     s = least(s, channels ? kScanMapEntries / channels : 1u);
@@ -48,7 +50,7 @@ inline uint64_t clip_chunk(uint64_t total)         // elements of a block
 // ---- the output layer's cross entropy ------------------------------------------------
 // Products of rows run in 16-bit matrix instructions.  fp32 rows are scaled and cut into
 // two fp16 parts of 11 bits each; the three products that reach 22 bits are summed.  (Three
-// bf16 parts and six products, 24 bits, took 187 instead of XXX us at 2,048 x 256 on 4,096; the
+// bf16 parts and six products, 24 bits, took 187 us instead of 148 at 2,048 x 256 on 4,096; the
 // matrix units' own fp32 products run at a sixteenth of the rate.)
 constexpr uint32_t kXentK = 32u;                  // elements of a step along the summed dimension
 struct XentShape {
@@ -66,14 +68,18 @@ inline XentShape xent_shape(uint32_t rows, uint32_t dim, uint32_t vocab, uint32_
 }
 
 // The tile of a product M x N, and how many workgroups share the summed dimension of one
-// (only sums may be shared).
+// (only sums may be shared).  256 x 256 where that gives every CU one and the sum is long
+// enough to pay for its ends; us, 256 / 128: 4,096 x 4,096 on 131,072 bf16 14,340 / 19,490,
+// 4,096 x 256 on 8,192 142 / 149, and 7 x 1,024 on 32,000 (one step) 27 / 19 for dmatrix.
+// Shares for one workgroup to a CU (two to a CU: 512 x 512 on 8,192 bf16 71 us instead of
+// 57, for the sums' writes and reads).
 struct XentTile { uint32_t m, n, span, share; };  // span: entries along m of one wave
 constexpr uint32_t kXentShareTiles = 1024u;
 inline XentTile xent_tile(uint32_t M, uint32_t N, uint64_t steps, bool sums, uint32_t cus)
 {
     const uint64_t big = ((M + 255ull) / 256u) * ((N + 255ull) / 256u);
     XentTile t = N <= 32u ? XentTile{128u, 32u, 32u, 1u} : big >= cus && steps >= 8u ? XentTile{256u, 256u, 128u, 1u} : XentTile{128u, 128u, 64u, 1u};
-    const uint64_t tiles = (uint64_t)((M + t.m - 1u) / t.m) * ((N + t.n - 1u) / t.n), wanted = 2ull * cus;
+    const uint64_t tiles = (uint64_t)((M + t.m - 1u) / t.m) * ((N + t.n - 1u) / t.n), wanted = cus;
     if (!sums || tiles >= wanted || t.m == 256u) return t;
     const uint64_t s = least(least(wanted / tiles, steps / 4u), least(kXentShareTiles / tiles, 64u));
     t.share = s < 2u ? 1u : (uint32_t)s;

@@ -30,7 +30,7 @@ int main()
         const uint32_t cus = i % 2 ? 256u : 64u;
         // segments cover the steps, start at marks, none is empty, and their maps fit
         const uint32_t T = size_below(1u << 20), channels = size_below(1u << 22);
-        const ScanCut c = scan_cut((channels + 1u) / 2u, channels, T, cus);
+        const ScanCut c = scan_cut((channels + 1u) / 2u, channels, T, cus, 2u + i % 3u);
         CHECK(c.segments >= 1u && c.segments <= kScanSegments && (uint64_t)c.segments * c.seg_len >= T);
         CHECK((uint64_t)(c.segments - 1u) * c.seg_len < T);
         CHECK(c.segments == 1u || (c.seg_len % kScanMark == 0u && (uint64_t)c.segments * channels <= kScanMapEntries));
