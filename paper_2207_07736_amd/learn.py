@@ -381,11 +381,14 @@ class Learner:
             if o is t:
                 add((t.data_ptr(), 0, t.numel(), kind))
                 continue
-            if o is None or o.shape != t.shape or o.stride() != t.stride():
-                raise ValueError("out must have its tensor's shape and order in memory")
+            other = types.get(o.dtype) if o is not None else None
+            if other is None:
+                raise ValueError("out must be float32, bfloat16 or float16 tensors, of their tensors' shapes")
             if o.get_device() != ordinal or not o.is_contiguous():
                 here("out", o)
-            add((t.data_ptr(), o.data_ptr(), t.numel(), kind & 0xFFFFFFFF | self._dtype("out", o) << 32))
+            if o.shape != t.shape or (o.stride() != t.stride() and not (o.is_contiguous() and t.is_contiguous())):
+                raise ValueError("out must have its tensor's shape and order in memory")
+            add((t.data_ptr(), o.data_ptr(), t.numel(), kind & 0xFFFFFFFF | other & 0xFFFFFFFF00000000))
         table = array.array("Q", words)           # rows of an rlsim_tensor
         norm = self._empty((), dtype=self._f32, device=self.device)
         rlsim_learner_clip(self.h, table.buffer_info()[0], len(pairs), float(max_norm), norm.data_ptr())
