@@ -375,7 +375,7 @@ int rlsim_learner_create(uint32_t max_rows, uint32_t max_dim, uint32_t max_vocab
 enum { RLSIM_SCAN_MARK = 16 };                /* steps between two marks */
 typedef struct {
     int dtype;                                /* of x, gate, y, dy, dx and dgate */
-    uint32_t T, n, channels;                  /* each >= 1; T n channels <= 2^40 */
+    uint32_t T, n, channels;                  /* each in [1, 2^30]; T n channels <= 2^40 */
     const void* x;
     const void* gate;
     uint64_t x_step, x_seq;                   /* strides in elements, at most 2^40; seq ignored for n = 1, */
@@ -413,11 +413,12 @@ int rlsim_learner_scan_grad(rlsim_learner_t* h, const rlsim_scan* s, const rlsim
  * whatever its hidden state, and so does a row of weight 0 to the gradients.  In other
  * rows infinities and NaN do as in the formulas.
  *
- * Logits exist a piece of the vocabulary at a time.  They are sums of exact products in
- * fp32 (of fp32 factors: of products to 24 bits); the softmax is fp32; its difference
- * from the target enters the gradients' products rounded to the factors' type (fp16:
- * scaled by powers of two before; fp32: kept to 24 bits), which are summed in fp32 and
- * rounded once.
+ * Logits exist a piece of the vocabulary at a time.  They are fp32 sums of exact products
+ * (of fp32 factors: of products to 22 bits, where an entry counts to 2^-39 of its row's
+ * largest at least); the softmax is fp32; its difference from the target enters the
+ * gradients' products rounded to the factors' type (fp16: scaled by powers of two before;
+ * fp32: to 22 bits), which are summed in fp32 and rounded once.  A row of fp32 factors that
+ * is not finite gives NaN wherever it enters.
  *
  * stats holds each row's largest logit and sum of exp(z - largest): an output beside the
  * losses, and the input of a later call for gradients alone (loss NULL) of the same

@@ -45,12 +45,13 @@ struct XentTarget {
 };
 
 constexpr int kDzUp = 14;                         // see XentRefs
+__device__ __forceinline__ int ref_of(uint32_t stored) { return stored ? (int)stored - 1024 : 0; }
 
 // A gradient's last factor: 0 for dhidden's rows that do not count, whatever the product
 // is, and their weight where dz is without it; the power of two that dz was scaled by.
 struct OutScale {
     const XentRow* row;                           // dhidden, or null
-    const int32_t* ref;                           // dz carries 2^(kDzUp - *ref), or null
+    const uint32_t* ref;                          // dz carries 2^(kDzUp - ref), or null
     int32_t up;                                   // else the result is due 2^up
     uint32_t weigh;
     __device__ __forceinline__ float operator()(float x, uint32_t n) const
@@ -59,7 +60,7 @@ struct OutScale {
             if (row[n].target < 0) return 0.0f;
             if (weigh) x *= row[n].weight;
         }
-        return ldexpf(x, ref ? *ref - kDzUp : up);
+        return ldexpf(x, ref ? ref_of(*ref) - kDzUp : up);
     }
 };
 
@@ -81,14 +82,14 @@ struct XentGemm {
     const XentRow* row;                           // logits, gradient
     const int32_t* up_n;                          // fp32: exponents of the rows of hidden and of matrix,
     const int32_t* up_m;                          // what a factor was divided by
-    const int32_t* refs;                          // fp16, fp32: XentRefs' results
+    const uint32_t* refs;                         // fp16, fp32: XentRefs' results
     char* dz;                                     // [parts][rows_k][piece], with the rows' weights
     char* dz_plain;                               // fp16, fp32: without them (for dhidden), or null
     uint64_t dz_ld, dz_part;                      // bytes
     float* sum;                                   // gradients' products: [share][N][sum_ld]
     uint64_t sum_ld, sum_share;                   // elements
     uint32_t add;                                 // to what is there
-    const int32_t* sum_ref;                       // fp32, dhidden: refs' entry of the piece, or null
+    const uint32_t* sum_ref;                      // fp32, dhidden: refs' entry of the piece, or null
     char* out;                                    // gradients' products, rounded: [N][M]
     uint64_t out_ld;                              // bytes
     OutScale scale;
@@ -507,7 +508,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
             if (n < a.N) r = a.row[n];
             // fp16 and fp32: by powers of two, to below 2^kDzUp over the rows (with weights; fp32 also
             // with what the row of hidden was divided by) or over the piece (without weights)
-            int up = F == kHeadBF16 ? 0 : kDzUp - a.refs[0];
+            int up = F == kHeadBF16 ? 0 : kDzUp - ref_of(a.refs[0]);
             if (F == kHeadF32) up += a.up_n[min(n, a.N - 1u)];
             const float weight = r.weight;
 #pragma unroll
@@ -532,7 +533,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                         int up_m[8];
                         if (F == kHeadF32) {
 #pragma unroll
-                            for (uint32_t e = 0; e < 8u; ++e) up_m[e] = a.up_m[m_wave + i * 32u + (q + e / 4u) * 8u + e % 4u] + kDzUp - a.refs[1];
+                            for (uint32_t e = 0; e < 8u; ++e) up_m[e] = a.up_m[m_wave + i * 32u + (q + e / 4u) * 8u + e % 4u] + kDzUp - ref_of(a.refs[1]);
                         }
 #pragma unroll
                         for (uint32_t e = 0; e < 8u; ++e) {
@@ -566,7 +567,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                         float4* to = reinterpret_cast<float4*>(a.sum + blockIdx.y * a.sum_share + n * a.sum_ld + m);
                         float4 s{c[i][j][4u * q], c[i][j][4u * q + 1u], c[i][j][4u * q + 2u], c[i][j][4u * q + 3u]};
                         if (F == kHeadF32 && a.sum_ref) {        // pieces are scaled each by its own power of two
-                            const int up = *a.sum_ref - kDzUp;
+                            const int up = ref_of(*a.sum_ref) - kDzUp;
                             s = float4{ldexpf(s.x, up), ldexpf(s.y, up), ldexpf(s.z, up), ldexpf(s.w, up)};
                         }
                         if (a.add) {
@@ -664,20 +665,23 @@ struct XentRefs {
     const int32_t* up_n;                          // or null
     const int32_t* up_m;                          // or null
     uint32_t rows, count;
-    int32_t* out;                                 // null: none is wanted
+    uint32_t* out;                                // exponents and 1024, 0 for none; null: not wanted
+    uint32_t blocks;                              // more than one: out is 0 before
 };
-__device__ __forceinline__ void xent_refs(const XentRefs& a)
+constexpr uint32_t kRefRows = 4096u;              // of a workgroup
+__device__ __forceinline__ void xent_refs(const XentRefs& a, uint32_t block)
 {
     __shared__ uint32_t sh[2][4];
-    uint32_t top_n = 0u, top_m = 0u;              // exponents and 1024
-    for (uint32_t r = threadIdx.x; r < a.rows; r += 256u) {
+    uint32_t top_n = 0u, top_m = 0u;
+#pragma unroll 4
+    for (uint32_t r = block * 256u + threadIdx.x; r < a.rows; r += a.blocks * 256u) {
         const float w = a.weight ? a.weight[r] : 1.0f;
-        if (__builtin_fabsf(w) < __builtin_inff() && w != 0.0f && a.target(r) >= 0)
-            top_n = max(top_n, (uint32_t)(1024 + exponent_of(w) + 1 + (a.up_n ? a.up_n[r] : 0)));
+        const bool counts = __builtin_fabsf(w) < __builtin_inff() && w != 0.0f && a.target(r) >= 0;
+        if (counts) top_n = max(top_n, (uint32_t)(1024 + exponent_of(w) + 1 + (a.up_n ? a.up_n[r] : 0)));
     }
     if (a.up_m) {
 #pragma unroll 4
-        for (uint32_t v = 4u * threadIdx.x; v < a.count; v += 1024u) {
+        for (uint32_t v = 4u * (block * 256u + threadIdx.x); v < a.count; v += a.blocks * 1024u) {
             const int4 up = *reinterpret_cast<const int4*>(a.up_m + v);          // whole fours: copies end with steps
             top_m = max(top_m, (uint32_t)(1024 + max(max(up.x, up.y), max(up.z, up.w))));
         }
@@ -689,16 +693,18 @@ __device__ __forceinline__ void xent_refs(const XentRefs& a)
         sh[1][threadIdx.x / 64u] = top_m;
     }
     __syncthreads();
-    if (threadIdx.x == 0u) {
-        for (uint32_t w = 1; w < 4u; ++w) {
-            top_n = max(top_n, sh[0][w]);
-            top_m = max(top_m, sh[1][w]);
-        }
-        a.out[0] = top_n ? (int)top_n - 1024 : 0;
-        a.out[1] = top_m ? (int)top_m - 1024 : 0;
+    if (threadIdx.x < 2u) {
+        const uint32_t* const x = sh[threadIdx.x];
+        const uint32_t top = max(max(x[0], x[1]), max(x[2], x[3]));
+        if (a.blocks == 1u) a.out[threadIdx.x] = top;
+        else atomicMax(a.out + threadIdx.x, top);         // the order does not matter
     }
 }
-__global__ __launch_bounds__(256) void k_xent_refs(XentRefs a) { xent_refs(a); }
+__global__ __launch_bounds__(256) void k_xent_refs(XentRefs a) { xent_refs(a, blockIdx.x); }
+__global__ void k_xent_refs_none(uint32_t* out)
+{
+    if (threadIdx.x < 2u) out[threadIdx.x] = 0u;
+}
 
 // Rows as the products read them: whole steps wide; rows that do not count are 0 where they
 // are told.  fp32 rows are divided by a power of two, so that the largest entry is between
@@ -799,7 +805,7 @@ __global__ __launch_bounds__(256) void k_xent_join(XentJoin a, XentLay b, XentRe
     const uint32_t blocks = (a.rows + kJoinRows - 1u) / kJoinRows;
     if (blockIdx.x < blocks) xent_join(a, blockIdx.x);
     else if (blockIdx.x < blocks + b.blocks) xent_lay<F>(b, blockIdx.x - blocks);
-    else xent_refs(c);
+    else xent_refs(c, blockIdx.x - blocks - b.blocks);
 }
 
 // A gradient from its shares: summed in order, scaled, rounded once.
@@ -816,16 +822,16 @@ template <int F>
 __device__ __forceinline__ void xent_round(const XentRound& a, uint32_t block)
 {
     const uint32_t per = (a.dim + 3u) / 4u;       // of four entries
-    const uint64_t i = (uint64_t)block * 256u + threadIdx.x;
-    if (i >= (uint64_t)a.rows * per) return;
-    const uint32_t n = (uint32_t)(i / per), d = (uint32_t)(i % per) * 4u;
-    float4 s{0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint64_t i = (uint64_t)block * 256u + threadIdx.x; i < (uint64_t)a.rows * per; i += (uint64_t)a.blocks * 256u) {
+        const uint32_t n = (uint32_t)(i / per), d = (uint32_t)(i % per) * 4u;
+        float4 s{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
-    for (uint32_t k = 0; k < a.share; ++k) {
-        const float4 x = *reinterpret_cast<const float4*>(a.sum + k * a.share_ld + n * a.ld + d);
-        s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+        for (uint32_t k = 0; k < a.share; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(a.sum + k * a.share_ld + n * a.ld + d);
+            s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+        }
+        put_four<F>(a.out + n * a.out_ld, d, a.dim, a.scale(s.x, n), a.scale(s.y, n), a.scale(s.z, n), a.scale(s.w, n));
     }
-    put_four<F>(a.out + n * a.out_ld, d, a.dim, a.scale(s.x, n), a.scale(s.y, n), a.scale(s.z, n), a.scale(s.w, n));
 }
 template <int F>
 __global__ __launch_bounds__(256) void k_xent_round(XentRound a, XentRound b)

@@ -61,7 +61,7 @@ struct LearnDevice {
 };
 
 constexpr uint64_t kScanMaxStride = 1ull << 40, kXentMaxStride = 1ull << 32, kMaxElements = 1ull << 40;
-constexpr uint32_t kMaxTensors = 1u << 20;
+constexpr uint32_t kMaxTensors = 1u << 20, kScanMost = 1u << 30;
 
 bool known_type(int d) { return d == RLSIM_F32 || d == RLSIM_BF16 || d == RLSIM_F16; }
 uint32_t type_bytes(int d) { return d == RLSIM_F32 ? 4u : 2u; }
@@ -133,8 +133,8 @@ uint64_t plane_bytes(const Plane& p, const rlsim_scan& s)
 int check_scan(rlsim_learner* h, const char* who, const rlsim_scan* s, const Plane* planes, int count)
 {
     if (!known_type(s->dtype)) return learn_fail(h, RLSIM_EINVAL, "%s: unknown dtype", who);
-    if (s->T == 0u || s->n == 0u || s->channels == 0u)
-        return learn_fail(h, RLSIM_EINVAL, "%s: T, n and channels must be at least 1", who);
+    if (s->T == 0u || s->n == 0u || s->channels == 0u || s->T > kScanMost || s->n > kScanMost || s->channels > kScanMost)
+        return learn_fail(h, RLSIM_EINVAL, "%s: T, n and channels must be in [1, 2^30]", who);
     if ((uint64_t)s->T * s->n > kMaxElements / s->channels)
         return learn_fail(h, RLSIM_EINVAL, "%s: more than 2^40 elements", who);
     for (int i = 0; i < count; ++i) {
@@ -233,8 +233,9 @@ void launch_lays(const rlsim_learner* h, XentLay a, XentLay b)
 template <int F>
 void launch_round(const rlsim_learner* h, XentRound a, XentRound b)
 {
-    a.blocks = (uint32_t)(((uint64_t)a.rows * ((a.dim + 3u) / 4u) + 255u) / 256u);
-    b.blocks = (uint32_t)(((uint64_t)b.rows * ((b.dim + 3u) / 4u) + 255u) / 256u);
+    // a launch holds fewer than 2^32 threads
+    a.blocks = (uint32_t)std::min<uint64_t>(((uint64_t)a.rows * ((a.dim + 3u) / 4u) + 255u) / 256u, 1u << 21);
+    b.blocks = (uint32_t)std::min<uint64_t>(((uint64_t)b.rows * ((b.dim + 3u) / 4u) + 255u) / 256u, 1u << 21);
     if (a.blocks + b.blocks) hipLaunchKernelGGL(k_xent_round<F>, dim3(a.blocks + b.blocks), dim3(256), 0, h->stream, a, b);
 }
 
@@ -261,7 +262,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     const char* const matrix = static_cast<const char*>(x.matrix);
     auto* up_n = reinterpret_cast<int32_t*>(w + o.up_n);
     auto* up_m = reinterpret_cast<int32_t*>(w + o.up_m);
-    auto* refs = reinterpret_cast<int32_t*>(w + o.refs);
+    auto* refs = reinterpret_cast<uint32_t*>(w + o.refs);
 
     const bool hidden_direct = P == 1u && as_they_are(x.hidden, x.hidden_stride, x.dim);
     const bool direct = P == 1u && as_they_are(x.matrix, x.matrix_stride, x.dim);
@@ -314,7 +315,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     j.loss = x.loss;
     j.row = grad ? row : nullptr;
     if (x.loss) {
-        const uint32_t width = direct ? x.vocab : s.piece;
+        const uint32_t width = direct ? (uint32_t)std::min<uint64_t>(x.vocab, xent_width(s.rows_k)) : s.piece;
         for (uint32_t v0 = 0u; v0 < x.vocab; v0 += width) {
             const uint32_t count = std::min(width, x.vocab - v0);
             piece(v0, count);
@@ -334,9 +335,11 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     l.blocks = lay_blocks<F>(l);
     // fp16, fp32: dz's powers of two (fp32: of the piece that the loss left in the copy)
     XentRefs refs_of{target, x.weight, F == kHeadF32 ? up_n : nullptr, F == kHeadF32 ? up_m : nullptr, x.rows,
-                     z.M, F != kHeadBF16 && grad ? refs : nullptr};
-    hipLaunchKernelGGL(k_xent_join<F>, dim3((x.rows + kJoinRows - 1u) / kJoinRows + l.blocks + (refs_of.out ? 1u : 0u)), dim3(256), 0,
-                       h->stream, j, l, refs_of);
+                     z.M, F != kHeadBF16 && grad ? refs : nullptr, 0u};
+    if (refs_of.out) refs_of.blocks = (x.rows + kRefRows - 1u) / kRefRows;
+    if (refs_of.blocks > 1u) hipLaunchKernelGGL(k_xent_refs_none, dim3(1), dim3(64), 0, h->stream, refs);
+    hipLaunchKernelGGL(k_xent_join<F>, dim3((x.rows + kJoinRows - 1u) / kJoinRows + l.blocks + refs_of.blocks), dim3(256), 0, h->stream,
+                       j, l, refs_of);
     if (!grad) return;
 
     const uint64_t dim4 = up_to(x.dim, 4u);
@@ -349,7 +352,7 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     gx.products = gw.products = z.products;
     gx.M = gw.M = x.dim;
     gx.sum_ld = gw.sum_ld = dim4;
-    const int32_t* const ref = F == kHeadBF16 ? nullptr : refs;
+    const uint32_t* const ref = F == kHeadBF16 ? nullptr : refs;
     // what the products are short of (fp32's dhidden: its sums are not)
     const OutScale scale_x = plain ? OutScale{row, nullptr, F == kHeadF16 ? -kDzUp : 0, 1u} : OutScale{row, ref, 0, 0u};
     const OutScale scale_w{nullptr, ref, 0, 0u};
@@ -376,7 +379,8 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         piece(v0, count);
         if (F == kHeadF32 && anew) {
             refs_of.count = count;
-            hipLaunchKernelGGL(k_xent_refs, dim3(1), dim3(256), 0, h->stream, refs_of);
+            if (refs_of.blocks > 1u) hipLaunchKernelGGL(k_xent_refs_none, dim3(1), dim3(64), 0, h->stream, refs);
+            hipLaunchKernelGGL(k_xent_refs, dim3(refs_of.blocks), dim3(256), 0, h->stream, refs_of);
         }
         launch_gemm<D, F, false, false, kXentDz>(h, z, xent_tile(count, x.rows, (uint64_t)s.dim_k / kXentK * z.products, false, h->cus));
         if (x.dhidden) {

@@ -114,6 +114,8 @@ inline XentWork xent_work(const XentShape& s)
     o.end = at;
     return o;
 }
+// Entries of the vocabulary in one launch for the losses: its tiles' threads stay below 2^32.
+inline uint64_t xent_width(uint32_t rows_k) { return most((1ull << 36) / rows_k / 256u * 256u, 256u); }
 // A handle's workspace: enough for every call within its bounds.
 inline uint64_t xent_bound(uint32_t rows, uint32_t dim, uint32_t vocab, uint32_t parts)
 {

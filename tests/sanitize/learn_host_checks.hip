@@ -75,11 +75,14 @@ int main()
     SCAN(c.gate = nullptr, "NULL");
     SCAN(c.y = nullptr, "NULL");
     SCAN(c.dtype = 7, "dtype");
-    SCAN(c.T = 0, "at least 1");
-    SCAN(c.n = 0, "at least 1");
-    SCAN(c.channels = 0, "at least 1");
-    SCAN((c.T = ~0u, c.n = ~0u), "2^40");
-    SCAN((c.T = 1u << 31, c.n = 1u << 31, c.channels = 1u << 31), "2^40");
+    SCAN(c.T = 0, "[1, 2^30]");
+    SCAN(c.n = 0, "[1, 2^30]");
+    SCAN(c.channels = 0, "[1, 2^30]");
+    SCAN(c.T = ~0u, "[1, 2^30]");
+    SCAN(c.n = (1u << 30) + 1u, "[1, 2^30]");
+    SCAN(c.channels = ~0u, "[1, 2^30]");
+    SCAN((c.T = 1u << 30, c.n = 1u << 30, c.channels = 1), "2^40");
+    SCAN((c.T = 1u << 30, c.n = 1u << 30, c.channels = 1u << 30), "2^40");
     SCAN(c.x = (const char*)f + 2, "aligned");
     SCAN((c.dtype = RLSIM_BF16, c.gate = (const char*)f + 1), "aligned");
     SCAN(c.state = (const float*)((const char*)f + 2), "aligned");

@@ -73,6 +73,39 @@ def test_target_types(learner, target_type, dtype):
     _check(learner, hidden, matrix, target.to(target_type), weight)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_two_actions_and_many_rows(dtype):
+    """A control policy's output layer: more rows than one workgroup weighs."""
+    import paper_2207_07736_amd as rl
+    learner = rl.Learner(100003, 24, 2)
+    try:
+        _check(learner, *_inputs(100003, 24, 2, dtype, seed=9))
+    finally:
+        learner.close()
+
+
+@pytest.mark.parametrize("scale", (2.0 ** -60, 2.0 ** 60))
+def test_fp32_rows_of_any_size(learner, scale):
+    """Rows, entries of the vocabulary and weights that differ by powers of two up to 2^120."""
+    hidden, matrix, target, weight = _inputs(70, 96, 600, torch.float32)
+    by_row = torch.exp2((torch.arange(70, device="cuda") % 9 - 4.0) * 3.0)
+    by_entry = torch.exp2(-(torch.arange(600, device="cuda") % 7) * 2.0)
+    hidden, matrix = hidden * by_row[:, None] * scale, matrix * by_entry[:, None] / scale
+    hidden[3], matrix[11] = 0.0, 0.0
+    _check(learner, hidden, matrix, target, weight * torch.exp2((torch.arange(70, device="cuda") % 5) * 6.0 - 12.0))
+
+
+def test_a_workspace_too_large():
+    import paper_2207_07736_amd as rl
+    with pytest.raises(rl.RlsimError) as e:
+        rl.Learner(1 << 22, 1 << 16, 1 << 20)
+    assert e.value.code == rl.RLSIM_ENOMEM
+    made = rl.Learner(4, 4, 4)
+    x = torch.zeros((4, 4), device="cuda")
+    assert float(made.cross_entropy(x, x, torch.zeros(4, dtype=torch.int32, device="cuda"), grad=False)[0]) == pytest.approx(1.386294, abs=1e-6)
+    made.close()
+
+
 def test_targets_outside(learner):
     hidden, matrix, target, _ = _inputs(8, 64, 100, torch.bfloat16)
     target[:] = torch.tensor([0, 99, 100, -1, -100, 2 ** 40, -2 ** 62, 50])

@@ -63,9 +63,17 @@ int main()
                 CHECK(t.share == 1u && t.m % t.span == 0u);
                 all += (n + t.m - 1u) / t.m * (t.m / t.span);
             }
-            CHECK(8ull * all * s.rows_k <= o.x - o.part);
-            const XentTile t = xent_tile(v, r, s.dim_k / kXentK * (parts == 1u ? 1u : 3u), false, cus);
-            CHECK(8ull * ((v + t.m - 1u) / t.m * (t.m / t.span)) * s.rows_k <= o.x - o.part);
+            CHECK(8ull * all * s.rows_k <= o.up_n - o.part);
+            all = 0;
+            const uint32_t width = (uint32_t)(v < xent_width(s.rows_k) ? v : xent_width(s.rows_k));
+            for (uint32_t v0 = 0; v0 < v; v0 += width) {
+                const uint32_t n = width < v - v0 ? width : v - v0;
+                const XentTile t = xent_tile(n, r, s.dim_k / kXentK * (parts == 1u ? 1u : 3u), false, cus);
+                all += (n + t.m - 1u) / t.m * (t.m / t.span);
+                // a launch holds fewer than 2^32 threads
+                CHECK((uint64_t)((n + t.m - 1u) / t.m) * ((r + t.n - 1u) / t.n) * 512u < 1ull << 32);
+            }
+            CHECK(8ull * all * s.rows_k <= o.up_n - o.part);
         }
     }
     printf("learn dispatch: OK\n");
