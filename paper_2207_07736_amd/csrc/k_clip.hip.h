@@ -25,6 +25,7 @@ struct ClipArgs {
     uint8_t dtype[kClipTensors], out_dtype[kClipTensors];
     uint32_t count, base;                 // tensors; blocks of the launches before
     uint32_t blocks;                      // of the whole call
+    uint32_t past_cache;                  // more bytes than the last-level cache holds
     uint64_t chunk;                       // elements of a block
     double max_norm;
     double* sums;                         // [blocks]
@@ -85,7 +86,9 @@ __device__ __forceinline__ double clip_squares(const char* p, uint64_t from, uin
     return s;
 }
 
-template <int D, int O, uint32_t NT>
+// STREAM: outputs that the last-level cache would not keep go past it, and leave it to what
+// the norm's pass has read last, which is scaled first.
+template <int D, int O, uint32_t NT, bool STREAM>
 __device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t from, uint64_t to, float scale)
 {
     using To = Elem<O>;
@@ -95,7 +98,12 @@ __device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t fr
                      struct __attribute__((packed, aligned(To::kBytes))) Run { typename To::Word w[E]; } r;
 #pragma unroll
                      for (uint32_t e = 0; e < E; ++e) r.w[e] = To::word(Elem<D>::get(v, e) * scale);
-                     *reinterpret_cast<Run*>(out + i * To::kBytes) = r;
+                     if (STREAM) {
+                         typedef uint32_t Words __attribute__((ext_vector_type(E * To::kBytes / 4u), aligned(2)));
+                         __builtin_nontemporal_store(__builtin_bit_cast(Words, r), reinterpret_cast<Words*>(out + i * To::kBytes));
+                     } else {
+                         *reinterpret_cast<Run*>(out + i * To::kBytes) = r;
+                     }
                  },
                  [&](float x, uint64_t i) { reinterpret_cast<typename To::Word*>(out)[i] = To::word(x * scale); });
 }
@@ -122,7 +130,7 @@ __device__ __forceinline__ double squares_of(const ClipArgs& a, uint32_t block)
                                      : clip_squares<kHeadF16, NT>(a.t[k].data, from, to);
 }
 
-template <uint32_t NT>
+template <uint32_t NT, bool STREAM>
 __device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, float scale)
 {
     const uint32_t k = clip_tensor(a, block);
@@ -131,9 +139,9 @@ __device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, f
     const uint64_t from = (uint64_t)(block - a.first[k]) * a.chunk, to = min(from + a.chunk, t.elements);
     auto to_type = [&](auto in) {
         constexpr int D = decltype(in)::value;
-        if (a.out_dtype[k] == kHeadF32) clip_scale<D, kHeadF32, NT>(t.data, t.out, from, to, scale);
-        else if (a.out_dtype[k] == kHeadBF16) clip_scale<D, kHeadBF16, NT>(t.data, t.out, from, to, scale);
-        else clip_scale<D, kHeadF16, NT>(t.data, t.out, from, to, scale);
+        if (a.out_dtype[k] == kHeadF32) clip_scale<D, kHeadF32, NT, STREAM>(t.data, t.out, from, to, scale);
+        else if (a.out_dtype[k] == kHeadBF16) clip_scale<D, kHeadBF16, NT, STREAM>(t.data, t.out, from, to, scale);
+        else clip_scale<D, kHeadF16, NT, STREAM>(t.data, t.out, from, to, scale);
     };
     if (a.dtype[k] == kHeadF32) to_type(std::integral_constant<int, kHeadF32>{});
     else if (a.dtype[k] == kHeadBF16) to_type(std::integral_constant<int, kHeadBF16>{});
@@ -159,7 +167,11 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a)
     for (uint32_t i = threadIdx.x; i < a.blocks; i += 256u) s += a.sums[i];
     const double norm = sqrt(group_sum<256>(s, sh));
     if (a.base + blockIdx.x == 0u && threadIdx.x == 0u) *a.norm = (float)norm;
-    if (a.count) scale_block<256u>(a, a.first[a.count] - 1u - blockIdx.x, clip_factor(norm, a.max_norm));
+    if (!a.count) return;
+    const uint32_t block = a.first[a.count] - 1u - blockIdx.x;     // from the end: what was read last
+    const float scale = clip_factor(norm, a.max_norm);
+    if (a.past_cache) scale_block<256u, true>(a, block, scale);
+    else scale_block<256u, false>(a, block, scale);
 }
 
 // Few elements: one workgroup, one launch.  Its waves take blocks in turn.
@@ -172,7 +184,7 @@ __global__ __launch_bounds__(1024) void k_clip_small(ClipArgs a)
     const double norm = sqrt(group_sum<1024>(s, sh));
     if (threadIdx.x == 0u) *a.norm = (float)norm;
     const float scale = clip_factor(norm, a.max_norm);
-    for (uint32_t b = wave; b < blocks; b += 16u) scale_block<64u>(a, b, scale);
+    for (uint32_t b = wave; b < blocks; b += 16u) scale_block<64u, false>(a, b, scale);
 }
 
 }  // namespace rlsim_dev

@@ -61,6 +61,7 @@ struct LearnDevice {
 };
 
 constexpr uint64_t kScanMaxStride = 1ull << 40, kXentMaxStride = 1ull << 32, kMaxElements = 1ull << 40;
+constexpr uint64_t kLearnCacheBytes = 256ull << 20;
 constexpr uint32_t kMaxTensors = 1u << 20, kScanMost = 1u << 30;
 
 bool known_type(int d) { return d == RLSIM_F32 || d == RLSIM_BF16 || d == RLSIM_F16; }
@@ -449,9 +450,14 @@ const char* clip_clash(const rlsim_tensor* t, uint32_t count, const float* norm,
 
 void run_clip(const rlsim_learner* h, const rlsim_tensor* t, uint32_t count, double max_norm, float* norm)
 {
-    uint64_t total = 0u;
-    for (uint32_t i = 0; i < count; ++i) total += t[i].elements;
+    uint64_t total = 0u, bytes = 0u;
+    for (uint32_t i = 0; i < count; ++i) {
+        total += t[i].elements;
+        bytes += t[i].elements * type_bytes(t[i].dtype);
+    }
     ClipArgs a{};
+    // us, 400 M bf16 into tensors of their own: 458, past the cache 427
+    a.past_cache = bytes > kLearnCacheBytes ? 1u : 0u;
     a.chunk = clip_chunk(total);
     a.max_norm = max_norm;
     a.sums = reinterpret_cast<double*>(h->work + h->clip_at);

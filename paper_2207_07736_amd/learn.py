@@ -156,7 +156,7 @@ class Learner:
     def _rows(self, name, t, shape, dtype):
         """Address and (step, sequence) strides of a [T, n, channels] tensor whose
         channels are consecutive elements."""
-        if t.shape != shape or t.dtype != dtype or t.get_device() != self._ordinal:
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._ordinal:
             raise ValueError(f"{name} must be {dtype}, {list(shape)}, on {self.device}")
         step, seq, one = t.stride()
         if one != 1 and shape[2] > 1:
@@ -179,17 +179,21 @@ class Learner:
             raise ValueError("done must be uint8 or bool")
         return self._plain("done", done, (T, n), done.dtype)
 
-    def _scan_args(self, x, gate, state, done, marks):
+    def _scan_args(self, x, gate, state, done, marks, y, y_step, y_seq, last):
         shape, kind = x.shape, x.dtype
-        dtype = self._dtype("x", x)
-        if len(shape) != 3:
-            raise ValueError("x must be 3-d, [T, n, channels]")
         T, n, channels = shape
         x_at, x_step, x_seq = self._rows("x", x, shape, kind)
         g_at, g_step, g_seq = self._rows("gate", gate, shape, kind)
-        return rlsim_scan(dtype, T, n, channels, x_at, g_at, x_step, x_seq, g_step, g_seq,
+        return rlsim_scan(self._dtypes[kind], T, n, channels, x_at, g_at, x_step, x_seq, g_step, g_seq,
                           None if state is None else self._plain("state", state, (n, channels)),
-                          None if done is None else self._ends(done, T, n), marks)
+                          None if done is None else self._ends(done, T, n), marks, y, y_step, y_seq, last)
+
+    def _scan_shape(self, x):
+        if x.dtype not in self._dtypes:
+            raise ValueError("x must be float32, bfloat16 or float16")
+        if x.dim() != 3:
+            raise ValueError("x must be 3-d, [T, n, channels]")
+        return x.shape
 
     def _like(self, x):
         """A new tensor of x's shape and order of its first two dimensions."""
@@ -211,20 +215,18 @@ class Learner:
         return self._scan(rlsim_learner_scan, x, gate, state, done, marks, last)
 
     def _scan(self, launch, x, gate, state, done, marks, last):
-        args = self._scan_args(x, gate, state, done, None)
-        T, n, channels = x.shape
+        T, n, channels = self._scan_shape(x)
         y = self._like(x)
+        y_step, y_seq, _ = y.stride()
         given = last is not None
-        if not given:
-            last = (self._empty((n, channels), dtype=self._f32, device=self.device) if state is None or not state.is_contiguous()
-                    else self._empty_like(state))
-        kept = None
-        if marks:
-            kept = self._empty((-(-T // RLSIM_SCAN_MARK), n, channels), dtype=self._f32, device=self.device)
-            args.marks = kept.data_ptr()
-        args.y = y.data_ptr()
-        args.y_step, args.y_seq, _ = y.stride()
-        args.last = self._plain("last", last, (n, channels)) if given else last.data_ptr()
+        if given:
+            at = self._plain("last", last, (n, channels))
+        else:
+            last = (self._empty_like(state) if state is not None and state.is_contiguous()
+                    else self._empty((n, channels), dtype=self._f32, device=self.device))
+            at = last.data_ptr()
+        kept = self._empty((-(-T // RLSIM_SCAN_MARK), n, channels), dtype=self._f32, device=self.device) if marks else None
+        args = self._scan_args(x, gate, state, done, kept.data_ptr() if marks else None, y.data_ptr(), y_step, y_seq, at)
         if T and n and channels:
             launch(self.h, args)
         elif n and channels:                      # no steps: the state as it was
@@ -243,21 +245,18 @@ class Learner:
         return self._scan_grad(rlsim_learner_scan_grad, x, gate, marks, dy, done, dlast)
 
     def _scan_grad(self, launch, x, gate, marks, dy, done, dlast):
-        args = self._scan_args(x, gate, None, done, None)
-        T, n, channels = shape = tuple(x.shape)
+        T, n, channels = shape = self._scan_shape(x)
         if marks is None:
             raise ValueError("marks are needed")
-        args.marks = self._plain("marks", marks, (-(-T // RLSIM_SCAN_MARK), n, channels))
+        args = self._scan_args(x, gate, None, done, self._plain("marks", marks, (-(-T // RLSIM_SCAN_MARK), n, channels)),
+                               None, 0, 0, None)
         dx, dgate = self._like(x), self._like(x)
         dstate = self._empty((n, channels), dtype=self._f32, device=self.device)
-        g = rlsim_scan_grad()
-        if dy is not None:
-            g.dy, g.dy_step, g.dy_seq = self._rows("dy", dy, shape, x.dtype)
-        g.dlast = self._plain("dlast", dlast, (n, channels))
-        g.dx, g.dx_step, g.dx_seq = dx.data_ptr(), dx.stride(0), dx.stride(1)
-        g.dgate, g.dgate_step, g.dgate_seq = dgate.data_ptr(), dgate.stride(0), dgate.stride(1)
-        g.dstate = dstate.data_ptr()
-        if dx.numel():
+        step, seq, _ = dx.stride()
+        g = rlsim_scan_grad(*((None, 0, 0) if dy is None else self._rows("dy", dy, shape, x.dtype)),
+                            self._plain("dlast", dlast, (n, channels)), dx.data_ptr(), dgate.data_ptr(), step, seq, step, seq,
+                            dstate.data_ptr())
+        if T and n and channels:
             launch(self.h, args, g)
         elif n and channels:
             dstate.zero_() if dlast is None else dstate.copy_(dlast)
@@ -296,7 +295,7 @@ class Learner:
         return self._cross_entropy(rlsim_learner_xent, hidden, matrix, target, weight, loss, grad, stats)
 
     def _cross_entropy(self, launch, hidden, matrix, target, weight, loss, grad, stats):
-        if grad not in (True, False, "hidden", "matrix"):
+        if grad is not True and grad is not False and grad != "hidden" and grad != "matrix":
             raise ValueError('grad must be True, False, "hidden" or "matrix"')
         if not loss and grad is False:
             raise ValueError("neither loss nor grad is wanted")
@@ -309,26 +308,28 @@ class Learner:
         vocab = matrix.shape[0]
         if target.dtype not in self._target:
             raise ValueError("target must be uint8, int32 or int64")
-        args = rlsim_xent(dtype, rows, dim, vocab, *self._matrix("hidden", hidden, rows, dim, hidden.dtype),
-                          *self._matrix("matrix", matrix, vocab, dim, hidden.dtype), self._target[target.dtype],
-                          self._plain("target", target, (rows,), target.dtype), self._plain("weight", weight, (rows,)))
-        out = []
+        h_at, h_stride = self._matrix("hidden", hidden, rows, dim, hidden.dtype)
+        m_at, m_stride = self._matrix("matrix", matrix, vocab, dim, hidden.dtype)
+        target_at = self._plain("target", target, (rows,), target.dtype)
+        weight_at, stats_at = self._plain("weight", weight, (rows,)), self._plain("stats", stats, (rows, 2))
+        out, loss_at, dh_at, dm_at = [], None, None, None
         if loss:
             losses = self._empty(rows, dtype=self._f32, device=self.device)
-            args.loss = losses.data_ptr()
+            loss_at = losses.data_ptr()
             out.append(losses)
-        args.stats = self._plain("stats", stats, (rows, 2))
-        if grad in (True, "hidden"):
-            dhidden = self._empty((rows, dim), dtype=hidden.dtype, device=self.device)
-            args.dhidden, args.dhidden_stride = dhidden.data_ptr(), dim
+        if grad is True or grad == "hidden":
+            dhidden = self._empty_like(hidden) if hidden.is_contiguous() else self._empty((rows, dim), dtype=hidden.dtype, device=self.device)
+            dh_at = dhidden.data_ptr()
             out.append(dhidden)
-        if grad in (True, "matrix"):
-            dmatrix = self._empty((vocab, dim), dtype=hidden.dtype, device=self.device)
-            args.dmatrix, args.dmatrix_stride = dmatrix.data_ptr(), dim
+        if grad is True or grad == "matrix":
+            dmatrix = self._empty_like(matrix) if matrix.is_contiguous() else self._empty((vocab, dim), dtype=hidden.dtype, device=self.device)
+            dm_at = dmatrix.data_ptr()
             out.append(dmatrix)
+        args = rlsim_xent(dtype, rows, dim, vocab, h_at, h_stride, m_at, m_stride, self._target[target.dtype], target_at,
+                          weight_at, loss_at, stats_at, dh_at, dim, dm_at, dim)
         if rows:
             launch(self.h, args)
-        elif grad in (True, "matrix"):            # an empty batch teaches nothing
+        elif dm_at is not None:                   # an empty batch teaches nothing
             out[-1].zero_()
         if loss and stats is not None:
             self._written(stats)
@@ -357,8 +358,8 @@ class Learner:
     def clip(self, tensors, max_norm: float, out=None):
         """Scale ``tensors`` (float32, bfloat16 or float16; None entries are skipped) in
         place by max_norm / norm where their global norm is finite and above ``max_norm``.
-        ``out``: tensors to write to instead, each of its tensor's shape and order in
-        memory, of any of the types.  Returns the norm before, a float32 number on the
+        ``out``: tensors to write to instead, each with its tensor's elements in the same
+        order in memory, of any of the types.  Returns the norm before, a float32 number on the
         device."""
         if not max_norm > 0:
             raise ValueError("max_norm must be > 0")
@@ -383,12 +384,15 @@ class Learner:
                 continue
             other = types.get(o.dtype) if o is not None else None
             if other is None:
-                raise ValueError("out must be float32, bfloat16 or float16 tensors, of their tensors' shapes")
-            if o.get_device() != ordinal or not o.is_contiguous():
+                raise ValueError("out must be float32, bfloat16 or float16 tensors")
+            n = t.numel()
+            if o.get_device() != ordinal or not o.is_contiguous() or not t.is_contiguous():
                 here("out", o)
-            if o.shape != t.shape or (o.stride() != t.stride() and not (o.is_contiguous() and t.is_contiguous())):
-                raise ValueError("out must have its tensor's shape and order in memory")
-            add((t.data_ptr(), o.data_ptr(), t.numel(), kind & 0xFFFFFFFF | other & 0xFFFFFFFF00000000))
+                if o.shape != t.shape or o.stride() != t.stride():
+                    raise ValueError("out must have its tensor's elements in the same order in memory")
+            if o.numel() != n:
+                raise ValueError("out must have as many elements as its tensor")
+            add((t.data_ptr(), o.data_ptr(), n, kind & 0xFFFFFFFF | other & 0xFFFFFFFF00000000))
         table = array.array("Q", words)           # rows of an rlsim_tensor
         norm = self._empty((), dtype=self._f32, device=self.device)
         rlsim_learner_clip(self.h, table.buffer_info()[0], len(pairs), float(max_norm), norm.data_ptr())
