@@ -396,7 +396,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         y.template cut<H>(a.K - t * 32u, lane);
     };
     auto one_step = [&](auto steady, uint32_t t, char* now, char* next, char* ahead) {
-        constexpr bool kSteady = decltype(steady)::value;        // three more steps are to come
+        constexpr bool kSteady = decltype(steady)::value;        // four more steps are to come
         reads_done();                             // of the first half
         x.template read<1>(now);
         y.template read<1>(now + OpA::kBytes);
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         constexpr std::true_type steady{};
         constexpr std::false_type ending{};
 #pragma unroll 1
-        for (; t + 6u < last; t += 4u) {
+        for (; t + 7u < last; t += 4u) {          // the last step is not among those loaded here: K may end in it
             one_step(steady, t, sh0, sh1, sh3);
             one_step(steady, t + 1u, sh1, sh2, sh0);
             one_step(steady, t + 2u, sh2, sh3, sh1);

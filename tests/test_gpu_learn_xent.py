@@ -164,15 +164,31 @@ def test_padded_rows_may_hold_anything(learner, dtype):
 
 
 @pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float16))
-def test_rows_that_end_within_a_step_keep_to_themselves(learner, dtype):
-    """Rows of 40 entries inside wider arrays of NaN: nothing behind a row's end is used."""
-    hidden, matrix, target, weight = _inputs(50, 40, 300, dtype)
-    wide_h = torch.full((50, 72), float("nan"), device="cuda", dtype=dtype)
-    wide_m = torch.full((300, 72), float("nan"), device="cuda", dtype=dtype)
-    wide_h[:, 8:48], wide_m[:, 8:48] = hidden, matrix
-    want = _check(learner, hidden, matrix, target, weight)
-    for a, b in zip(want, learner.cross_entropy(wide_h[:, 8:48], wide_m[:, 8:48], target, weight)):
-        assert torch.equal(a, b)
+@pytest.mark.parametrize("rows", (5, 50))
+def test_rows_that_end_within_a_step_keep_to_themselves(learner, rows, dtype):
+    """Rows of 8 k entries inside wider arrays of NaN, for sums of 1 to 11 steps of 32: nothing
+    behind a row's end is used."""
+    for dim in range(8, 352, 8):
+        hidden, matrix, target, weight = _inputs(rows, dim, 70, dtype, seed=dim)
+        wide_h = torch.full((rows, dim + 32), float("nan"), device="cuda", dtype=dtype)
+        wide_m = torch.full((70, dim + 32), float("nan"), device="cuda", dtype=dtype)
+        wide_h[:, 8:dim + 8], wide_m[:, 8:dim + 8] = hidden, matrix
+        want = learner.cross_entropy(hidden, matrix, target, weight)
+        for a, b in zip(want, learner.cross_entropy(wide_h[:, 8:dim + 8], wide_m[:, 8:dim + 8], target, weight)):
+            assert torch.isfinite(a).all() and torch.equal(a, b), dim
+
+
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float16))
+@pytest.mark.parametrize("rows", (5, 50))
+def test_a_vocabulary_that_ends_within_a_step_keeps_to_itself(learner, rows, dtype):
+    """The first rows of a longer matrix of NaN, for sums over 1 to 15 steps of 32 entries."""
+    for V in range(3, 480, 7):
+        hidden, matrix, target, weight = _inputs(rows, 64, V, dtype, seed=V)
+        long = torch.full((V + 40, 64), float("nan"), device="cuda", dtype=dtype)
+        long[:V] = matrix
+        want = learner.cross_entropy(hidden, matrix, target, weight)
+        for a, b in zip(want, learner.cross_entropy(hidden, long[:V], target, weight)):
+            assert torch.isfinite(a).all() and torch.equal(a, b), V
 
 
 @pytest.mark.parametrize("rows", (7, 100))
