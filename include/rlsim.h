@@ -415,14 +415,17 @@ int rlsim_learner_scan_grad(rlsim_learner_t* h, const rlsim_scan* s, const rlsim
  *
  * Logits exist a piece of the vocabulary at a time.  They are fp32 sums of exact products
  * (of fp32 factors: of products to 22 bits, where an entry counts to 2^-39 of its row's
- * largest at least); the softmax is fp32; its difference from the target enters the
- * gradients' products rounded to the factors' type (fp16: scaled by powers of two before;
- * fp32: to 22 bits), which are summed in fp32 and rounded once.  A row of fp32 factors that
- * is not finite gives NaN wherever it enters.
+ * largest at least); the softmax is fp32.  Its difference from the target enters dhidden's
+ * product rounded to the factors' type (fp32: to 22 bits), and dmatrix's, times the weight, to
+ * fp16 with powers of two (fp32: 22 bits; hidden's bf16 entries count to 2^-39 of their row's
+ * largest); both are summed in fp32 and rounded once.  A row of fp32 factors that is not
+ * finite gives NaN wherever it enters.
  *
- * stats holds each row's largest logit and sum of exp(z - largest): an output beside the
- * losses, and the input of a later call for gradients alone (loss NULL) of the same
- * hidden, matrix and target. */
+ * stats holds each row's largest logit, the sum of exp(z - largest) over the entries other
+ * than its target, and that of its target: an output beside the losses, and the input of a
+ * later call for gradients alone (loss NULL) of the same hidden, matrix and target.  The
+ * target's gradient is the others' share, not 1 minus its own: rows that know their target
+ * keep their losses' and gradients' digits. */
 typedef struct {
     int dtype;                                /* of hidden, matrix, dhidden and dmatrix */
     uint32_t rows, dim, vocab;                /* each >= 1, at most the handle's */
@@ -434,7 +437,7 @@ typedef struct {
     const void* target;                       /* [rows] */
     const float* weight;                      /* [rows] or NULL */
     float* loss;                              /* [rows] out, or NULL */
-    float* stats;                             /* [rows][2] or NULL */
+    float* stats;                             /* [rows][3] or NULL */
     void* dhidden;                            /* [rows][dim] out, or NULL */
     uint64_t dhidden_stride;
     void* dmatrix;                            /* [vocab][dim] out, or NULL */

@@ -28,6 +28,8 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 struct XentRow {
     float largest, inv_sum, weight;
     int32_t target;                               // -1: the row counts for nothing
+    float miss;                                   // 1 - softmax of the target, not as a difference
+    float unused[3];
 };
 
 // The rows' targets as given: -1 for one outside the vocabulary.
@@ -54,13 +56,21 @@ struct OutScale {
     const uint32_t* ref;                          // dz carries 2^(kDzUp - ref), or null
     int32_t up;                                   // else the result is due 2^up
     uint32_t weigh;
-    __device__ __forceinline__ float operator()(float x, uint32_t n) const
+    // for row n, found once
+    struct Row {
+        float by;
+        int up;
+        bool counts;
+        __device__ __forceinline__ float operator()(float x) const { return counts ? ldexpf(x * by, up) : 0.0f; }
+    };
+    __device__ __forceinline__ Row at(uint32_t n) const
     {
+        Row r{1.0f, ref ? ref_of(*ref) - kDzUp : up, true};
         if (row) {
-            if (row[n].target < 0) return 0.0f;
-            if (weigh) x *= row[n].weight;
+            r.counts = row[n].target >= 0;
+            if (weigh) r.by = row[n].weight;
         }
-        return ldexpf(x, ref ? ref_of(*ref) - kDzUp : up);
+        return r;
     }
 };
 
@@ -80,11 +90,13 @@ struct XentGemm {
     float* zt;
     uint32_t part0, rows_k;
     const XentRow* row;                           // logits, gradient
-    const int32_t* up_n;                          // fp32: exponents of the rows of hidden and of matrix,
-    const int32_t* up_m;                          // what a factor was divided by
-    const uint32_t* refs;                         // fp16, fp32: XentRefs' results
-    char* dz;                                     // [parts][rows_k][piece], with the rows' weights
-    char* dz_plain;                               // fp16, fp32: without them (for dhidden), or null
+    const int32_t* up_n;                          // exponents of what rows of hidden (bf16: for dmatrix) and
+    const int32_t* up_m;                          // of matrix (fp32) were divided by
+    const uint32_t* refs;                         // XentRefs' results
+    char* dz_w;                                   // [dz_w_parts][rows_k][piece] for dmatrix: fp16, with the rows' weights, or null
+    char* dz;                                     // for dhidden: of the factors' type, without them, or null
+    uint32_t dz_w_parts;
+    uint32_t dz_stack;                            // bf16, fp16: rows from dz's first part to its second, or 0: one part
     uint64_t dz_ld, dz_part;                      // bytes
     float* sum;                                   // gradients' products: [share][N][sum_ld]
     uint64_t sum_ld, sum_share;                   // elements
@@ -345,15 +357,17 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     const char* const B0 = a.B + OpB::first(n_base, a.N, a.ldb);
     const uint64_t step_a = AA ? 32u * a.lda : 64u, step_b = BA ? 32u * a.ldb : 64u;
 
-    // the parts of product p, small products first: (1,0) (0,1) (0,0)
+    // the parts of product p, small products first: (1,0) (0,1) (0,0), or (0,1) (0,0) where only B
+    // has two
+    constexpr bool kProducts = F == kHeadF32 || (F == kHeadF16 && BA);
     const uint32_t all = a.steps * a.products;
     const uint32_t first = (uint32_t)((uint64_t)all * blockIdx.y / a.share);
     const uint32_t last = (uint32_t)((uint64_t)all * (blockIdx.y + 1u) / a.share);
     uint32_t product = first / a.steps, step = first % a.steps;
     const char *pa, *pb;
     auto locate = [&]() {
-        const uint32_t i = a.products == 1u ? 0u : product == 0u;
-        const uint32_t j = a.products == 1u ? 0u : product == 1u;
+        const uint32_t i = a.products == 1u ? 0u : F == kHeadF32 && product == 0u;
+        const uint32_t j = a.products == 1u ? 0u : product + 2u == a.products;
         pa = A0 + i * a.part_a + step * step_a;
         pb = B0 + j * a.part_b + step * step_b;
     };
@@ -367,7 +381,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
         pa += step_a;
         pb += step_b;
         ++step;
-        if (F == kHeadF32 && step == a.steps) {
+        if (kProducts && step == a.steps) {
             step = 0u;
             ++product;
             if (product < a.products) locate();
@@ -481,7 +495,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
     for (uint32_t j = 0; j < FN; ++j) {
         const uint32_t n = n_base + wn * (BN / WN) + j * 32u + lane % 32u;
         if (EPI == kXentLoss) {
-            // largest logit and sum of this wave's entries of row n, and the target's logit
+            // largest logit of this wave's entries of row n, their sum without the target's, and
+            // the target's logit
             float top = -__builtin_inff();
             const int32_t target = n < a.N ? a.target(n) : -1;
 #pragma unroll
@@ -499,17 +514,20 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
 #pragma unroll
             for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
-                for (uint32_t e = 0; e < 16u; ++e) sum += exp_of(c[i][j][e] - from);
+                for (uint32_t e = 0; e < 16u; ++e) {
+                    const uint32_t v = a.m0 + m_wave + i * 32u + e / 4u * 8u + e % 4u;
+                    sum += (int32_t)v == target ? 0.0f : exp_of(c[i][j][e] - from);
+                }
             sum += __shfl_xor(sum, 32);
             if (lane < 32u && n < a.N) a.part[(uint64_t)(a.part0 + tm * WM + wm) * a.rows_k + n] = float2{top, sum};
         }
         if (EPI == kXentDz) {
             XentRow r{0.0f, 0.0f, 0.0f, -1};
             if (n < a.N) r = a.row[n];
-            // fp16 and fp32: by powers of two, to below 2^kDzUp over the rows (with weights; fp32 also
-            // with what the row of hidden was divided by) or over the piece (without weights)
-            int up = F == kHeadBF16 ? 0 : kDzUp - ref_of(a.refs[0]);
-            if (F == kHeadF32) up += a.up_n[min(n, a.N - 1u)];
+            // by powers of two to below 2^kDzUp: over the rows, with weights and what the rows of
+            // hidden were divided by, or (fp32) over the piece
+            int up = kDzUp - ref_of(a.refs[0]);
+            if (F != kHeadF16) up += a.up_n[min(n, a.N - 1u)];
             const float weight = r.weight;
 #pragma unroll
             for (uint32_t i = 0; i < FM; ++i)
@@ -519,40 +537,47 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                     for (uint32_t e = 0; e < 4u; ++e) {
                         const uint32_t v = a.m0 + m_wave + i * 32u + q * 8u + e;
                         float p = exp_of(c[i][j][4u * q + e] - r.largest) * r.inv_sum;
-                        if ((int32_t)v == r.target) p -= 1.0f;
+                        if ((int32_t)v == r.target) p = -r.miss;
                         c[i][j][4u * q + e] = v >= a.vocab || r.target < 0 ? 0.0f : p;
                     }
                 }
             if (n < a.rows_k) {
-                char* const to = a.dz + n * a.dz_ld;
 #pragma unroll
                 for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
                     for (uint32_t q = 0; q < 4u; q += 2u) {
-                        uint16_t w[2][8], plain[2][8];
-                        int up_m[8];
-                        if (F == kHeadF32) {
+                        constexpr uint32_t P = F == kHeadF32 ? 2u : 1u;
+                        const uint64_t at = n * a.dz_ld + 2u * (m_base + wm * (BM / WM) + i * 32u + (q + lane / 32u) * 8u);
+                        if (a.dz_w) {
+                            uint16_t w[2][8];
 #pragma unroll
-                            for (uint32_t e = 0; e < 8u; ++e) up_m[e] = a.up_m[m_wave + i * 32u + (q + e / 4u) * 8u + e % 4u] + kDzUp - ref_of(a.refs[1]);
-                        }
-#pragma unroll
-                        for (uint32_t e = 0; e < 8u; ++e) {
-                            const float p = c[i][j][4u * q + e];
-                            const float pw = p == 0.0f ? 0.0f : p * weight;
-                            if (F == kHeadF32) {
-                                cut2(ldexpf(pw, up), w[0][e], w[1][e]);
-                                cut2(ldexpf(p, up_m[e]), plain[0][e], plain[1][e]);
-                            } else {
-                                w[0][e] = Elem<D>::word(F == kHeadF16 ? ldexpf(pw, up) : pw);
-                                plain[0][e] = F == kHeadF16 ? Elem<D>::word(ldexpf(p, kDzUp)) : (uint16_t)0;
+                            for (uint32_t e = 0; e < 8u; ++e) {
+                                const float p = c[i][j][4u * q + e], pw = p == 0.0f ? 0.0f : ldexpf(p * weight, up);
+                                if (F != kHeadBF16) cut2(pw, w[0][e], w[1][e]);
+                                else w[0][e] = Elem<kHeadF16>::word(pw);
                             }
+                            *reinterpret_cast<u32x4*>(a.dz_w + at) = eight_of(w[0]);
+                            if (F == kHeadF32 || (F == kHeadF16 && a.dz_w_parts == 2u))
+                                *reinterpret_cast<u32x4*>(a.dz_w + at + a.dz_part) = eight_of(w[1]);
                         }
-                        const uint64_t m = m_base + wm * (BM / WM) + i * 32u + (q + lane / 32u) * 8u;
+                        if (a.dz && !(a.dz_stack && n >= a.dz_stack)) {
+                            uint16_t w[2][8];
 #pragma unroll
-                        for (uint32_t s = 0; s < (F == kHeadF32 ? 2u : 1u); ++s) {
-                            *reinterpret_cast<u32x4*>(to + s * a.dz_part + 2u * m) = eight_of(w[s]);
-                            if (F != kHeadBF16 && a.dz_plain)
-                                *reinterpret_cast<u32x4*>(a.dz_plain + n * a.dz_ld + s * a.dz_part + 2u * m) = eight_of(plain[s]);
+                            for (uint32_t e = 0; e < 8u; ++e) {
+                                const float p = c[i][j][4u * q + e];
+                                if (F == kHeadBF16) {
+                                    w[0][e] = Elem<kHeadBF16>::word(p);
+                                    w[1][e] = Elem<kHeadBF16>::word(p - Elem<kHeadBF16>::one(w[0][e]));
+                                }
+                                if (F == kHeadF16) cut2(ldexpf(p, kDzUp), w[0][e], w[1][e]);
+                                if (F == kHeadF32) {
+                                    const int up_m = a.up_m[m_wave + i * 32u + (q + e / 4u) * 8u + e % 4u];
+                                    cut2(ldexpf(p, up_m + kDzUp - ref_of(a.refs[1])), w[0][e], w[1][e]);
+                                }
+                            }
+#pragma unroll
+                            for (uint32_t s = 0; s < P; ++s) *reinterpret_cast<u32x4*>(a.dz + at + s * a.dz_part) = eight_of(w[s]);
+                            if (P == 1u && a.dz_stack) *reinterpret_cast<u32x4*>(a.dz + at + a.dz_stack * a.dz_ld) = eight_of(w[1]);
                         }
                     }
             }
@@ -579,7 +604,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                 }
         }
         if (EPI == kXentOut && n < a.N) {
-            auto scale = [&](float x) { return F == kHeadBF16 ? x : a.scale(x, n); };
+            const OutScale::Row scale = a.scale.at(n);
             char* const to = a.out + n * a.out_ld;
             if (F == kHeadF32) {
 #pragma unroll
@@ -604,7 +629,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
 }
 
 // Rows' largest logits and sums from their parts (or as given), the losses, and what the
-// gradient's tiles need of a row.
+// gradient's tiles need of a row.  The target's own term is kept out of the sums: of a row
+// whose softmax is nearly all its target's, the loss and the target's gradient are the rest,
+// which 1 minus the softmax would round away.
 struct XentJoin {
     const float2* part;                           // null: stats is an input
     uint32_t parts, rows, rows_k;
@@ -644,19 +671,30 @@ __device__ __forceinline__ void xent_join(const XentJoin& a, uint32_t block)
         return;
     }
     if (r >= a.rows) return;
-    if (!a.part) s = reinterpret_cast<const float2*>(a.stats)[r];
-    else if (a.stats) reinterpret_cast<float2*>(a.stats)[r] = s;
     const int32_t target = a.target(r);
-    if (a.loss) a.loss[r] = target < 0 ? 0.0f : logf(s.y) + (s.x - a.zt[r]);
+    float own = 0.0f;                             // the target's term
+    if (a.part) {
+        if (target >= 0) own = exp_of(a.zt[r] - (s.x == -__builtin_inff() ? 0.0f : s.x));
+        if (a.stats) {
+            a.stats[3u * (uint64_t)r] = s.x;
+            a.stats[3u * (uint64_t)r + 1u] = s.y;
+            a.stats[3u * (uint64_t)r + 2u] = own;
+        }
+    } else {
+        s = float2{a.stats[3u * (uint64_t)r], a.stats[3u * (uint64_t)r + 1u]};
+        own = a.stats[3u * (uint64_t)r + 2u];
+    }
+    if (a.loss) a.loss[r] = target < 0 ? 0.0f : own == 1.0f ? log1pf(s.y) : logf(s.y + own) + (s.x - a.zt[r]);
     if (a.row) {
         const float w = a.weight ? a.weight[r] : 1.0f;
         const bool counts = target >= 0 && w != 0.0f;
-        a.row[r] = XentRow{s.x, 1.0f / s.y, counts ? w : 0.0f, counts ? target : -1};
+        const float inv_sum = 1.0f / (s.y + own);
+        a.row[r] = XentRow{s.x, inv_sum, counts ? w : 0.0f, counts ? target : -1, s.y * inv_sum, {}};
     }
 }
 
-// The powers of two that dz of fp16 and fp32 calls is scaled by, so that the largest that it
-// can be is just below 2^kDzUp (a probability below 2^-14 would lose bits of fp16):
+// The powers of two that dz is scaled by where it is held in fp16, so that the largest that
+// it can be is just below 2^kDzUp (a probability below 2^-14 would lose bits of fp16):
 //   out[0]  for dmatrix, a bound of |weight| 2^up_n over the rows that count
 //   out[1]  for dhidden (fp32), of 2^up_m over the piece
 struct XentRefs {
@@ -707,8 +745,9 @@ __global__ void k_xent_refs_none(uint32_t* out)
 }
 
 // Rows as the products read them: whole steps wide; rows that do not count are 0 where they
-// are told.  fp32 rows are divided by a power of two, so that the largest entry is between
-// 2^14 and 2^15, and cut in two parts.
+// are told.  Cut rows are divided by a power of two, so that the largest entry is between
+// 2^14 and 2^15, and held in fp16: fp32 in two parts, bf16 in one (exactly, but for what is
+// below 2^-28 of the largest).
 struct XentLay {
     const char* from;                             // [R][C]
     uint64_t ld;                                  // bytes
@@ -717,20 +756,24 @@ struct XentLay {
     uint64_t part;                                // bytes
     XentTarget target;                            // p null: all rows count
     const float* weight;
-    int32_t* up;                                  // fp32: [tall] exponents of what rows were divided by, or null
+    int32_t* up;                                  // cut: [tall] exponents of what rows were divided by, or null
+    uint32_t cut;
     uint32_t blocks;
     __device__ __forceinline__ bool counts(uint32_t r) const
     {
         return r < R && (!target.p || (target(r) >= 0 && !(weight && weight[r] == 0.0f)));
     }
 };
-// fp32: a wave to a row.
-__device__ __forceinline__ void xent_lay32(const XentLay& a, uint32_t block)
+// Cut: a wave to a row.
+template <int F>
+__device__ __forceinline__ void xent_cut(const XentLay& a, uint32_t block)
 {
-    struct __attribute__((packed, aligned(4))) Four { float x[4]; };
+    using El = Elem<F>;
+    using Word = typename El::Word;
+    struct __attribute__((packed, aligned(El::kBytes))) Four { Word x[4]; };
     const uint32_t lane = threadIdx.x % 64u;
     for (uint32_t r = uniform(block * 4u + threadIdx.x / 64u); r < a.tall; r += a.blocks * 4u) {
-        const float* const from = reinterpret_cast<const float*>(a.from + r * a.ld);
+        const Word* const from = reinterpret_cast<const Word*>(a.from + r * a.ld);
         const bool counts = a.counts(r);
         auto load = [&](uint32_t c) {
             Four f{};
@@ -748,7 +791,7 @@ __device__ __forceinline__ void xent_lay32(const XentLay& a, uint32_t block)
             const Four f = load(c);
 #pragma unroll
             for (uint32_t e = 0; e < 4u; ++e) {
-                const uint32_t bits = __builtin_bit_cast(uint32_t, f.x[e]) & 0x7FFFFFFFu;
+                const uint32_t bits = __builtin_bit_cast(uint32_t, El::one(f.x[e])) & 0x7FFFFFFFu;
                 top = max(top, bits < 0x7F800000u ? bits : 0u);
             }
         }
@@ -759,18 +802,19 @@ __device__ __forceinline__ void xent_lay32(const XentLay& a, uint32_t block)
             const Four f = load(c);
             uint16_t hi[4], lo[4];
 #pragma unroll
-            for (uint32_t e = 0; e < 4u; ++e) cut2(ldexpf(f.x[e], -up), hi[e], lo[e]);
+            for (uint32_t e = 0; e < 4u; ++e) cut2(ldexpf(El::one(f.x[e]), -up), hi[e], lo[e]);
             char* const to = a.to + ((uint64_t)r * a.wide + c) * 2u;
             *reinterpret_cast<uint2*>(to) = uint2{hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16};
-            *reinterpret_cast<uint2*>(to + a.part) = uint2{lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16};
+            if (F == kHeadF32)
+                *reinterpret_cast<uint2*>(to + a.part) = uint2{lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16};
         }
     }
 }
 template <int F>
 __device__ __forceinline__ void xent_lay(const XentLay& a, uint32_t block)
 {
-    if (F == kHeadF32) {
-        xent_lay32(a, block);
+    if (F != kHeadF16 && a.cut) {
+        xent_cut<F>(a, block);
         return;
     }
     const uint32_t per = a.wide / 8u;
@@ -792,20 +836,19 @@ __device__ __forceinline__ void xent_lay(const XentLay& a, uint32_t block)
     }
 }
 
-// Two copies in one launch, or the rows' sums, a copy and the powers of two.
+// Three copies in one launch; the rows' sums and the powers of two in one.
 template <int F>
-__global__ __launch_bounds__(256) void k_xent_lays(XentLay a, XentLay b)
+__global__ __launch_bounds__(256) void k_xent_lays(XentLay a, XentLay b, XentLay c)
 {
     if (blockIdx.x < a.blocks) xent_lay<F>(a, blockIdx.x);
-    else xent_lay<F>(b, blockIdx.x - a.blocks);
+    else if (blockIdx.x < a.blocks + b.blocks) xent_lay<F>(b, blockIdx.x - a.blocks);
+    else xent_lay<F>(c, blockIdx.x - a.blocks - b.blocks);
 }
-template <int F>
-__global__ __launch_bounds__(256) void k_xent_join(XentJoin a, XentLay b, XentRefs c)
+__global__ __launch_bounds__(256) void k_xent_join(XentJoin a, XentRefs c)
 {
     const uint32_t blocks = (a.rows + kJoinRows - 1u) / kJoinRows;
     if (blockIdx.x < blocks) xent_join(a, blockIdx.x);
-    else if (blockIdx.x < blocks + b.blocks) xent_lay<F>(b, blockIdx.x - blocks);
-    else xent_refs(c, blockIdx.x - blocks - b.blocks);
+    else xent_refs(c, blockIdx.x - blocks);
 }
 
 // A gradient from its shares: summed in order, scaled, rounded once.
@@ -813,6 +856,7 @@ struct XentRound {
     const float* sum;
     uint64_t ld, share_ld;
     uint32_t share, rows, dim;
+    uint32_t stack;                               // rows to the second part's sums, or 0
     OutScale scale;
     char* out;
     uint64_t out_ld;                              // bytes
@@ -830,7 +874,17 @@ __device__ __forceinline__ void xent_round(const XentRound& a, uint32_t block)
             const float4 x = *reinterpret_cast<const float4*>(a.sum + k * a.share_ld + n * a.ld + d);
             s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
         }
-        put_four<F>(a.out + n * a.out_ld, d, a.dim, a.scale(s.x, n), a.scale(s.y, n), a.scale(s.z, n), a.scale(s.w, n));
+        if (a.stack) {
+            float4 t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+            for (uint32_t k = 0; k < a.share; ++k) {
+                const float4 x = *reinterpret_cast<const float4*>(a.sum + k * a.share_ld + (n + a.stack) * a.ld + d);
+                t.x += x.x, t.y += x.y, t.z += x.z, t.w += x.w;
+            }
+            s.x += t.x, s.y += t.y, s.z += t.z, s.w += t.w;
+        }
+        const OutScale::Row scale = a.scale.at(n);
+        put_four<F>(a.out + n * a.out_ld, d, a.dim, scale(s.x), scale(s.y), scale(s.z), scale(s.w));
     }
 }
 template <int F>

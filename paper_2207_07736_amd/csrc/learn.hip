@@ -216,19 +216,20 @@ void launch_gemm(const rlsim_learner* h, XentGemm a, const XentTile& t)
 }
 
 // A copy's workgroups; none for one that is not made.
-template <int F>
 uint32_t lay_blocks(const XentLay& a)
 {
-    const uint64_t blocks = F == kHeadF32 ? (a.tall + 3ull) / 4u : ((uint64_t)a.tall * (a.wide / 8u) + 255u) / 256u;
+    const uint64_t blocks = a.cut ? (a.tall + 3ull) / 4u : ((uint64_t)a.tall * (a.wide / 8u) + 255u) / 256u;
     return (uint32_t)std::min<uint64_t>(blocks, 1u << 21);
 }
 
 template <int F>
-void launch_lays(const rlsim_learner* h, XentLay a, XentLay b)
+void launch_lays(const rlsim_learner* h, XentLay a, XentLay b, XentLay c)
 {
-    a.blocks = lay_blocks<F>(a);
-    b.blocks = lay_blocks<F>(b);
-    if (a.blocks + b.blocks) hipLaunchKernelGGL(k_xent_lays<F>, dim3(a.blocks + b.blocks), dim3(256), 0, h->stream, a, b);
+    a.blocks = lay_blocks(a);
+    b.blocks = lay_blocks(b);
+    c.blocks = lay_blocks(c);
+    const uint32_t all = a.blocks + b.blocks + c.blocks;
+    if (all) hipLaunchKernelGGL(k_xent_lays<F>, dim3(all), dim3(256), 0, h->stream, a, b, c);
 }
 
 template <int F>
@@ -284,10 +285,14 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
     z.ldb = hidden_direct ? x.hidden_stride * e : 2ull * s.dim_k;
     z.part_b = 2ull * s.dim_k * x.rows;
     z.lda = direct ? x.matrix_stride * e : 2ull * s.dim_k;
-    XentLay hidden_lay{};                         // made with the first piece of the matrix
+    constexpr uint32_t cut = F == kHeadF32 ? 1u : 0u;
+    XentLay hidden_lay{}, masked_lay{};           // made with the first piece of the matrix
     if (!hidden_direct)
         hidden_lay = XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, x.rows, w + o.x,
-                             z.part_b, {}, nullptr, up_n, 0u};
+                             z.part_b, {}, nullptr, cut ? up_n : nullptr, cut, 0u};
+    if (x.dmatrix)                                // rows that do not count may hold anything
+        masked_lay = XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, s.rows_k, w + o.xm,
+                             2ull * s.dim_k * s.rows_k, target, x.weight, F == kHeadBF16 ? up_n : nullptr, F != kHeadF16 ? 1u : 0u, 0u};
 
     // The piece of the vocabulary from v0, as the products read it.
     uint32_t laid = ~0u;                          // the piece that is copied now
@@ -300,9 +305,9 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         XentLay l{};
         if (!direct && laid != v0)
             l = XentLay{from, x.matrix_stride * e, count, x.dim, s.dim_k, (uint32_t)up_to(count, kXentK), w + o.w, z.part_a,
-                        {}, nullptr, up_m, 0u};
-        launch_lays<F>(h, hidden_lay, l);
-        hidden_lay = XentLay{};
+                        {}, nullptr, cut ? up_m : nullptr, cut, 0u};
+        launch_lays<F>(h, hidden_lay, masked_lay, l);
+        hidden_lay = masked_lay = XentLay{};
         laid = v0;
     };
 
@@ -327,52 +332,47 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
         }
         j.part = part;
     }
-    // before a call for gradients alone, the first piece's copies
-    if (!x.loss && F == kHeadF32) piece(0u, std::min(s.piece, x.vocab));
-    XentLay l{};                                  // for dmatrix: rows that do not count may hold anything
-    if (x.dmatrix)
-        l = XentLay{static_cast<const char*>(x.hidden), x.hidden_stride * e, x.rows, x.dim, s.dim_k, s.rows_k, w + o.xm,
-                    2ull * s.dim_k * s.rows_k, target, x.weight, nullptr, 0u};
-    l.blocks = lay_blocks<F>(l);
-    // fp16, fp32: dz's powers of two (fp32: of the piece that the loss left in the copy)
-    XentRefs refs_of{target, x.weight, F == kHeadF32 ? up_n : nullptr, F == kHeadF32 ? up_m : nullptr, x.rows,
-                     z.M, F != kHeadBF16 && grad ? refs : nullptr, 0u};
+    // before a call for gradients alone, the first copies
+    if (!x.loss) piece(0u, std::min(s.piece, x.vocab));
+    // dz's powers of two (fp32: of the piece that the loss left in the copy)
+    XentRefs refs_of{target, x.weight, F != kHeadF16 && x.dmatrix ? up_n : nullptr, F == kHeadF32 ? up_m : nullptr, x.rows,
+                     z.M, grad ? refs : nullptr, 0u};
     if (refs_of.out) refs_of.blocks = (x.rows + kRefRows - 1u) / kRefRows;
     if (refs_of.blocks > 1u) hipLaunchKernelGGL(k_xent_refs_none, dim3(1), dim3(64), 0, h->stream, refs);
-    hipLaunchKernelGGL(k_xent_join<F>, dim3((x.rows + kJoinRows - 1u) / kJoinRows + l.blocks + refs_of.blocks), dim3(256), 0, h->stream,
-                       j, l, refs_of);
+    hipLaunchKernelGGL(k_xent_join, dim3((x.rows + kJoinRows - 1u) / kJoinRows + refs_of.blocks), dim3(256), 0, h->stream, j, refs_of);
     if (!grad) return;
 
     const uint64_t dim4 = up_to(x.dim, 4u);
-    const bool plain = F == kHeadF32 ? x.dhidden != nullptr : F == kHeadF16 && x.weight && x.dhidden;
-    z.dz = w + o.dz;
-    z.dz_plain = plain ? w + o.dz_plain : nullptr;
+    z.dz_w = x.dmatrix ? w + o.dz_w : nullptr;
+    z.dz_w_parts = F == kHeadF32 || (F == kHeadF16 && x.rows <= kXentFewRows) ? 2u : 1u;
+    const uint32_t stack = F != kHeadF32 && x.rows <= kXentStackRows ? kXentStackRows : 0u;
+    z.dz_stack = stack;
+    z.dz = x.dhidden ? w + o.dz : nullptr;
     z.dz_ld = 2ull * s.piece;
     z.dz_part = z.dz_ld * s.rows_k;
     XentGemm gx{}, gw{};                          // dhidden's and dmatrix's products
-    gx.products = gw.products = z.products;
+    gx.products = z.products;
+    gw.products = F == kHeadF32 ? 3u : z.dz_w_parts;
     gx.M = gw.M = x.dim;
     gx.sum_ld = gw.sum_ld = dim4;
-    const uint32_t* const ref = F == kHeadBF16 ? nullptr : refs;
     // what the products are short of (fp32's dhidden: its sums are not)
-    const OutScale scale_x = plain ? OutScale{row, nullptr, F == kHeadF16 ? -kDzUp : 0, 1u} : OutScale{row, ref, 0, 0u};
-    const OutScale scale_w{nullptr, ref, 0, 0u};
+    const OutScale scale_x{row, nullptr, F == kHeadF16 ? -kDzUp : 0, 1u}, scale_w{nullptr, refs, 0, 0u};
     gx.sum_ref = F == kHeadF32 ? refs + 1 : nullptr;
     gw.scale = scale_w;
     gx.lda = z.lda;
-    gx.B = plain ? z.dz_plain : z.dz;
+    gx.B = z.dz;
     gx.ldb = gw.ldb = z.dz_ld;
     gx.part_b = gw.part_b = z.dz_part;
-    gx.N = x.rows;
+    gx.N = stack ? 2u * stack : x.rows;
     gx.sum = reinterpret_cast<float*>(w + o.dx);
-    gx.sum_share = x.rows * dim4;
+    gx.sum_share = gx.N * dim4;
     gw.A = w + o.xm;
     gw.lda = 2ull * s.dim_k;
     gw.part_a = gw.lda * s.rows_k;
-    gw.B = z.dz;
+    gw.B = z.dz_w;
     gw.K = s.rows_k;
     gw.sum = reinterpret_cast<float*>(w + o.dw);
-    const XentTile tx = xent_tile(x.dim, x.rows, (uint64_t)s.piece / kXentK * z.products, true, h->cus);
+    const XentTile tx = xent_tile(x.dim, gx.N, (uint64_t)s.piece / kXentK * z.products, true, h->cus);
     for (uint32_t v0 = 0u; v0 < x.vocab; v0 += s.piece) {
         const uint32_t count = std::min(s.piece, x.vocab - v0);
         XentRound rx{}, rw{};
@@ -398,16 +398,16 @@ void run_xent(const rlsim_learner* h, const rlsim_xent& x)
             if (t.share == 1u) {
                 gw.out = out;
                 gw.out_ld = x.dmatrix_stride * e;
-                launch_gemm<D, F, true, true, kXentOut>(h, gw, t);
+                launch_gemm<kHeadF16, F, true, true, kXentOut>(h, gw, t);
             } else {
                 gw.sum_share = count * dim4;
-                launch_gemm<D, F, true, true, kXentSum>(h, gw, t);
-                rw = XentRound{gw.sum, dim4, gw.sum_share, t.share, count, x.dim, scale_w, out, x.dmatrix_stride * e, 0u};
+                launch_gemm<kHeadF16, F, true, true, kXentSum>(h, gw, t);
+                rw = XentRound{gw.sum, dim4, gw.sum_share, t.share, count, x.dim, 0u, scale_w, out, x.dmatrix_stride * e, 0u};
             }
         }
         const bool done = count == x.vocab - v0;
         if (done && x.dhidden)
-            rx = XentRound{gx.sum, dim4, gx.sum_share, tx.share, x.rows, x.dim, scale_x, static_cast<char*>(x.dhidden),
+            rx = XentRound{gx.sum, dim4, gx.sum_share, tx.share, x.rows, x.dim, stack, scale_x, static_cast<char*>(x.dhidden),
                            x.dhidden_stride * e, 0u};
         launch_round<F>(h, rx, rw);
     }
@@ -642,12 +642,12 @@ int rlsim_learner_xent(rlsim_learner_t* h, const rlsim_xent* x)
         b.add(m.name, m.p, ((m.rows - 1u) * m.stride + x->dim) * e, m.written);
     }
     if (!on_boundary(x->target, (uint64_t)x->target_bytes)) return learn_fail(h, RLSIM_EINVAL, "%s: target is not aligned to its element size", who);
-    if (!on_boundary(x->weight, 4u) || !on_boundary(x->loss, 4u) || !on_boundary(x->stats, 8u))
-        return learn_fail(h, RLSIM_EINVAL, "%s: weight or loss is not 4-byte aligned, or stats not 8-byte", who);
+    if (!on_boundary(x->weight, 4u) || !on_boundary(x->loss, 4u) || !on_boundary(x->stats, 4u))
+        return learn_fail(h, RLSIM_EINVAL, "%s: weight, loss or stats is not 4-byte aligned", who);
     b.add("target", x->target, (uint64_t)x->rows * (uint64_t)x->target_bytes, false);
     b.add("weight", x->weight, 4ull * x->rows, false);
     b.add("loss", x->loss, 4ull * x->rows, true);
-    b.add("stats", x->stats, 8ull * x->rows, x->loss != nullptr);
+    b.add("stats", x->stats, 12ull * x->rows, x->loss != nullptr);
     const char *one, *two;
     if (b.clash(&one, &two)) return learn_fail(h, RLSIM_EINVAL, "%s: %s overlaps %s", who, one, two);
     const uint32_t parts = x->dtype == RLSIM_F32 ? 2u : 1u;

@@ -66,7 +66,9 @@ struct XentShape {
 inline XentShape xent_shape(uint32_t rows, uint32_t dim, uint32_t vocab, uint32_t parts)
 {
     XentShape s{rows, dim, vocab, parts, (uint32_t)up_to(dim, kXentK), (uint32_t)up_to(rows, kXentK), 0u};
-    uint64_t p = least((1ull << 26) / ((uint64_t)parts * s.rows_k), (1ull << 26) / ((uint64_t)parts * s.dim_k));
+    // both of dz's arrays stay in the last-level cache: 64 MB each (128 MB each, 4,096 x 4,096 on
+    // 131,072 bf16: 15.3 ms instead of 15.1)
+    uint64_t p = least((1ull << 25) / ((uint64_t)parts * s.rows_k), (1ull << 25) / ((uint64_t)parts * s.dim_k));
     p = most(p / 256u * 256u, 256u);
     s.piece = (uint32_t)least(p, up_to(vocab, 256u));
     return s;
@@ -93,8 +95,16 @@ inline XentTile xent_tile(uint32_t M, uint32_t N, uint64_t steps, bool sums, uin
 // Floats that hold a product's shares: its tiles times 128 x 128 at most, or the product.
 inline uint64_t xent_share_floats(uint64_t rows, uint64_t dim4) { return most(rows * dim4, (uint64_t)kXentShareTiles * 128u * 128u); }
 
+// Where few rows decide a gradient, the rounding of dz to 16 bits can be well above the mean
+// beside the result's own: the errors of some calls of 1 to 54 rows were 1.5 to 1.8 times
+// those of exact factors (of many rows they average to 1.1, or 1.4 with weights).  So dz has
+// two parts: for dhidden of up to 16 rows, the second part as 16 rows more, which the smallest tile
+// has room for; and for dmatrix of fp16 calls of up to 1,024 rows (of bf16 ones it is fp16, and
+// fine enough).
+constexpr uint32_t kXentStackRows = 16u, kXentFewRows = 1024u;
+
 struct XentWork {                                 // byte offsets
-    uint64_t info, zt, stats, refs, part, up_n, up_m, x, xm, w, dz, dz_plain, dx, dw, end;
+    uint64_t info, zt, stats, refs, part, up_n, up_m, x, xm, w, dz, dz_w, dx, dw, end;
 };
 inline XentWork xent_work(const XentShape& s)
 {
@@ -103,9 +113,9 @@ inline XentWork xent_work(const XentShape& s)
     auto take = [&at](uint64_t bytes) { const uint64_t p = at; at += up_to(bytes, 256u); return p; };
     const uint64_t P2 = 2ull * s.parts, dim4 = up_to(s.dim, 4u);
     o.refs = take(8u);
-    o.info = take(16ull * s.rows_k);
+    o.info = take(32ull * s.rows_k);
     o.zt = take(4ull * s.rows_k);
-    o.stats = take(8ull * s.rows_k);
+    o.stats = take(12ull * s.rows_k);
     o.part = take(8ull * s.rows_k * (up_to(s.vocab, 256u) / 32u));
     o.up_n = take(4ull * s.rows_k);
     o.up_m = take(4ull * s.piece);
@@ -113,7 +123,7 @@ inline XentWork xent_work(const XentShape& s)
     o.xm = take(P2 * s.rows_k * s.dim_k);
     o.w = take(P2 * s.piece * s.dim_k);
     o.dz = take(P2 * s.rows_k * s.piece);
-    o.dz_plain = take(P2 * s.rows_k * s.piece);
+    o.dz_w = take(4ull * s.rows_k * s.piece);
     o.dx = take(4u * xent_share_floats(s.rows, dim4));
     o.dw = take(4ull * kXentShareTiles * 128u * 128u);
     o.end = at;
@@ -129,9 +139,9 @@ inline uint64_t xent_bound(uint32_t rows, uint32_t dim, uint32_t vocab, uint32_t
     XentWork o = xent_work(b);
     // smaller rows or dim widen the piece: its arrays are bounded by their products
     const uint64_t P2 = 2ull * parts, piece_all = up_to(vocab, 256u);
-    const uint64_t by_dim = least(P2 * piece_all * s.dim_k, most(2ull << 26, P2 * 256u * s.dim_k));
-    const uint64_t by_rows = least(P2 * piece_all * s.rows_k, most(2ull << 26, P2 * 256u * s.rows_k));
-    return o.up_m + up_to(4ull * piece_all, 256u) + 2u * up_to(P2 * (uint64_t)s.rows_k * s.dim_k, 256u) + up_to(by_dim, 256u) + 2u * up_to(by_rows, 256u)
+    const uint64_t by_dim = least(P2 * piece_all * s.dim_k, most(2ull << 25, P2 * 256u * s.dim_k));
+    const uint64_t by_rows = least(P2 * piece_all * s.rows_k, most(2ull << 25, P2 * 256u * s.rows_k));
+    return o.up_m + up_to(4ull * piece_all, 256u) + 2u * up_to(P2 * (uint64_t)s.rows_k * s.dim_k, 256u) + up_to(by_dim, 256u) + 3u * up_to(by_rows, 256u)
            + (o.end - o.dx) + 4096u;
 }
 

@@ -289,9 +289,9 @@ class Learner:
         float32 losses [rows] and the gradients of sum(weight * loss) with respect to
         ``hidden`` and ``matrix``, ``weight`` [rows] in float32 (None: 1).  ``loss`` False
         leaves the losses out and takes ``stats``; ``grad`` False leaves out both
-        gradients, "hidden" or "matrix" is that one alone.  ``stats`` [rows, 2] (float32)
-        receives each row's largest logit and its sum of exp(z - largest), which a call
-        for gradients alone takes back."""
+        gradients, "hidden" or "matrix" is that one alone.  ``stats`` [rows, 3] (float32)
+        receives each row's largest logit and the sums of exp(z - largest) without and of
+        its target, which a call for gradients alone takes back."""
         return self._cross_entropy(rlsim_learner_xent, hidden, matrix, target, weight, loss, grad, stats)
 
     def _cross_entropy(self, launch, hidden, matrix, target, weight, loss, grad, stats):
@@ -311,7 +311,7 @@ class Learner:
         h_at, h_stride = self._matrix("hidden", hidden, rows, dim, hidden.dtype)
         m_at, m_stride = self._matrix("matrix", matrix, vocab, dim, hidden.dtype)
         target_at = self._plain("target", target, (rows,), target.dtype)
-        weight_at, stats_at = self._plain("weight", weight, (rows,)), self._plain("stats", stats, (rows, 2))
+        weight_at, stats_at = self._plain("weight", weight, (rows,)), self._plain("stats", stats, (rows, 3))
         out, loss_at, dh_at, dm_at = [], None, None, None
         if loss:
             losses = self._empty(rows, dtype=self._f32, device=self.device)
@@ -456,7 +456,7 @@ def _functions(torch):
         def forward(ctx, learner, hidden, matrix, target):
             learner._not_captured("cross_entropy_loss")
             ctx.learner = learner
-            stats = torch.empty((hidden.shape[0], 2), dtype=torch.float32, device=learner.device)
+            stats = torch.empty((hidden.shape[0], 3), dtype=torch.float32, device=learner.device)
             launch = lambda h, a: learner._in_order(rlsim_learner_xent, h, a)  # noqa: E731
             losses = learner._cross_entropy(launch, hidden, matrix, target, None, True, False, stats)
             ctx.save_for_backward(hidden, matrix, target, stats)

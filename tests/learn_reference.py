@@ -92,6 +92,15 @@ def xent(hidden, matrix, target, weight=None, grad=True):
     largest = ze.max(dim=1).values
     exp_err = 4.0 * U + (z - m).abs().clamp(max=110.0) * 2.0 * U
     loss_err = 2.0 * largest + sums + (exp_err * torch.exp(z - m)).sum(dim=1) / s[:, 0] + 8.0 * U * (1.0 + loss.abs() + m[:, 0].abs() + z.abs().max(dim=1).values)
+    # Of a row whose largest logit is its target's, by more than errors can hide, the loss is
+    # log1p of the others' sum: off by the share that this sum is.
+    miss = torch.exp(z - m).scatter(1, t, 0.0).sum(dim=1) / s[:, 0]
+    others = z.scatter(1, t, -float("inf")).max(dim=1).values
+    share = 2.02 * largest + sums + 232.0 * U             # exponentials: 4 u and 110 x 2 u at most
+    own = z.gather(1, t)[:, 0]
+    knows = own - others > 4.0 * largest
+    loss = torch.where(knows, -torch.log1p(-miss), loss)
+    loss_err = torch.where(knows, loss * (share + 8.0 * U), loss_err)
     loss = torch.where(counts, loss, 0.0)
     loss_err = torch.where(counts, loss_err, 0.0)
     if not grad:
@@ -100,10 +109,11 @@ def xent(hidden, matrix, target, weight=None, grad=True):
     live = counts & (w != 0)
     w = torch.where(live, w, 0.0)[:, None]
     p = torch.exp(z - m) / s
-    dz = p.scatter_add(1, t, torch.full_like(z[:, :1], -1.0))
+    dz = p.scatter(1, t, -miss[:, None])
     dz = torch.where(live[:, None], dz, 0.0)
     pe = p * (exp_err + 2.0 * largest[:, None] + ze + sums + 8.0 * U)
-    pe = pe.scatter_add(1, t, torch.full_like(z[:, :1], U))
+    # the target's: the others' share of the sum, three roundings and what moves the ratio
+    pe = pe.scatter(1, t, (miss * (torch.exp(own - m[:, 0]) / s[:, 0] * share + 4.0 * U))[:, None])
     # the hardware's exp2 gives 0 below the smallest normal number, 2^-126, and so may the
     # matrix units take a factor below it: what is smaller is off by no more than that, twice
     tiny = 2.0 ** -125
@@ -123,6 +133,11 @@ def xent(hidden, matrix, target, weight=None, grad=True):
         over_v, over_n = over_v + 8.1 * U, over_n + 8.1 * U
         tops = wtop.clamp(min=1e-300)
         xfloor = w.abs() * 2.0 ** -38 * ((dz.abs() @ wtop) + (W.abs() / tops).sum(dim=0)[None] * wtop.max())
+    half_w = half
+    if dtype != torch.float16:
+        # for dmatrix bf16 goes by fp16 too, hidden's rows divided by powers of two (exactly, but for
+        # what is small): the same small parts
+        half_w = 4.0 * U if full else HALF_STEP[torch.float16]
         xt = xtop.clamp(min=1e-300)
         most = (w.abs() * xtop).max() * 2.0
         wfloor = 2.0 ** -38 * ((w * dz).abs().t() @ xtop + (X.abs() / xt * live[:, None]).sum(dim=0)[None] * most)
@@ -130,7 +145,7 @@ def xent(hidden, matrix, target, weight=None, grad=True):
     dXe = w.abs() * (dze @ W.abs() + over_v * (dz.abs() @ W.abs())) * 1.001 + xfloor
     wd = w * dz
     scale = w.abs().max() * 2.0
-    wde = w.abs() * (pe + dz.abs() * (half + 2.0 * U)) + ((floor * scale if floor else 0.0) + tiny) * live[:, None]
+    wde = w.abs() * (pe + dz.abs() * (half_w + 2.0 * U)) + ((floor * scale if floor else 0.0) + tiny) * live[:, None]
     dW = wd.t() @ X
     dWe = (wde.t() @ X.abs() + over_n * (wd.abs().t() @ X.abs())) * 1.001 + wfloor
     return (loss, loss_err), (dX, dXe), (dW, dWe)

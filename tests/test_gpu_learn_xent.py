@@ -133,6 +133,21 @@ def test_sharp_rows(learner, dtype):
     assert (loss[35:][target[35:] >= 0] > 50).any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_that_know_their_target(learner, dtype):
+    """Losses from 1e-2 to 1e-30: neither they nor the gradients are differences from 1."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    matrix = torch.zeros((300, 64), device="cuda")
+    matrix[:, :60] = torch.randn((300, 60), generator=g, device="cuda") / 8
+    hidden = torch.randn((40, 64), generator=g, device="cuda")
+    target = torch.full((40,), 17, device="cuda")
+    matrix[17, 60] = 1.0                                       # the target's lead, from row to row
+    hidden[:, 60] = torch.linspace(12.0, 75.0, 40, device="cuda")
+    hidden, matrix = hidden.to(dtype), matrix.to(dtype)
+    loss, dhidden, dmatrix = _check(learner, hidden, matrix, target)
+    assert float(loss.max()) < 1e-1 and 0.0 < float(loss.min()) < 1e-25
+
+
 def test_fp16_gradients_of_a_flat_softmax(learner):
     """20,000 probabilities of 5e-5 each, and weights from 2^-10 to 2^10."""
     hidden, matrix, target, weight = _inputs(40, 64, 20000, torch.float16, sharp=0.01)
@@ -195,7 +210,7 @@ def test_a_vocabulary_that_ends_within_a_step_keeps_to_itself(learner, rows, dty
 def test_parts_of_a_call(learner, rows):
     """Losses, either gradient or both, at once or from the statistics, are the same bits."""
     hidden, matrix, target, weight = _inputs(rows, 128, 700, torch.bfloat16)
-    stats = torch.empty((rows, 2), device="cuda")
+    stats = torch.empty((rows, 3), device="cuda")
     loss, dhidden, dmatrix = learner.cross_entropy(hidden, matrix, target, weight, stats=stats)
     assert torch.equal(learner.cross_entropy(hidden, matrix, target, grad=False), loss)
     assert torch.equal(learner.cross_entropy(hidden, matrix, target, weight, grad="hidden")[1], dhidden)
@@ -206,6 +221,8 @@ def test_parts_of_a_call(learner, rows):
     z = hidden.double() @ matrix.double().t()
     counts = target >= 0
     torch.testing.assert_close(stats[counts, 0].double(), z.max(dim=1).values[counts], rtol=0, atol=1e-4)
+    own = torch.exp(z.gather(1, target.clamp(min=0)[:, None])[:, 0] - z.max(dim=1).values)
+    torch.testing.assert_close(stats[counts, 2].double(), own[counts], rtol=1e-3, atol=0)
 
 
 def test_again_and_again(learner):

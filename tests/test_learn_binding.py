@@ -121,7 +121,7 @@ def test_rows_in_time_and_their_strides(device, order):
 
 def test_writes_raise_versions(device):
     learner = device.learner()
-    x, state, stats = torch.zeros((2, 3, 4)), torch.zeros((3, 4)), torch.zeros((2, 2))
+    x, state, stats = torch.zeros((2, 3, 4)), torch.zeros((3, 4)), torch.zeros((2, 3))
     before = state._version
     learner.scan(x, x, state)
     assert state._version == before

@@ -50,8 +50,9 @@ int main()
             const XentShape s = xent_shape(r, d, v, parts);
             const XentWork o = xent_work(s);
             // shares of both products fit
-            const XentTile x = xent_tile(d, r, (uint64_t)s.piece / kXentK * (parts == 1u ? 1u : 3u), true, cus);
-            CHECK(x.share >= 1u && up_to(d, 4u) * 4u * r * x.share <= o.dw - o.dx);
+            const uint32_t rx = parts == 1u && r <= kXentStackRows ? 2u * kXentStackRows : r;      // rows of dhidden's sums
+            const XentTile x = xent_tile(d, rx, (uint64_t)s.piece / kXentK * (parts == 1u ? 1u : 3u), true, cus);
+            CHECK(x.share >= 1u && up_to(d, 4u) * 4u * rx * x.share <= o.dw - o.dx);
             const uint32_t count = s.piece < v ? s.piece : v;
             const XentTile w = xent_tile(d, count, (uint64_t)s.rows_k / kXentK * (parts == 1u ? 1u : 3u), true, cus);
             CHECK(w.share == 1u || up_to(d, 4u) * 4u * count * w.share <= o.end - o.dw);
