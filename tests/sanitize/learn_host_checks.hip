@@ -180,7 +180,7 @@ int main()
     XENT(c.hidden = (const char*)f + 1, "aligned");
     XENT((c.target_bytes = 8, c.target = f + 5001), "aligned");
     XENT(c.weight = (const float*)((const char*)f + 1), "aligned");
-    XENT(c.stats = f + 5301, "aligned");
+    XENT(c.stats = (float*)((char*)f + 5300 * 4 + 1), "aligned");
     XENT(c.dhidden = f, "overlaps");
     XENT(c.dmatrix = f + 1000, "overlaps");
     XENT(c.dmatrix = f + 6100, "overlaps");
