@@ -442,6 +442,8 @@ int rlsim_create(uint32_t n_envs, uint32_t state_words, const rlsim_cfg* cfg, rl
     if (e == hipSuccess && h->wide) e = hipMemset(h->pad_s, 0, pad_bytes);
     if (e == hipSuccess && h->wide) e = hipMemset(h->pad_a, 0, pad_bytes);
     if (e == hipSuccess && h->wide) e = hipMemset(h->pad_b, 0, pad_bytes);
+    // they run on the null stream, which the handle's stream need not wait for
+    if (e == hipSuccess && h->wide) e = hipStreamSynchronize(nullptr);
     if (e != hipSuccess) {
         int rc = (e == hipErrorOutOfMemory) ? fail(nullptr, RLSIM_ENOMEM, "rlsim_create: device allocation failed")
                                             : hip_fail(nullptr, e, "rlsim_create: hipMalloc");
