@@ -52,8 +52,14 @@ def _ptr(t):
 
 def probe_store(n: int, K: int, obs, action, reward, done, stream=None) -> None:
     """Write K trajectory rows for n envs (torch tensors laid out as rlsim_traj)
-    with no simulation; raises ValueError on a rejected argument."""
+    with no simulation, after what the current stream has been given; raises
+    ValueError on a rejected argument."""
     s = None if stream is None else (stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+    if hasattr(stream, "wait_stream") and getattr(obs, "is_cuda", False):
+        import torch
+        current = torch.cuda.current_stream(obs.device)
+        if current.cuda_stream != s:
+            stream.wait_stream(current)
     rc = probe_lib.rlsim_probe_store(int(n), int(K), _ptr(obs), _ptr(action), _ptr(reward), _ptr(done), s)
     if rc != 0:
         raise ValueError(f"rlsim_probe_store rejected its arguments (status {rc})")

@@ -1,0 +1,22 @@
+"""probe_store on a stream of its own comes after what the current stream has been given."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+def test_a_store_follows_a_fill_of_the_current_stream():
+    from paper_2207_07736_amd import Trajectory
+    from paper_2207_07736_amd.probe import probe_store
+    n, K = 1 << 16, 8
+    tr = Trajectory(K, n, stats=False)
+    busy = torch.empty(1 << 28, dtype=torch.float32, device="cuda")
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        torch.cuda.synchronize()
+        for _ in range(10):
+            busy.fill_(1.0)                       # the fill of done waits for these
+        tr.done.fill_(9)
+        probe_store(n, K, tr.obs, tr.action, tr.reward, tr.done, stream=s)
+        torch.cuda.synchronize()
+        assert int((tr.done == 9).sum()) == 0
