@@ -3,7 +3,9 @@
 //   a_t = sigmoid(gate_t), h_t = a_t h'_{t-1} + (1 - a_t) x_t, h'_t = done_t ? 0 : h_t
 //
 // A step is an affine map of the state, so a stretch of steps is one too (two numbers a
-// channel).  Where there are channels enough, a thread goes through all steps of its two
+// channel), but for the end of an episode, which takes 0 in place of the state whatever the
+// state is: a product of 0 would hand on a NaN or an infinity as a NaN.  A map that holds an
+// end says so, and its sum is taken as it is.  Where there are channels enough, a thread goes through all steps of its two
 // channels; where there are not, time is cut into segments: one launch finds each
 // segment's map, the next joins them to the state each segment starts from, and the third
 // goes through the rows.  Backward is the same from the end.  No result depends on how the
@@ -34,8 +36,8 @@ struct ScanArgs {
     const uint8_t* done;
     float* marks;
     float* last;                 // forward: last; backward: dstate; or null
-    float* map_a;                // [segments][n channels]: a segment's map, product and
-    float* map_b;                // sum; once joined, the state that the segment starts from
+    float* map_a;                // [segments][n channels]: a segment's map, product (or kScanReset)
+    float* map_b;                // and sum; once joined, the state that the segment starts from
     uint32_t T, n, channels, groups, segments, seg_len;
     uint32_t backward;
 };
@@ -52,6 +54,17 @@ __device__ __forceinline__ Gate gate_of(float g)
     const float s = E * r;
     return g >= 0.0f ? Gate{r, s} : Gate{s, r};
 }
+
+// A map's product: of gates, at least 2^-149 while none of them is 0, so that an infinite state
+// stays one however far it is carried; kScanReset where an episode ends within the map.
+constexpr float kScanReset = -1.0f;
+__device__ __forceinline__ float scan_product(float p, float q)
+{
+    return __builtin_fmaxf(p * q, __builtin_fminf(__builtin_fminf(p, q), 0x1p-149f));
+}
+// What a map makes of the state h, and of a map before it.
+__device__ __forceinline__ float scan_through(float p, float q, float h) { return p < 0.0f ? q : __builtin_fmaf(p, h, q); }
+__device__ __forceinline__ float scan_joined(float p, float after) { return after < 0.0f ? after : p < 0.0f ? p : scan_product(p, after); }
 
 // V consecutive elements as loaded, turned to floats when used.
 template <int D, int V>
@@ -141,11 +154,13 @@ __device__ __forceinline__ uint32_t ends_of(const ScanArgs& a, uint32_t t, uint3
 }
 
 // Steps [t0, t1) forward for one thread, U at a time: the loads of a run are made before
-// its first step.  ROWS: y and the marks are written; else only the map is kept.
+// its first step.  ROWS: y and the marks are written; else only the map is kept, and whether an
+// episode ends in it returned.
 template <int D, int V, uint32_t U, bool WIDE, bool ROWS>
-__device__ __forceinline__ void scan_forward(const ScanArgs& a, const Lane<V>& l, uint32_t t0, uint32_t t1, float (&h)[V],
+__device__ __forceinline__ bool scan_forward(const ScanArgs& a, const Lane<V>& l, uint32_t t0, uint32_t t1, float (&h)[V],
                                              float (&prod)[V])
 {
+    uint32_t reset = 0u;
     const auto ox = lane_offset<WIDE, D, V>(l, a.x_seq), og = lane_offset<WIDE, D, V>(l, a.gate_seq),
                oy = lane_offset<WIDE, D, V>(l, a.y_seq);
     for (uint32_t t = t0; t < t1; t += U) {
@@ -157,6 +172,7 @@ __device__ __forceinline__ void scan_forward(const ScanArgs& a, const Lane<V>& l
             g[u].load(a.gate + at * a.gate_step + og);
         }
         const uint32_t ends = ends_of<U>(a, t, t1, l.seq);
+        if (!ROWS) reset |= ends;
         if (ROWS && a.marks && (U == kScanMark || t % kScanMark == 0u)) l.put(a.marks + (uint64_t)(t / kScanMark) * a.n * a.channels, h);
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
@@ -169,12 +185,13 @@ __device__ __forceinline__ void scan_forward(const ScanArgs& a, const Lane<V>& l
                     h[i] = __builtin_fmaf(k.a, h[i], k.take * x[u].get(i));
                     out[i] = h[i];
                     if (end) h[i] = 0.0f;
-                    if (!ROWS) prod[i] = end ? 0.0f : prod[i] * k.a;
+                    if (!ROWS) prod[i] = scan_product(prod[i], k.a);
                 }
                 if (ROWS) Channels<D, V>::store(a.y + (uint64_t)(t + u) * a.y_step + oy, out, l.from);
             }
         }
     }
+    return reset != 0u;
 }
 
 template <int D, int V, bool WIDE>
@@ -187,7 +204,10 @@ __global__ __launch_bounds__(256) void k_scan_maps(ScanArgs a)
         float h[V], prod[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) { h[i] = 0.0f; prod[i] = 1.0f; }
-        scan_forward<D, V, kScanMark, WIDE, false>(a, l, t0, t1, h, prod);
+        if (scan_forward<D, V, kScanMark, WIDE, false>(a, l, t0, t1, h, prod)) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) prod[i] = kScanReset;
+        }
         const uint64_t at = (uint64_t)s * a.n * a.channels;
         l.put(a.map_a + at, prod);
         l.put(a.map_b + at, h);
@@ -210,8 +230,8 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs a)
 #pragma unroll 4
         for (uint32_t j = j0; j < j1; ++j) {
             const float p = a.map_a[at(j)], q = a.map_b[at(j)];
-            B = __builtin_fmaf(p, B, q);
-            A *= p;
+            B = scan_through(p, q, B);
+            A = scan_joined(A, p);
         }
     }
     sa[y][x] = A;
@@ -219,12 +239,12 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs a)
     __syncthreads();
     if (c >= C) return;
     float h = a.state ? a.state[c] : 0.0f;
-    for (uint32_t k = 0; k < y; ++k) h = __builtin_fmaf(sa[k][x], h, sb[k][x]);
+    for (uint32_t k = 0; k < y; ++k) h = scan_through(sa[k][x], sb[k][x], h);
 #pragma unroll 4
     for (uint32_t j = j0; j < j1; ++j) {
         const float p = a.map_a[at(j)], q = a.map_b[at(j)];
         a.map_b[at(j)] = h;
-        h = __builtin_fmaf(p, h, q);
+        h = scan_through(p, q, h);
     }
 }
 
@@ -268,6 +288,7 @@ __global__ __launch_bounds__(256) void k_scan_back_maps(ScanArgs a)
         const Lane<V> l(a, q);
         const auto og = lane_offset<WIDE, D, V>(l, a.gate_seq), od = lane_offset<WIDE, D, V>(l, a.dy_seq);
         float P[V], Q[V];
+        uint32_t reset = 0u;
 #pragma unroll
         for (int i = 0; i < V; ++i) { P[i] = 1.0f; Q[i] = 0.0f; }
         for (uint32_t left = t1 - t0; left != 0u;) {
@@ -280,6 +301,7 @@ __global__ __launch_bounds__(256) void k_scan_back_maps(ScanArgs a)
                 if (a.dy) d[u].load(a.dy + at * a.dy_step + od);
             }
             const uint32_t ends = ends_of<U>(a, t, t + run, l.seq);
+            reset |= ends;
 #pragma unroll
             for (uint32_t k = 0; k < U; ++k) {
                 const uint32_t u = U - 1u - k;
@@ -289,12 +311,16 @@ __global__ __launch_bounds__(256) void k_scan_back_maps(ScanArgs a)
                     for (int i = 0; i < V; ++i) {
                         const Gate w = gate_of(g[u].get(i));
                         const float e = (a.dy ? d[u].get(i) : 0.0f) + (end ? 0.0f : Q[i]);
-                        P[i] = end ? 0.0f : P[i] * w.a;
+                        P[i] = scan_product(P[i], w.a);
                         Q[i] = w.a * e;
                     }
                 }
             }
             left -= run;
+        }
+        if (reset) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) P[i] = kScanReset;
         }
         l.put(a.map_a + s * C, P);
         l.put(a.map_b + s * C, Q);
