@@ -461,7 +461,8 @@ typedef struct {
     int dtype, out_dtype;                     /* out_dtype is ignored in place */
 } rlsim_tensor;
 
-/* norm: device float, out.  tensors is a HOST array that the call does not keep.
+/* norm: device float, out (+inf where it is above fp32's numbers; the scaling goes by its
+ * 64 bits).  tensors is a HOST array that the call does not keep.
  * Errors: EINVAL (NULL h, norm or, with count > 0, tensors; count > 2^20; max_norm
  * not > 0; NULL data, a misaligned pointer or unknown dtype; an output over another
  * tensor's data or output, norm among them); EDEVICE. */

@@ -89,10 +89,27 @@ __device__ __forceinline__ double clip_squares(const char* p, uint64_t from, uin
     return s;
 }
 
+// max_norm / norm as by 2^up: up is 0 but for factors below fp32's normal numbers, which would
+// lose digits that the products have.
+struct ClipFactor {
+    float by;
+    int up;
+    __device__ __forceinline__ float operator()(float x) const { return ldexpf(x * by, up); }
+};
+__device__ __forceinline__ ClipFactor clip_factor(double norm, double max_norm)
+{
+    if (!(norm > max_norm && norm < (double)__builtin_inff())) return ClipFactor{1.0f, 0};
+    const double f = max_norm / norm;
+    if (f >= 0x1p-126) return ClipFactor{(float)f, 0};
+    int up;
+    const float by = (float)frexp(f, &up);
+    return ClipFactor{by, up};
+}
+
 // STREAM: outputs that the last-level cache would not keep go past it, and leave it to what
 // the norm's pass has read last, which is scaled first.
 template <int D, int O, uint32_t NT, bool STREAM>
-__device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t from, uint64_t to, float scale)
+__device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t from, uint64_t to, ClipFactor scale)
 {
     using To = Elem<O>;
     each_vector<D, NT>(p, from, to,
@@ -100,7 +117,7 @@ __device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t fr
                      constexpr uint32_t E = Elem<D>::kPerVec;
                      struct __attribute__((packed, aligned(To::kBytes))) Run { typename To::Word w[E]; } r;
 #pragma unroll
-                     for (uint32_t e = 0; e < E; ++e) r.w[e] = To::word(Elem<D>::get(v, e) * scale);
+                     for (uint32_t e = 0; e < E; ++e) r.w[e] = To::word(scale(Elem<D>::get(v, e)));
                      if (STREAM) {
                          typedef uint32_t Words __attribute__((ext_vector_type(E * To::kBytes / 4u), aligned(2)));
                          __builtin_nontemporal_store(__builtin_bit_cast(Words, r), reinterpret_cast<Words*>(out + i * To::kBytes));
@@ -108,7 +125,7 @@ __device__ __forceinline__ void clip_scale(const char* p, char* out, uint64_t fr
                          *reinterpret_cast<Run*>(out + i * To::kBytes) = r;
                      }
                  },
-                 [&](float x, uint64_t i) { reinterpret_cast<typename To::Word*>(out)[i] = To::word(x * scale); });
+                 [&](float x, uint64_t i) { reinterpret_cast<typename To::Word*>(out)[i] = To::word(scale(x)); });
 }
 
 // The tensor of a block of the launch.
@@ -134,11 +151,11 @@ __device__ __forceinline__ double squares_of(const ClipArgs& a, uint32_t block)
 }
 
 template <uint32_t NT, bool STREAM>
-__device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, float scale)
+__device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, ClipFactor scale)
 {
     const uint32_t k = clip_tensor(a, block);
     const ClipTensor& t = a.t[k];
-    if (scale == 1.0f && t.data == t.out) return;
+    if (scale.by == 1.0f && scale.up == 0 && t.data == t.out) return;
     const uint64_t from = (uint64_t)(block - a.first[k]) * a.chunk, to = min(from + a.chunk, t.elements);
     auto to_type = [&](auto in) {
         constexpr int D = decltype(in)::value;
@@ -149,11 +166,6 @@ __device__ __forceinline__ void scale_block(const ClipArgs& a, uint32_t block, f
     if (a.dtype[k] == kHeadF32) to_type(std::integral_constant<int, kHeadF32>{});
     else if (a.dtype[k] == kHeadBF16) to_type(std::integral_constant<int, kHeadBF16>{});
     else to_type(std::integral_constant<int, kHeadF16>{});
-}
-
-__device__ __forceinline__ float clip_factor(double norm, double max_norm)
-{
-    return norm > max_norm && norm < (double)__builtin_inff() ? (float)(max_norm / norm) : 1.0f;
 }
 
 __global__ __launch_bounds__(256) void k_clip_squares(ClipArgs a)
@@ -172,7 +184,7 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a)
     if (a.base + blockIdx.x == 0u && threadIdx.x == 0u) *a.norm = (float)norm;
     if (!a.count) return;
     const uint32_t block = a.first[a.count] - 1u - blockIdx.x;     // from the end: what was read last
-    const float scale = clip_factor(norm, a.max_norm);
+    const ClipFactor scale = clip_factor(norm, a.max_norm);
     if (a.past_cache) scale_block<256u, true>(a, block, scale);
     else scale_block<256u, false>(a, block, scale);
 }
@@ -186,7 +198,7 @@ __global__ __launch_bounds__(1024) void k_clip_small(ClipArgs a)
     for (uint32_t b = wave; b < blocks; b += 16u) s += squares_of<64u>(a, b);
     const double norm = sqrt(group_sum<1024>(s, sh));
     if (threadIdx.x == 0u) *a.norm = (float)norm;
-    const float scale = clip_factor(norm, a.max_norm);
+    const ClipFactor scale = clip_factor(norm, a.max_norm);
     for (uint32_t b = wave; b < blocks; b += 16u) scale_block<64u, false>(a, b, scale);
 }
 
