@@ -55,10 +55,12 @@ def probe_store(n: int, K: int, obs, action, reward, done, stream=None) -> None:
     with no simulation, after what the current stream has been given; raises
     ValueError on a rejected argument."""
     s = None if stream is None else (stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
-    if hasattr(stream, "wait_stream") and getattr(obs, "is_cuda", False):
+    if getattr(obs, "is_cuda", False):
         import torch
         current = torch.cuda.current_stream(obs.device)
-        if current.cuda_stream != s:
+        if current.cuda_stream != (s or 0):
+            if not hasattr(stream, "wait_stream"):
+                stream = torch.cuda.ExternalStream(s, device=obs.device) if s else torch.cuda.default_stream(obs.device)
             stream.wait_stream(current)
     rc = probe_lib.rlsim_probe_store(int(n), int(K), _ptr(obs), _ptr(action), _ptr(reward), _ptr(done), s)
     if rc != 0:
