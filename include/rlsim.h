@@ -411,7 +411,9 @@ int rlsim_learner_scan_grad(rlsim_learner_t* h, const rlsim_scan* s, const rlsim
  *   dhidden, dmatrix = the gradients of sum_r weight_r loss_r (weight NULL: 1).
  * A row whose target is outside [0, vocab) has loss 0 and adds nothing to a gradient
  * whatever its hidden state, and so does a row of weight 0 to the gradients.  In other
- * rows infinities and NaN do as in the formulas.
+ * rows a logit of -inf has no share; one of +inf or NaN makes the row's loss, and what the
+ * row gives to the gradients, NaN; and a weight that is not finite makes what its row gives
+ * to the gradients so.
  *
  * Logits exist a piece of the vocabulary at a time.  They are fp32 sums of exact products
  * (of fp32 factors: of products to 22 bits, where an entry counts to 2^-39 of its row's

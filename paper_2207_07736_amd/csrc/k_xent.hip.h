@@ -561,7 +561,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                             uint16_t w[2][8];
 #pragma unroll
                             for (uint32_t e = 0; e < 8u; ++e) {
-                                const float p = c[i][j][4u * q + e], pw = p == 0.0f ? 0.0f : ldexpf(p * weight, up);
+                                const float pw = ldexpf(c[i][j][4u * q + e] * weight, up);      // of rows that do not count 0 by 0
                                 if (F != kHeadBF16) cut2(pw, w[0][e], w[1][e]);
                                 else w[0][e] = Elem<kHeadF16>::word(pw);
                             }
