@@ -361,8 +361,9 @@ int rlsim_learner_create(uint32_t max_rows, uint32_t max_dim, uint32_t max_vocab
  * h'_t being 0 where done_t is not 0 (an episode ended with step t) and h_t otherwise;
  * h'_{-1} = state (NULL: 0), last = h'_{T-1}.  Channels of a row are consecutive elements;
  * rows of step t and sequence i start at t step_stride + i seq_stride elements (rows of
- * [T][n][channels] and of [n][T][channels] alike).  All of it is fp32 inside; y is
- * rounded once.
+ * [T][n][channels] and of [n][T][channels] alike).  All of it is fp32 inside, a_t and
+ * 1 - a_t each within (2 |gate_t| + 8) 2^-24 of themselves (or 2^-126); y is rounded
+ * once.
  *
  * With dy the gradient of the y (NULL: 0) and dlast that of last (NULL: 0),
  *   e_t = dy_t + (done_t ? 0 : a_{t+1} e_{t+1}),  e_{T-1} = dy_{T-1} + (done_{T-1} ? 0 : dlast),
@@ -418,10 +419,13 @@ int rlsim_learner_scan_grad(rlsim_learner_t* h, const rlsim_scan* s, const rlsim
  * Logits exist a piece of the vocabulary at a time.  They are fp32 sums of exact products
  * (of fp32 factors: of products to 22 bits, where an entry counts to 2^-39 of its row's
  * largest at least); the softmax is fp32.  Its difference from the target enters dhidden's
- * product rounded to the factors' type (fp32: to 22 bits), and dmatrix's, times the weight, to
- * fp16 with powers of two (fp32: 22 bits; hidden's bf16 entries count to 2^-39 of their row's
- * largest); both are summed in fp32 and rounded once.  A row of fp32 factors that is not
- * finite gives NaN wherever it enters.
+ * product rounded to the factors' type (fp16: probabilities below 2^-28 lose digits and below
+ * 2^-39 count as 0; fp32: 22 bits), and dmatrix's, times the weight, to fp16 with powers of two:
+ * where weight x softmax (fp32 and bf16: x the row's largest entry in hidden) is below 2^-28
+ * of the most that a row of the call could have, it loses digits, and below 2^-39 counts as 0
+ * (fp32: 22 bits, the same end; hidden's bf16 entries count to 2^-39 of their row's largest).
+ * Both are summed in fp32 and rounded once.  A row of fp32 factors that is not finite gives
+ * NaN wherever it enters.
  *
  * stats holds each row's largest logit, the sum of exp(z - largest) over the entries other
  * than its target, and that of its target: an output beside the losses, and the input of a

@@ -13,9 +13,12 @@
 //
 // What bounds it, where there is enough of it, is memory: two channels a thread, 16 steps'
 // loads under way before the first is used.  200 x 4,096 x 64 fp32: forward 133 us = 4.8 TB/s,
-// backward 211 us = 5.0 TB/s (a large copy: 4.9).  65,536 x 2,048 bf16, cut: maps 131 us = 4.1
-// TB/s each way, rows 165 us = 5.1 and 311 us = 4.4; reading the rows twice is the price of
-// the cut.  Small calls are bound by a run's chain and, where cut, by three launches.
+// backward 211 us = 5.0 TB/s (a large copy: 4.9).  65,536 x 2,048 bf16, cut: maps 129 and 133 us
+// = 4.1 TB/s, rows 164 us = 5.1 and 308 us = 4.4; reading the rows twice is the price of the
+// cut.  Small calls are bound by a run's chain and, where cut, by three launches.  With a few
+// waves to a CU the loads of a run wait for the run before it: 1,000 x 2,048 x 64 in bf16
+// 278 us forward and 408 backward for floors of 161 and 268.  Backward in fp16 is slower yet
+// (1,083 us there) and keeps some registers in scratch memory; without that it takes 847.
 #pragma once
 
 #include <type_traits>
@@ -42,8 +45,9 @@ struct ScanArgs {
     uint32_t backward;
 };
 
-// sigmoid(g) and 1 - sigmoid(g), each to a few units of the last place: the smaller of the
-// two is never a difference.  The reciprocal is the hardware's with one Newton step.
+// sigmoid(g) and 1 - sigmoid(g): the smaller of the two is never a difference.  Each is within
+// (2 |g| + 8) 2^-24 of itself: exp2's argument is |g| log2(e) in 24 bits, so the smaller one
+// loses digits as it gets small.  The reciprocal is the hardware's with one Newton step.
 struct Gate { float a, take; };
 __device__ __forceinline__ Gate gate_of(float g)
 {

@@ -12,8 +12,8 @@
 //
 // The logits are computed twice (for the sums; for dz, piece by piece): 8 rows dim vocab
 // operations for a loss with its gradients, where an array of all logits would allow 6.
-// 4,096 rows of 4,096 on 131,072 in bf16, ms: sums 3.57 (1,230 TFLOP/s), dz 4.08 (1,080),
-// dhidden 3.76 (1,170), dmatrix 3.61 (1,220); the library's plain product reaches 1,475 to 1,495.
+// 4,096 rows of 4,096 on 131,072 in bf16, ms: sums 3.53 (1,246 TFLOP/s), dz 4.03 (1,091),
+// dhidden 3.72 (1,182), dmatrix 3.59 (1,226); the library's plain product reaches 1,475 to 1,495.
 // The matrix units are busy for 71 % of the sums' cycles and 53, 63 and 67 % of the others', at
 // 1.55 to 1.84 GHz.  The dz launches write 134 MB each; 224 MB reach memory.  Tried, TFLOP/s of
 // the sums beside 1,209 to 1,234 in the same run: four waves of 128 x 128 with 512 registers
@@ -557,6 +557,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                     for (uint32_t q = 0; q < 4u; q += 2u) {
                         constexpr uint32_t P = F == kHeadF32 ? 2u : 1u;
                         const uint64_t at = n * a.dz_ld + 2u * (m_base + wm * (BM / WM) + i * 32u + (q + lane / 32u) * 8u);
+                        // dmatrix's factor: fp16 has 3 bits more than bf16, at the price of one scale
+                        // for the call.  Below 2^-28 of the call's largest |weight| x 2^up_n an entry
+                        // loses digits, below 2^-39 it is 0.  fp32 has two parts, and fp16 where few
+                        // rows decide (kXentFewRows).
                         if (a.dz_w) {
                             uint16_t w[2][8];
 #pragma unroll
@@ -569,6 +573,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_xent_gemm(XentGemm a)
                             if (F == kHeadF32 || (F == kHeadF16 && a.dz_w_parts == 2u))
                                 *reinterpret_cast<u32x4*>(a.dz_w + at + a.dz_part) = eight_of(w[1]);
                         }
+                        // dhidden's factor, in the type that the matrix is multiplied in: bf16, whose
+                        // rounding averages out over the vocabulary; fp16 times 2^kDzUp, so that
+                        // probabilities from 2^-28 on keep their digits; a second part as rows where
+                        // there is room (kXentStackRows); two parts for fp32.
                         if (a.dz && !(a.dz_stack && n >= a.dz_stack)) {
                             uint16_t w[2][8];
 #pragma unroll
