@@ -13,8 +13,8 @@
 //
 // What bounds it, where there is enough of it, is memory: two channels a thread, 16 steps'
 // loads under way before the first is used.  200 x 4,096 x 64 fp32: forward 133 us = 4.8 TB/s,
-// backward 211 us = 5.0 TB/s (a large copy: 4.9).  65,536 x 2,048 bf16, cut: maps 129 and 133 us
-// = 4.1 TB/s, rows 164 us = 5.1 and 308 us = 4.4; reading the rows twice is the price of the
+// backward 211 us = 5.0 TB/s (a large copy: 4.9).  65,536 x 2,048 bf16, cut: maps 133 and 136 us
+// = 4.0 TB/s, rows 166 us = 5.1 and 313 us = 4.3; reading the rows twice is the price of the
 // cut.  Small calls are bound by a run's chain and, where cut, by three launches.  With a few
 // waves to a CU the loads of a run wait for the run before it: 1,000 x 2,048 x 64 in bf16
 // 278 us forward and 408 backward for floors of 161 and 268.  Backward in fp16 is slower yet
@@ -59,16 +59,26 @@ __device__ __forceinline__ Gate gate_of(float g)
     return g >= 0.0f ? Gate{r, s} : Gate{s, r};
 }
 
-// A map's product: of gates, at least 2^-149 while none of them is 0, so that an infinite state
-// stays one however far it is carried; kScanReset where an episode ends within the map.
-constexpr float kScanReset = -1.0f;
+// A map's product: of gates, kScanTiny at least while none of them is 0; kScanReset where an
+// episode ends within the map.
+constexpr float kScanReset = -1.0f, kScanTiny = 0x1p-149f;
 __device__ __forceinline__ float scan_product(float p, float q)
 {
-    return __builtin_fmaxf(p * q, __builtin_fminf(__builtin_fminf(p, q), 0x1p-149f));
+    return __builtin_fmaxf(p * q, __builtin_fminf(__builtin_fminf(p, q), kScanTiny));
 }
-// What a map makes of the state h, and of a map before it.
-__device__ __forceinline__ float scan_through(float p, float q, float h) { return p < 0.0f ? q : __builtin_fmaf(p, h, q); }
-__device__ __forceinline__ float scan_joined(float p, float after) { return after < 0.0f ? after : p < 0.0f ? p : scan_product(p, after); }
+// What a map makes of the state h, and of a map before it.  An infinite state stays one however
+// far it is carried; of a finite one the tiny product leaves nothing.
+__device__ __forceinline__ float scan_through(float p, float q, float h)
+{
+    const float carried = __builtin_fmaf(p == kScanTiny ? 0.0f : p, h, q);
+    const float kept = __builtin_fabsf(h) == __builtin_inff() && p > 0.0f ? h + q : carried;
+    return p < 0.0f ? q : kept;
+}
+__device__ __forceinline__ float scan_joined(float p, float after)
+{
+    const float least = __builtin_fminf(p, after);
+    return least < 0.0f ? least : scan_product(p, after);
+}
 
 // V consecutive elements as loaded, turned to floats when used.
 template <int D, int V>
@@ -229,14 +239,30 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs a)
     const uint64_t c = (uint64_t)blockIdx.x * 16u + x;
     const uint32_t run = (a.segments + 15u) / 16u, j0 = min(y * run, a.segments), j1 = min(j0 + run, a.segments);
     auto at = [&](uint32_t j) { return (uint64_t)(a.backward ? a.segments - 1u - j : j) * C + c; };
+    // a few maps' loads at a time, before the first is used
+    constexpr uint32_t U = 4u;
+    auto each = [&](auto f) {
+        for (uint32_t j = j0; j < j1; j += U) {
+            float p[U], q[U];
+#pragma unroll
+            for (uint32_t u = 0; u < U; ++u) {
+                const uint64_t k = at(min(j + u, j1 - 1u));
+                p[u] = a.map_a[k];
+                q[u] = a.map_b[k];
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < U; ++u) {
+                const bool in = j + u < j1;       // else the map that changes nothing
+                f(j + u, in ? p[u] : 1.0f, in ? q[u] : 0.0f);
+            }
+        }
+    };
     float A = 1.0f, B = 0.0f;
     if (c < C) {
-#pragma unroll 4
-        for (uint32_t j = j0; j < j1; ++j) {
-            const float p = a.map_a[at(j)], q = a.map_b[at(j)];
+        each([&](uint32_t, float p, float q) {
             B = scan_through(p, q, B);
             A = scan_joined(A, p);
-        }
+        });
     }
     sa[y][x] = A;
     sb[y][x] = B;
@@ -244,12 +270,10 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanArgs a)
     if (c >= C) return;
     float h = a.state ? a.state[c] : 0.0f;
     for (uint32_t k = 0; k < y; ++k) h = scan_through(sa[k][x], sb[k][x], h);
-#pragma unroll 4
-    for (uint32_t j = j0; j < j1; ++j) {
-        const float p = a.map_a[at(j)], q = a.map_b[at(j)];
-        a.map_b[at(j)] = h;
+    each([&](uint32_t j, float p, float q) {
+        if (j < j1) a.map_b[at(j)] = h;
         h = scan_through(p, q, h);
-    }
+    });
 }
 
 // What a thread's segment starts from.

@@ -143,3 +143,20 @@ def test_through_autograd(learner, T, n, d):
     h.backward(dy)
     assert torch.isfinite(leaves[0].grad).all() and torch.isfinite(leaves[2].grad).all()
     assert torch.equal(torch.isnan(leaves[1].grad), into | bad)
+
+
+def test_a_large_state_fades(learner):
+    """Gates of 0.018 and no input: what a product below the smallest number carries of a finite
+    state is nothing, not the smallest number's share."""
+    T, n, d = 512, 2, 5
+    x, gate = torch.zeros((T, n, d), device="cuda"), torch.full((T, n, d), -4.0, device="cuda")
+    state = torch.full((n, d), 1e30, device="cuda")
+    y, last = learner.scan(x, gate, state)
+    t = torch.arange(1, T + 1, device="cuda", dtype=torch.float64)[:, None, None]
+    # each gate is off by 16 units of 2^-24 at most
+    most = state.double() * torch.exp(t * (math.log(1.0 / (1.0 + math.exp(4.0))) + 2.0 ** -19)) + 2.0 ** -149
+    assert (y >= 0).all() and (y.double() <= most).all() and not last.any()
+    dy = torch.zeros_like(x)
+    marks = learner.scan(x, gate, state, marks=True)[2]
+    dx, _, dstate = learner.scan_grad(x, gate, marks, dy, None, state)
+    assert (dx >= 0).all() and (dx.double() <= most.flip(0) * 57.0).all() and not dstate.any()
